@@ -54,8 +54,10 @@ typedef enum {
   SGA_ERR_HIP = -5
 } sga_status;
 
-/* Storage type of Q, K, V and O.  Accumulation is always fp32. */
-typedef enum { SGA_F32 = 0, SGA_F16 = 1 } sga_dtype;
+/* Storage type of Q, K, V and O.  Accumulation is always fp32.  SGA_BF16 is taken by the entry
+   points of serving alone (sga_rotary, sga_cache_append, sga_attention_paged); the others refuse
+   it as an unknown type. */
+typedef enum { SGA_F32 = 0, SGA_F16 = 1, SGA_BF16 = 2 } sga_dtype;
 
 /* Mask families of Section II-C. */
 typedef enum {
@@ -339,6 +341,134 @@ sga_status sga_attention_forward_static(const void* Q, const void* K, const void
                                         const int64_t* row_ptr, const int32_t* col_idx, void* O,
                                         int64_t L, int32_t H, int32_t d, float scale, void* stream,
                                         int32_t dtype, float* lse, int64_t nnz, int32_t path);
+
+/*
+ * ---- Serving: rotary positions, a paged cache, attention of new tokens over it -------------------
+ *
+ * A program that generates text has the keys and values of earlier tokens in a cache and gets
+ * new tokens in chunks: a prompt, a piece of one, a single token.  For every layer it rotates
+ * queries and keys by their positions, writes keys and values into the cache and attends over it:
+ *   sga_cache_append     (rotates K and Q on the way)     then     sga_attention_paged
+ * and sga_rotary is the rotation alone, for the calls above that have the whole sequence at
+ * hand, and its gradient.  Storage: SGA_F32, SGA_F16 or SGA_BF16.
+ *
+ * Tensors of tokens are given as sga_rows: element (h, t, c) at data[h * head_stride +
+ * t * row_stride + c].  Strides are in elements; both [H][T][d] and what a projection leaves,
+ * [T][H][d] or a part of its rows, can be passed as they are.  Written tensors have to hold
+ * every element at an address of its own.
+ */
+typedef struct {
+  void* data;                /* device (only read through where the call says "read")       */
+  int64_t head_stride;
+  int64_t row_stride;
+} sga_rows;
+
+/* Which channels of a head turn together, pair i of channels / 2 by position * frequencies[i]. */
+typedef enum {
+  SGA_ROTARY_HALF = 0,        /* channels i and i + channels / 2                              */
+  SGA_ROTARY_INTERLEAVED = 1  /* channels 2 i and 2 i + 1                                     */
+} sga_rotary_layout;
+
+typedef struct {
+  uint32_t struct_bytes;      /* = sizeof(sga_rotary_desc)                                    */
+  int32_t layout;             /* sga_rotary_layout                                            */
+  int32_t channels;           /* leading channels of a head that turn: even, 2 .. d; the others
+                                 pass unchanged                                               */
+  float magnitude;            /* multiplies the turned channels (1 unless a long-context
+                                 scaling asks for another)                                    */
+  const double* frequencies;  /* device, [channels / 2], radians per position                 */
+} sga_rotary_desc;
+
+/*
+ * Rotary positions.  With a, b the channels of pair i and t = position * frequencies[i],
+ *   a' = magnitude * (a cos t - b sin t),   b' = magnitude * (a sin t + b cos t)
+ * or, with inverse != 0, the same with -t: for the gradient G of the result, the inverse of G
+ * is the gradient of the input.  The angles are formed and reduced in 64 bits, without loss at any
+ * position; sines and products are taken in 32, and results rounded once.
+ *   X          read, Y written, [H][L][d]; Y may be X (same address and strides), else they must
+ *              not overlap
+ *   positions  device, int64 [L], or NULL: row t has position first + t.  |position| < 2^52
+ *   L >= 0 (no row: nothing is done, addresses may be NULL), H 1..65535, d 2..1024
+ * Errors: SGA_ERR_INVALID_ARG (null pointers, sizes, an unknown layout or dtype, a foreign struct, an address
+ * that is no multiple of the element's size, Y at X's address with other strides).
+ */
+sga_status sga_rotary(const sga_rows* X, const sga_rows* Y, const int64_t* positions, int64_t first, int64_t L, int32_t H,
+                      int32_t d, const sga_rotary_desc* rotary, int32_t inverse, int32_t dtype, void* stream);
+
+/*
+ * New tokens of several sequences and the pages that hold their keys and values.
+ *   Cache    K and V each [n_pages][Hkv][page_size][d]: a page is page_size tokens of every key
+ *            head, page_stride elements (>= Hkv * page_size * d) behind the one before it.
+ *   Tokens   packed in rows of Q, K, V, O: sequence s has rows seq_ptr[s] .. seq_ptr[s+1] - 1;
+ *            seq_ptr[0] = 0, non-decreasing, seq_ptr[n_seqs] <= n_tokens.  Rows behind the last
+ *            sequence are padding: not read, and left as they were in every output.
+ *   Position row seq_ptr[s] + t is token seq_len[s] - new + t of its sequence, where new =
+ *            seq_ptr[s+1] - seq_ptr[s]: seq_len counts the new tokens.
+ *   Page     token j of sequence s is row j % page_size of page page_table[s][j / page_size].
+ *            Entries outside 0 .. n_pages - 1 are no page (-1 for one given back behind a
+ *            window): nothing is written there, and attention passes over their tokens.
+ * Lengths and pages are read on the device, so a captured call follows them: positions below 0
+ * and tokens beyond the page table's columns are treated like tokens without a page, and a
+ * seq_ptr that decreases or passes n_tokens gives wrong rows but no access outside the buffers.
+ * Sequences may share pages that this call only reads; no two tokens of a call may be
+ * written to the same place.
+ */
+typedef struct {
+  uint32_t struct_bytes;      /* = sizeof(sga_paged_batch)                                    */
+  int32_t n_seqs;             /* >= 0                                                         */
+  int64_t n_tokens;           /* rows of the packed tensors, 0 .. 2^31 - 1                    */
+  int64_t n_pages;            /* pages of the cache, 1 .. 2^31 - 1                            */
+  int64_t page_stride;        /* elements from page to page                                   */
+  int32_t page_size;          /* tokens of a page, 1 .. 65536                                 */
+  int32_t pages_per_seq;      /* columns of page_table, >= 1; * page_size <= 2^31 - 1024      */
+  const int32_t* page_table;  /* device, [n_seqs][pages_per_seq]                              */
+  const int64_t* seq_ptr;     /* device, [n_seqs + 1]                                         */
+  const int32_t* seq_len;     /* device, [n_seqs]                                             */
+} sga_paged_batch;
+
+/*
+ * Writes the keys and values of new tokens into their pages, the keys rotated by their
+ * positions (rotary NULL: as they are), and in the same pass rotates the queries beside them.
+ *   K, V       read, [Hkv][n_tokens][d]
+ *   cache_k, cache_v   device, written at the new tokens' places only
+ *   Q, Q_out   both NULL, or read and written, [Hq][n_tokens][d] (Q_out may be Q); Q_out is
+ *              written for every token of a sequence, also where its page is missing.
+ *              A call with Q needs rotary.
+ * Errors: SGA_ERR_INVALID_ARG as for sga_rotary, and for a foreign or impossible batch.
+ */
+sga_status sga_cache_append(const sga_rows* K, const sga_rows* V, void* cache_k, void* cache_v, const sga_paged_batch* batch,
+                            int32_t Hkv, int32_t d, const sga_rotary_desc* rotary, const sga_rows* Q, const sga_rows* Q_out,
+                            int32_t Hq, int32_t dtype, void* stream);
+
+/*
+ * Attention of new tokens over the paged cache: for every head h and new token at position i
+ *   O[h][i] = sum_j softmax_j(scale * Q[h][i] . K[h / (Hq / Hkv)][j]) V[h / (Hq / Hkv)][j]
+ * over the tokens j < seq_len of its sequence that the mask lets it see, j <= i if causal.
+ * (sga_cache_append of the same batch first: the new tokens are in the cache.)
+ *   mask       host.  SGA_MASK_SLIDING or SGA_MASK_GLOBAL_LOCAL over mask->L tokens (window >= L:
+ *              every token); tokens at positions >= L are outside the mask: not seen, and
+ *              nothing is seen by them.  (The split of long sequences over the chip is sized by L or
+ *              by what the page table holds, whichever is less.)
+ *   Q          read, [Hq][n_tokens][d];  O written, same shape;  O must not overlap Q
+ *   cache_k, cache_v   read
+ *   Hq         a multiple of Hkv: consecutive query heads share a key head
+ *   lse        device, float [Hq][n_tokens], optional
+ *   workspace  device, 256-byte aligned, optional: partial states of split sequences.  With one of
+ *              sga_paged_workspace_bytes a few long sequences spread over the chip; without one, or
+ *              with a smaller one, each group of queries and key head is one workgroup's work.
+ * A token that sees nothing gets O = 0, lse = -inf.  Tokens that a query does not see have no
+ * influence on it, whatever their keys and values hold (infinities, NaN, memory never written).
+ * Supported: d = 32, 64, 128, 256.  Addresses and strides are multiples of 16 bytes.  Results do not
+ * depend on the order in which the work runs.  Kernels only: nothing is allocated and the host does not wait.
+ * Errors: SGA_ERR_INVALID_ARG, SGA_ERR_UNSUPPORTED (d, other mask kinds), SGA_ERR_OVERFLOW
+ * (n_tokens * Hq / Hkv / 16 + n_seqs of 2^24 and more: cut such a call by sequences).
+ */
+sga_status sga_paged_workspace_bytes(const sga_paged_batch* batch, const sga_mask_desc* mask, int32_t Hq, int32_t Hkv,
+                                     int32_t d, int32_t dtype, size_t* bytes_out);
+sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const void* cache_v, const sga_paged_batch* batch,
+                               const sga_mask_desc* mask, int32_t causal, const sga_rows* O, int32_t Hq, int32_t Hkv,
+                               int32_t d, float scale, int32_t dtype, float* lse, void* workspace, size_t workspace_bytes,
+                               void* stream);
 
 /*
  * Benchmark hook: timing of the dominant attention kernel of each forward call.

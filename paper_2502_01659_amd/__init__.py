@@ -16,7 +16,10 @@ from .binding import (SgaError, PATH_AUTO, PATH_GATHER, PATH_TILE, PATH_TILE_SPL
                       GRAPH_ROWS_SHARE_KEYS, GRAPH_ROWS_EVEN, graph_prepare, attention_forward_prepared, attention_accumulate_prepared,
                       sga_graph_prepare, sga_attention_forward_prepared,
                       sga_attention_accumulate_prepared,
-                      sga_static_scratch_init, sga_static_scratch_bytes, sga_attention_forward_static)
+                      sga_static_scratch_init, sga_static_scratch_bytes, sga_attention_forward_static,
+                      sga_rotary, sga_cache_append, sga_paged_workspace_bytes, sga_attention_paged,
+                      Rotary, rotary_frequencies, rotary, PagedBatch, cache_append,
+                      paged_workspace_bytes, alloc_paged_workspace, attention_paged)
 
 __all__ = [
     "SgaError", "PATH_AUTO", "PATH_GATHER", "PATH_TILE", "PATH_TILE_SPLIT", "load", "lib_path",
@@ -31,4 +34,7 @@ __all__ = [
     "graph_prepare", "attention_forward_prepared", "attention_accumulate_prepared",
     "sga_graph_prepare", "sga_attention_forward_prepared", "sga_attention_accumulate_prepared",
     "sga_static_scratch_init", "sga_static_scratch_bytes", "sga_attention_forward_static",
+    "sga_rotary", "sga_cache_append", "sga_paged_workspace_bytes", "sga_attention_paged",
+    "Rotary", "rotary_frequencies", "rotary", "PagedBatch", "cache_append",
+    "paged_workspace_bytes", "alloc_paged_workspace", "attention_paged",
 ]

@@ -48,6 +48,22 @@ class GraphPlan(ctypes.Structure):
     ]
 
 
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("head_stride", ctypes.c_int64), ("row_stride", ctypes.c_int64)]
+
+
+class _RotaryDesc(ctypes.Structure):
+    _fields_ = [("struct_bytes", ctypes.c_uint32), ("layout", ctypes.c_int32), ("channels", ctypes.c_int32),
+                ("magnitude", ctypes.c_float), ("frequencies", ctypes.c_void_p)]
+
+
+class _PagedBatch(ctypes.Structure):
+    _fields_ = [("struct_bytes", ctypes.c_uint32), ("n_seqs", ctypes.c_int32), ("n_tokens", ctypes.c_int64),
+                ("n_pages", ctypes.c_int64), ("page_stride", ctypes.c_int64), ("page_size", ctypes.c_int32),
+                ("pages_per_seq", ctypes.c_int32), ("page_table", ctypes.c_void_p), ("seq_ptr", ctypes.c_void_p),
+                ("seq_len", ctypes.c_void_p)]
+
+
 GRAPH_TILES_COVER_ALL, GRAPH_TILE_PARTS_FIT, GRAPH_ROW_CHUNKS_FIT, GRAPH_ROWS_SHARE_KEYS, GRAPH_ROWS_EVEN = 1, 2, 4, 8, 16
 
 
@@ -103,6 +119,16 @@ def load():
     lib.sga_attention_forward_static.restype = ctypes.c_int
     lib.sga_attention_forward_static.argtypes = [vp, vp, vp, vp, vp, vp, i64, i32, i32, f32, vp,
                                                  i32, vp, i64, i32]
+    rows, batch, rotary_desc = P(_Rows), P(_PagedBatch), P(_RotaryDesc)
+    lib.sga_rotary.restype = ctypes.c_int
+    lib.sga_rotary.argtypes = [rows, rows, vp, i64, i64, i32, i32, rotary_desc, i32, i32, vp]
+    lib.sga_cache_append.restype = ctypes.c_int
+    lib.sga_cache_append.argtypes = [rows, rows, vp, vp, batch, i32, i32, rotary_desc, rows, rows, i32, i32, vp]
+    lib.sga_paged_workspace_bytes.restype = ctypes.c_int
+    lib.sga_paged_workspace_bytes.argtypes = [batch, P(_MaskDesc), i32, i32, i32, i32, P(ctypes.c_size_t)]
+    lib.sga_attention_paged.restype = ctypes.c_int
+    lib.sga_attention_paged.argtypes = [rows, vp, vp, batch, P(_MaskDesc), i32, rows, i32, i32, i32, f32, i32, vp, vp,
+                                        ctypes.c_size_t, vp]
     lib.sga_profile_last_kernel.restype = ctypes.c_char_p
     lib.sga_profile_last_kernel.argtypes = []
     _lib = lib
@@ -225,6 +251,34 @@ def sga_profile_collect(capacity=4096):
 
 def sga_profile_last_kernel():
     return load().sga_profile_last_kernel().decode()
+
+
+def _ref(struct):
+    return ctypes.byref(struct) if struct is not None else None
+
+
+def sga_rotary(X, Y, positions, first, L, H, d, rotary_desc, inverse, dtype_code, stream):
+    """X, Y: _Rows or None; rotary_desc: _RotaryDesc or None"""
+    return load().sga_rotary(_ref(X), _ref(Y), positions, first, L, H, d, _ref(rotary_desc), inverse, dtype_code, stream)
+
+
+def sga_cache_append(K, V, cache_k, cache_v, batch, Hkv, d, rotary_desc, Q, Q_out, Hq, dtype_code, stream):
+    return load().sga_cache_append(_ref(K), _ref(V), cache_k, cache_v, _ref(batch), Hkv, d, _ref(rotary_desc), _ref(Q),
+                                   _ref(Q_out), Hq, dtype_code, stream)
+
+
+def sga_paged_workspace_bytes(batch, spec: MaskSpec, Hq, Hkv, d, dtype_code):
+    """-> (status, bytes)"""
+    dsc, out = _desc(spec), ctypes.c_size_t(0)
+    st = load().sga_paged_workspace_bytes(_ref(batch), ctypes.byref(dsc), Hq, Hkv, d, dtype_code, ctypes.byref(out))
+    return st, out.value
+
+
+def sga_attention_paged(Q, cache_k, cache_v, batch, spec, causal, O, Hq, Hkv, d, scale, dtype_code, lse, workspace,
+                        workspace_bytes_, stream):
+    dsc = _desc(spec)
+    return load().sga_attention_paged(_ref(Q), cache_k, cache_v, _ref(batch), ctypes.byref(dsc), causal, _ref(O), Hq, Hkv, d,
+                                      scale, dtype_code, lse, workspace, workspace_bytes_, stream)
 
 
 # ---- tensor-level helpers ---------------------------------------------------------
@@ -494,3 +548,269 @@ def attention_accumulate_prepared(Q, K, V, row_ptr, col_idx, scale, plan, worksp
     _prepared_call(sga_attention_accumulate_prepared, "sga_attention_accumulate_prepared", Q, K, V,
                    row_ptr, col_idx, scale, plan, O, lse, workspace, path)
     return O, lse
+
+
+# ---- serving: rotary positions, a paged cache, attention of new tokens over it --------------------
+_SERVING_CODE = {"torch.float32": 0, "torch.float16": 1, "torch.bfloat16": 2, "f32": 0, "f16": 1, "bf16": 2}
+_LAYOUT_CODE = {"half": 0, "interleaved": 1}
+
+
+def _serving_code(dtype):
+    code = _SERVING_CODE.get(str(dtype))
+    if code is None:
+        raise TypeError(f"unsupported storage dtype {dtype}")
+    return code
+
+
+class _here:
+    """Makes a tensor's device the current one, if it is not, and gives its current stream."""
+
+    def __init__(self, device):
+        import torch
+        self.device = device
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        import torch
+        if self.guard is not None:
+            self.guard.__enter__()
+        return torch.cuda.current_stream().cuda_stream
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _strides(t, name, written=False):
+    """_Rows of a [H, T, d] tensor whose channels lie side by side.  A written one has to hold each element once."""
+    H, T, d = t.shape
+    sh, st = (t.stride(0) if H > 1 else 0), (t.stride(1) if T > 1 else 0)
+    if d > 1 and t.stride(2) != 1:
+        raise ValueError(f"the channels of {name} must be contiguous")
+    if written and t.numel() > 0:
+        (low, n_low), (high, n_high) = sorted(((sh, H), (st, T))) if H > 1 and T > 1 else (((0, 1), (sh or st, max(H, T))))
+        if (n_low > 1 and low < d) or (n_high > 1 and high < low * (n_low - 1) + d):
+            raise ValueError(f"rows of {name} overlap")
+    return _Rows(t.data_ptr(), sh, st)
+
+
+def _check_tokens(t, name, like=None, T=None):
+    if t.dim() != 3 or not t.is_cuda:
+        raise ValueError(f"{name} must be a [H, T, d] device tensor")
+    if T is not None and t.shape[1] != T:
+        raise ValueError(f"{name} must have the batch's {T} tokens")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[2] != like.shape[2]):
+        raise ValueError(f"{name} must share dtype, device and head dimension")
+
+
+def rotary_frequencies(channels, base=10000.0, scaling=None, factor=1.0, original_length=0, slow_turns=1.0, fast_turns=32.0,
+                       device="cuda"):
+    """Frequencies base^(-2 i / channels), i < channels / 2, for Rotary, scaled for contexts `factor` times as long as the
+    trained `original_length`.  Returns (float64 [channels / 2], magnitude).
+
+    scaling  None        as they are
+             "linear"    positions shrink: every frequency divided by factor
+             "base"      the base grows by factor^(channels / (channels - 2)): the lowest frequency shrinks by
+                         factor, the highest stays
+             "parts"     by the turns that a pair makes over original_length: from fast_turns on its frequency
+                         stays, up to slow_turns it is divided by factor, between them in proportion; the magnitude
+                         is 1 + ln(factor) / 10
+    """
+    import math
+    import torch
+    if channels < 2 or channels % 2 != 0 or not base > 0 or not factor >= 1:
+        raise ValueError("channels must be even and positive, base positive, factor at least 1")
+    magnitude = 1.0
+    if scaling == "base":
+        if channels == 2:
+            raise ValueError("scaling of the base needs more than two channels")
+        base = base * factor ** (channels / (channels - 2))
+    f = base ** (-torch.arange(0, channels, 2, dtype=torch.float64) / channels)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "parts":
+        if original_length < 1 or not 0 <= slow_turns < fast_turns:
+            raise ValueError("scaling by parts needs the trained length and slow_turns < fast_turns")
+        keep = ((original_length * f / (2 * math.pi) - slow_turns) / (fast_turns - slow_turns)).clamp(0.0, 1.0)
+        f = f * (keep + (1.0 - keep) / factor)
+        magnitude = 1.0 + 0.1 * math.log(factor)
+    elif scaling not in (None, "base"):
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return f.to(device), magnitude
+
+
+class Rotary:
+    """Which channels turn, how fast, and in which layout (sga_rotary_desc).  frequencies: float64 [channels / 2] on the
+    device, radians per position; layout "half" (channels i and i + channels / 2) or "interleaved" (2 i and 2 i + 1)."""
+
+    def __init__(self, frequencies, layout="half", magnitude=1.0):
+        if str(frequencies.dtype) != "torch.float64" or frequencies.dim() != 1 or frequencies.numel() < 1 \
+                or not frequencies.is_contiguous() or not frequencies.is_cuda:
+            raise ValueError("frequencies must be a contiguous float64 device tensor [channels / 2]")
+        if layout not in _LAYOUT_CODE:
+            raise ValueError(f"unknown layout {layout!r}")
+        self.frequencies = frequencies
+        self.channels = 2 * frequencies.numel()
+        self._desc = _RotaryDesc(ctypes.sizeof(_RotaryDesc), _LAYOUT_CODE[layout], self.channels, float(magnitude),
+                                 frequencies.data_ptr())
+
+    def _check(self, t):
+        if self.frequencies.device != t.device:
+            raise ValueError("the rotary frequencies are on another device")
+
+
+def rotary(X, rotary, positions=None, first=0, inverse=False, out=None):
+    """Rotate [H, L, d] by position: row t has positions[t] (int64 [L]), or first + t.  inverse=True turns back: of a
+    gradient, that is the gradient of the input.  out may be X."""
+    _check_tokens(X, "X")
+    rotary._check(X)
+    H, L, d = X.shape
+    if positions is not None and (str(positions.dtype) != "torch.int64" or positions.shape != (L,)
+                                  or not positions.is_contiguous() or positions.device != X.device):
+        raise ValueError("positions must be contiguous int64 [L] on X's device")
+    if out is None:
+        import torch
+        out = torch.empty_like(X)
+    elif out.shape != X.shape or out.dtype != X.dtype or out.device != X.device:
+        raise ValueError("out must match X in shape, dtype and device")
+    x, y, code = _strides(X, "X"), _strides(out, "out", written=True), _serving_code(X.dtype)
+    with _here(X.device) as stream:
+        st = sga_rotary(x, y, positions.data_ptr() if positions is not None else None, int(first), L, H, d, rotary._desc,
+                        int(bool(inverse)), code, stream)
+    if st != 0:
+        raise SgaError(st, "sga_rotary")
+    return out
+
+
+class PagedBatch:
+    """New tokens of several sequences and the pages of their keys and values (sga_paged_batch).
+
+    page_table  int32 [S, columns]: page of tokens c * page_size .. of a sequence, -1 where there is none
+    seq_ptr     int64 [S + 1]: sequence s has rows seq_ptr[s] .. seq_ptr[s + 1] - 1 of the packed tensors
+    seq_len     int32 [S]: tokens of the sequence, the new ones among them
+    n_tokens    rows of the packed tensors (rows behind the last sequence are padding)
+    page_size, n_pages   of the caches [n_pages, Hkv, page_size, d]
+    The arrays are read when the calls run, so a program may write new lengths and pages into them.
+    """
+
+    def __init__(self, page_table, seq_ptr, seq_len, n_tokens, page_size, n_pages):
+        if str(page_table.dtype) != "torch.int32" or page_table.dim() != 2 or not page_table.is_contiguous():
+            raise ValueError("page_table must be contiguous int32 [S, columns]")
+        S, columns = page_table.shape
+        if str(seq_ptr.dtype) != "torch.int64" or seq_ptr.shape != (S + 1,) or not seq_ptr.is_contiguous():
+            raise ValueError("seq_ptr must be contiguous int64 [S + 1]")
+        if str(seq_len.dtype) != "torch.int32" or seq_len.shape != (S,) or not seq_len.is_contiguous():
+            raise ValueError("seq_len must be contiguous int32 [S]")
+        if not page_table.is_cuda or seq_ptr.device != page_table.device or seq_len.device != page_table.device:
+            raise ValueError("page_table, seq_ptr and seq_len must be tensors of one device")
+        self.page_table, self.seq_ptr, self.seq_len = page_table, seq_ptr, seq_len
+        self.n_tokens, self.page_size, self.n_pages = int(n_tokens), int(page_size), int(n_pages)
+        self.device = page_table.device
+        self._structs = {}
+
+    def _struct(self, page_stride):
+        s = self._structs.get(page_stride)
+        if s is None:
+            S, columns = self.page_table.shape
+            s = _PagedBatch(ctypes.sizeof(_PagedBatch), S, self.n_tokens, self.n_pages, page_stride, self.page_size, columns,
+                            self.page_table.data_ptr(), self.seq_ptr.data_ptr(), self.seq_len.data_ptr())
+            self._structs[page_stride] = s
+        return s
+
+    def _caches(self, like, cache_k, cache_v):
+        """The batch's record for these caches, and their key heads."""
+        if like.device != self.device:
+            raise ValueError("the batch is on another device")
+        d, page = like.shape[2], self.page_size
+        for t in (cache_k, cache_v):
+            if t.dim() != 4 or t.shape != cache_k.shape or t.shape[0] != self.n_pages or t.shape[2] != page or t.shape[3] != d:
+                raise ValueError("the caches must both be [n_pages, Hkv, page_size, d]")
+            if t.dtype != like.dtype or t.device != like.device:
+                raise ValueError("the caches must share dtype and device with the tokens")
+            sp, sh, st, sc = t.stride()
+            if sc != 1 or (page > 1 and st != d) or (t.shape[1] > 1 and sh != page * d):
+                raise ValueError("every page of a cache must be contiguous")
+            if self.n_pages > 1 and (sp != cache_k.stride(0) or sp < t.shape[1] * page * d):
+                raise ValueError("the pages of a cache must not overlap, and both caches must have them at one distance")
+        Hkv = cache_k.shape[1]
+        return self._struct(cache_k.stride(0) if self.n_pages > 1 else Hkv * page * d), Hkv
+
+
+def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None):
+    """Write the batch's new keys (rotated) and values, [Hkv, n_tokens, d], into their pages, and rotate the queries Q
+    beside them.  Returns Q_out (which may be Q) if Q is given."""
+    _check_tokens(K, "K", T=batch.n_tokens)
+    _check_tokens(V, "V", like=K, T=batch.n_tokens)
+    struct, Hkv = batch._caches(K, cache_k, cache_v)
+    if K.shape[0] != Hkv or V.shape[0] != Hkv:
+        raise ValueError("K and V must have the caches' heads")
+    q = q_out = None
+    Hq = 0
+    if rotary is not None:
+        rotary._check(K)
+    if Q is not None:
+        if rotary is None:
+            raise ValueError("queries are rotated: a call with Q needs rotary")
+        _check_tokens(Q, "Q", like=K, T=batch.n_tokens)
+        if Q_out is None:
+            import torch
+            Q_out = torch.empty_like(Q)
+        else:
+            _check_tokens(Q_out, "Q_out", like=Q, T=batch.n_tokens)
+            if Q_out.shape != Q.shape:
+                raise ValueError("Q_out must match Q")
+        q, q_out, Hq = _strides(Q, "Q"), _strides(Q_out, "Q_out", written=True), Q.shape[0]
+    elif Q_out is not None:
+        raise ValueError("Q_out without Q")
+    k, v, code = _strides(K, "K"), _strides(V, "V"), _serving_code(K.dtype)
+    with _here(K.device) as stream:
+        st = sga_cache_append(k, v, cache_k.data_ptr(), cache_v.data_ptr(), struct, Hkv, K.shape[2],
+                              rotary._desc if rotary is not None else None, q, q_out, Hq, code, stream)
+    if st != 0:
+        raise SgaError(st, "sga_cache_append")
+    return Q_out
+
+
+def paged_workspace_bytes(batch, spec: MaskSpec, Hq, Hkv, d, dtype) -> int:
+    st, n = sga_paged_workspace_bytes(batch._struct(Hkv * batch.page_size * d), spec, Hq, Hkv, d, _serving_code(dtype))
+    if st != 0:
+        raise SgaError(st, "sga_paged_workspace_bytes")
+    return n
+
+
+def alloc_paged_workspace(batch, spec: MaskSpec, Hq, Hkv, d, dtype):
+    """Workspace for attention_paged calls of this batch and mask (calls that overlap in time need one each)."""
+    import torch
+    return torch.empty(paged_workspace_bytes(batch, spec, Hq, Hkv, d, dtype), dtype=torch.uint8, device=batch.device)
+
+
+def attention_paged(Q, cache_k, cache_v, batch, spec: MaskSpec, scale, causal=True, O=None, lse=None, workspace=None,
+                    want_lse=False):
+    """Attention of the batch's new tokens, Q [Hq, n_tokens, d], over the paged cache under a sliding or global + local mask
+    of spec.L tokens (window >= L: every token), of earlier tokens only if causal.  Consecutive Hq / Hkv query heads share
+    a key head.  Returns O (and lse [Hq, n_tokens] if requested); a token that sees nothing has O = 0, lse = -inf."""
+    import torch
+    _check_tokens(Q, "Q", T=batch.n_tokens)
+    struct, Hkv = batch._caches(Q, cache_k, cache_v)
+    Hq, T, d = Q.shape
+    if O is None:
+        O = torch.empty_like(Q)
+    elif O.shape != Q.shape or O.dtype != Q.dtype or O.device != Q.device:
+        raise ValueError("O must match Q in shape, dtype and device")
+    if want_lse and lse is None:
+        lse = torch.empty((Hq, T), dtype=torch.float32, device=Q.device)
+    if lse is not None and (lse.shape != (Hq, T) or lse.dtype != torch.float32 or not lse.is_contiguous()
+                            or lse.device != Q.device):
+        raise ValueError("lse must be contiguous float32 [Hq, n_tokens] on Q's device")
+    ws_ptr, ws_n = None, 0
+    if workspace is not None and workspace.numel() > 0:
+        if workspace.device != Q.device or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on Q's device")
+        ws_ptr, ws_n = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    q, o, code = _strides(Q, "Q"), _strides(O, "O", written=True), _serving_code(Q.dtype)
+    with _here(Q.device) as stream:
+        st = sga_attention_paged(q, cache_k.data_ptr(), cache_v.data_ptr(), struct, spec, int(bool(causal)), o, Hq, Hkv, d,
+                                 float(scale), code, lse.data_ptr() if lse is not None else None, ws_ptr, ws_n, stream)
+    if st != 0:
+        raise SgaError(st, "sga_attention_paged")
+    return (O, lse) if lse is not None else O

@@ -7,7 +7,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsga.so")
 
-SOURCES = ["api.hip", "mask_builder.hip", "attention_gather.hip", "attention_tile.hip"]
+SOURCES = ["api.hip", "mask_builder.hip", "attention_gather.hip", "attention_tile.hip",
+           "paged_cache.hip", "attention_paged.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -1,5 +1,6 @@
 // C ABI of libsga.so: argument validation and dispatch.  See include/sga.h for the contract.
 #include "sga_internal.h"
+#include "serving.h"
 
 #include <atomic>
 #include <cstring>
@@ -437,6 +438,184 @@ sga_status sga_attention_forward_static(const void* Q, const void* K, const void
   if (found != SGA_OK) return found;
   return run_explicit_call(Q, K, V, row_ptr, col_idx, O, L, H, d, scale, stream, dtype, lse, ws,
                            kScratchBytes, path, false);
+}
+
+}  // extern "C"
+
+// ---- serving ----------------------------------------------------------------------------------
+namespace {
+
+int element_bytes(int32_t dtype) { return dtype == SGA_F32 ? 4 : 2; }
+
+bool aligned_to(const void* p, int bytes) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(bytes - 1)) == 0; }
+
+bool valid_rows(const sga_rows* x, int32_t dtype) { return x && x->data && aligned_to(x->data, element_bytes(dtype)); }
+
+// ... whose address and strides are multiples of 16 bytes
+bool wide_rows(const sga_rows* x, int32_t dtype) {
+  const int64_t step = 16 / element_bytes(dtype);
+  return x && x->data && aligned16(x->data) && x->head_stride % step == 0 && x->row_stride % step == 0;
+}
+
+bool serving_dtype(int32_t dtype) { return dtype == SGA_F32 || dtype == SGA_F16 || dtype == SGA_BF16; }
+
+bool valid_rotary(const sga_rotary_desc* r, int32_t d) {
+  return r && r->struct_bytes == sizeof(sga_rotary_desc) &&
+         (r->layout == SGA_ROTARY_HALF || r->layout == SGA_ROTARY_INTERLEAVED) && r->channels >= 2 && r->channels <= d &&
+         r->channels % 2 == 0 && r->frequencies && aligned_to(r->frequencies, 8);
+}
+
+RotaryArgs rotary_args(const sga_rotary_desc* r, int32_t inverse) {
+  if (!r) return RotaryArgs{nullptr, 1.f, 0, 0, 0};
+  return RotaryArgs{r->frequencies, r->magnitude, r->channels, r->layout == SGA_ROTARY_INTERLEAVED, inverse != 0};
+}
+
+RowsArg rows_arg(const sga_rows& src, const sga_rows& dst, int32_t heads, bool rotate) {
+  return RowsArg{src.data, dst.data, src.head_stride, src.row_stride, dst.head_stride, dst.row_stride, heads, rotate, 0};
+}
+
+// In place means the same elements: the same address with other strides would mix them.
+bool apart_or_same(const sga_rows& x, const sga_rows& y) {
+  return x.data != y.data || (x.head_stride == y.head_stride && x.row_stride == y.row_stride);
+}
+
+constexpr int32_t kMaxRotaryDim = 1024;
+
+// What a batch has to be whatever it is used for.  (A batch without tokens needs no arrays.)
+bool valid_batch(const sga_paged_batch* b, int32_t Hkv, int32_t d) {
+  if (!b || b->struct_bytes != sizeof(sga_paged_batch) || b->n_seqs < 0) return false;
+  if (b->n_tokens < 0 || b->n_tokens >= (int64_t(1) << 31)) return false;
+  if (b->n_pages < 1 || b->n_pages >= (int64_t(1) << 31) || b->page_size < 1 || b->page_size > 65536) return false;
+  if (b->pages_per_seq < 1 || (int64_t)b->pages_per_seq * b->page_size > (int64_t(1) << 31) - 1024) return false;
+  if (b->page_stride < (int64_t)Hkv * b->page_size * d) return false;
+  if (b->n_tokens == 0 || b->n_seqs == 0) return true;
+  return b->page_table && b->seq_ptr && b->seq_len && aligned_to(b->page_table, 4) && aligned_to(b->seq_len, 4) &&
+         aligned_to(b->seq_ptr, 8);
+}
+
+PagedArgs batch_args(const sga_paged_batch& b) {
+  PagedArgs a{};
+  a.page_table = b.page_table; a.seq_ptr = b.seq_ptr; a.seq_len = b.seq_len;
+  a.page_stride = b.page_stride;
+  a.n_pages = (uint32_t)b.n_pages;
+  a.n_seqs = b.n_seqs; a.n_tokens = (int32_t)b.n_tokens; a.pages_per_seq = b.pages_per_seq;
+  a.page = fast_div((uint32_t)b.page_size);
+  return a;
+}
+
+// The part of an attention call that its workspace depends on.
+sga_status paged_shape(const sga_paged_batch* batch, const sga_mask_desc* mask, int32_t causal, int32_t Hq, int32_t Hkv,
+                       int32_t d, int32_t dtype, PagedAttention& a) {
+  if (!serving_dtype(dtype) || Hkv < 1 || Hq < 1 || Hq > 65535 || Hq % Hkv != 0) return SGA_ERR_INVALID_ARG;
+  if (d != 32 && d != 64 && d != 128 && d != 256) return SGA_ERR_UNSUPPORTED;
+  if (!valid_batch(batch, Hkv, d)) return SGA_ERR_INVALID_ARG;
+  const sga_status st = mask_validate(mask);
+  if (st != SGA_OK) return st;
+  if (mask->kind != SGA_MASK_SLIDING && mask->kind != SGA_MASK_GLOBAL_LOCAL) return SGA_ERR_UNSUPPORTED;
+  a.batch = batch_args(*batch);
+  a.Hq = Hq; a.Hkv = Hkv; a.group = fast_div((uint32_t)(Hq / Hkv));
+  a.L = (int32_t)mask->L;
+  a.window = mask->window;
+  a.n_global = mask->kind == SGA_MASK_GLOBAL_LOCAL ? mask->n_global : 0;
+  a.causal = causal != 0;
+  a.d = d; a.dtype = dtype;
+  return SGA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+sga_status sga_rotary(const sga_rows* X, const sga_rows* Y, const int64_t* positions, int64_t first, int64_t L, int32_t H,
+                      int32_t d, const sga_rotary_desc* rotary, int32_t inverse, int32_t dtype, void* stream) {
+  if (!X || !Y || !serving_dtype(dtype) || L < 0 || L >= (int64_t(1) << 31) || H < 1 || H > 65535) return SGA_ERR_INVALID_ARG;
+  if (d < 2 || d > kMaxRotaryDim || !valid_rotary(rotary, d)) return SGA_ERR_INVALID_ARG;
+  if (L == 0) return SGA_OK;
+  if (!valid_rows(X, dtype) || !valid_rows(Y, dtype) || !apart_or_same(*X, *Y)) return SGA_ERR_INVALID_ARG;
+  if (positions && !aligned_to(positions, 8)) return SGA_ERR_INVALID_ARG;
+  (void)hipGetLastError();   // drop stale errors of earlier, unrelated runtime calls
+  RotateArgs a{};
+  a.tensor[0] = rows_arg(*X, *Y, H, true);
+  a.n_tensors = 1;
+  a.n_rows = (int32_t)L; a.d = d;
+  a.positions = positions; a.first = first;
+  a.rotary = rotary_args(rotary, inverse);
+  a.dtype = dtype;
+  a.stream = static_cast<hipStream_t>(stream);
+  return launch_rotate(a);
+}
+
+sga_status sga_cache_append(const sga_rows* K, const sga_rows* V, void* cache_k, void* cache_v, const sga_paged_batch* batch,
+                            int32_t Hkv, int32_t d, const sga_rotary_desc* rotary, const sga_rows* Q, const sga_rows* Q_out,
+                            int32_t Hq, int32_t dtype, void* stream) {
+  if (!K || !V || !serving_dtype(dtype) || Hkv < 1 || Hkv > 65535 || d < 2 || d > kMaxRotaryDim) return SGA_ERR_INVALID_ARG;
+  if ((rotary && !valid_rotary(rotary, d)) || !valid_batch(batch, Hkv, d)) return SGA_ERR_INVALID_ARG;
+  if ((Q != nullptr) != (Q_out != nullptr) || (Q && (!rotary || Hq < 1 || Hq > 65535))) return SGA_ERR_INVALID_ARG;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return SGA_OK;
+  if (!valid_rows(K, dtype) || !valid_rows(V, dtype) || !cache_k || !cache_v) return SGA_ERR_INVALID_ARG;
+  if (!aligned_to(cache_k, element_bytes(dtype)) || !aligned_to(cache_v, element_bytes(dtype))) return SGA_ERR_INVALID_ARG;
+  if (Q && (!valid_rows(Q, dtype) || !valid_rows(Q_out, dtype) || !apart_or_same(*Q, *Q_out))) return SGA_ERR_INVALID_ARG;
+  (void)hipGetLastError();
+  RotateArgs a{};
+  const int64_t head = (int64_t)batch->page_size * d;      // from head to head within a page
+  int n = 0;
+  if (Q) a.tensor[n++] = rows_arg(*Q, *Q_out, Hq, true);
+  a.tensor[n] = rows_arg(*K, sga_rows{cache_k, head, 0}, Hkv, rotary != nullptr);
+  a.tensor[n++].paged = 1;
+  a.tensor[n] = rows_arg(*V, sga_rows{cache_v, head, 0}, Hkv, false);
+  a.tensor[n++].paged = 1;
+  a.n_tensors = n;
+  a.n_rows = (int32_t)batch->n_tokens; a.d = d;
+  a.rotary = rotary_args(rotary, 0);
+  a.batch = batch_args(*batch);
+  a.dtype = dtype;
+  a.stream = static_cast<hipStream_t>(stream);
+  return launch_rotate(a);
+}
+
+sga_status sga_paged_workspace_bytes(const sga_paged_batch* batch, const sga_mask_desc* mask, int32_t Hq, int32_t Hkv,
+                                     int32_t d, int32_t dtype, size_t* bytes_out) {
+  if (!bytes_out) return SGA_ERR_INVALID_ARG;
+  PagedAttention a{};
+  const sga_status st = paged_shape(batch, mask, 0, Hq, Hkv, d, dtype, a);
+  if (st != SGA_OK) return st;
+  size_t most = 0;
+  for (a.causal = 0; a.causal < 2 && batch->n_tokens > 0 && batch->n_seqs > 0; ++a.causal) {
+    const PagedPlan p = plan_paged(a);
+    if (p.slots == 0) return SGA_ERR_OVERFLOW;
+    most = p.bytes > most ? p.bytes : most;
+  }
+  *bytes_out = most;
+  return SGA_OK;
+}
+
+sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const void* cache_v, const sga_paged_batch* batch,
+                               const sga_mask_desc* mask, int32_t causal, const sga_rows* O, int32_t Hq, int32_t Hkv,
+                               int32_t d, float scale, int32_t dtype, float* lse, void* workspace, size_t workspace_bytes,
+                               void* stream) {
+  if (!Q || !O) return SGA_ERR_INVALID_ARG;
+  PagedAttention a{};
+  const sga_status st = paged_shape(batch, mask, causal, Hq, Hkv, d, dtype, a);
+  if (st != SGA_OK) return st;
+  if (workspace ? (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 : workspace_bytes != 0) return SGA_ERR_INVALID_ARG;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return SGA_OK;
+  if (!wide_rows(Q, dtype) || !wide_rows(O, dtype) || Q->data == O->data) return SGA_ERR_INVALID_ARG;
+  if (!cache_k || !cache_v || !aligned16(cache_k) || !aligned16(cache_v)) return SGA_ERR_INVALID_ARG;
+  if (batch->page_stride % (16 / element_bytes(dtype)) != 0 || !aligned_to(lse, 4)) return SGA_ERR_INVALID_ARG;
+  const PagedPlan plan = plan_paged(a);
+  if (plan.slots == 0) return SGA_ERR_OVERFLOW;
+  (void)hipGetLastError();
+  a.Q = Q->data; a.q_head = Q->head_stride; a.q_row = Q->row_stride;
+  a.O = O->data; a.o_head = O->head_stride; a.o_row = O->row_stride;
+  a.cache_k = cache_k; a.cache_v = cache_v;
+  a.lse = lse;
+  a.scale = scale;
+  a.slots = plan.slots;
+  const bool split = plan.splits > 1 && workspace_bytes >= plan.bytes;
+  a.splits = split ? plan.splits : 1;
+  a.partials = split ? static_cast<float*>(workspace) : nullptr;
+  a.stream = static_cast<hipStream_t>(stream);
+  return launch_paged(a);
 }
 
 }  // extern "C"

@@ -1,0 +1,437 @@
+"""Rotary positions, appending to a paged cache and attention over it, against their definitions in 64 bits."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_01659_amd as sga
+import serving_oracle as S
+from sga_inputs import MaskSpec, KIND_GLOBAL_LOCAL, KIND_SLIDING
+
+pytestmark = pytest.mark.gpu
+DTYPE = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def host(t):
+    return t.double().cpu().numpy()
+
+
+def tokens(H, T, d, dtype, seed, layout="token"):
+    """[H, T, d]: a view of [T, H, d] ("token"), of [T, H + 3, d + 16] ("slice"), or contiguous ("head")."""
+    g = torch.Generator().manual_seed(seed)
+    if layout == "head":
+        x = torch.randn(H, T, d, generator=g)
+        return x.to(DTYPE[dtype]).cuda()
+    extra = (3, 16) if layout == "slice" else (0, 0)
+    x = torch.randn(T, H + extra[0], d + extra[1], generator=g).to(DTYPE[dtype]).cuda()
+    return x[:, :H, :d].transpose(0, 1)
+
+
+def within(got, want, bar):
+    got = host(got) if isinstance(got, torch.Tensor) else got
+    assert np.array_equal(np.isfinite(got), np.isfinite(want))
+    fine = np.isfinite(want)
+    over = np.abs(got[fine] - want[fine]) - bar[fine]
+    assert over.size == 0 or over.max() <= 0, (float(over.max()), float((np.abs(got[fine] - want[fine]) / (bar[fine] + 1e-300)).max()))
+    return True
+
+
+# ---- rotary ---------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("H,T,d,channels,memory", [
+    (1, 1, 64, 64, "head"), (32, 1, 128, 128, "token"), (3, 65, 128, 64, "token"), (8, 257, 64, 32, "head"),
+    (5, 33, 256, 256, "slice"), (2, 9, 32, 16, "token"), (4, 31, 80, 20, "token"), (3, 17, 7, 6, "head"),
+    (1, 3000, 64, 64, "token"), (7, 13, 96, 2, "slice"), (2, 5, 1024, 1024, "head"),
+])
+def test_rotary(dtype, layout, H, T, d, channels, memory):
+    freqs, _ = sga.rotary_frequencies(channels)
+    rot = sga.Rotary(freqs, layout=layout, magnitude=1.25)
+    x = tokens(H, T, d, dtype, T + d, memory)
+    for inverse, positions, first in ((False, None, 0), (True, None, 131071), (False, torch.arange(T).cuda() * 7 - 3, 0)):
+        print("rotary", dtype, layout, H, T, d, channels, memory, inverse, flush=True)
+        at = positions.cpu().numpy() if positions is not None else first + np.arange(T)
+        want, size = S.rotate(host(x), at, freqs.cpu().numpy(), layout, 1.25, inverse)
+        bar = S.rotate_bar(want, size, dtype)
+        bar[..., channels:] = 0                                # passed on as they are
+        got = sga.rotary(x, rot, positions=positions, first=first, inverse=inverse)
+        assert got.shape == x.shape and within(got, want, bar)
+        same = x.clone() if memory != "slice" else tokens(H, T, d, dtype, T + d, memory)
+        assert sga.rotary(same, rot, positions=positions, first=first, inverse=inverse, out=same) is same
+        assert torch.equal(same, got)
+
+
+def test_rotary_far_positions():
+    """The angles keep their 2^-25 at 160 million tokens and at 2^50."""
+    freqs, _ = sga.rotary_frequencies(64)
+    x = tokens(2, 4096, 64, "f32", 5)
+    for first in (160_000_000 - 4096, (1 << 31) - 5000, -(1 << 33), (1 << 50) + 12345):
+        # the definition's product in exact integers: a frequency is m / 2^e, an angle modulo 2 pi needs pi to 160 bits
+        two_pi = 2 * 314159265358979323846264338327950288419716939937510582097494459230781640628620899 * 10 ** 10
+        angle = np.zeros((4096, 32))
+        for k, f in enumerate(freqs.cpu().tolist()):
+            num, den = f.as_integer_ratio()
+            unit = 10 ** 90
+            for t in range(0, 4096, 64):
+                turns = (num * (first + t) * unit // den) % two_pi
+                angle[t, k] = float(turns) / float(unit)
+        rows = np.arange(0, 4096, 64)
+        a, b = host(x)[:, rows, :32], host(x)[:, rows, 32:]
+        cos, sin = np.cos(angle[rows]), np.sin(angle[rows])
+        want = np.concatenate((a * cos - b * sin, a * sin + b * cos), -1)
+        size = np.concatenate((np.abs(a) + np.abs(b),) * 2, -1)
+        got = sga.rotary(x, sga.Rotary(freqs), first=first)
+        assert within(host(got)[:, rows], want, S.rotate_bar(want, size, "f32"))
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotary_gradient(layout):
+    """The inverse of G is the gradient of <G, rotary(X)>: against differences in 64 bits and against the product."""
+    freqs, magnitude = sga.rotary_frequencies(32, scaling="parts", factor=8.0, original_length=4096)
+    rot = sga.Rotary(freqs, layout=layout, magnitude=magnitude)
+    x, g = tokens(3, 70, 64, "f32", 1), tokens(3, 70, 64, "f32", 2)
+    dx = host(sga.rotary(g, rot, first=900, inverse=True))
+    f = lambda z: (S.rotate(z, 900 + np.arange(70), freqs.cpu().numpy(), layout, magnitude)[0] * host(g)).sum()
+    X = host(x)
+    for h, t, c in ((0, 0, 0), (1, 33, 17), (2, 69, 31), (0, 5, 40), (2, 1, 63)):
+        up, down = X.copy(), X.copy()
+        up[h, t, c] += 1e-3
+        down[h, t, c] -= 1e-3
+        # linear in x: the difference quotient is exact but for 64-bit rounding of the sum
+        assert abs((f(up) - f(down)) / 2e-3 - dx[h, t, c]) <= 1e-6 * (1 + abs(dx[h, t, c]))
+    y = host(sga.rotary(x, rot, first=900))
+    # <G, Y> = <dX, X>: both sides are sums of 13,440 products, each off by less than 2^-20 of its pair's sizes
+    assert abs((host(g) * y).sum() - (dx * X).sum()) <= 2.0 ** -20 * np.abs(X).sum() * 4
+
+
+def test_rotary_without_rows_and_capture():
+    freqs, _ = sga.rotary_frequencies(64)
+    rot = sga.Rotary(freqs)
+    assert sga.rotary(torch.empty(4, 0, 64, device="cuda"), rot).shape == (4, 0, 64)
+    x, out = tokens(8, 300, 64, "f16", 3), torch.empty(8, 300, 64, dtype=torch.float16, device="cuda")
+    at = torch.arange(300).cuda()
+    sga.rotary(x, rot, positions=at, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sga.rotary(x, rot, positions=at, out=out)
+    for step in range(3):
+        at += 1000
+        x.mul_(0.5)
+        graph.replay()
+        assert torch.equal(out, sga.rotary(x, rot, positions=at))
+
+
+# ---- append ---------------------------------------------------------------------------------------
+def batch_of(new, length, page, spare=2, padding=0, seed=0, columns=None, missing=()):
+    """Random page tables for sequences of these lengths; `missing`: (sequence, column, entry) put in afterwards."""
+    rng = np.random.default_rng(seed)
+    columns = columns or max(1, max([-(-n // page) for n in length], default=1))
+    need = [-(-n // page) for n in length]
+    n_pages = max(1, sum(need) + spare)
+    order = rng.permutation(n_pages)
+    table = np.full((len(new), columns), -1, dtype=np.int32)
+    at = 0
+    for s, n in enumerate(need):
+        table[s, :n], at = order[at:at + n], at + n
+    for s, c, entry in missing:
+        table[s, c] = entry
+    ptr = np.concatenate(([0], np.cumsum(new))).astype(np.int64)
+    T = int(ptr[-1]) + padding
+    dev = [torch.from_numpy(x).cuda() for x in (table, ptr, np.array(length, dtype=np.int32))]
+    return sga.PagedBatch(*dev, T, page, n_pages), table, ptr, np.array(length), n_pages, T
+
+
+def caches(n_pages, Hkv, page, d, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    return [torch.randn(n_pages, Hkv, page, d, generator=g).to(DTYPE[dtype]).cuda() for _ in range(2)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("new,length,page,Hq,Hkv,d,channels,layout,padding", [
+    ([1], [1], 16, 4, 1, 64, 64, "half", 0),
+    ([1] * 70, list(range(1, 71)), 16, 8, 8, 128, 128, "half", 3),
+    ([5, 0, 130, 1], [5, 9, 300, 64], 24, 6, 2, 128, 64, "interleaved", 7),
+    ([33, 2], [33, 1000], 1, 3, 3, 64, 64, "half", 0),
+    ([40, 41], [100, 41], 7, 2, 1, 80, 20, "half", 1),
+    ([300], [700], 256, 16, 4, 256, 256, "interleaved", 0),
+    ([64, 1, 1, 17], [64, 65, 2000, 33], 64, 4, 4, 32, 32, "half", 0),
+])
+def test_append(dtype, new, length, page, Hq, Hkv, d, channels, layout, padding):
+    print("append", dtype, new[:4], page, d, flush=True)
+    batch, table, ptr, lens, n_pages, T = batch_of(new, length, page, padding=padding, seed=len(new))
+    ck, cv = caches(n_pages, Hkv, page, d, dtype, 9)
+    K, V, Q = tokens(Hkv, T, d, dtype, 1), tokens(Hkv, T, d, dtype, 2, "slice"), tokens(Hq, T, d, dtype, 3)
+    freqs, magnitude = sga.rotary_frequencies(channels, scaling="linear", factor=2.0)
+    want = S.append(host(K), host(V), host(ck), host(cv), table, ptr, lens, freqs.cpu().numpy(), layout, magnitude, host(Q))
+    out = torch.full((Hq, T, d), 7.0, dtype=DTYPE[dtype], device="cuda")
+    sga.cache_append(K, V, ck, cv, batch, rotary=sga.Rotary(freqs, layout, magnitude), Q=Q, Q_out=out)
+    bar = S.rotate_bar(want[0], want[2], dtype)
+    bar[want[2] == 0] = 0                                     # not written, or not turned
+    assert within(ck, want[0], bar)
+    assert np.array_equal(host(cv), want[1])
+    q = host(out)
+    real = np.isfinite(want[3])
+    assert (q[~real] == 7.0).all()                           # padding rows are left as they were
+    assert within(q[real], want[3][real], S.rotate_bar(want[3], want[4], dtype)[real])
+    # without rotation, the values as they are
+    ck2, cv2 = caches(n_pages, Hkv, page, d, dtype, 9)
+    plain = S.append(host(K), host(V), host(ck2), host(cv2), table, ptr, lens, None, "half", 1.0)
+    sga.cache_append(K, V, ck2, cv2, batch)
+    assert np.array_equal(host(ck2), plain[0]) and np.array_equal(host(cv2), plain[1])
+    # queries in place
+    mine = Q.clone()
+    assert sga.cache_append(K, V, ck2, cv2, batch, rotary=sga.Rotary(freqs, layout, magnitude), Q=mine, Q_out=mine) is mine
+    assert torch.equal(mine[:, :int(ptr[-1])], out[:, :int(ptr[-1])])
+
+
+def test_append_passes_over_missing_pages():
+    """No page, a page that does not exist, positions before the first token and behind the table's last column."""
+    batch, table, ptr, lens, n_pages, T = batch_of([40, 30, 50], [40, 64, 60], 16, columns=4,
+                                                   missing=[(0, 1, -1), (1, 3, 10 ** 6), (2, 3, -7)])
+    batch.seq_len[1] = 20                                     # its first ten tokens lie before position 0
+    batch.seq_len[2] = 70                                     # its last six behind column 3
+    lens[1], lens[2] = 20, 70
+    ck, cv = caches(n_pages, 2, 16, 64, "f32", 4)
+    K, V, Q = (tokens(2, T, 64, "f32", s) for s in (1, 2, 3))
+    freqs, _ = sga.rotary_frequencies(64)
+    want = S.append(host(K), host(V), host(ck), host(cv), table, ptr, lens, freqs.cpu().numpy(), "half", 1.0, host(Q))
+    sga.cache_append(K, V, ck, cv, batch, rotary=sga.Rotary(freqs))
+    bar = S.rotate_bar(want[0], want[2], "f32")
+    bar[want[2] == 0] = 0
+    assert within(ck, want[0], bar) and np.array_equal(host(cv), want[1])
+
+
+# ---- attention ------------------------------------------------------------------------------------
+def check_attention(dtype, new, length, page, Hq, Hkv, d, spec, causal=True, padding=0, memory="token", missing=(), scale=None,
+                    workspace=True, rotten=True, seed=0, change=None, columns=None):
+    print("attend", dtype, new[:6], length[:6], page, Hq, Hkv, d, spec, causal, flush=True)
+    batch, table, ptr, lens, n_pages, T = batch_of(new, length, page, padding=padding, seed=seed, missing=missing, columns=columns)
+    ck, cv = caches(n_pages, Hkv, page, d, dtype, seed + 1)
+    if rotten:                                               # memory that no token was written to may hold anything
+        used = torch.zeros(n_pages, page, dtype=torch.bool)
+        for s, n in enumerate(length):
+            p, r = S.places(table, s, np.arange(min(n, table.shape[1] * page)), page, n_pages)
+            used[p[p >= 0], r[p >= 0]] = True
+        used = used.cuda()[:, None, :, None]
+        ck, cv = torch.where(used, ck, float("nan")), torch.where(used, cv, float("inf"))
+    if change:
+        change(ck, cv, table)
+    Q = tokens(Hq, T, d, dtype, seed + 3, memory)
+    scale = 1 / math.sqrt(d) if scale is None else scale
+    want, want_lse, bar, lse_bar = S.attend(host(Q), host(ck), host(cv), table, ptr, lens, spec, scale, causal, dtype)
+    O = torch.full((Hq, T, d), 7.0, dtype=DTYPE[dtype], device="cuda")
+    lse = torch.full((Hq, T), 7.0, device="cuda")
+    ws = sga.alloc_paged_workspace(batch, spec, Hq, Hkv, d, dtype) if workspace else None
+    sga.attention_paged(Q, ck, cv, batch, spec, scale, causal=causal, O=O, lse=lse, workspace=ws)
+    end = int(ptr[-1])
+    assert (host(O)[:, end:] == 7.0).all() and (host(lse)[:, end:] == 7.0).all()
+    assert within(host(O)[:, :end], want[:, :end], bar[:, :end])
+    assert within(host(lse)[:, :end], want_lse[:, :end], lse_bar[:, :end])
+    return O, lse
+
+
+def full(L):
+    return MaskSpec(KIND_SLIDING, L, window=L)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("d", [32, 64, 128, 256])
+@pytest.mark.parametrize("page", [16, 24, 1])
+def test_attention_types(dtype, d, page):
+    check_attention(dtype, [1, 3, 20], [77, 40, 20], page, 4, 2, d, full(96), padding=2)
+    check_attention(dtype, [1, 9], [130, 50], page, 3, 1, d, MaskSpec(KIND_GLOBAL_LOCAL, 144, window=17, n_global=5))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("Hq,Hkv", [(1, 1), (5, 5), (6, 2), (7, 1), (16, 2), (40, 2), (64, 1)])
+def test_attention_shared_heads(dtype, Hq, Hkv):
+    check_attention(dtype, [1, 1, 6], [1, 33, 100], 16, Hq, Hkv, 64, full(112))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("spec", [
+    full(160), MaskSpec(KIND_SLIDING, 160, window=0), MaskSpec(KIND_SLIDING, 160, window=1), MaskSpec(KIND_SLIDING, 160, window=31),
+    MaskSpec(KIND_SLIDING, 160, window=70), MaskSpec(KIND_GLOBAL_LOCAL, 160, window=3, n_global=1),
+    MaskSpec(KIND_GLOBAL_LOCAL, 160, window=20, n_global=40), MaskSpec(KIND_GLOBAL_LOCAL, 160, window=0, n_global=0),
+    MaskSpec(KIND_GLOBAL_LOCAL, 160, window=5, n_global=160), MaskSpec(KIND_SLIDING, 100, window=40),
+])
+def test_attention_masks(dtype, causal, spec):
+    # whole prompts, pieces in the middle, single tokens; sequences that pass the mask's length
+    check_attention(dtype, [150, 37, 1, 0, 64], [150, 90, 144, 12, 64], 16, 4, 2, 64, spec, causal=causal)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_split_sequences(dtype):
+    """Few long sequences: pieces of the keys on workgroups of their own, joined afterwards."""
+    for page in (16, 40):
+        check_attention(dtype, [1, 2, 1], [5000, 1203, 1], page, 8, 2, 64, full(5008))
+        check_attention(dtype, [1, 2, 1], [5000, 1203, 1], page, 8, 2, 64, full(5008), workspace=False)
+        check_attention(dtype, [2, 1], [3000, 2999], page, 2, 1, 128, MaskSpec(KIND_GLOBAL_LOCAL, 3000, window=1500, n_global=70))
+
+
+@pytest.mark.parametrize("memory", ["head", "token", "slice"])
+def test_attention_strides(memory):
+    check_attention("f16", [7, 1, 30], [40, 90, 30], 32, 6, 3, 64, full(96), memory=memory)
+
+
+def test_attention_of_given_back_pages():
+    """Pages behind a window are gone; a window that reaches into a missing page passes over it; a row may be left empty."""
+    spec = MaskSpec(KIND_SLIDING, 400, window=50)
+    gone = [(0, c, -1) for c in range(0, 21)]                # tokens 0 .. 335 of 400: all that the window leaves
+    check_attention("f16", [1, 1], [400, 390], 16, 4, 4, 64, spec, missing=gone)
+    check_attention("f32", [3, 1], [400, 390], 16, 4, 4, 64, spec, missing=gone + [(0, 22, -1), (1, 24, 10 ** 7)])
+    check_attention("f32", [3, 1], [400, 390], 16, 4, 4, 64, spec, missing=[(0, c, -1) for c in range(25)])
+    check_attention("bf16", [3, 1], [400, 390], 5, 4, 4, 64, spec, missing=[(1, c, -1) for c in range(70, 78)])
+
+
+@pytest.mark.parametrize("page", [16, 24])
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+def test_attention_of_infinities_that_are_not_seen(dtype, page):
+    """Keys and values of a token hold infinities and NaN: rows that do not see it are as if it were not there."""
+    def spoil(ck, cv, table):
+        for token, k, v in ((20, float("nan"), 1.0), (41, 1.0, float("inf")), (60, 1.0, float("nan"))):
+            ck[table[0, token // page], 0, token % page, 3] *= k
+            cv[table[0, token // page], 0, token % page, 5] *= v
+
+    for causal in (True, False):
+        # 80 rows of a prompt whose windows of 4 hold one of the three tokens or none
+        batch, table, ptr, lens, n_pages, T = batch_of([80], [80], page, seed=0)
+        ck, cv = caches(n_pages, 2, page, 64, dtype, 1)
+        clean = [ck.clone(), cv.clone()]
+        spoil(ck, cv, table)
+        spec = MaskSpec(KIND_SLIDING, 80, window=4)
+        Q = tokens(2, T, 64, dtype, 3)
+        got = host(sga.attention_paged(Q, ck, cv, batch, spec, 0.125, causal=causal))
+        want, _, bar, _ = S.attend(host(Q), host(clean[0]), host(clean[1]), table, ptr, lens, spec, 0.125, causal, dtype)
+        i = np.arange(80)
+        sees = lambda token: (np.abs(i - token) <= 4) & ((token <= i) | (not causal))
+        assert np.isnan(got[0, sees(20)]).all()
+        assert (~np.isfinite(got[0, sees(41), 5])).all() and (~np.isfinite(got[0, sees(60), 5])).all()
+        for h in range(2):
+            free = ~(sees(20) | sees(41) | sees(60)) if h == 0 else i >= 0
+            assert within(got[h, free], want[h, free], bar[h, free])
+        rest = [c for c in range(64) if c != 5]
+        only_v = (sees(41) | sees(60)) & ~sees(20)
+        assert within(got[0][only_v][:, rest], want[0][only_v][:, rest], bar[0][only_v][:, rest])
+
+
+def test_attention_of_one_key_and_large_scores():
+    O, lse = check_attention("bf16", [1, 1], [1, 1], 16, 4, 4, 128, full(16))
+    check_attention("f32", [5], [64], 16, 2, 1, 64, full(64), scale=6.0)       # one key takes nearly all
+    check_attention("f32", [5], [64], 16, 2, 1, 64, full(64), scale=-0.5)
+    check_attention("f16", [5], [64], 16, 2, 1, 64, full(64), scale=0.0)
+
+
+def test_attention_far_pages():
+    """A cache of more than 2^31 elements, the tokens in its last pages."""
+    page, Hkv, d = 64, 8, 128
+    n_pages = (1 << 31) // (page * Hkv * d) + 40
+    ck, cv = (torch.empty(n_pages, Hkv, page, d, dtype=torch.float16, device="cuda") for _ in range(2))
+    table = np.array([[n_pages - 1, 0, n_pages - 3]], dtype=np.int32)
+    ptr, lens = np.array([0, 150]), np.array([150])
+    batch = sga.PagedBatch(*(torch.from_numpy(x).cuda() for x in (table, ptr, lens.astype(np.int32))), 150, page, n_pages)
+    K, V, Q = (tokens(h, 150, d, "f16", s) for h, s in ((8, 1), (8, 2), (16, 3)))
+    sga.cache_append(K, V, ck, cv, batch)
+    near = np.array([[0, 1, 2]], dtype=np.int32)
+    small = [c[torch.from_numpy(table[0].astype(np.int64)).cuda()] for c in (ck, cv)]
+    for t in range(150):
+        assert torch.equal(small[0][t // page, :, t % page], K[:, t])
+    spec = full(150)
+    want, _, bar, _ = S.attend(host(Q), host(small[0]), host(small[1]), near, ptr, lens, spec, 0.1, True, "f16")
+    assert within(sga.attention_paged(Q, ck, cv, batch, spec, 0.1), want, bar)
+
+
+def test_attention_without_tokens():
+    batch, *_ = batch_of([0, 0], [5, 9], 16)
+    ck, cv = caches(batch.n_pages, 2, 16, 64, "f16", 1)
+    Q = torch.empty(4, 0, 64, dtype=torch.float16, device="cuda")
+    assert sga.attention_paged(Q, ck, cv, batch, full(16), 0.1).shape == (4, 0, 64)
+    sga.cache_append(Q[:2], Q[:2], ck, cv, batch)
+
+
+# ---- together --------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("d,G", [(64, 1), (128, 4)])
+def test_generation_step_by_step_is_the_whole_sequence(dtype, d, G):
+    """Prompts in pieces, then single tokens, through the cache; against the framework's call on the whole sequence,
+    the mask as an explicit graph."""
+    Hkv, page, w, g = 2, 16, 40, 3
+    Hq, L = Hkv * G, [200, 131]
+    spec = MaskSpec(KIND_GLOBAL_LOCAL, 208, window=w, n_global=g)
+    freqs, magnitude = sga.rotary_frequencies(d, scaling="parts", factor=4.0, original_length=64)
+    rot, scale = sga.Rotary(freqs, "half", magnitude), 1 / math.sqrt(d)
+    Q, K, V = ([tokens(h, n, d, dtype, 10 * k + s) for s, n in enumerate(L)] for k, h in ((1, Hq), (2, Hkv), (3, Hkv)))
+    batch0, table, *_ , n_pages, _ = batch_of([1, 1], L, page)
+    ck, cv = caches(n_pages, Hkv, page, d, dtype, 1)
+    done = [0, 0]
+    O = [torch.empty_like(q) for q in Q]
+    dev_table = batch0.page_table
+    for take in [(64, 100), (1, 1), (70, 1), (33, 0), (0, 7)] + [(1, 1)] * 40:
+        n = [min(t, L[s] - done[s]) for s, t in enumerate(take)]
+        if sum(n) == 0:
+            continue
+        ptr = torch.tensor([0, n[0], n[0] + n[1]], device="cuda")
+        lens = torch.tensor([done[0] + n[0], done[1] + n[1]], dtype=torch.int32, device="cuda")
+        batch = sga.PagedBatch(dev_table, ptr, lens, sum(n), page, n_pages)
+        q, k, v = (torch.cat([x[s][:, done[s]:done[s] + n[s]] for s in range(2)], 1) for x in (Q, K, V))
+        q = sga.cache_append(k, v, ck, cv, batch, rotary=rot, Q=q)
+        ws = sga.alloc_paged_workspace(batch, spec, Hq, Hkv, d, dtype)
+        o = sga.attention_paged(q, ck, cv, batch, spec, scale, workspace=ws)
+        for s in range(2):
+            O[s][:, done[s]:done[s] + n[s]] = o[:, int(ptr[s]):int(ptr[s + 1])]
+            done[s] += n[s]
+    for s in range(2):
+        n = done[s]
+        i, j = np.arange(n)[:, None], np.arange(n)[None]
+        see = (j <= i) & ((i - j <= w) | (j < g) | (i < g))
+        row_ptr = torch.from_numpy(np.concatenate(([0], see.sum(1).cumsum())).astype(np.int64)).cuda()
+        col = torch.from_numpy(np.nonzero(see)[1].astype(np.int32)).cuda()
+        q = sga.rotary(Q[s][:, :n].contiguous(), rot)
+        k = sga.rotary(K[s][:, :n].repeat_interleave(G, 0).contiguous(), rot)
+        v = V[s][:, :n].repeat_interleave(G, 0).contiguous()
+        whole = sga.attention_forward(q, k, v, row_ptr, col, scale)
+        # two calls within the framework's bars of the same number: 1e-5 (fp32), 2e-3 (fp16), relative to 1 + |O|
+        off = (whole.float() - O[s][:, :n].float()).abs() / (1 + whole.float().abs())
+        assert off.max().item() <= 2 * {"f32": 1e-5, "f16": 2e-3}[dtype]
+
+
+def test_captured_steps_follow_the_lengths():
+    """Append and attention captured once, replayed while lengths and tokens change, against eager calls."""
+    Hq, Hkv, d, page, L = 8, 2, 64, 16, 4000
+    spec = MaskSpec(KIND_GLOBAL_LOCAL, L, window=1000, n_global=4)
+    batch, table, *_, n_pages, T = batch_of([1, 1, 1], [L, L, L], page)
+    batch.seq_len.copy_(torch.tensor([1, 700, 3000], dtype=torch.int32))
+    ck, cv = caches(n_pages, Hkv, page, d, "f16", 2)
+    freqs, _ = sga.rotary_frequencies(d)
+    rot = sga.Rotary(freqs)
+    ws = sga.alloc_paged_workspace(batch, spec, Hq, Hkv, d, "f16")
+    K, V, Q = (tokens(h, T, d, "f16", s) for h, s in ((Hkv, 1), (Hkv, 2), (Hq, 3)))
+    q, O = torch.empty_like(Q), torch.empty_like(Q)
+    lse = torch.empty(Hq, T, device="cuda")
+
+    def step(q, O, lse, ck, cv, ws):
+        sga.cache_append(K, V, ck, cv, batch, rotary=rot, Q=Q, Q_out=q)
+        sga.attention_paged(q, ck, cv, batch, spec, 0.125, O=O, lse=lse, workspace=ws)
+
+    step(q, O, lse, ck, cv, ws)
+    torch.cuda.synchronize()
+    ck2, cv2 = ck.clone(), cv.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(q, O, lse, ck, cv, ws)
+    side = torch.cuda.Stream()
+    ws2 = torch.empty_like(ws)
+    q2, O2, lse2 = torch.empty_like(q), torch.empty_like(O), torch.empty_like(lse)
+    for k in range(5):
+        batch.seq_len += 37
+        K.add_(0.1)
+        graph.replay()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):                       # another stream, another workspace
+            step(q2, O2, lse2, ck2, cv2, ws2)
+        side.synchronize()
+        assert torch.equal(O, O2) and torch.equal(lse, lse2) and torch.equal(q, q2)
+    assert torch.isfinite(O).all()
