@@ -610,6 +610,7 @@ sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const voi
   a.cache_k = cache_k; a.cache_v = cache_v;
   a.lse = lse;
   a.scale = scale;
+  a.tile_rows = plan.tile_rows;
   a.slots = plan.slots;
   const bool split = plan.splits > 1 && workspace_bytes >= plan.bytes;
   a.splits = split ? plan.splits : 1;

@@ -27,6 +27,7 @@ constexpr int kBlock = 32;            // keys of a block
 constexpr int kRows = 16;             // rows of a tile
 constexpr int kWaves = 4;             // wavefronts of a workgroup, which take its blocks in turn
 constexpr int kPieceBlocks = 4 * kWaves;   // fewest blocks of a piece of a split tile
+constexpr int kTokenRows = 64;        // sequences with more rows than this on average take tiles of 128 rows
 
 __device__ __forceinline__ int64_t uniform64(int64_t v) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
@@ -74,21 +75,22 @@ __device__ __forceinline__ Sight sight_of(const PagedAttention& a, int32_t p, in
   return {p > a.window ? p - a.window : 0, far < last ? (int32_t)far : last, a.n_global < last + 1 ? a.n_global : last + 1};
 }
 
-// The tile of slot i: sequence s owns the slots from seq_ptr[s] * group / kRows + s, which are enough for it and follow
+// The tile of slot i: sequence s owns the slots from seq_ptr[s] * group / kTileRows + s, which are enough for it and follow
 // from seq_ptr alone.  False: an empty slot.  All lanes call it.
+template <int kTileRows>
 __device__ __forceinline__ bool tile_of(const PagedAttention& a, int32_t slot, Tile& t) {
   const PagedArgs& b = a.batch;
   const int64_t group = a.group.value;
-  auto first_slot = [&](int32_t s) { return (int64_t)row_of_sequence(b, s) * group / kRows + s; };
+  auto first_slot = [&](int32_t s) { return (int64_t)row_of_sequence(b, s) * group / kTileRows + s; };
   t.seq = __builtin_amdgcn_readfirstlane(last_not_above(b.n_seqs, slot, first_slot));
   t.begin = __builtin_amdgcn_readfirstlane(row_of_sequence(b, t.seq));
   const int32_t end = __builtin_amdgcn_readfirstlane(row_of_sequence(b, t.seq + 1));
   t.length = __builtin_amdgcn_readfirstlane(b.seq_len[t.seq]);
   t.n_new = end > t.begin ? end - t.begin : 0;
-  const int64_t first = ((int64_t)slot - (t.begin * group / kRows + t.seq)) * kRows, rows = t.n_new * group;
+  const int64_t first = ((int64_t)slot - (t.begin * group / kTileRows + t.seq)) * kTileRows, rows = t.n_new * group;
   if (first < 0 || first >= rows) return false;
   t.first = (int32_t)first;
-  t.count = rows - first < kRows ? (int32_t)(rows - first) : kRows;
+  t.count = rows - first < kTileRows ? (int32_t)(rows - first) : kTileRows;
   const int64_t room = (int64_t)b.pages_per_seq * b.page.value;
   int64_t kept = t.length < 0 ? 0 : t.length;
   kept = kept < room ? kept : room;
@@ -109,6 +111,18 @@ __device__ __forceinline__ bool tile_of(const PagedAttention& a, int32_t slot, T
   t.lead = (lead + kBlock - 1) / kBlock;
   t.blocks = t.lead + (last >= t.base ? (last - t.base) / kBlock + 1 : 0);
   return true;
+}
+
+__device__ __forceinline__ int32_t first_key(const Tile& t, int32_t block) {
+  return block < t.lead ? block * kBlock : t.base + (block - t.lead) * kBlock;
+}
+// Element offset of token j's row within a key head of the cache, -1 if it has no page.  (j may lie behind the last token,
+// up to a block's end.)
+__device__ __forceinline__ int64_t place_of(const PagedArgs& b, int32_t seq, int32_t j, int32_t d) {
+  const uint32_t column = quotient((uint32_t)j, b.page);
+  if (column >= (uint32_t)b.pages_per_seq) return -1;
+  const uint32_t page = (uint32_t)b.page_table[(int64_t)seq * b.pages_per_seq + column];
+  return page < b.n_pages ? (int64_t)page * b.page_stride + (int64_t)((uint32_t)j - column * b.page.value) * d : -1;
 }
 
 // Pieces of a tile: at least kPieceBlocks blocks each.
@@ -187,6 +201,58 @@ struct Core<float, D> {
   }
 };
 
+// Walks the blocks [block, end) in steps of `step` for one row, key by key, and adds nothing for a key that it does not see:
+// the products above cannot leave a key out, and 0 times an infinity or NaN in it is NaN.  Only where a tile's result is not
+// finite.  A lane ends with channels lane, lane + 64, ...; top and sum are the wavefront's.
+template <typename T, int D>
+__device__ __forceinline__ void attend_row(const PagedAttention& a, const Tile& tile, int32_t head_kv, int32_t flat,
+                                           int32_t block, int32_t end, int32_t step, float& top, float& sum,
+                                           float (&o)[(D + 63) / 64]) {
+  const int lane = threadIdx.x & (kWave - 1);
+  const PagedArgs& b = a.batch;
+  const int32_t group = (int32_t)a.group.value, token = (int32_t)quotient((uint32_t)flat, a.group);
+  const Sight sight = sight_of(a, tile.length - tile.n_new + token, tile.kept);
+  const T* const q = static_cast<const T*>(a.Q) + (int64_t)(head_kv * group + (flat - token * group)) * a.q_head +
+                     (int64_t)(tile.begin + token) * a.q_row;
+  const int64_t in_head = (int64_t)head_kv * b.page.value * D;
+  top = -INFINITY;
+  sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < (D + 63) / 64; ++c) o[c] = 0.f;
+  for (; block < end; block += step) {
+    const int32_t j = first_key(tile, block) + (lane & (kBlock - 1));
+    const int64_t at = place_of(b, tile.seq, j, D);
+    const bool sees = at >= 0 && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
+    float s = -INFINITY;
+    if (sees) {
+      const T* const k = static_cast<const T*>(a.cache_k) + in_head + at;
+      float x = 0.f;
+      for (int c = 0; c < D; ++c) x = fmaf((float)q[c], (float)k[c], x);
+      s = x * (a.scale * kLog2e);
+    }
+    float best = s;
+#pragma unroll
+    for (int off = 1; off < kBlock; off <<= 1) best = fmaxf(best, __shfl_xor(best, off, kWave));
+    best = fmaxf(best, top);
+    const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top - best) : 1.f;
+    top = best;
+    const float p = sees ? __builtin_amdgcn_exp2f(s - (top > -INFINITY ? top : 0.f)) : 0.f;
+    sum *= keep;
+#pragma unroll
+    for (int c = 0; c < (D + 63) / 64; ++c) o[c] *= keep;
+    for (uint32_t left = (uint32_t)__ballot(sees); left; left &= left - 1) {
+      const int from = __ffs(left) - 1;
+      const float w = __shfl(p, from, kWave);
+      const int32_t low = __shfl((int32_t)at, from, kWave), high = __shfl((int32_t)(at >> 32), from, kWave);
+      const T* const v = static_cast<const T*>(a.cache_v) + in_head + ((int64_t)high << 32 | (uint32_t)low);
+      sum += w;
+#pragma unroll
+      for (int c = 0; c < (D + 63) / 64; ++c)
+        if (lane + 64 * c < D) o[c] = fmaf(w, (float)v[lane + 64 * c], o[c]);
+    }
+  }
+}
+
 // Where the rows of a block's keys are.  kWholeTiles: pages hold multiples of 16 tokens, so a 16-key tile lies in one.
 struct Places {
   int64_t tile[2];           // kWholeTiles: element offset of the tile's first row (wave-uniform)
@@ -205,7 +271,7 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
   const int m = lane & 15, g = lane >> 4;
   const int32_t slot = blockIdx.x, head_kv = blockIdx.y, piece = blockIdx.z;
   Tile tile;
-  if (!tile_of(a, slot, tile)) return;
+  if (!tile_of<kRows>(a, slot, tile)) return;
   const Pieces pieces = pieces_of(tile.blocks, a.splits);
   if (piece >= pieces.count) return;
   const int32_t group = (int32_t)a.group.value;
@@ -235,31 +301,19 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
   const int64_t in_head = (int64_t)head_kv * b.page.value * D;
   const T* const cache_k = static_cast<const T*>(a.cache_k) + in_head;
   const T* const cache_v = static_cast<const T*>(a.cache_v) + in_head;
-  const int32_t* const table = b.page_table + (int64_t)tile.seq * b.pages_per_seq;
-
-  auto first_key = [&](int32_t block) {
-    return block < tile.lead ? block * kBlock : tile.base + (block - tile.lead) * kBlock;
-  };
-  // element offset of key j's row, -1 if it has no page.  (j may lie behind the last token, up to the block's end.)
-  auto place_of = [&](int32_t j) -> int64_t {
-    const uint32_t column = quotient((uint32_t)j, b.page);
-    if (column >= (uint32_t)b.pages_per_seq) return -1;
-    const uint32_t page = (uint32_t)table[column];
-    return page < b.n_pages ? (int64_t)page * b.page_stride + (int64_t)((uint32_t)j - column * b.page.value) * D : -1;
-  };
   auto find = [&](int32_t block) {
     Places at;
-    const int32_t j0 = first_key(block);
+    const int32_t j0 = first_key(tile, block);
     at.held = 0;
     if constexpr (kWholeTiles) {
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        const int64_t o = uniform64(place_of(j0 + 16 * t));
+        const int64_t o = uniform64(place_of(b, tile.seq, j0 + 16 * t, D));
         at.held |= (o >= 0 ? 1u : 0u) << t;
         at.tile[t] = o >= 0 ? o : 0;
       }
     } else {
-      const int64_t o = place_of(j0 + (lane & 31));
+      const int64_t o = place_of(b, tile.seq, j0 + (lane & 31), D);
       at.held = (uint32_t)__ballot(o >= 0);
       const int64_t safe = o >= 0 ? o : 0;
 #pragma unroll
@@ -291,9 +345,8 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
   float top, sum;
   float4v o[kRun];
 
-  // One walk over the wavefront's blocks.  only >= 0: for that row alone, with the values of every key that it does not
-  // see taken as 0 (a product cannot leave a key out: 0 times an infinity or NaN is NaN).
-  auto walk = [&](int only) {
+  // one walk over the wavefront's blocks
+  auto walk = [&]() {
     top = -INFINITY;
     sum = 0.f;
 #pragma unroll
@@ -304,7 +357,7 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
     load_k(at);
     load_v(at);
     for (; block < end_block; block += kWaves) {
-      const int32_t j0 = first_key(block);
+      const int32_t j0 = first_key(tile, block);
       const uint32_t held = at.held;
       const bool more = block + kWaves < end_block;
       float4v s[2] = {core.scores(0), core.scores(1)};
@@ -317,16 +370,12 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
       float p[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) p[e] = s[e / 4][e % 4] * (a.scale * kLog2e);
-      uint32_t seen = 0xFF;
       if (!whole) {
-        seen = 0;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int in_block = 16 * (e / 4) + 4 * g + e % 4, j = j0 + in_block;
           const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
-          const bool sees = there && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
-          seen |= (sees ? 1u : 0u) << e;
-          p[e] = sees ? p[e] : -INFINITY;
+          p[e] = there && ((j >= sight.lo && j <= sight.hi) || j < sight.lead) ? p[e] : -INFINITY;
         }
       }
       float best = p[0];
@@ -347,13 +396,12 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
         sum += p[e];
       }
       // values of keys that no row sees (behind the last token, without a page) may be anything
-      if (only >= 0 || !all_held || j0 + kBlock > tile.kept) {
-        const uint32_t row_seen = __shfl(seen, (lane & 48) | (only >= 0 ? only : 0), kWave);
+      if (!all_held || j0 + kBlock > tile.kept) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int in_block = 16 * (e / 4) + 4 * g + e % 4;
           const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
-          const bool use = only >= 0 ? (row_seen >> e) & 1 : there && j0 + in_block < tile.kept;
+          const bool use = there && j0 + in_block < tile.kept;
 #pragma unroll
           for (int c = 0; c < kRun; ++c) core.v[e][c] = use ? core.v[e][c] : (T)0.f;
         }
@@ -362,9 +410,14 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
       if (more) load_v(at);
     }
   };
-  auto deposit = [&](bool mine) {
+  walk();
+  bool finite = true;
+#pragma unroll
+  for (int c = 0; c < kRun; ++c)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) finite = finite && __builtin_isfinite(o[c][r]);
+  if (__all(finite)) {
     const float total = row_sum(sum);
-    if (!mine) return;
 #pragma unroll
     for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -373,19 +426,17 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
       tops[wave][m] = top;
       sums[wave][m] = total;
     }
-  };
-  walk(-1);
-  bool finite = true;
-#pragma unroll
-  for (int c = 0; c < kRun; ++c)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) finite = finite && __builtin_isfinite(o[c][r]);
-  if (__all(finite)) {
-    deposit(true);
   } else {
     for (int row = 0; row < tile.count; ++row) {
-      walk(row);
-      deposit(m == row);
+      float x[(D + 63) / 64];
+      attend_row<T, D>(a, tile, head_kv, tile.first + row, first_block + wave, end_block, kWaves, top, sum, x);
+#pragma unroll
+      for (int c = 0; c < (D + 63) / 64; ++c)
+        if (lane + 64 * c < D) out[wave][row][lane + 64 * c] = x[c];
+      if (lane == 0) {
+        tops[wave][row] = top;
+        sums[wave][row] = sum;
+      }
     }
   }
   __syncthreads();
@@ -431,30 +482,408 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
     a.lse[(int64_t)h * b.n_tokens + at_row] = (high + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-// Joins the pieces of the tiles that are split, in their order.
+// ---- many new tokens: tiles of 128 rows ---------------------------------------------------------------------
+// 16-bit storage, pages of multiples of 16 tokens.  Four wavefronts own 32 rows each and share every block of keys: K and V
+// are copied global -> LDS without registers, once per workgroup, into a ring of four blocks, three ahead; the
+// barrier that opens a block also frees the one before it.  Products of 32 x 32 x 16: S^T = K Q^T and O^T += V^T P^T, a lane's
+// row is lane % 32 in both, and the keys that it holds of S^T are those that it feeds as P.  The scores of the
+// next block are issued ahead of this block's exponentials, so matrix and vector units have work at once.
+// The reference of a row's exponentials (m) is raised only when its numerators grow past 2^14: what matters is that they
+// stay in the range of the storage type, and the sums l and O are in 32 bits whatever their reference.
+// P is rounded to the storage type once (fp16 2^-11, bf16 2^-8 of each numerator, independent of each other): the matrix
+// cores bound this kernel, and a second term for it would cost a half more.  l sums the unrounded numerators.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short short4v __attribute__((ext_vector_type(4)));
+
+constexpr int kChunkRows = 128, kChunkSlots = 4;
+constexpr int kChunkAhead = kChunkSlots - 1;
+constexpr float kMostNumerators = 16384.f;
+
+__device__ __forceinline__ floatx16 matrix32(vec_t<f16_t, 8> a, vec_t<f16_t, 8> b, floatx16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ floatx16 matrix32(vec_t<bf16_t, 8> a, vec_t<bf16_t, 8> b, floatx16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// The value of the lane 32 positions away.
+__device__ __forceinline__ float other_half(float x, int h) {
+  const unsigned xi = __builtin_bit_cast(unsigned, x);
+  const auto r = __builtin_amdgcn_permlane32_swap(xi, xi, false, false);
+  return __builtin_bit_cast(float, h ? r[0] : r[1]);
+}
+
+// s_waitcnt vmcnt(N): all but the N most recently issued vector memory operations have completed.
+template <int N>
+__device__ __forceinline__ void wait_loads_except() {
+  static_assert(N >= 0 && N <= 63, "vmcnt immediate");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
+}
+
+// A block of 32 keys in LDS: rows of D channels, their 16-byte pieces permuted within the row so that the reads
+// below meet every bank equally often (LDS delivers 256 bytes of distinct banks at a time).
+template <int D>
+struct ChunkBlock {
+  static constexpr int kRowBytes = 2 * D, kRowPieces = D / 8, kBytes = kBlock * kRowBytes;
+  static constexpr int kCopyRows = 1024 / kRowBytes;             // rows of one copy instruction
+  static constexpr int kCopies = 8 / kCopyRows;                  // copies of a wavefront's 8 rows
+  static constexpr int kRowsPer256 = kRowBytes < 256 ? 256 / kRowBytes : 1;
+  // K: 16 neighbouring rows are read at one piece index
+  static __device__ __forceinline__ int k_turn(int row) { return row / kRowsPer256 & (kRowPieces < 16 ? kRowPieces - 1 : 15); }
+  // V: four neighbouring rows at four neighbouring pieces
+  static __device__ __forceinline__ int v_turn(int row) { return D >= 128 ? (row & 3) << 2 : (row >> 1 & 1) << 2; }
+};
+
 template <typename T, int D>
+__global__ __attribute__((amdgpu_waves_per_eu(D > 128 ? 1 : 2, D > 128 ? 1 : 2))) __launch_bounds__(kWaves* kWave) void
+paged_chunk_kernel(PagedAttention a) {
+  using B = ChunkBlock<D>;
+  using Piece = vec_t<T, 8>;
+  constexpr int kSlotBytes = 2 * B::kBytes, kPer = 2 * B::kCopies;    // copies of a wavefront per block
+  constexpr int kSteps = D / 16, kTiles = D / 32;
+  __shared__ __align__(16) char ring[kChunkSlots * kSlotBytes];
+  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int n = lane & 31, h = lane >> 5;
+  // Workgroup i runs on XCD i % 8: a key head stays on one XCD, or on 8 / Hkv of them, whose L2 then holds the keys that
+  // its tiles share.  Late tiles first: causal, they have the most keys.
+  int32_t head_kv, rest;
+  {
+    const uint32_t id = blockIdx.x, per_head = (uint32_t)a.slots * a.splits, heads = a.Hkv;
+    if (heads % 8 == 0) {
+      const uint32_t turn = (id / 8) / per_head;
+      head_kv = id % 8 + 8 * turn;
+      rest = id / 8 - turn * per_head;
+    } else if (8 % heads == 0) {
+      head_kv = id % 8 % heads;
+      rest = id / 8 * (8 / heads) + id % 8 / heads;
+    } else {
+      head_kv = id / per_head;
+      rest = id - head_kv * per_head;
+    }
+    if ((uint32_t)rest >= per_head) return;
+  }
+  const int32_t piece = rest / a.slots, slot = a.slots - 1 - (rest - piece * a.slots);
+  Tile tile;
+  if (!tile_of<kChunkRows>(a, slot, tile)) return;
+  const Pieces pieces = pieces_of(tile.blocks, a.splits);
+  if (piece >= pieces.count) return;
+  const int32_t group = (int32_t)a.group.value;
+  const PagedArgs& b = a.batch;
+  const int32_t first_block = piece * pieces.blocks;
+  const int32_t end_block = min(first_block + pieces.blocks, tile.blocks);
+
+  // this lane's row
+  const int32_t own_first = 32 * wave, row = own_first + n;
+  const bool exists = row < tile.count;
+  const int32_t flat = tile.first + (exists ? row : tile.count - 1);
+  const int32_t token = (int32_t)quotient((uint32_t)flat, a.group), head = head_kv * group + (flat - token * group);
+  Sight sight = sight_of(a, tile.length - tile.n_new + token, tile.kept);
+  if (own_first >= tile.count) sight = Sight{0, -1, 0};                // a wavefront without rows only copies
+  Piece qf[kSteps];
+  {
+    const T* q = static_cast<const T*>(a.Q) + (int64_t)head * a.q_head + (int64_t)(tile.begin + token) * a.q_row + 8 * h;
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) qf[i] = *reinterpret_cast<const Piece*>(q + 16 * i);
+    // (a mask puts -inf into scores before the scale: the scale is positive from here on)
+    if (!(a.scale > 0.f)) {
+#pragma unroll
+      for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) qf[i][e] = a.scale == 0.f ? (T)((float)qf[i][e] * 0.f) : -qf[i][e];
+    }
+  }
+  const float factor = a.scale == 0.f ? 1.f : fabsf(a.scale) * kLog2e;
+  int32_t lo_min = sight.lo, lo_max = sight.lo, hi_min = sight.hi, hi_max = sight.hi, lead_max = sight.lead;
+#pragma unroll
+  for (int off = 1; off < 32; off <<= 1) {
+    lo_min = min(lo_min, __shfl_xor(lo_min, off, kWave));
+    lo_max = max(lo_max, __shfl_xor(lo_max, off, kWave));
+    hi_min = min(hi_min, __shfl_xor(hi_min, off, kWave));
+    hi_max = max(hi_max, __shfl_xor(hi_max, off, kWave));
+    lead_max = max(lead_max, __shfl_xor(lead_max, off, kWave));
+  }
+  lo_min = __builtin_amdgcn_readfirstlane(lo_min);
+  lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+  hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+  hi_max = __builtin_amdgcn_readfirstlane(hi_max);
+  lead_max = __builtin_amdgcn_readfirstlane(lead_max);
+
+  // ---- copies
+  const int64_t in_head = (int64_t)head_kv * b.page.value * D;
+  const char* const cache_k = reinterpret_cast<const char*>(static_cast<const T*>(a.cache_k) + in_head);
+  const char* const cache_v = reinterpret_cast<const char*>(static_cast<const T*>(a.cache_v) + in_head);
+  // (read as constants: scalar loads, which leave the count of vector memory operations to the copies)
+  const auto* const table = (const int32_t __attribute__((address_space(4)))*)(uintptr_t)(b.page_table + (int64_t)tile.seq * b.pages_per_seq);
+  const int copy_row = 8 * wave + lane / B::kRowPieces, copy_at = lane % B::kRowPieces;   // rows follow by kCopyRows
+  struct Entries {
+    int32_t page[2];
+  };
+  auto entries_of = [&](int32_t block) {
+    const int32_t j0 = first_key(tile, block < end_block ? block : end_block - 1);
+    Entries e;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t column = quotient((uint32_t)(j0 + 16 * t), b.page);
+      e.page[t] = table[column < (uint32_t)b.pages_per_seq ? column : (uint32_t)b.pages_per_seq - 1];
+    }
+    return e;
+  };
+  uint32_t helds = 0;                                                 // two bits for each block of the ring
+  auto issue = [&](int32_t block, const Entries& e) {
+    const int32_t j0 = first_key(tile, block < end_block ? block : end_block - 1);
+    uint32_t held = 0;
+    int64_t at = 0;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint32_t j = (uint32_t)(j0 + 16 * t), column = quotient(j, b.page);
+      const bool there = column < (uint32_t)b.pages_per_seq && (uint32_t)e.page[t] < b.n_pages;
+      held |= (there ? 1u : 0u) << t;
+      if (t == wave / 2) at = there ? (int64_t)e.page[t] * b.page_stride + (int64_t)(j - column * b.page.value) * D : 0;
+    }
+    const int ring_slot = (block - first_block) % kChunkSlots;
+    helds = (helds & ~(3u << 2 * ring_slot)) | held << 2 * ring_slot;
+    char* dst = ring + ring_slot * kSlotBytes + wave * (B::kCopies * 1024);
+    const char* const k_row = cache_k + 2 * at;
+    const char* const v_row = cache_v + 2 * at;
+#pragma unroll
+    for (int i = 0; i < B::kCopies; ++i) {
+      const int r = copy_row + i * B::kCopyRows, in_tile = r & 15;
+      copy16_to_lds_untracked(k_row + in_tile * B::kRowBytes + (copy_at ^ B::k_turn(r)) * 16, dst + i * 1024);
+      copy16_to_lds_untracked(v_row + in_tile * B::kRowBytes + (copy_at ^ B::v_turn(r)) * 16, dst + B::kBytes + i * 1024);
+    }
+  };
+  auto held_of = [&](int32_t block) { return helds >> 2 * ((block - first_block) % kChunkSlots) & 3u; };
+  // this wavefront's rows of a block's V that are no token's: 0, whatever memory held (its own copies have landed)
+  auto clear_values = [&](int32_t block) {
+    const int32_t j0 = first_key(tile, block);
+    const uint32_t held = held_of(block);
+    if (held == 3u && j0 + kBlock <= tile.kept) return;
+    char* dst = ring + (block - first_block) % kChunkSlots * kSlotBytes + B::kBytes + wave * (B::kCopies * 1024);
+#pragma unroll
+    for (int i = 0; i < B::kCopies; ++i) {
+      const int r = copy_row + i * B::kCopyRows;
+      if (!(held >> (wave / 2) & 1) || j0 + r >= tile.kept) *reinterpret_cast<uint4*>(dst + i * 1024 + lane * 16) = uint4{0, 0, 0, 0};
+    }
+  };
+  Entries next{};
+  // Opens a block: every wavefront has waited for its own copies of this block and the next one, and everyone is
+  // done with the block before, whose slot takes the next copy.
+  auto publish = [&](int32_t block) {
+    wait_loads_except<kPer*(kChunkAhead - 2)>();
+    if (block == first_block) clear_values(block);
+    if (block + 1 < end_block) clear_values(block + 1);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    issue(block + kChunkAhead, next);
+    next = entries_of(block + kChunkAhead + 1);
+  };
+
+  // ---- arithmetic
+  floatx16 o[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) o[t] = floatx16{0};
+  float top = -INFINITY, sum = 0.f;
+  const char* v_base[kTiles];
+  {
+    const int i = lane & 15, r = 4 * h + (i >> 2);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+      v_base[t] = ring + B::kBytes + r * B::kRowBytes + ((4 * t + 2 * (lane >> 4 & 1) + (i >> 1 & 1)) ^ B::v_turn(r)) * 16 + (i & 1) * 8;
+  }
+  const char* const k_base = ring + n * B::kRowBytes;
+  const int k_turn = B::k_turn(n);
+  auto meets = [&](int32_t block) {
+    const int32_t j0 = first_key(tile, block);
+    return (j0 <= hi_max && j0 + kBlock - 1 >= lo_min) || j0 < lead_max;
+  };
+  auto products = [&](int32_t block, floatx16& s) {
+    const char* const at = k_base + (block - first_block) % kChunkSlots * kSlotBytes;
+    s = floatx16{0};
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i)
+      s = matrix32(*reinterpret_cast<const Piece*>(at + ((2 * i + h) ^ k_turn) * 16), qf[i], s);
+  };
+  auto read_v = [&](const char* at) {
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)at);
+  };
+  // accumulator register r holds key 8 (r / 4) + 4 h + r % 4 of the block
+  auto weigh = [&](int32_t block, floatx16& s) {
+    const int32_t j0 = first_key(tile, block);
+    const uint32_t held = held_of(block);
+    if (!(held == 3u && j0 >= lo_max && j0 + kBlock - 1 <= hi_min)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int in_block = 8 * (r / 4) + 4 * h + r % 4, j = j0 + in_block;
+        const bool sees = (held >> (r / 8) & 1) && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
+        s[r] = sees ? s[r] : -INFINITY;
+      }
+    }
+    Piece ph[2];
+    float total = 0.f;
+    auto numerators = [&](float against) {
+      total = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], factor, -against));
+        total += p;
+        ph[r / 8][r % 8] = (T)p;
+      }
+    };
+    numerators(top);                       // (before a row's first key: infinite or NaN)
+    if (__any(!(total < kMostNumerators))) {
+      float best = s[0];
+#pragma unroll
+      for (int r = 1; r < 16; ++r) best = fmaxf(best, s[r]);
+      best = fmaxf(best, other_half(best, h)) * factor;
+      best = fmaxf(best, top);
+      const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top - best) : 1.f;
+      top = best;
+      sum *= keep;
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[t][r] *= keep;
+      numerators(top > -INFINITY ? top : 0.f);
+    }
+    sum += total;
+    const int at = (block - first_block) % kChunkSlots * kSlotBytes;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        const char* const v = v_base[t] + at + 16 * u * B::kRowBytes;
+        const short4v low = read_v(v), high = read_v(v + 8 * B::kRowBytes);
+        const vec_t<short, 8> both = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
+        o[t] = matrix32(__builtin_bit_cast(Piece, both), ph[u], o[t]);
+      }
+  };
+  auto step = [&](int32_t block, floatx16& cur, floatx16& nxt) {
+    const bool more = block + 1 < end_block;
+    if (more && meets(block + 1)) products(block + 1, nxt);
+    if (meets(block)) weigh(block, cur);
+    if (more) publish(block + 1);
+  };
+
+  if (first_block < end_block) {
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) asm volatile("" : "+v"(qf[i]));   // Q has arrived: from here on only the copies are counted
+    for (int i = 0; i < kChunkAhead; ++i) issue(first_block + i, entries_of(first_block + i));
+    next = entries_of(first_block + kChunkAhead);
+    floatx16 s_a, s_b;
+    publish(first_block);
+    if (meets(first_block)) products(first_block, s_a);
+    for (int32_t block = first_block; block < end_block; block += 2) {
+      step(block, s_a, s_b);
+      if (block + 1 < end_block) step(block + 1, s_b, s_a);
+    }
+    // every copy has landed and every wavefront is done with the ring: its space takes the results
+    wait_loads_except<0>();
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  }
+  if (own_first >= tile.count) return;
+  const int own_count = min(tile.count - own_first, 32);
+  float* const part = pieces.count > 1 ? a.partials + (((int64_t)slot * a.Hkv + head_kv) * a.splits + piece) * (kChunkRows * (D + 2))
+                                       : nullptr;
+  auto place_out = [&](int32_t r, int32_t& h_out, int32_t& row_out) {
+    const int32_t f = tile.first + own_first + r, tok = (int32_t)quotient((uint32_t)f, a.group);
+    h_out = head_kv * group + (f - tok * group);
+    row_out = tile.begin + tok;
+  };
+  bool finite = true;
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) finite = finite && __builtin_isfinite(o[t][r]);
+  if (!__all(finite)) {
+    for (int r = 0; r < own_count; ++r) {
+      float x[(D + 63) / 64], row_top, row_total;
+      attend_row<T, D>(a, tile, head_kv, tile.first + own_first + r, first_block, end_block, 1, row_top, row_total, x);
+      if (part) {
+#pragma unroll
+        for (int c = 0; c < (D + 63) / 64; ++c) part[(own_first + r) * D + lane + 64 * c] = x[c];
+        if (lane == 0) {
+          part[kChunkRows * D + own_first + r] = row_top;
+          part[kChunkRows * (D + 1) + own_first + r] = row_total;
+        }
+        continue;
+      }
+      int32_t h_out, row_out;
+      place_out(r, h_out, row_out);
+      const float inv = row_total != 0.f ? 1.f / row_total : 0.f;
+      T* to = static_cast<T*>(a.O) + (int64_t)h_out * a.o_head + (int64_t)row_out * a.o_row;
+#pragma unroll
+      for (int c = 0; c < (D + 63) / 64; ++c) to[lane + 64 * c] = (T)(x[c] * inv);
+      if (a.lse && lane == 0)
+        a.lse[(int64_t)h_out * b.n_tokens + row_out] = (row_top + __builtin_amdgcn_logf(row_total)) * kLn2;
+    }
+    return;
+  }
+  const float total = sum + other_half(sum, h);
+  if (part) {
+    if (!exists) return;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<float4v*>(part + row * D + 32 * t + 8 * g + 4 * h) =
+            float4v{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
+    if (h == 0) {
+      part[kChunkRows * D + row] = top;
+      part[kChunkRows * (D + 1) + row] = total;
+    }
+    return;
+  }
+  // A lane holds pieces of its own row; the rows go through LDS and leave whole.
+  const float inv = total != 0.f ? 1.f / total : 0.f;
+  constexpr int kPitch = B::kRowBytes + 16;
+  static_assert(kWaves * 32 * kPitch <= kChunkSlots * kSlotBytes, "the results fit the ring");
+  char* const mine = ring + wave * (32 * kPitch);
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      vec_t<T, 4> w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) w[e] = (T)(o[t][4 * g + e] * inv);
+      *reinterpret_cast<vec_t<T, 4>*>(mine + n * kPitch + (32 * t + 8 * g + 4 * h) * 2) = w;
+    }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < 32 * B::kRowPieces / kWave; ++i) {
+    const int r = lane / B::kRowPieces + i * (kWave / B::kRowPieces), at = lane % B::kRowPieces;
+    if (r < own_count) {
+      int32_t h_out, row_out;
+      place_out(r, h_out, row_out);
+      *reinterpret_cast<Piece*>(static_cast<T*>(a.O) + (int64_t)h_out * a.o_head + (int64_t)row_out * a.o_row + at * 8) =
+          *reinterpret_cast<const Piece*>(mine + r * kPitch + at * 16);
+    }
+  }
+  if (a.lse && h == 0 && exists) a.lse[(int64_t)head * b.n_tokens + tile.begin + token] = (top + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
+// Joins the pieces of the tiles that are split, in their order.
+template <typename T, int D, int kTileRows>
 __global__ __launch_bounds__(kWaves* kWave) void paged_merge_kernel(PagedAttention a) {
   constexpr int kPer = D / 16;
   const int tid = threadIdx.x;
-  const int32_t slot = blockIdx.x, head_kv = blockIdx.y;
+  const int32_t slot = blockIdx.x / (kTileRows / 16), head_kv = blockIdx.y;
   Tile tile;
-  if (!tile_of(a, slot, tile)) return;
+  if (!tile_of<kTileRows>(a, slot, tile)) return;
   const Pieces pieces = pieces_of(tile.blocks, a.splits);
   if (pieces.count <= 1) return;
-  const int row = tid / 16, channel = tid % 16 * kPer;
+  const int row = blockIdx.x % (kTileRows / 16) * 16 + tid / 16, channel = tid % 16 * kPer;
   if (row >= tile.count) return;
-  const float* part = a.partials + ((int64_t)slot * a.Hkv + head_kv) * a.splits * (kRows * (D + 2));
+  const float* part = a.partials + ((int64_t)slot * a.Hkv + head_kv) * a.splits * (kTileRows * (D + 2));
   float high = -INFINITY;
-  for (int i = 0; i < pieces.count; ++i) high = fmaxf(high, part[(int64_t)i * kRows * (D + 2) + kRows * D + row]);
+  for (int i = 0; i < pieces.count; ++i) high = fmaxf(high, part[(int64_t)i * kTileRows * (D + 2) + kTileRows * D + row]);
   const float against = high > -INFINITY ? high : 0.f;
   float total = 0.f, x[kPer];
 #pragma unroll
   for (int c = 0; c < kPer; ++c) x[c] = 0.f;
   for (int i = 0; i < pieces.count; ++i) {
-    const float* p = part + (int64_t)i * kRows * (D + 2);
-    if (p[kRows * (D + 1) + row] == 0.f) continue;
-    const float weight = __builtin_amdgcn_exp2f(p[kRows * D + row] - against);
-    total += weight * p[kRows * (D + 1) + row];
+    const float* p = part + (int64_t)i * kTileRows * (D + 2);
+    if (p[kTileRows * (D + 1) + row] == 0.f) continue;
+    const float weight = __builtin_amdgcn_exp2f(p[kTileRows * D + row] - against);
+    total += weight * p[kTileRows * (D + 1) + row];
 #pragma unroll
     for (int c = 0; c < kPer; ++c) x[c] += weight * p[row * D + channel + c];
   }
@@ -473,13 +902,26 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_merge_kernel(PagedAttenti
 
 template <typename T, int D>
 sga_status launch_paged_as(const PagedAttention& a) {
+  if (a.tile_rows == kChunkRows) {
+    if constexpr (sizeof(T) == 2 && D >= 64) {
+      const int64_t per_head = (int64_t)a.slots * a.splits;
+      int64_t groups = per_head * a.Hkv;
+      if (a.Hkv < 8 && 8 % a.Hkv == 0) groups = (per_head + 8 / a.Hkv - 1) / (8 / a.Hkv) * 8;
+      profile_mark_begin(a.stream, "paged_chunk_kernel");
+      paged_chunk_kernel<T, D><<<dim3((unsigned)groups), kWaves * kWave, 0, a.stream>>>(a);
+      profile_mark_end(a.stream);
+      if (a.splits > 1)
+        paged_merge_kernel<T, D, kChunkRows><<<dim3((unsigned)a.slots * (kChunkRows / 16), (unsigned)a.Hkv), kWaves * kWave, 0, a.stream>>>(a);
+      return hip_status(hipGetLastError());
+    }
+  }
   const dim3 grid((unsigned)a.slots, (unsigned)a.Hkv, (unsigned)a.splits);
   profile_mark_begin(a.stream, "paged_kernel");
   if (a.batch.page.value % 16 == 0) paged_kernel<T, D, true><<<grid, kWaves * kWave, 0, a.stream>>>(a);
   else paged_kernel<T, D, false><<<grid, kWaves * kWave, 0, a.stream>>>(a);
   profile_mark_end(a.stream);
   if (a.splits > 1)
-    paged_merge_kernel<T, D><<<dim3((unsigned)a.slots, (unsigned)a.Hkv), kWaves * kWave, 0, a.stream>>>(a);
+    paged_merge_kernel<T, D, kRows><<<dim3((unsigned)a.slots, (unsigned)a.Hkv), kWaves * kWave, 0, a.stream>>>(a);
   return hip_status(hipGetLastError());
 }
 
@@ -496,21 +938,26 @@ sga_status launch_paged_type(const PagedAttention& a) {
 }  // namespace
 
 PagedPlan plan_paged(const PagedAttention& a) {
-  PagedPlan p{1, 0, 0};
-  const int64_t slots = (int64_t)a.batch.n_tokens * a.group.value / kRows + a.batch.n_seqs;
-  if (slots * kWaves * kWave >= int64_t(1) << 32) return PagedPlan{0, 0, 0};
-  p.slots = (int32_t)slots;
+  PagedPlan p{kRows, 1, 0, 0};
+  const int64_t all_rows = (int64_t)a.batch.n_tokens * a.group.value;
+  if (a.dtype != SGA_F32 && a.d >= 64 && a.batch.page.value % 16 == 0 && all_rows > (int64_t)kTokenRows * a.batch.n_seqs)
+    p.tile_rows = kChunkRows;
+  const int64_t slots = all_rows / p.tile_rows + a.batch.n_seqs;
+  // (a grid holds fewer than 2^32 threads along a side)
+  if (slots >= int64_t(1) << 24) return p;
   // keys that a tile meets at most
-  const int64_t rows = kRows / (int64_t)a.group.value + 2;
+  const int64_t tokens = p.tile_rows / (int64_t)a.group.value + 2;
   const int64_t room = (int64_t)a.batch.pages_per_seq * a.batch.page.value;
   int64_t keys = a.L < room ? a.L : room;
-  const int64_t wide = (a.causal ? 1 : 2) * (int64_t)a.window + rows + a.n_global + 3 * kBlock;
+  const int64_t wide = (a.causal ? 1 : 2) * (int64_t)a.window + tokens + a.n_global + 3 * kBlock;
   if (wide < keys && !(a.n_global > 0 && !a.causal)) keys = wide;
   const int64_t blocks = (keys + kBlock - 1) / kBlock + 2;
   const int64_t most = (blocks + kPieceBlocks - 1) / kPieceBlocks, wanted = (1024 + slots * a.Hkv - 1) / (slots * a.Hkv);
   p.splits = (int32_t)(most < wanted ? most : wanted);
   if (p.splits < 1) p.splits = 1;
-  if (p.splits > 1) p.bytes = (size_t)slots * a.Hkv * p.splits * kRows * (a.d + 2) * sizeof(float);
+  if (p.tile_rows == kChunkRows && slots * p.splits * a.Hkv + 8 >= int64_t(1) << 24) return p;
+  p.slots = (int32_t)slots;
+  if (p.splits > 1) p.bytes = (size_t)slots * a.Hkv * p.splits * p.tile_rows * (a.d + 2) * sizeof(float);
   return p;
 }
 

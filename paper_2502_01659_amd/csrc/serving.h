@@ -102,6 +102,7 @@ struct PagedAttention {
   int32_t L, window, n_global, causal;
   float scale;
   float* partials;           // partial states of split tiles
+  int32_t tile_rows;
   int32_t splits;            // most pieces that a tile is cut into
   int32_t slots;             // tiles of a key head, some of them empty
   int32_t d, dtype;
@@ -109,7 +110,8 @@ struct PagedAttention {
 };
 // Pieces and partial states that a call may use.
 struct PagedPlan {
-  int32_t splits, slots;
+  int32_t tile_rows;         // rows of a tile: which kernel takes the call
+  int32_t splits, slots;     // slots 0: too many for one launch
   size_t bytes;
 };
 PagedPlan plan_paged(const PagedAttention& a);

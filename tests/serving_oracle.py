@@ -76,8 +76,9 @@ def append(K, V, cache_k, cache_v, page_table, seq_ptr, seq_len, freqs, layout, 
     return ck, cv, size, q, q_size
 
 
-def attend(Q, cache_k, cache_v, page_table, seq_ptr, seq_len, spec, scale, causal, dtype):
-    """(O, lse, bar of O, bar of lse), float64; rows of no sequence are NaN."""
+def attend(Q, cache_k, cache_v, page_table, seq_ptr, seq_len, spec, scale, causal, dtype, once=False):
+    """(O, lse, bar of O, bar of lse), float64; rows of no sequence are NaN.  once: probabilities are rounded to the
+    storage type once, as the kernel of long chunks does."""
     Hq, T, d = Q.shape
     n_pages, Hkv, page, _ = cache_k.shape
     O, lse = np.full((Hq, T, d), np.nan), np.full((Hq, T), np.nan)
@@ -107,7 +108,7 @@ def attend(Q, cache_k, cache_v, page_table, seq_ptr, seq_len, spec, scale, causa
                     + 2.0 ** -22 * (1 + np.abs(z).max(1, keepdims=True))
                 # probabilities enter the products as two numbers of the storage type: what is left is a half step of a half
                 # step (fp16: or half its smallest step, 2^-25); sums over n keys in 32 bits: sqrt(n) half steps and to spare
-                parts = {"f32": 0.0, "f16": 2.0 ** -21, "bf16": 2.0 ** -15}[dtype]
+                parts = {"f32": 0.0, "f16": 2.0 ** -21, "bf16": 2.0 ** -15}[dtype] if not once else HALF_STEP[dtype]
                 share = e @ np.abs(v) / l
                 O_bar[heads, row] = share * (2 * off + parts + (4 + np.sqrt(len(p))) * 2.0 ** -23) \
                     + np.abs(O[heads, row]) * HALF_STEP[dtype]

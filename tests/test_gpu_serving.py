@@ -204,6 +204,11 @@ def test_append_passes_over_missing_pages():
 
 
 # ---- attention ------------------------------------------------------------------------------------
+def long_chunks(dtype, T, n_seqs, group, d, page):
+    """Calls whose sequences bring more than 64 rows on average take tiles of 128 rows."""
+    return dtype != "f32" and d >= 64 and page % 16 == 0 and T * group > 64 * n_seqs
+
+
 def check_attention(dtype, new, length, page, Hq, Hkv, d, spec, causal=True, padding=0, memory="token", missing=(), scale=None,
                     workspace=True, rotten=True, seed=0, change=None, columns=None):
     print("attend", dtype, new[:6], length[:6], page, Hq, Hkv, d, spec, causal, flush=True)
@@ -220,11 +225,17 @@ def check_attention(dtype, new, length, page, Hq, Hkv, d, spec, causal=True, pad
         change(ck, cv, table)
     Q = tokens(Hq, T, d, dtype, seed + 3, memory)
     scale = 1 / math.sqrt(d) if scale is None else scale
-    want, want_lse, bar, lse_bar = S.attend(host(Q), host(ck), host(cv), table, ptr, lens, spec, scale, causal, dtype)
+    long = long_chunks(dtype, T, len(new), Hq // Hkv, d, page)
+    want, want_lse, bar, lse_bar = S.attend(host(Q), host(ck), host(cv), table, ptr, lens, spec, scale, causal, dtype, long)
     O = torch.full((Hq, T, d), 7.0, dtype=DTYPE[dtype], device="cuda")
     lse = torch.full((Hq, T), 7.0, device="cuda")
     ws = sga.alloc_paged_workspace(batch, spec, Hq, Hkv, d, dtype) if workspace else None
+    assert sga.sga_profile_enable(1) == 0
     sga.attention_paged(Q, ck, cv, batch, spec, scale, causal=causal, O=O, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    kernel = sga.sga_profile_last_kernel()
+    sga.sga_profile_enable(0)
+    assert kernel == ("paged_chunk_kernel" if long else "paged_kernel")
     end = int(ptr[-1])
     assert (host(O)[:, end:] == 7.0).all() and (host(lse)[:, end:] == 7.0).all()
     assert within(host(O)[:, :end], want[:, :end], bar[:, :end])
@@ -305,7 +316,8 @@ def test_attention_of_infinities_that_are_not_seen(dtype, page):
         spec = MaskSpec(KIND_SLIDING, 80, window=4)
         Q = tokens(2, T, 64, dtype, 3)
         got = host(sga.attention_paged(Q, ck, cv, batch, spec, 0.125, causal=causal))
-        want, _, bar, _ = S.attend(host(Q), host(clean[0]), host(clean[1]), table, ptr, lens, spec, 0.125, causal, dtype)
+        want, _, bar, _ = S.attend(host(Q), host(clean[0]), host(clean[1]), table, ptr, lens, spec, 0.125, causal, dtype,
+                                   long_chunks(dtype, T, 1, 1, 64, page))
         i = np.arange(80)
         sees = lambda token: (np.abs(i - token) <= 4) & ((token <= i) | (not causal))
         assert np.isnan(got[0, sees(20)]).all()
@@ -325,6 +337,32 @@ def test_attention_of_one_key_and_large_scores():
     check_attention("f16", [5], [64], 16, 2, 1, 64, full(64), scale=0.0)
 
 
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_long_chunks(dtype, d, causal):
+    """Tiles of 128 rows: ragged ends, tiles of few rows, several pieces, global tokens before the window, missing pages."""
+    check_attention(dtype, [129, 1, 300], [129, 40, 700], 16, 2, 2, d, full(704), causal=causal, padding=5)
+    check_attention(dtype, [97], [600], 48, 3, 1, d, MaskSpec(KIND_SLIDING, 608, window=33), causal=causal, memory="slice")
+    check_attention(dtype, [70, 0, 65], [3000, 7, 65], 16, 4, 1, d, MaskSpec(KIND_GLOBAL_LOCAL, 3008, window=1200, n_global=70),
+                    causal=causal)
+    check_attention(dtype, [130], [1000], 32, 2, 2, d, full(1000), causal=causal, missing=[(0, 3, -1), (0, 17, 10 ** 6), (0, 31, -9)])
+    check_attention(dtype, [200], [150], 16, 2, 1, d, full(160), causal=causal)      # the first 50 lie before position 0
+    check_attention(dtype, [100], [100], 16, 5, 5, d, MaskSpec(KIND_SLIDING, 80, window=0), causal=causal, workspace=False)
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+def test_attention_long_chunks_of_uneven_scores(dtype):
+    """Scores that grow along the keys raise the reference again and again; one key that takes all; a zero and a negative scale."""
+    def grow(ck, cv, table):
+        for t in range(400):
+            ck[table[0, t // 16], :, t % 16] *= 0.02 * t
+    for scale in (1.0, -1.0, 0.0, 0.01):
+        check_attention(dtype, [140], [400], 16, 2, 1, 64, full(400), scale=scale, change=grow)
+    check_attention(dtype, [200], [200], 16, 12, 12, 64, MaskSpec(KIND_SLIDING, 200, window=200))
+    check_attention(dtype, [200], [200], 16, 4, 2, 64, MaskSpec(KIND_SLIDING, 200, window=200), causal=False)
+
+
 def test_attention_far_pages():
     """A cache of more than 2^31 elements, the tokens in its last pages."""
     page, Hkv, d = 64, 8, 128
@@ -340,7 +378,7 @@ def test_attention_far_pages():
     for t in range(150):
         assert torch.equal(small[0][t // page, :, t % page], K[:, t])
     spec = full(150)
-    want, _, bar, _ = S.attend(host(Q), host(small[0]), host(small[1]), near, ptr, lens, spec, 0.1, True, "f16")
+    want, _, bar, _ = S.attend(host(Q), host(small[0]), host(small[1]), near, ptr, lens, spec, 0.1, True, "f16", True)
     assert within(sga.attention_paged(Q, ck, cv, batch, spec, 0.1), want, bar)
 
 
