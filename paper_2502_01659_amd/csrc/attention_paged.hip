@@ -520,6 +520,18 @@ __device__ __forceinline__ void wait_loads_except() {
   __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
+// Two times 16 bytes per lane from k and v plus the lane's offsets into LDS at `to` and `to` + apart, + 16 * lane each: without
+// registers and behind the compiler's back, completion is waited for by count (wait_loads_except) and a barrier.  (M0
+// holds the address in LDS; the compiler's own value is put back.)
+__device__ __forceinline__ void copy_pieces(const void* k, uint32_t k_offset, const void* v, uint32_t v_offset, uint32_t to,
+                                            uint32_t apart) {
+  uint32_t kept;
+  asm volatile(
+      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\t"
+      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %6\n\ts_mov_b32 m0, %0"
+      : "=&s"(kept) : "s"(to), "v"(k_offset), "s"(k), "s"(to + apart), "v"(v_offset), "s"(v) : "memory");
+}
+
 // A block of 32 keys in LDS: rows of D channels, their 16-byte pieces permuted within the row so that the reads
 // below meet every bank equally often (LDS delivers 256 bytes of distinct banks at a time).
 template <int D>
@@ -615,66 +627,56 @@ paged_chunk_kernel(PagedAttention a) {
   // (read as constants: scalar loads, which leave the count of vector memory operations to the copies)
   const auto* const table = (const int32_t __attribute__((address_space(4)))*)(uintptr_t)(b.page_table + (int64_t)tile.seq * b.pages_per_seq);
   const int copy_row = 8 * wave + lane / B::kRowPieces, copy_at = lane % B::kRowPieces;   // rows follow by kCopyRows
-  struct Entries {
-    int32_t page[2];
+  uint32_t k_from[B::kCopies], v_from[B::kCopies];       // this lane's bytes, from its 16-key tile's first row on
+#pragma unroll
+  for (int i = 0; i < B::kCopies; ++i) {
+    const int r = copy_row + i * B::kCopyRows;
+    k_from[i] = (r & 15) * B::kRowBytes + (copy_at ^ B::k_turn(r)) * 16;
+    v_from[i] = (r & 15) * B::kRowBytes + (copy_at ^ B::v_turn(r)) * 16;
+  }
+  const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(char __attribute__((address_space(3)))*)ring);
+  // The place of this wavefront's rows in the block that is copied next: its page's column and the row within it follow each
+  // other without divisions, and the column's entry is loaded a block ahead of its use.
+  const uint32_t page = b.page.value, columns_step = page == 16 ? 2 : 0, rows_step = page == 16 ? 0 : kBlock;
+  int32_t next_block = first_block, entry = 0;
+  uint32_t column = 0, in_page = 0;
+  auto look_up = [&]() {
+    entry = table[column < (uint32_t)b.pages_per_seq ? column : (uint32_t)b.pages_per_seq - 1];
   };
-  auto entries_of = [&](int32_t block) {
-    const int32_t j0 = first_key(tile, block < end_block ? block : end_block - 1);
-    Entries e;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint32_t column = quotient((uint32_t)(j0 + 16 * t), b.page);
-      e.page[t] = table[column < (uint32_t)b.pages_per_seq ? column : (uint32_t)b.pages_per_seq - 1];
-    }
-    return e;
+  auto start_at = [&](int32_t block) {
+    const uint32_t j = (uint32_t)(first_key(tile, block) + 16 * (wave / 2));
+    column = quotient(j, b.page);
+    in_page = j - column * page;
+    look_up();
   };
-  uint32_t helds = 0;                                                 // two bits for each block of the ring
-  auto issue = [&](int32_t block, const Entries& e) {
-    const int32_t j0 = first_key(tile, block < end_block ? block : end_block - 1);
-    uint32_t held = 0;
-    int64_t at = 0;
+  auto issue = [&]() {                   // copies next_block, or the last one again
+    const bool there = column < (uint32_t)b.pages_per_seq && (uint32_t)entry < b.n_pages;
+    const int64_t at = there ? (int64_t)entry * b.page_stride + (int64_t)in_page * D : 0;
+    const uint32_t to = ring_at + ((uint32_t)(next_block - first_block) % kChunkSlots * kSlotBytes + wave * (B::kCopies * 1024));
+    const char* const k_tile = cache_k + 2 * at;
+    const char* const v_tile = cache_v + 2 * at;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const uint32_t j = (uint32_t)(j0 + 16 * t), column = quotient(j, b.page);
-      const bool there = column < (uint32_t)b.pages_per_seq && (uint32_t)e.page[t] < b.n_pages;
-      held |= (there ? 1u : 0u) << t;
-      if (t == wave / 2) at = there ? (int64_t)e.page[t] * b.page_stride + (int64_t)(j - column * b.page.value) * D : 0;
-    }
-    const int ring_slot = (block - first_block) % kChunkSlots;
-    helds = (helds & ~(3u << 2 * ring_slot)) | held << 2 * ring_slot;
-    char* dst = ring + ring_slot * kSlotBytes + wave * (B::kCopies * 1024);
-    const char* const k_row = cache_k + 2 * at;
-    const char* const v_row = cache_v + 2 * at;
-#pragma unroll
-    for (int i = 0; i < B::kCopies; ++i) {
-      const int r = copy_row + i * B::kCopyRows, in_tile = r & 15;
-      copy16_to_lds_untracked(k_row + in_tile * B::kRowBytes + (copy_at ^ B::k_turn(r)) * 16, dst + i * 1024);
-      copy16_to_lds_untracked(v_row + in_tile * B::kRowBytes + (copy_at ^ B::v_turn(r)) * 16, dst + B::kBytes + i * 1024);
-    }
-  };
-  auto held_of = [&](int32_t block) { return helds >> 2 * ((block - first_block) % kChunkSlots) & 3u; };
-  // this wavefront's rows of a block's V that are no token's: 0, whatever memory held (its own copies have landed)
-  auto clear_values = [&](int32_t block) {
-    const int32_t j0 = first_key(tile, block);
-    const uint32_t held = held_of(block);
-    if (held == 3u && j0 + kBlock <= tile.kept) return;
-    char* dst = ring + (block - first_block) % kChunkSlots * kSlotBytes + B::kBytes + wave * (B::kCopies * 1024);
-#pragma unroll
-    for (int i = 0; i < B::kCopies; ++i) {
-      const int r = copy_row + i * B::kCopyRows;
-      if (!(held >> (wave / 2) & 1) || j0 + r >= tile.kept) *reinterpret_cast<uint4*>(dst + i * 1024 + lane * 16) = uint4{0, 0, 0, 0};
+    for (int i = 0; i < B::kCopies; ++i) copy_pieces(k_tile, k_from[i], v_tile, v_from[i], to + i * 1024, B::kBytes);
+    ++next_block;
+    if (next_block < end_block) {
+      if (next_block == tile.lead) {
+        start_at(next_block);
+      } else {
+        column += columns_step;
+        in_page += rows_step;
+        const bool over = in_page >= page;
+        column += over ? 1 : 0;
+        in_page -= over ? page : 0;
+        look_up();
+      }
     }
   };
-  Entries next{};
   // Opens a block: every wavefront has waited for its own copies of this block and the next one, and everyone is
   // done with the block before, whose slot takes the next copy.
-  auto publish = [&](int32_t block) {
+  auto publish = [&]() {
     wait_loads_except<kPer*(kChunkAhead - 2)>();
-    if (block == first_block) clear_values(block);
-    if (block + 1 < end_block) clear_values(block + 1);
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    issue(block + kChunkAhead, next);
-    next = entries_of(block + kChunkAhead + 1);
+    issue();
   };
 
   // ---- arithmetic
@@ -691,90 +693,175 @@ paged_chunk_kernel(PagedAttention a) {
   }
   const char* const k_base = ring + n * B::kRowBytes;
   const int k_turn = B::k_turn(n);
+  auto slot_of = [&](int32_t block) { return (uint32_t)(block - first_block) % kChunkSlots * kSlotBytes; };
   auto meets = [&](int32_t block) {
     const int32_t j0 = first_key(tile, block);
     return (j0 <= hi_max && j0 + kBlock - 1 >= lo_min) || j0 < lead_max;
   };
-  auto products = [&](int32_t block, floatx16& s) {
-    const char* const at = k_base + (block - first_block) % kChunkSlots * kSlotBytes;
+  auto read_k = [&](int32_t block, Piece (&k)[kSteps]) {
+    const char* const at = k_base + slot_of(block);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) k[i] = *reinterpret_cast<const Piece*>(at + ((2 * i + h) ^ k_turn) * 16);
+  };
+  auto products = [&](const Piece (&k)[kSteps], floatx16& s) {
     s = floatx16{0};
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-      s = matrix32(*reinterpret_cast<const Piece*>(at + ((2 * i + h) ^ k_turn) * 16), qf[i], s);
+    for (int i = 0; i < kSteps; ++i) s = matrix32(k[i], qf[i], s);
   };
-  auto read_v = [&](const char* at) {
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)at);
-  };
-  // accumulator register r holds key 8 (r / 4) + 4 h + r % 4 of the block
-  auto weigh = [&](int32_t block, floatx16& s) {
-    const int32_t j0 = first_key(tile, block);
-    const uint32_t held = held_of(block);
-    if (!(held == 3u && j0 >= lo_max && j0 + kBlock - 1 <= hi_min)) {
+  auto read_v = [&](int32_t block, int u, Piece (&v)[kTiles]) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const int in_block = 8 * (r / 4) + 4 * h + r % 4, j = j0 + in_block;
-        const bool sees = (held >> (r / 8) & 1) && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
-        s[r] = sees ? s[r] : -INFINITY;
-      }
+    for (int t = 0; t < kTiles; ++t) {
+      const char* const at = v_base[t] + slot_of(block) + 16 * u * B::kRowBytes;
+      const short4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)at);
+      const short4v high =
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(at + 8 * B::kRowBytes));
+      const vec_t<short, 8> both = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
+      v[t] = __builtin_bit_cast(Piece, both);
     }
-    Piece ph[2];
+  };
+  // Accumulator register r holds key 8 (r / 4) + 4 h + r % 4 of the block.
+  auto numerators = [&](const floatx16& s, float against, Piece (&p)[2]) {
     float total = 0.f;
-    auto numerators = [&](float against) {
-      total = 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[r], factor, -against));
-        total += p;
-        ph[r / 8][r % 8] = (T)p;
-      }
-    };
-    numerators(top);                       // (before a row's first key: infinite or NaN)
-    if (__any(!(total < kMostNumerators))) {
-      float best = s[0];
+    for (int r = 0; r < 16; ++r) {
+      const float x = __builtin_amdgcn_exp2f(fmaf(s[r], factor, -against));
+      total += x;
+      p[r / 8][r % 8] = (T)x;
+    }
+    return total;
+  };
+  // the reference of the rows' numerators becomes their largest score so far
+  auto raise = [&](const floatx16& s) {
+    float best = s[0];
 #pragma unroll
-      for (int r = 1; r < 16; ++r) best = fmaxf(best, s[r]);
-      best = fmaxf(best, other_half(best, h)) * factor;
-      best = fmaxf(best, top);
-      const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top - best) : 1.f;
-      top = best;
-      sum *= keep;
+    for (int r = 1; r < 16; ++r) best = fmaxf(best, s[r]);
+    best = fmaxf(best, other_half(best, h)) * factor;
+    best = fmaxf(best, top);
+    const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top - best) : 1.f;
+    top = best;
+    sum *= keep;
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t)
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) o[t][r] *= keep;
-      numerators(top > -INFINITY ? top : 0.f);
+      for (int r = 0; r < 16; ++r) o[t][r] *= keep;
+  };
+  auto weigh = [&](int32_t block, const floatx16& s, float total, Piece (&p)[2]) {
+    if (__any(!(total < kMostNumerators))) {          // (before a row's first key: infinite or NaN)
+      raise(s);
+      total = numerators(s, top > -INFINITY ? top : 0.f, p);
     }
     sum += total;
-    const int at = (block - first_block) % kChunkSlots * kSlotBytes;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
+    for (int u = 0; u < 2; ++u) {
+      Piece v[kTiles];
+      read_v(block, u, v);
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) {
-        const char* const v = v_base[t] + at + 16 * u * B::kRowBytes;
-        const short4v low = read_v(v), high = read_v(v + 8 * B::kRowBytes);
-        const vec_t<short, 8> both = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
-        o[t] = matrix32(__builtin_bit_cast(Piece, both), ph[u], o[t]);
-      }
+      for (int t = 0; t < kTiles; ++t) o[t] = matrix32(v[t], p[u], o[t]);
+    }
   };
-  auto step = [&](int32_t block, floatx16& cur, floatx16& nxt) {
-    const bool more = block + 1 < end_block;
-    if (more && meets(block + 1)) products(block + 1, nxt);
-    if (meets(block)) weigh(block, cur);
-    if (more) publish(block + 1);
+
+  // Does any of the workgroup's keys miss its page?  Where none does, and that is nearly always, no block asks again.
+  bool missing = false;
+  auto held_of = [&](int32_t j0) {      // bit t: the 16-key tile t of the block at key j0 has a page
+    uint32_t held = 3u;
+    if (missing) {
+      held = 0;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t c = quotient((uint32_t)(j0 + 16 * t), b.page);
+        if (c < (uint32_t)b.pages_per_seq && (uint32_t)table[c] < b.n_pages) held |= 1u << t;
+      }
+    }
+    return held;
+  };
+  // A block that some row of the wavefront does not see whole.
+  auto edge = [&](int32_t block) {
+    publish();
+    const int32_t j0 = first_key(tile, block);
+    if (missing || j0 + kBlock > tile.kept) {
+      // values that are no token's: 0, whatever memory held, each wavefront in its own rows (every wavefront is here)
+      const uint32_t held = held_of(j0);
+      char* const dst = ring + slot_of(block) + B::kBytes + wave * (B::kCopies * 1024);
+#pragma unroll
+      for (int i = 0; i < B::kCopies; ++i)
+        if (!(held >> (wave / 2) & 1) || j0 + copy_row + i * B::kCopyRows >= tile.kept)
+          *reinterpret_cast<uint4*>(dst + i * 1024 + lane * 16) = uint4{0, 0, 0, 0};
+      asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    if (!meets(block)) return;
+    Piece k[kSteps], p[2];
+    floatx16 s;
+    read_k(block, k);
+    products(k, s);
+    const uint32_t held = held_of(j0);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int in_block = 8 * (r / 4) + 4 * h + r % 4, j = j0 + in_block;
+      const bool sees = (held >> (r / 8) & 1) && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
+      s[r] = sees ? s[r] : -INFINITY;
+    }
+    const float total = numerators(s, top, p);
+    weigh(block, s, total, p);
+  };
+  // A block that every row sees whole, its scores at hand; those of the next one are issued ahead of its exponentials.
+  auto inside = [&](int32_t block, floatx16& s, floatx16& ahead) {
+    Piece k[kSteps], p[2];
+    read_k(block + 1, k);
+    products(k, ahead);
+    const float total = numerators(s, top, p);
+    weigh(block, s, total, p);
   };
 
   if (first_block < end_block) {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) asm volatile("" : "+v"(qf[i]));   // Q has arrived: from here on only the copies are counted
-    for (int i = 0; i < kChunkAhead; ++i) issue(first_block + i, entries_of(first_block + i));
-    next = entries_of(first_block + kChunkAhead);
-    floatx16 s_a, s_b;
-    publish(first_block);
-    if (meets(first_block)) products(first_block, s_a);
-    for (int32_t block = first_block; block < end_block; block += 2) {
-      step(block, s_a, s_b);
-      if (block + 1 < end_block) step(block + 1, s_b, s_a);
+    start_at(first_block);
+    for (int i = 0; i < kChunkAhead; ++i) issue();
+    for (int32_t i = first_block + (int32_t)tid; i < end_block; i += kWaves * kWave) {
+      const int32_t j0 = first_key(tile, i);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) missing = missing || place_of(b, tile.seq, j0 + 16 * t, D) < 0;
     }
+    missing = __syncthreads_or(missing);
+    // blocks [inner, outer) are seen whole by every row (none where pages are missing)
+    int32_t inner = end_block, outer = end_block;
+    if (!missing) {
+      const int32_t from = lo_max <= tile.base ? 0 : (lo_max - tile.base + kBlock - 1) / kBlock;
+      const int32_t to = hi_min + 1 <= tile.base ? 0 : (hi_min + 1 - tile.base) / kBlock;
+      inner = max(max(first_block, tile.lead), tile.lead + from);
+      outer = min(end_block, tile.lead + to);
+      if (inner >= outer) inner = outer = end_block;
+    }
+    int32_t block = first_block;
+    for (; block < inner; ++block) edge(block);
+    if (block < outer) {
+      floatx16 s_a, s_b;
+      {
+        Piece k[kSteps];
+        publish();
+        read_k(block, k);
+        products(k, s_a);
+      }
+      for (; block + 2 < outer; block += 2) {
+        inside(block, s_a, s_b);
+        publish();
+        inside(block + 1, s_b, s_a);
+        publish();
+      }
+      Piece p[2];
+      if (block + 1 < outer) {
+        inside(block, s_a, s_b);
+        publish();
+        const float total = numerators(s_b, top, p);
+        weigh(block + 1, s_b, total, p);
+        block += 2;
+      } else {
+        const float total = numerators(s_a, top, p);
+        weigh(block, s_a, total, p);
+        ++block;
+      }
+    }
+    for (; block < end_block; ++block) edge(block);
     // every copy has landed and every wavefront is done with the ring: its space takes the results
     wait_loads_except<0>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
