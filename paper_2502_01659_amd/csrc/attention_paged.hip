@@ -532,18 +532,14 @@ __device__ __forceinline__ void copy_pieces(const void* k, uint32_t k_offset, co
       : "=&s"(kept) : "s"(to), "v"(k_offset), "s"(k), "s"(to + apart), "v"(v_offset), "s"(v) : "memory");
 }
 
-// A block of 32 keys in LDS: rows of D channels, their 16-byte pieces permuted within the row so that the reads
-// below meet every bank equally often (LDS delivers 256 bytes of distinct banks at a time).
+// A block of 32 keys in LDS: groups of 32 channels, in a group the 32 keys' rows of 64 bytes.  What the products read then
+// differs by constants from one or two addresses per lane, and 16 lanes' pieces (K: four rows apart they would share
+// banks, so a row's four pieces are permuted; V: eight rows in a row) meet every bank once.
 template <int D>
 struct ChunkBlock {
-  static constexpr int kRowBytes = 2 * D, kRowPieces = D / 8, kBytes = kBlock * kRowBytes;
-  static constexpr int kCopyRows = 1024 / kRowBytes;             // rows of one copy instruction
-  static constexpr int kCopies = 8 / kCopyRows;                  // copies of a wavefront's 8 rows
-  static constexpr int kRowsPer256 = kRowBytes < 256 ? 256 / kRowBytes : 1;
-  // K: 16 neighbouring rows are read at one piece index
-  static __device__ __forceinline__ int k_turn(int row) { return row / kRowsPer256 & (kRowPieces < 16 ? kRowPieces - 1 : 15); }
-  // V: four neighbouring rows at four neighbouring pieces
-  static __device__ __forceinline__ int v_turn(int row) { return D >= 128 ? (row & 3) << 2 : (row >> 1 & 1) << 2; }
+  static constexpr int kRowBytes = 2 * D, kBytes = kBlock * kRowBytes, kGroupBytes = kBlock * 64;
+  static constexpr int kCopies = D / 64;      // copies of a wavefront: 16 rows of as many groups
+  static __device__ __forceinline__ int k_turn(int row) { return row >> 2 & 3; }
 };
 
 template <typename T, int D>
@@ -626,14 +622,12 @@ paged_chunk_kernel(PagedAttention a) {
   const char* const cache_v = reinterpret_cast<const char*>(static_cast<const T*>(a.cache_v) + in_head);
   // (read as constants: scalar loads, which leave the count of vector memory operations to the copies)
   const auto* const table = (const int32_t __attribute__((address_space(4)))*)(uintptr_t)(b.page_table + (int64_t)tile.seq * b.pages_per_seq);
-  const int copy_row = 8 * wave + lane / B::kRowPieces, copy_at = lane % B::kRowPieces;   // rows follow by kCopyRows
-  uint32_t k_from[B::kCopies], v_from[B::kCopies];       // this lane's bytes, from its 16-key tile's first row on
-#pragma unroll
-  for (int i = 0; i < B::kCopies; ++i) {
-    const int r = copy_row + i * B::kCopyRows;
-    k_from[i] = (r & 15) * B::kRowBytes + (copy_at ^ B::k_turn(r)) * 16;
-    v_from[i] = (r & 15) * B::kRowBytes + (copy_at ^ B::v_turn(r)) * 16;
-  }
+  // Wavefront w copies 16-key tile w / 2, half of the groups: lane l 16 bytes of row l / 4.  (Bytes from the tile's first row on;
+  // the groups follow at 64 bytes.)
+  const int copy_row = 16 * (wave / 2) + lane / 4;
+  const uint32_t copy_from = (lane / 4) * B::kRowBytes + (wave % 2) * (B::kCopies * 64);
+  const uint32_t k_from = copy_from + ((lane & 3) ^ B::k_turn(copy_row)) * 16, v_from = copy_from + (lane & 3) * 16;
+  const uint32_t own_part = (wave % 2) * (B::kCopies * B::kGroupBytes) + (wave / 2) * 1024;
   const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(char __attribute__((address_space(3)))*)ring);
   // The place of this wavefront's rows in the block that is copied next: its page's column and the row within it follow each
   // other without divisions, and the column's entry is loaded a block ahead of its use.
@@ -652,11 +646,11 @@ paged_chunk_kernel(PagedAttention a) {
   auto issue = [&]() {                   // copies next_block, or the last one again
     const bool there = column < (uint32_t)b.pages_per_seq && (uint32_t)entry < b.n_pages;
     const int64_t at = there ? (int64_t)entry * b.page_stride + (int64_t)in_page * D : 0;
-    const uint32_t to = ring_at + ((uint32_t)(next_block - first_block) % kChunkSlots * kSlotBytes + wave * (B::kCopies * 1024));
+    const uint32_t to = ring_at + ((uint32_t)(next_block - first_block) % kChunkSlots * kSlotBytes + own_part);
     const char* const k_tile = cache_k + 2 * at;
     const char* const v_tile = cache_v + 2 * at;
 #pragma unroll
-    for (int i = 0; i < B::kCopies; ++i) copy_pieces(k_tile, k_from[i], v_tile, v_from[i], to + i * 1024, B::kBytes);
+    for (int i = 0; i < B::kCopies; ++i) copy_pieces(k_tile + 64 * i, k_from, v_tile + 64 * i, v_from, to + i * B::kGroupBytes, B::kBytes);
     ++next_block;
     if (next_block < end_block) {
       if (next_block == tile.lead) {
@@ -684,24 +678,18 @@ paged_chunk_kernel(PagedAttention a) {
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) o[t] = floatx16{0};
   float top = -INFINITY, sum = 0.f;
-  const char* v_base[kTiles];
-  {
-    const int i = lane & 15, r = 4 * h + (i >> 2);
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t)
-      v_base[t] = ring + B::kBytes + r * B::kRowBytes + ((4 * t + 2 * (lane >> 4 & 1) + (i >> 1 & 1)) ^ B::v_turn(r)) * 16 + (i & 1) * 8;
-  }
-  const char* const k_base = ring + n * B::kRowBytes;
-  const int k_turn = B::k_turn(n);
+  const int vi = lane & 15;
+  const char* const v_base = ring + B::kBytes + (4 * h + (vi >> 2)) * 64 + (lane >> 4 & 1) * 32 + (vi & 3) * 8;
+  const char* const k_base[2] = {ring + n * 64 + (h ^ B::k_turn(n)) * 16, ring + n * 64 + ((2 + h) ^ B::k_turn(n)) * 16};
   auto slot_of = [&](int32_t block) { return (uint32_t)(block - first_block) % kChunkSlots * kSlotBytes; };
   auto meets = [&](int32_t block) {
     const int32_t j0 = first_key(tile, block);
     return (j0 <= hi_max && j0 + kBlock - 1 >= lo_min) || j0 < lead_max;
   };
   auto read_k = [&](int32_t block, Piece (&k)[kSteps]) {
-    const char* const at = k_base + slot_of(block);
+    const char* const at[2] = {k_base[0] + slot_of(block), k_base[1] + slot_of(block)};
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) k[i] = *reinterpret_cast<const Piece*>(at + ((2 * i + h) ^ k_turn) * 16);
+    for (int i = 0; i < kSteps; ++i) k[i] = *reinterpret_cast<const Piece*>(at[i & 1] + i / 2 * B::kGroupBytes);
   };
   auto products = [&](const Piece (&k)[kSteps], floatx16& s) {
     s = floatx16{0};
@@ -711,10 +699,10 @@ paged_chunk_kernel(PagedAttention a) {
   auto read_v = [&](int32_t block, int u, Piece (&v)[kTiles]) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const char* const at = v_base[t] + slot_of(block) + 16 * u * B::kRowBytes;
+      const char* const at = v_base + slot_of(block) + t * B::kGroupBytes + 16 * u * 64;
       const short4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)at);
       const short4v high =
-          __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(at + 8 * B::kRowBytes));
+          __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(at + 8 * 64));
       const vec_t<short, 8> both = __builtin_shufflevector(low, high, 0, 1, 2, 3, 4, 5, 6, 7);
       v[t] = __builtin_bit_cast(Piece, both);
     }
@@ -781,11 +769,11 @@ paged_chunk_kernel(PagedAttention a) {
     if (missing || j0 + kBlock > tile.kept) {
       // values that are no token's: 0, whatever memory held, each wavefront in its own rows (every wavefront is here)
       const uint32_t held = held_of(j0);
-      char* const dst = ring + slot_of(block) + B::kBytes + wave * (B::kCopies * 1024);
+      char* const dst = ring + slot_of(block) + B::kBytes + own_part;
+      if (!(held >> (wave / 2) & 1) || j0 + copy_row >= tile.kept) {
 #pragma unroll
-      for (int i = 0; i < B::kCopies; ++i)
-        if (!(held >> (wave / 2) & 1) || j0 + copy_row + i * B::kCopyRows >= tile.kept)
-          *reinterpret_cast<uint4*>(dst + i * 1024 + lane * 16) = uint4{0, 0, 0, 0};
+        for (int i = 0; i < B::kCopies; ++i) *reinterpret_cast<uint4*>(dst + i * B::kGroupBytes + lane * 16) = uint4{0, 0, 0, 0};
+      }
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
     if (!meets(block)) return;
@@ -921,7 +909,7 @@ paged_chunk_kernel(PagedAttention a) {
   }
   // A lane holds pieces of its own row; the rows go through LDS and leave whole.
   const float inv = total != 0.f ? 1.f / total : 0.f;
-  constexpr int kPitch = B::kRowBytes + 16;
+  constexpr int kPitch = B::kRowBytes + 16, kRowPieces = D / 8;
   static_assert(kWaves * 32 * kPitch <= kChunkSlots * kSlotBytes, "the results fit the ring");
   char* const mine = ring + wave * (32 * kPitch);
 #pragma unroll
@@ -935,8 +923,8 @@ paged_chunk_kernel(PagedAttention a) {
     }
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
-  for (int i = 0; i < 32 * B::kRowPieces / kWave; ++i) {
-    const int r = lane / B::kRowPieces + i * (kWave / B::kRowPieces), at = lane % B::kRowPieces;
+  for (int i = 0; i < 32 * kRowPieces / kWave; ++i) {
+    const int r = lane / kRowPieces + i * (kWave / kRowPieces), at = lane % kRowPieces;
     if (r < own_count) {
       int32_t h_out, row_out;
       place_out(r, h_out, row_out);
