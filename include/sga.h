@@ -398,7 +398,7 @@ sga_status sga_rotary(const sga_rows* X, const sga_rows* Y, const int64_t* posit
 /*
  * New tokens of several sequences and the pages that hold their keys and values.
  *   Cache    K and V each [n_pages][Hkv][page_size][d]: a page is page_size tokens of every key
- *            head, page_stride elements (>= Hkv * page_size * d) behind the one before it.
+ *            head, page_stride elements (Hkv * page_size * d or more, below 2^32) behind the one before it.
  *   Tokens   packed in rows of Q, K, V, O: sequence s has rows seq_ptr[s] .. seq_ptr[s+1] - 1;
  *            seq_ptr[0] = 0, non-decreasing, seq_ptr[n_seqs] <= n_tokens.  Rows behind the last
  *            sequence are padding: not read, and left as they were in every output.

@@ -487,7 +487,7 @@ bool valid_batch(const sga_paged_batch* b, int32_t Hkv, int32_t d) {
   if (b->n_tokens < 0 || b->n_tokens >= (int64_t(1) << 31)) return false;
   if (b->n_pages < 1 || b->n_pages >= (int64_t(1) << 31) || b->page_size < 1 || b->page_size > 65536) return false;
   if (b->pages_per_seq < 1 || (int64_t)b->pages_per_seq * b->page_size > (int64_t(1) << 31) - 1024) return false;
-  if (b->page_stride < (int64_t)Hkv * b->page_size * d) return false;
+  if (b->page_stride < (int64_t)Hkv * b->page_size * d || b->page_stride >= (int64_t(1) << 32)) return false;
   if (b->n_tokens == 0 || b->n_seqs == 0) return true;
   return b->page_table && b->seq_ptr && b->seq_len && aligned_to(b->page_table, 4) && aligned_to(b->seq_len, 4) &&
          aligned_to(b->seq_ptr, 8);
@@ -611,6 +611,7 @@ sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const voi
   a.lse = lse;
   a.scale = scale;
   a.tile_rows = plan.tile_rows;
+  a.page_pieces = (uint32_t)(batch->page_stride / (16 / element_bytes(dtype)));
   a.slots = plan.slots;
   const bool split = plan.splits > 1 && workspace_bytes >= plan.bytes;
   a.splits = split ? plan.splits : 1;

@@ -520,16 +520,31 @@ __device__ __forceinline__ void wait_loads_except() {
   __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | ((N >> 4) << 14));
 }
 
-// Two times 16 bytes per lane from k and v plus the lane's offsets into LDS at `to` and `to` + apart, + 16 * lane each: without
-// registers and behind the compiler's back, completion is waited for by count (wait_loads_except) and a barrier.  (M0
-// holds the address in LDS; the compiler's own value is put back.)
-__device__ __forceinline__ void copy_pieces(const void* k, uint32_t k_offset, const void* v, uint32_t v_offset, uint32_t to,
-                                            uint32_t apart) {
+// kCopies times 16 bytes per lane from k, the lane's offset and 64 bytes for each copy before on, into LDS at `to` + 16 * lane and
+// `step` further on each, and then from v likewise: without registers and behind the compiler's back, completion is waited
+// for by count (wait_loads_except) and a barrier.  (M0 holds the address in LDS; the compiler's own value is put back.)
+template <int kCopies, int kStep, int kApart>
+__device__ __forceinline__ void copy_pieces(const char* k, uint32_t k_offset, const char* v, uint32_t v_offset, uint32_t to) {
   uint32_t kept;
-  asm volatile(
-      "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\t"
-      "s_mov_b32 m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %6\n\ts_mov_b32 m0, %0"
-      : "=&s"(kept) : "s"(to), "v"(k_offset), "s"(k), "s"(to + apart), "v"(v_offset), "s"(v) : "memory");
+  if constexpr (kCopies == 1) {
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %5\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\t"
+        "s_add_u32 m0, m0, %6\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %3, %4\n\ts_mov_b32 m0, %0"
+        : "=&s"(kept) : "v"(k_offset), "s"(k), "v"(v_offset), "s"(v), "s"(to), "i"(kApart) : "memory", "scc");
+  } else {
+    static_assert(kCopies % 2 == 0, "copies in pairs");
+#pragma unroll
+    for (int i = 0; i < kCopies; i += 2)
+      asm volatile(
+          "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %7\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %3\n\t"
+          "s_add_u32 m0, m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %3\n\t"
+          "s_add_u32 m0, m0, %9\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %4, %6\n\t"
+          "s_add_u32 m0, m0, %8\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %5, %6\n\ts_mov_b32 m0, %0"
+          : "=&s"(kept)
+          : "v"(k_offset + 64 * i), "v"(k_offset + 64 * i + 64), "s"(k), "v"(v_offset + 64 * i), "v"(v_offset + 64 * i + 64), "s"(v),
+            "s"(to + i * kStep), "i"(kStep), "i"(kApart - kStep)
+          : "memory", "scc");
+  }
 }
 
 // A block of 32 keys in LDS: groups of 32 channels, in a group the 32 keys' rows of 64 bytes.  What the products read then
@@ -630,13 +645,13 @@ paged_chunk_kernel(PagedAttention a) {
   const uint32_t own_part = (wave % 2) * (B::kCopies * B::kGroupBytes) + (wave / 2) * 1024;
   const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(char __attribute__((address_space(3)))*)ring);
   // The place of this wavefront's rows in the block that is copied next: its page's column and the row within it follow each
-  // other without divisions, and the column's entry is loaded a block ahead of its use.
+  // other without divisions, and the column's entry is loaded a block ahead of its use.  An entry that is no page
+  // is read as some page (what it copies is hidden), a column behind the last as the last.
   const uint32_t page = b.page.value, columns_step = page == 16 ? 2 : 0, rows_step = page == 16 ? 0 : kBlock;
-  int32_t next_block = first_block, entry = 0;
-  uint32_t column = 0, in_page = 0;
-  auto look_up = [&]() {
-    entry = table[column < (uint32_t)b.pages_per_seq ? column : (uint32_t)b.pages_per_seq - 1];
-  };
+  const uint32_t last_column = b.pages_per_seq - 1, last_page = b.n_pages - 1;
+  int32_t next_block = first_block;
+  uint32_t column = 0, in_page = 0, entry = 0, next_at = ring_at + own_part;
+  auto look_up = [&]() { entry = (uint32_t)table[min(column, last_column)]; };
   auto start_at = [&](int32_t block) {
     const uint32_t j = (uint32_t)(first_key(tile, block) + 16 * (wave / 2));
     column = quotient(j, b.page);
@@ -644,23 +659,19 @@ paged_chunk_kernel(PagedAttention a) {
     look_up();
   };
   auto issue = [&]() {                   // copies next_block, or the last one again
-    const bool there = column < (uint32_t)b.pages_per_seq && (uint32_t)entry < b.n_pages;
-    const int64_t at = there ? (int64_t)entry * b.page_stride + (int64_t)in_page * D : 0;
-    const uint32_t to = ring_at + ((uint32_t)(next_block - first_block) % kChunkSlots * kSlotBytes + own_part);
-    const char* const k_tile = cache_k + 2 * at;
-    const char* const v_tile = cache_v + 2 * at;
-#pragma unroll
-    for (int i = 0; i < B::kCopies; ++i) copy_pieces(k_tile + 64 * i, k_from, v_tile + 64 * i, v_from, to + i * B::kGroupBytes, B::kBytes);
-    ++next_block;
-    if (next_block < end_block) {
+    const uint64_t at = ((uint64_t)min(entry, last_page) * a.page_pieces << 4) + in_page * B::kRowBytes;
+    copy_pieces<B::kCopies, B::kGroupBytes, B::kBytes>(cache_k + at, k_from, cache_v + at, v_from, next_at);
+    next_at = ring_at + ((next_at - ring_at + kSlotBytes) & (kChunkSlots * kSlotBytes - 1));
+    if (++next_block < end_block) {
       if (next_block == tile.lead) {
         start_at(next_block);
       } else {
         column += columns_step;
         in_page += rows_step;
-        const bool over = in_page >= page;
-        column += over ? 1 : 0;
-        in_page -= over ? page : 0;
+        if (in_page >= page) {
+          in_page -= page;
+          ++column;
+        }
         look_up();
       }
     }
@@ -686,8 +697,8 @@ paged_chunk_kernel(PagedAttention a) {
     const int32_t j0 = first_key(tile, block);
     return (j0 <= hi_max && j0 + kBlock - 1 >= lo_min) || j0 < lead_max;
   };
-  auto read_k = [&](int32_t block, Piece (&k)[kSteps]) {
-    const char* const at[2] = {k_base[0] + slot_of(block), k_base[1] + slot_of(block)};
+  auto read_k = [&](uint32_t slot_at, Piece (&k)[kSteps]) {
+    const char* const at[2] = {k_base[0] + slot_at, k_base[1] + slot_at};
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) k[i] = *reinterpret_cast<const Piece*>(at[i & 1] + i / 2 * B::kGroupBytes);
   };
@@ -696,10 +707,10 @@ paged_chunk_kernel(PagedAttention a) {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) s = matrix32(k[i], qf[i], s);
   };
-  auto read_v = [&](int32_t block, int u, Piece (&v)[kTiles]) {
+  auto read_v = [&](uint32_t slot_at, int u, Piece (&v)[kTiles]) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const char* const at = v_base + slot_of(block) + t * B::kGroupBytes + 16 * u * 64;
+      const char* const at = v_base + slot_at + t * B::kGroupBytes + 16 * u * 64;
       const short4v low = __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)at);
       const short4v high =
           __builtin_amdgcn_ds_read_tr16_b64_v4i16((short4v __attribute__((address_space(3)))*)(at + 8 * 64));
@@ -733,7 +744,7 @@ paged_chunk_kernel(PagedAttention a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[t][r] *= keep;
   };
-  auto weigh = [&](int32_t block, const floatx16& s, float total, Piece (&p)[2]) {
+  auto weigh = [&](uint32_t slot_at, const floatx16& s, float total, Piece (&p)[2]) {
     if (__any(!(total < kMostNumerators))) {          // (before a row's first key: infinite or NaN)
       raise(s);
       total = numerators(s, top > -INFINITY ? top : 0.f, p);
@@ -742,7 +753,7 @@ paged_chunk_kernel(PagedAttention a) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       Piece v[kTiles];
-      read_v(block, u, v);
+      read_v(slot_at, u, v);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t) o[t] = matrix32(v[t], p[u], o[t]);
     }
@@ -779,7 +790,7 @@ paged_chunk_kernel(PagedAttention a) {
     if (!meets(block)) return;
     Piece k[kSteps], p[2];
     floatx16 s;
-    read_k(block, k);
+    read_k(slot_of(block), k);
     products(k, s);
     const uint32_t held = held_of(j0);
 #pragma unroll
@@ -789,15 +800,18 @@ paged_chunk_kernel(PagedAttention a) {
       s[r] = sees ? s[r] : -INFINITY;
     }
     const float total = numerators(s, top, p);
-    weigh(block, s, total, p);
+    weigh(slot_of(block), s, total, p);
   };
   // A block that every row sees whole, its scores at hand; those of the next one are issued ahead of its exponentials.
-  auto inside = [&](int32_t block, floatx16& s, floatx16& ahead) {
+  uint32_t here = 0;                    // its slot
+  auto after = [](uint32_t slot_at) { return (slot_at + kSlotBytes) & (kChunkSlots * kSlotBytes - 1); };
+  auto inside = [&](floatx16& s, floatx16& ahead) {
     Piece k[kSteps], p[2];
-    read_k(block + 1, k);
+    read_k(after(here), k);
     products(k, ahead);
     const float total = numerators(s, top, p);
-    weigh(block, s, total, p);
+    weigh(here, s, total, p);
+    here = after(here);
   };
 
   if (first_block < end_block) {
@@ -824,28 +838,29 @@ paged_chunk_kernel(PagedAttention a) {
     for (; block < inner; ++block) edge(block);
     if (block < outer) {
       floatx16 s_a, s_b;
+      here = slot_of(block);
       {
         Piece k[kSteps];
         publish();
-        read_k(block, k);
+        read_k(here, k);
         products(k, s_a);
       }
       for (; block + 2 < outer; block += 2) {
-        inside(block, s_a, s_b);
+        inside(s_a, s_b);
         publish();
-        inside(block + 1, s_b, s_a);
+        inside(s_b, s_a);
         publish();
       }
       Piece p[2];
       if (block + 1 < outer) {
-        inside(block, s_a, s_b);
+        inside(s_a, s_b);
         publish();
         const float total = numerators(s_b, top, p);
-        weigh(block + 1, s_b, total, p);
+        weigh(here, s_b, total, p);
         block += 2;
       } else {
         const float total = numerators(s_a, top, p);
-        weigh(block, s_a, total, p);
+        weigh(here, s_a, total, p);
         ++block;
       }
     }

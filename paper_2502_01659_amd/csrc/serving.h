@@ -101,6 +101,7 @@ struct PagedAttention {
   FastDiv group;             // Hq / Hkv
   int32_t L, window, n_global, causal;
   float scale;
+  uint32_t page_pieces;      // 16-byte pieces from page to page
   float* partials;           // partial states of split tiles
   int32_t tile_rows;
   int32_t splits;            // most pieces that a tile is cut into
