@@ -582,7 +582,7 @@ sga_status sga_paged_workspace_bytes(const sga_paged_batch* batch, const sga_mas
   size_t most = 0;
   for (a.causal = 0; a.causal < 2 && batch->n_tokens > 0 && batch->n_seqs > 0; ++a.causal) {
     const PagedPlan p = plan_paged(a);
-    if (p.slots == 0) return SGA_ERR_OVERFLOW;
+    if (p.groups == 0) return SGA_ERR_OVERFLOW;
     most = p.bytes > most ? p.bytes : most;
   }
   *bytes_out = most;
@@ -603,7 +603,7 @@ sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const voi
   if (!cache_k || !cache_v || !aligned16(cache_k) || !aligned16(cache_v)) return SGA_ERR_INVALID_ARG;
   if (batch->page_stride % (16 / element_bytes(dtype)) != 0 || !aligned_to(lse, 4)) return SGA_ERR_INVALID_ARG;
   const PagedPlan plan = plan_paged(a);
-  if (plan.slots == 0) return SGA_ERR_OVERFLOW;
+  if (plan.groups == 0) return SGA_ERR_OVERFLOW;
   (void)hipGetLastError();
   a.Q = Q->data; a.q_head = Q->head_stride; a.q_row = Q->row_stride;
   a.O = O->data; a.o_head = O->head_stride; a.o_row = O->row_stride;
@@ -612,10 +612,10 @@ sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const voi
   a.scale = scale;
   a.tile_rows = plan.tile_rows;
   a.page_pieces = (uint32_t)(batch->page_stride / (16 / element_bytes(dtype)));
+  a.groups = plan.groups;
+  a.partials = plan.bytes > 0 && workspace_bytes >= plan.bytes ? static_cast<float*>(workspace) : nullptr;
   a.slots = plan.slots;
-  const bool split = plan.splits > 1 && workspace_bytes >= plan.bytes;
-  a.splits = split ? plan.splits : 1;
-  a.partials = split ? static_cast<float*>(workspace) : nullptr;
+  a.splits = a.partials ? plan.splits : 1;
   a.stream = static_cast<hipStream_t>(stream);
   return launch_paged(a);
 }

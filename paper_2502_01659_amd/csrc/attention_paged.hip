@@ -26,7 +26,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kBlock = 32;            // keys of a block
 constexpr int kRows = 16;             // rows of a tile
 constexpr int kWaves = 4;             // wavefronts of a workgroup, which take its blocks in turn
-constexpr int kPieceBlocks = 4 * kWaves;   // fewest blocks of a piece of a split tile
+constexpr int kPieceBlocks = 16;      // fewest blocks of a piece of a split tile of 128 rows
+constexpr int kChunkPieces = 2048;
 constexpr int kTokenRows = 64;        // sequences with more rows than this on average take tiles of 128 rows
 
 __device__ __forceinline__ int64_t uniform64(int64_t v) {
@@ -75,33 +76,34 @@ __device__ __forceinline__ Sight sight_of(const PagedAttention& a, int32_t p, in
   return {p > a.window ? p - a.window : 0, far < last ? (int32_t)far : last, a.n_global < last + 1 ? a.n_global : last + 1};
 }
 
-// The tile of slot i: sequence s owns the slots from seq_ptr[s] * group / kTileRows + s, which are enough for it and follow
-// from seq_ptr alone.  False: an empty slot.  All lanes call it.
-template <int kTileRows>
-__device__ __forceinline__ bool tile_of(const PagedAttention& a, int32_t slot, Tile& t) {
-  const PagedArgs& b = a.batch;
-  const int64_t group = a.group.value;
-  auto first_slot = [&](int32_t s) { return (int64_t)row_of_sequence(b, s) * group / kTileRows + s; };
-  t.seq = __builtin_amdgcn_readfirstlane(last_not_above(b.n_seqs, slot, first_slot));
-  t.begin = __builtin_amdgcn_readfirstlane(row_of_sequence(b, t.seq));
-  const int32_t end = __builtin_amdgcn_readfirstlane(row_of_sequence(b, t.seq + 1));
-  t.length = __builtin_amdgcn_readfirstlane(b.seq_len[t.seq]);
-  t.n_new = end > t.begin ? end - t.begin : 0;
-  const int64_t first = ((int64_t)slot - (t.begin * group / kTileRows + t.seq)) * kTileRows, rows = t.n_new * group;
-  if (first < 0 || first >= rows) return false;
-  t.first = (int32_t)first;
-  t.count = rows - first < kTileRows ? (int32_t)(rows - first) : kTileRows;
-  const int64_t room = (int64_t)b.pages_per_seq * b.page.value;
-  int64_t kept = t.length < 0 ? 0 : t.length;
+// Tokens of a sequence that can be seen.
+__device__ __forceinline__ int32_t kept_of(const PagedAttention& a, int32_t length) {
+  const int64_t room = (int64_t)a.batch.pages_per_seq * a.batch.page.value;
+  int64_t kept = length < 0 ? 0 : length;
   kept = kept < room ? kept : room;
-  t.kept = (int32_t)(kept < a.L ? kept : a.L);
+  return (int32_t)(kept < a.L ? kept : a.L);
+}
+
+// Tile t of a sequence.
+template <int kTileRows>
+__device__ __forceinline__ Tile tile_of(const PagedAttention& a, int32_t seq, int32_t begin, int32_t n_new, int32_t length,
+                                        int32_t index) {
+  Tile t;
+  t.seq = seq;
+  t.begin = begin;
+  t.n_new = n_new;
+  t.length = length;
+  const int64_t left = (int64_t)n_new * a.group.value - (int64_t)index * kTileRows;
+  t.first = index * kTileRows;
+  t.count = left < kTileRows ? (int32_t)left : kTileRows;
+  t.kept = kept_of(a, length);
   // the rows' keys: positions grow with the rows, and so do both ends of what they see
   const int32_t p0 = t.length - t.n_new + (int32_t)quotient((uint32_t)t.first, a.group);
   const int32_t p1 = t.length - t.n_new + (int32_t)quotient((uint32_t)(t.first + t.count - 1), a.group);
   // (rows before 0 and from L on see nothing; a global row sees from 0 on, and then so does what follows)
   const int32_t from = p0 < 0 ? 0 : p0, to = p1 < a.L ? p1 : a.L - 1;
   t.lead = t.base = t.blocks = 0;
-  if (from > to) return true;
+  if (from > to) return t;
   const Sight low = sight_of(a, from, t.kept), high = sight_of(a, to, t.kept);
   // (not causal: a global row sees to the end)
   const int32_t last = low.hi > high.hi ? low.hi : high.hi;
@@ -110,7 +112,267 @@ __device__ __forceinline__ bool tile_of(const PagedAttention& a, int32_t slot, T
   lead = lead < t.base ? lead : t.base;
   t.lead = (lead + kBlock - 1) / kBlock;
   t.blocks = t.lead + (last >= t.base ? (last - t.base) / kBlock + 1 : 0);
+  return t;
+}
+
+// ---- the division of a call's work ---------------------------------------------------------------------------
+// All work lies on one line: sequences, in each its key heads, in each its tiles, each about as long as the keys that
+// it meets and kTileCost for itself.  The line is cut into equal shares, one for each workgroup that the chip holds, whatever the
+// lengths of the sequences are; a cut falls inside a tile where tiles are long, and the tile's parts are then joined.
+// Lengths are estimates (a tile's blocks are counted when it is met; a cut goes to the block in proportion) that follow from
+// the sequence alone: tile u < t1 is a0 + u * step long, the others a1.  Causal, the keys grow with the tiles until the
+// window is full; otherwise the tiles of global rows see everything and the others a window.
+constexpr uint32_t kTileCost = 64;
+constexpr uint32_t kLeastShare = 512;      // keys of the smallest share
+constexpr uint32_t kWholeTiles = 32;       // tiles shorter than this part of a share are not cut
+
+__device__ __forceinline__ uint64_t quotient64(uint64_t n, uint64_t d) {
+  return (n | d) >> 32 ? n / d : (uint64_t)((uint32_t)n / (uint32_t)d);
+}
+__device__ __forceinline__ uint64_t uniform64u(uint64_t v) { return (uint64_t)uniform64((int64_t)v); }
+__device__ __forceinline__ uint64_t from_lane(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), lane) << 32 |
+         (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, lane);
+}
+
+struct SequenceWork {
+  int32_t begin, n_new, length;
+  uint32_t tiles, a0, a1, t1;
+  uint64_t per_head;
+  // length of the first t tiles
+  __device__ __forceinline__ uint64_t before(uint32_t t, uint32_t step) const {
+    const uint64_t n = t < t1 ? t : t1;
+    return n * a0 + (uint64_t)step * (n * (n - 1) / 2) + (uint64_t)(t - (uint32_t)n) * a1;
+  }
+  __device__ __forceinline__ uint32_t length_of(uint32_t t, uint32_t step) const { return t < t1 ? a0 + t * step : a1; }
+};
+
+template <int kTileRows>
+__device__ __forceinline__ uint32_t step_of(const PagedAttention& a) { return a.causal ? kTileRows / a.group.value : 0; }
+
+template <int kTileRows>
+__device__ __forceinline__ SequenceWork work_of(const PagedAttention& a, int32_t s) {
+  SequenceWork w{};
+  const PagedArgs& b = a.batch;
+  if (s >= b.n_seqs) return w;
+  w.begin = row_of_sequence(b, s);
+  const int32_t end = row_of_sequence(b, s + 1);
+  w.length = b.seq_len[s];
+  w.n_new = end > w.begin ? end - w.begin : 0;
+  w.tiles = (uint32_t)(((int64_t)w.n_new * a.group.value + kTileRows - 1) / kTileRows);
+  const int64_t kept = kept_of(a, w.length), old = (int64_t)w.length - w.n_new, step = kTileRows / a.group.value;
+  int64_t window = (a.causal ? 1 : 2) * (int64_t)a.window + step + 1 + a.n_global;
+  window = window < kept ? window : kept;
+  w.a1 = (uint32_t)window + kTileCost;
+  if (a.causal) {
+    int64_t first = old + step + 1;
+    first = first < 0 ? 0 : first < window ? first : window;
+    w.a0 = (uint32_t)first + kTileCost;
+    if (step > 0 && first < window) {
+      const int64_t ramp = (window - first + step - 1) / step;
+      w.t1 = ramp < w.tiles ? (uint32_t)ramp : w.tiles;
+    } else {
+      w.a0 = w.a1;
+    }
+  } else {
+    w.a0 = (uint32_t)kept + kTileCost;
+    if (old < a.n_global) {
+      const int64_t global = ((a.n_global - (old < 0 ? 0 : old)) * (int64_t)a.group.value + kTileRows - 1) / kTileRows;
+      w.t1 = global < w.tiles ? (uint32_t)global : w.tiles;
+    }
+  }
+  w.per_head = w.before(w.tiles, (uint32_t)(a.causal ? step : 0));
+  return w;
+}
+
+// The thread's index, as if read anew: what follows from it is not kept in registers from one part of a share to the next.
+__device__ __forceinline__ int thread_again() {
+  int t = threadIdx.x;
+  asm volatile("" : "+v"(t));
+  return t;
+}
+
+// A part of a tile that a share holds: [from, to) of the tile's length `extent`.
+struct Part {
+  int32_t seq, begin, n_new, length, tile, head;
+  uint32_t from, to, extent;
+  int32_t there;             // 0: the share is done
+};
+
+// A workgroup's walk along its share.  It lies in LDS, since it is needed between the parts only; the first wavefront
+// walks, all its lanes with the same values but where they load a sequence each.
+template <int kTileRows>
+struct Share {
+  SequenceWork work[kWave];  // sequences chunk ..
+  uint64_t start[kWave];     // where each begins on the line
+  uint64_t behind;           // where the last one ends
+  uint64_t at, end, size;    // what is left of the share, and a whole one
+  int32_t chunk, lane;       // the current sequence is chunk + lane
+  uint32_t head, tile, offset, extent;     // current tile, the place in it, its length
+  Part part;
+
+  // 64 sequences from `from` on, which begins at `base` on the line
+  __device__ __forceinline__ void load(const PagedAttention& a, int32_t from, uint64_t base) {
+    const int l = threadIdx.x & (kWave - 1);
+    const SequenceWork w = work_of<kTileRows>(a, from + l);
+    const uint64_t own = w.per_head * (uint64_t)a.Hkv;
+    uint64_t sum = own;
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      const uint64_t below = (uint64_t)__shfl_up((unsigned long long)sum, off, kWave);
+      if (l >= off) sum += below;
+    }
+    work[l] = w;
+    start[l] = base + sum - own;
+    chunk = from;
+    behind = base + from_lane(sum, kWave - 1);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __device__ __forceinline__ void take_sequence() {
+    lane = 63 - __builtin_clzll(__ballot(start[threadIdx.x & (kWave - 1)] <= at) | 1);
+  }
+  // Finds the place `at`.
+  __device__ __forceinline__ void locate(const PagedAttention& a, uint32_t step) {
+    take_sequence();
+    const SequenceWork& now = work[lane];
+    const uint64_t in_seq = at - start[lane];
+    head = (uint32_t)quotient64(in_seq, now.per_head);
+    const uint64_t in_head = in_seq - head * now.per_head, ramp = now.before(now.t1, step);
+    if (in_head >= ramp) {
+      tile = now.t1 + (uint32_t)quotient64(in_head - ramp, now.a1);
+    } else {
+      uint32_t low = 0, high = now.t1;        // before(low) <= in_head < before(high)
+      while (high - low > 1) {
+        const uint32_t mid = (low + high) / 2;
+        if (now.before(mid, step) <= in_head) low = mid; else high = mid;
+      }
+      tile = low;
+    }
+    offset = (uint32_t)(in_head - now.before(tile, step));
+    extent = now.length_of(tile, step);
+  }
+  __device__ __forceinline__ bool whole() const { return (uint64_t)extent * kWholeTiles < size; }
+
+  // Share i of the call.  False: there is nothing in it.
+  __device__ __forceinline__ bool begin(const PagedAttention& a, uint32_t i) {
+    uint64_t total = 0;
+    for (int32_t c = 0; c < a.batch.n_seqs; c += kWave) {
+      load(a, c, total);
+      total = behind;
+    }
+    uint64_t each = quotient64(total + a.groups - 1, a.groups);
+    each = each > kLeastShare ? each : kLeastShare;
+    size = each;
+    at = each * i;
+    end = at + each < total ? at + each : total;
+    if (at >= total) return false;
+    if (a.batch.n_seqs > kWave) {
+      load(a, 0, 0);
+      while (behind <= at && chunk + kWave < a.batch.n_seqs) load(a, chunk + kWave, behind);
+    }
+    locate(a, step_of<kTileRows>(a));
+    return true;
+  }
+  // The part of the current tile that is in the share.
+  __device__ __forceinline__ void take_part(const PagedAttention& a) {
+    const bool uncut = !a.partials || whole();
+    if (uncut && offset > 0) {              // the share begins inside a tile that is not cut: with its beginning
+      at -= offset;
+      offset = 0;
+    }
+    part.there = 0;
+    if (at >= end) return;
+    const uint64_t left = end - at;
+    const uint32_t to = offset + left < extent ? offset + (uint32_t)left : extent;
+    if (uncut && to < extent) return;
+    const SequenceWork& now = work[lane];
+    if (tile >= now.tiles || head >= (uint32_t)a.Hkv) return;          // (lengths that change while the call runs)
+    part = Part{chunk + lane, now.begin, now.n_new, now.length, (int32_t)tile, (int32_t)head, offset, to, extent, 1};
+  }
+  // Goes on behind the part.
+  __device__ __forceinline__ void advance(const PagedAttention& a) {
+    at += part.to - offset;
+    offset = 0;
+    if (at < end) {
+      if (++tile == work[lane].tiles) {
+        tile = 0;
+        if (++head == (uint32_t)a.Hkv) {
+          head = 0;
+          while (at >= behind && chunk + kWave < a.batch.n_seqs) load(a, chunk + kWave, behind);
+          take_sequence();
+        }
+      }
+      extent = work[lane].length_of(tile, step_of<kTileRows>(a));
+    }
+    take_part(a);
+  }
+  // The first part of share i, or the next one; all wavefronts call it.
+  __device__ __forceinline__ Part next(const PagedAttention& a, uint32_t i, bool first) {
+    if (threadIdx.x < kWave) {
+      if (!first) advance(a);
+      else if (begin(a, i)) take_part(a);
+      else part.there = 0;
+    }
+    __syncthreads();
+    Part p;
+    p.seq = __builtin_amdgcn_readfirstlane(part.seq);
+    p.begin = __builtin_amdgcn_readfirstlane(part.begin);
+    p.n_new = __builtin_amdgcn_readfirstlane(part.n_new);
+    p.length = __builtin_amdgcn_readfirstlane(part.length);
+    p.tile = __builtin_amdgcn_readfirstlane(part.tile);
+    p.head = __builtin_amdgcn_readfirstlane(part.head);
+    p.from = __builtin_amdgcn_readfirstlane(part.from);
+    p.to = __builtin_amdgcn_readfirstlane(part.to);
+    p.extent = __builtin_amdgcn_readfirstlane(part.extent);
+    p.there = __builtin_amdgcn_readfirstlane(part.there);
+    return p;
+  }
+};
+
+// Blocks [first, end) of a tile that the part [from, to) of its length `extent` stands for.
+__device__ __forceinline__ int32_t block_at(uint32_t place, uint32_t extent, int32_t blocks) {
+  if (place == 0) return 0;
+  if (place >= extent) return blocks;
+  return (int32_t)quotient64((uint64_t)place * (uint32_t)blocks, extent);
+}
+
+// A partial state of a tile: O [rows][D], then the rows' references and sums.
+template <int D, int kTileRows>
+__device__ __forceinline__ float* record_of(const PagedAttention& a, int64_t i) {
+  return a.partials + i * (kTileRows * (D + 2));
+}
+// Each share has two, of the tile that it begins within and of the one that it ends within.
+template <int D>
+__device__ __forceinline__ float* record_of_share(const PagedAttention& a, uint32_t share, bool begins_within) {
+  return record_of<D, kRows>(a, (int64_t)share * 2 + (begins_within ? 0 : 1));
+}
+
+// The tile of slot i (tiles of 128 rows): sequence s owns the slots from seq_ptr[s] * group / kTileRows + s, which are
+// enough for it and follow from seq_ptr alone.  False: an empty slot.  All lanes call it.
+template <int kTileRows>
+__device__ __forceinline__ bool tile_of_slot(const PagedAttention& a, int32_t slot, Tile& t) {
+  const PagedArgs& b = a.batch;
+  const int64_t group = a.group.value;
+  auto first_slot = [&](int32_t s) { return (int64_t)row_of_sequence(b, s) * group / kTileRows + s; };
+  const int32_t seq = __builtin_amdgcn_readfirstlane(last_not_above(b.n_seqs, slot, first_slot));
+  const int32_t begin = __builtin_amdgcn_readfirstlane(row_of_sequence(b, seq));
+  const int32_t end = __builtin_amdgcn_readfirstlane(row_of_sequence(b, seq + 1));
+  const int32_t length = __builtin_amdgcn_readfirstlane(b.seq_len[seq]);
+  const int32_t n_new = end > begin ? end - begin : 0;
+  const int64_t index = (int64_t)slot - (begin * group / kTileRows + seq);
+  if (index < 0 || index * kTileRows >= n_new * group) return false;
+  t = tile_of<kTileRows>(a, seq, begin, n_new, length, (int32_t)index);
   return true;
+}
+
+// Its pieces, at least kPieceBlocks blocks each.
+struct Pieces {
+  int32_t count, blocks;
+};
+__device__ __forceinline__ Pieces pieces_of(int32_t blocks, int32_t splits) {
+  const int32_t even = (blocks + splits - 1) / splits, each = even > kPieceBlocks ? even : kPieceBlocks;
+  const int32_t n = (blocks + each - 1) / each;
+  return {n > 0 ? n : 1, each};
 }
 
 __device__ __forceinline__ int32_t first_key(const Tile& t, int32_t block) {
@@ -123,17 +385,6 @@ __device__ __forceinline__ int64_t place_of(const PagedArgs& b, int32_t seq, int
   if (column >= (uint32_t)b.pages_per_seq) return -1;
   const uint32_t page = (uint32_t)b.page_table[(int64_t)seq * b.pages_per_seq + column];
   return page < b.n_pages ? (int64_t)page * b.page_stride + (int64_t)((uint32_t)j - column * b.page.value) * d : -1;
-}
-
-// Pieces of a tile: at least kPieceBlocks blocks each.
-struct Pieces {
-  int32_t count, blocks;
-};
-__device__ __forceinline__ Pieces pieces_of(int32_t blocks, int32_t splits) {
-  int32_t each = (blocks + splits - 1) / splits;
-  each = each > kPieceBlocks ? (each + kWaves - 1) / kWaves * kWaves : kPieceBlocks;
-  const int32_t n = (blocks + each - 1) / each;
-  return {n > 0 ? n : 1, each};
 }
 
 // Operands of 16-bit storage: eight values of a lane per product of 32.
@@ -253,6 +504,20 @@ __device__ __forceinline__ void attend_row(const PagedAttention& a, const Tile& 
   }
 }
 
+// Writes D / 16 channels of a finished row: o / total, and its lse.
+template <typename T, int D>
+__device__ __forceinline__ void store_row(const PagedAttention& a, const Tile& tile, int32_t head_kv, int32_t row, int32_t channel,
+                                          const float (&o)[D / 16], float top, float total) {
+  const int32_t group = (int32_t)a.group.value, flat = tile.first + row, token = (int32_t)quotient((uint32_t)flat, a.group);
+  const int32_t head = head_kv * group + (flat - token * group), at = tile.begin + token;
+  const float inv = total != 0.f ? 1.f / total : 0.f;
+  vec_t<T, D / 16> y;
+#pragma unroll
+  for (int c = 0; c < D / 16; ++c) y[c] = (T)(o[c] * inv);
+  *reinterpret_cast<vec_t<T, D / 16>*>(static_cast<T*>(a.O) + (int64_t)head * a.o_head + (int64_t)at * a.o_row + channel) = y;
+  if (a.lse && channel == 0) a.lse[(int64_t)head * a.batch.n_tokens + at] = (top + __builtin_amdgcn_logf(total)) * kLn2;
+}
+
 // Where the rows of a block's keys are.  kWholeTiles: pages hold multiples of 16 tokens, so a 16-key tile lies in one.
 struct Places {
   int64_t tile[2];           // kWholeTiles: element offset of the tile's first row (wave-uniform)
@@ -267,14 +532,16 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
   constexpr int kStride = D + 4;                          // floats of a row in LDS
   __shared__ __align__(16) float out[kWaves][kRows][kStride];
   __shared__ float tops[kWaves][kRows], sums[kWaves][kRows];
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int m = lane & 15, g = lane >> 4;
-  const int32_t slot = blockIdx.x, head_kv = blockIdx.y, piece = blockIdx.z;
-  Tile tile;
-  if (!tile_of<kRows>(a, slot, tile)) return;
-  const Pieces pieces = pieces_of(tile.blocks, a.splits);
-  if (piece >= pieces.count) return;
   const int32_t group = (int32_t)a.group.value;
+  __shared__ Share<kRows> share;
+  for (bool first_part = true;; first_part = false) {
+  const Part here = share.next(a, blockIdx.x, first_part);
+  if (!here.there) return;
+  const int tid = thread_again(), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int m = lane & 15, g = lane >> 4;
+  const int32_t head_kv = here.head;
+  const Tile tile = tile_of<kRows>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
+  float* const part = here.from == 0 && here.to == here.extent ? nullptr : record_of_share<D>(a, blockIdx.x, here.from > 0);
 
   // this lane's row
   const int32_t flat = tile.first + (m < tile.count ? m : 0);
@@ -340,8 +607,8 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
     }
   };
 
-  const int32_t first_block = piece * pieces.blocks;
-  const int32_t end_block = min(first_block + pieces.blocks, tile.blocks);
+  const int32_t first_block = block_at(here.from, here.extent, tile.blocks);
+  const int32_t end_block = block_at(here.to, here.extent, tile.blocks);
   float top, sum;
   float4v o[kRun];
 
@@ -444,42 +711,35 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
   // the wavefronts' states of a row, added in their order
   constexpr int kPer = D * kRows / (kWaves * kWave);       // channels of a thread: D / 16
   const int row = tid / (D / kPer), channel = tid % (D / kPer) * kPer;
-  if (row >= tile.count) return;
-  float high = -INFINITY;
+  if (row < tile.count) {
+    float high = -INFINITY;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) high = fmaxf(high, tops[w][row]);
-  const float against = high > -INFINITY ? high : 0.f;
-  float total = 0.f, x[kPer];
+    for (int w = 0; w < kWaves; ++w) high = fmaxf(high, tops[w][row]);
+    const float against = high > -INFINITY ? high : 0.f;
+    float total = 0.f, x[kPer];
 #pragma unroll
-  for (int c = 0; c < kPer; ++c) x[c] = 0.f;
+    for (int c = 0; c < kPer; ++c) x[c] = 0.f;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (sums[w][row] == 0.f) continue;                     // no key seen
-    const float weight = __builtin_amdgcn_exp2f(tops[w][row] - against);
-    total += weight * sums[w][row];
+    for (int w = 0; w < kWaves; ++w) {
+      if (sums[w][row] == 0.f) continue;                   // no key seen
+      const float weight = __builtin_amdgcn_exp2f(tops[w][row] - against);
+      total += weight * sums[w][row];
 #pragma unroll
-    for (int c = 0; c < kPer; ++c) x[c] += weight * out[w][row][channel + c];
-  }
-  if (pieces.count > 1) {
-    float* part = a.partials + (((int64_t)slot * a.Hkv + head_kv) * a.splits + piece) * (kRows * (D + 2));
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) part[row * D + channel + c] = x[c];
-    if (channel == 0) {
-      part[kRows * D + row] = high;
-      part[kRows * (D + 1) + row] = total;
+      for (int c = 0; c < kPer; ++c) x[c] += weight * out[w][row][channel + c];
     }
-    return;
-  }
-  const int32_t f = tile.first + row, tok = (int32_t)quotient((uint32_t)f, a.group);
-  const int32_t h = head_kv * group + (f - tok * group), at_row = tile.begin + tok;
-  const float inv = total != 0.f ? 1.f / total : 0.f;
-  T* to = static_cast<T*>(a.O) + (int64_t)h * a.o_head + (int64_t)at_row * a.o_row + channel;
-  vec_t<T, kPer> y;
+    if (part) {
 #pragma unroll
-  for (int c = 0; c < kPer; ++c) y[c] = (T)(x[c] * inv);
-  *reinterpret_cast<vec_t<T, kPer>*>(to) = y;
-  if (a.lse && channel == 0)
-    a.lse[(int64_t)h * b.n_tokens + at_row] = (high + __builtin_amdgcn_logf(total)) * kLn2;
+      for (int c = 0; c < kPer; ++c) part[row * D + channel + c] = x[c];
+      if (channel == 0) {
+        part[kRows * D + row] = high;
+        part[kRows * (D + 1) + row] = total;
+      }
+    } else {
+      store_row<T, D>(a, tile, head_kv, row, channel, x, high, total);
+    }
+  }
+  __syncthreads();                                         // the next part's states take the same space
+  }
 }
 
 // ---- many new tokens: tiles of 128 rows ---------------------------------------------------------------------
@@ -587,7 +847,7 @@ paged_chunk_kernel(PagedAttention a) {
   }
   const int32_t piece = rest / a.slots, slot = a.slots - 1 - (rest - piece * a.slots);
   Tile tile;
-  if (!tile_of<kChunkRows>(a, slot, tile)) return;
+  if (!tile_of_slot<kChunkRows>(a, slot, tile)) return;
   const Pieces pieces = pieces_of(tile.blocks, a.splits);
   if (piece >= pieces.count) return;
   const int32_t group = (int32_t)a.group.value;
@@ -871,8 +1131,8 @@ paged_chunk_kernel(PagedAttention a) {
   }
   if (own_first >= tile.count) return;
   const int own_count = min(tile.count - own_first, 32);
-  float* const part = pieces.count > 1 ? a.partials + (((int64_t)slot * a.Hkv + head_kv) * a.splits + piece) * (kChunkRows * (D + 2))
-                                       : nullptr;
+  float* const part = pieces.count > 1
+                          ? record_of<D, kChunkRows>(a, ((int64_t)slot * a.Hkv + head_kv) * a.splits + piece) : nullptr;
   auto place_out = [&](int32_t r, int32_t& h_out, int32_t& row_out) {
     const int32_t f = tile.first + own_first + r, tok = (int32_t)quotient((uint32_t)f, a.group);
     h_out = head_kv * group + (f - tok * group);
@@ -950,68 +1210,84 @@ paged_chunk_kernel(PagedAttention a) {
   if (a.lse && h == 0 && exists) a.lse[(int64_t)head * b.n_tokens + tile.begin + token] = (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-// Joins the pieces of the tiles that are split, in their order.
-template <typename T, int D, int kTileRows>
-__global__ __launch_bounds__(kWaves* kWave) void paged_merge_kernel(PagedAttention a) {
+// Joins parts of a tile, in their order: record(i) for i < count; 16 rows from row0 on.
+template <typename T, int D, int kTileRows, typename Record>
+__device__ __forceinline__ void join_parts(const PagedAttention& a, const Tile& tile, int32_t head_kv, int32_t row0, int32_t count,
+                                           Record record) {
   constexpr int kPer = D / 16;
-  const int tid = threadIdx.x;
-  const int32_t slot = blockIdx.x / (kTileRows / 16), head_kv = blockIdx.y;
-  Tile tile;
-  if (!tile_of<kTileRows>(a, slot, tile)) return;
-  const Pieces pieces = pieces_of(tile.blocks, a.splits);
-  if (pieces.count <= 1) return;
-  const int row = blockIdx.x % (kTileRows / 16) * 16 + tid / 16, channel = tid % 16 * kPer;
+  const int row = row0 + threadIdx.x / 16, channel = threadIdx.x % 16 * kPer;
   if (row >= tile.count) return;
-  const float* part = a.partials + ((int64_t)slot * a.Hkv + head_kv) * a.splits * (kTileRows * (D + 2));
   float high = -INFINITY;
-  for (int i = 0; i < pieces.count; ++i) high = fmaxf(high, part[(int64_t)i * kTileRows * (D + 2) + kTileRows * D + row]);
+  for (int32_t i = 0; i < count; ++i) high = fmaxf(high, record(i)[kTileRows * D + row]);
   const float against = high > -INFINITY ? high : 0.f;
   float total = 0.f, x[kPer];
 #pragma unroll
   for (int c = 0; c < kPer; ++c) x[c] = 0.f;
-  for (int i = 0; i < pieces.count; ++i) {
-    const float* p = part + (int64_t)i * kTileRows * (D + 2);
-    if (p[kTileRows * (D + 1) + row] == 0.f) continue;
+  for (int32_t i = 0; i < count; ++i) {
+    const float* const p = record(i);
+    if (p[kTileRows * (D + 1) + row] == 0.f) continue;      // no key seen
     const float weight = __builtin_amdgcn_exp2f(p[kTileRows * D + row] - against);
     total += weight * p[kTileRows * (D + 1) + row];
 #pragma unroll
     for (int c = 0; c < kPer; ++c) x[c] += weight * p[row * D + channel + c];
   }
-  const int32_t group = (int32_t)a.group.value;
-  const int32_t f = tile.first + row, tok = (int32_t)quotient((uint32_t)f, a.group);
-  const int32_t h = head_kv * group + (f - tok * group), at_row = tile.begin + tok;
-  const float inv = total != 0.f ? 1.f / total : 0.f;
-  T* to = static_cast<T*>(a.O) + (int64_t)h * a.o_head + (int64_t)at_row * a.o_row + channel;
-  vec_t<T, kPer> y;
-#pragma unroll
-  for (int c = 0; c < kPer; ++c) y[c] = (T)(x[c] * inv);
-  *reinterpret_cast<vec_t<T, kPer>*>(to) = y;
-  if (a.lse && channel == 0)
-    a.lse[(int64_t)h * a.batch.n_tokens + at_row] = (high + __builtin_amdgcn_logf(total)) * kLn2;
+  store_row<T, D>(a, tile, head_kv, row, channel, x, high, total);
+}
+
+// ... of the tile that ends in share i and begins in an earlier one
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves* kWave) void paged_join_kernel(PagedAttention a) {
+  const uint32_t index = blockIdx.x + 1;
+  __shared__ Share<kRows> share;
+  if (threadIdx.x < kWave) {
+    // (an uncut tile is no part; one that goes on behind this share is joined by a later one)
+    share.part.there = 0;
+    if (share.begin(a, index) && share.offset > 0 && !share.whole() && share.at - share.offset + share.extent <= share.end)
+      share.take_part(a);
+  }
+  __syncthreads();
+  const Part here = share.part;
+  if (!here.there) return;
+  const Tile tile = tile_of<kRows>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
+  const uint32_t from = (uint32_t)quotient64(share.size * index - here.from, share.size);
+  join_parts<T, D, kRows>(a, tile, here.head, 0, index - from + 1,
+                          [&](int32_t i) { return record_of_share<D>(a, from + i, i > 0); });
+}
+
+// ... of a slot's tile of 128 rows that is split
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves* kWave) void paged_chunk_join_kernel(PagedAttention a) {
+  const int32_t slot = blockIdx.x / (kChunkRows / 16), head_kv = blockIdx.y;
+  Tile tile;
+  if (!tile_of_slot<kChunkRows>(a, slot, tile)) return;
+  const Pieces pieces = pieces_of(tile.blocks, a.splits);
+  if (pieces.count <= 1) return;
+  const int64_t first = ((int64_t)slot * a.Hkv + head_kv) * a.splits;
+  join_parts<T, D, kChunkRows>(a, tile, head_kv, blockIdx.x % (kChunkRows / 16) * 16, pieces.count,
+                               [&](int32_t i) { return record_of<D, kChunkRows>(a, first + i); });
 }
 
 template <typename T, int D>
 sga_status launch_paged_as(const PagedAttention& a) {
+  const dim3 block(kWaves * kWave);
   if (a.tile_rows == kChunkRows) {
     if constexpr (sizeof(T) == 2 && D >= 64) {
       const int64_t per_head = (int64_t)a.slots * a.splits;
       int64_t groups = per_head * a.Hkv;
       if (a.Hkv < 8 && 8 % a.Hkv == 0) groups = (per_head + 8 / a.Hkv - 1) / (8 / a.Hkv) * 8;
       profile_mark_begin(a.stream, "paged_chunk_kernel");
-      paged_chunk_kernel<T, D><<<dim3((unsigned)groups), kWaves * kWave, 0, a.stream>>>(a);
+      paged_chunk_kernel<T, D><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
       profile_mark_end(a.stream);
       if (a.splits > 1)
-        paged_merge_kernel<T, D, kChunkRows><<<dim3((unsigned)a.slots * (kChunkRows / 16), (unsigned)a.Hkv), kWaves * kWave, 0, a.stream>>>(a);
-      return hip_status(hipGetLastError());
+        paged_chunk_join_kernel<T, D><<<dim3((unsigned)a.slots * (kChunkRows / 16), (unsigned)a.Hkv), block, 0, a.stream>>>(a);
     }
+    return hip_status(hipGetLastError());
   }
-  const dim3 grid((unsigned)a.slots, (unsigned)a.Hkv, (unsigned)a.splits);
   profile_mark_begin(a.stream, "paged_kernel");
-  if (a.batch.page.value % 16 == 0) paged_kernel<T, D, true><<<grid, kWaves * kWave, 0, a.stream>>>(a);
-  else paged_kernel<T, D, false><<<grid, kWaves * kWave, 0, a.stream>>>(a);
+  if (a.batch.page.value % 16 == 0) paged_kernel<T, D, true><<<dim3(a.groups), block, 0, a.stream>>>(a);
+  else paged_kernel<T, D, false><<<dim3(a.groups), block, 0, a.stream>>>(a);
   profile_mark_end(a.stream);
-  if (a.splits > 1)
-    paged_merge_kernel<T, D, kRows><<<dim3((unsigned)a.slots, (unsigned)a.Hkv), kWaves * kWave, 0, a.stream>>>(a);
+  if (a.partials && a.groups > 1) paged_join_kernel<T, D><<<dim3(a.groups - 1), block, 0, a.stream>>>(a);
   return hip_status(hipGetLastError());
 }
 
@@ -1028,26 +1304,34 @@ sga_status launch_paged_type(const PagedAttention& a) {
 }  // namespace
 
 PagedPlan plan_paged(const PagedAttention& a) {
-  PagedPlan p{kRows, 1, 0, 0};
+  PagedPlan p{kRows, 0, 0, 1, 0};
   const int64_t all_rows = (int64_t)a.batch.n_tokens * a.group.value;
   if (a.dtype != SGA_F32 && a.d >= 64 && a.batch.page.value % 16 == 0 && all_rows > (int64_t)kTokenRows * a.batch.n_seqs)
     p.tile_rows = kChunkRows;
-  const int64_t slots = all_rows / p.tile_rows + a.batch.n_seqs;
-  // (a grid holds fewer than 2^32 threads along a side)
-  if (slots >= int64_t(1) << 24) return p;
+  const int64_t tiles = all_rows / p.tile_rows + a.batch.n_seqs;
+  if (tiles >= int64_t(1) << 24) return p;                 // (rows of a sequence are counted in 31 bits)
   // keys that a tile meets at most
-  const int64_t tokens = p.tile_rows / (int64_t)a.group.value + 2;
-  const int64_t room = (int64_t)a.batch.pages_per_seq * a.batch.page.value;
+  const int64_t room = (int64_t)a.batch.pages_per_seq * a.batch.page.value, step = p.tile_rows / (int64_t)a.group.value;
   int64_t keys = a.L < room ? a.L : room;
-  const int64_t wide = (a.causal ? 1 : 2) * (int64_t)a.window + tokens + a.n_global + 3 * kBlock;
-  if (wide < keys && !(a.n_global > 0 && !a.causal)) keys = wide;
-  const int64_t blocks = (keys + kBlock - 1) / kBlock + 2;
-  const int64_t most = (blocks + kPieceBlocks - 1) / kPieceBlocks, wanted = (1024 + slots * a.Hkv - 1) / (slots * a.Hkv);
-  p.splits = (int32_t)(most < wanted ? most : wanted);
-  if (p.splits < 1) p.splits = 1;
-  if (p.tile_rows == kChunkRows && slots * p.splits * a.Hkv + 8 >= int64_t(1) << 24) return p;
-  p.slots = (int32_t)slots;
-  if (p.splits > 1) p.bytes = (size_t)slots * a.Hkv * p.splits * p.tile_rows * (a.d + 2) * sizeof(float);
+  const int64_t window = (a.causal ? 1 : 2) * (int64_t)a.window + step + 1 + a.n_global;
+  if (window < keys && !(a.n_global > 0 && !a.causal)) keys = window;
+  if (p.tile_rows == kChunkRows) {
+    // pieces of tiles until the chip has four rounds of them, so that uneven sequences come out even
+    const int64_t blocks = (keys + kBlock - 1) / kBlock + 2, most = (blocks + kPieceBlocks - 1) / kPieceBlocks;
+    const int64_t wanted = (kChunkPieces + tiles * a.Hkv - 1) / (tiles * a.Hkv);
+    p.splits = (int32_t)(most < wanted ? most : wanted);
+    if (tiles * p.splits * a.Hkv + 8 >= int64_t(1) << 24) return p;         // (a grid holds fewer than 2^32 threads)
+    p.groups = (int32_t)(tiles * p.splits * a.Hkv);
+    p.slots = (int32_t)tiles;
+    if (p.splits > 1) p.bytes = (size_t)p.groups * kChunkRows * (a.d + 2) * sizeof(float);
+    return p;
+  }
+  // workgroups that the chip holds at once, and that have the least share to do if every tile met all the keys that it can
+  const int wide = a.d * (a.dtype == SGA_F32 ? 2 : 1);
+  const int64_t groups = wide > 256 ? 256 : wide > 64 ? 512 : 1024;
+  const int64_t work = (tiles * a.Hkv * (keys + kTileCost) + kLeastShare - 1) / kLeastShare;
+  p.groups = (int32_t)(work < groups ? (work > 1 ? work : 1) : groups);
+  if (p.groups > 1) p.bytes = (size_t)p.groups * 2 * kRows * (a.d + 2) * sizeof(float);
   return p;
 }
 

@@ -102,17 +102,16 @@ struct PagedAttention {
   int32_t L, window, n_global, causal;
   float scale;
   uint32_t page_pieces;      // 16-byte pieces from page to page
-  float* partials;           // partial states of split tiles
-  int32_t tile_rows;
-  int32_t splits;            // most pieces that a tile is cut into
-  int32_t slots;             // tiles of a key head, some of them empty
+  float* partials;           // partial states of tiles that are cut; null: none is
+  int32_t tile_rows, groups, splits, slots;      // the plan's
   int32_t d, dtype;
   hipStream_t stream;
 };
-// Pieces and partial states that a call may use.
+// The kernel, the workgroups and the partial states of a call.
 struct PagedPlan {
   int32_t tile_rows;         // rows of a tile: which kernel takes the call
-  int32_t splits, slots;     // slots 0: too many for one launch
+  int32_t groups;            // workgroups (tiles of 16 rows: each with an equal share of the work); 0: the call is too large
+  int32_t slots, splits;     // tiles of 128 rows: of a key head, some of them empty, and the most pieces of one
   size_t bytes;
 };
 PagedPlan plan_paged(const PagedAttention& a);

@@ -93,12 +93,14 @@ def test_workspace_rule():
         assert st == 0
         return n
     assert size(1, 1, 65536, 65536) > 0                       # one long sequence is split
-    assert size(1, 1, 65536, 65536) < 1 << 26
-    assert size(1024, 1024, 65536, 65536) == 0                # sequences enough for the chip
-    assert size(4, 32768, 65536, 65536) == 0
-    assert size(1, 1, 65536, 100) == 0                        # a narrow window is one piece
+    assert size(1, 1, 65536, 65536) < 1 << 25
+    assert size(64, 64, 65536, 65536) == size(4096, 4096, 1 << 20, 1 << 20) < 1 << 24      # two tiles for each share
+    assert size(4, 32768, 65536, 65536) == 0                  # tiles of 128 rows enough for the chip
+    assert 0 < size(4, 1024, 65536, 65536) < 1 << 29
+    assert size(1, 1, 256, 256, Hq=1, Hkv=1) == 0             # a short one is one share
+    assert size(1, 1, 65536, 100, Hq=1, Hkv=1) == 0           # a narrow window too
+    assert size(1, 1, 1 << 20, 1 << 20, Hq=1, Hkv=1, columns=4) == 0          # the page table holds 64 tokens
     assert sga.sga_paged_workspace_bytes(batch(n_tokens=0), MaskSpec(KIND_SLIDING, 64), 4, 2, 64, 1) == (0, 0)
-    assert size(1, 1, 1 << 20, 1 << 20, columns=4) == 0       # the page table holds 64 tokens
     assert sga.sga_paged_workspace_bytes(batch(n_tokens=0), MaskSpec(KIND_SLIDING, 0), 4, 2, 64, 1)[0] == -1
 
 
