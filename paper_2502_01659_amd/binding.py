@@ -253,32 +253,26 @@ def sga_profile_last_kernel():
     return load().sga_profile_last_kernel().decode()
 
 
-def _ref(struct):
-    return ctypes.byref(struct) if struct is not None else None
-
-
 def sga_rotary(X, Y, positions, first, L, H, d, rotary_desc, inverse, dtype_code, stream):
     """X, Y: _Rows or None; rotary_desc: _RotaryDesc or None"""
-    return load().sga_rotary(_ref(X), _ref(Y), positions, first, L, H, d, _ref(rotary_desc), inverse, dtype_code, stream)
+    return load().sga_rotary(X, Y, positions, first, L, H, d, rotary_desc, inverse, dtype_code, stream)
 
 
 def sga_cache_append(K, V, cache_k, cache_v, batch, Hkv, d, rotary_desc, Q, Q_out, Hq, dtype_code, stream):
-    return load().sga_cache_append(_ref(K), _ref(V), cache_k, cache_v, _ref(batch), Hkv, d, _ref(rotary_desc), _ref(Q),
-                                   _ref(Q_out), Hq, dtype_code, stream)
+    return load().sga_cache_append(K, V, cache_k, cache_v, batch, Hkv, d, rotary_desc, Q, Q_out, Hq, dtype_code, stream)
 
 
 def sga_paged_workspace_bytes(batch, spec: MaskSpec, Hq, Hkv, d, dtype_code):
     """-> (status, bytes)"""
-    dsc, out = _desc(spec), ctypes.c_size_t(0)
-    st = load().sga_paged_workspace_bytes(_ref(batch), ctypes.byref(dsc), Hq, Hkv, d, dtype_code, ctypes.byref(out))
+    out = ctypes.c_size_t(0)
+    st = load().sga_paged_workspace_bytes(batch, _desc(spec), Hq, Hkv, d, dtype_code, ctypes.byref(out))
     return st, out.value
 
 
 def sga_attention_paged(Q, cache_k, cache_v, batch, spec, causal, O, Hq, Hkv, d, scale, dtype_code, lse, workspace,
                         workspace_bytes_, stream):
-    dsc = _desc(spec)
-    return load().sga_attention_paged(_ref(Q), cache_k, cache_v, _ref(batch), ctypes.byref(dsc), causal, _ref(O), Hq, Hkv, d,
-                                      scale, dtype_code, lse, workspace, workspace_bytes_, stream)
+    return load().sga_attention_paged(Q, cache_k, cache_v, batch, _desc(spec), causal, O, Hq, Hkv, d, scale, dtype_code, lse,
+                                      workspace, workspace_bytes_, stream)
 
 
 # ---- tensor-level helpers ---------------------------------------------------------
@@ -562,35 +556,30 @@ def _serving_code(dtype):
     return code
 
 
-class _here:
-    """Makes a tensor's device the current one, if it is not, and gives its current stream."""
-
-    def __init__(self, device):
-        import torch
-        self.device = device
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        import torch
-        if self.guard is not None:
-            self.guard.__enter__()
-        return torch.cuda.current_stream().cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _enqueue(index, call, *args):
+    """call(*args, stream) on the current stream of device `index`, made the current device meanwhile.  A step of generation is a
+    few short calls, so what the host does for each counts: torch.cuda.current_stream() alone takes 2.7 us, the raw
+    handle of the same stream 0.1."""
+    import torch
+    if torch._C._cuda_getDevice() == index:
+        return call(*args, torch._C._cuda_getCurrentRawStream(index))
+    with torch.cuda.device(index):
+        return call(*args, torch._C._cuda_getCurrentRawStream(index))
 
 
 def _strides(t, name, written=False):
     """_Rows of a [H, T, d] tensor whose channels lie side by side.  A written one has to hold each element once."""
     H, T, d = t.shape
-    sh, st = (t.stride(0) if H > 1 else 0), (t.stride(1) if T > 1 else 0)
-    if d > 1 and t.stride(2) != 1:
+    sh, st, sc = t.stride()
+    if sc != 1 and d > 1:
         raise ValueError(f"the channels of {name} must be contiguous")
-    if written and t.numel() > 0:
-        (low, n_low), (high, n_high) = sorted(((sh, H), (st, T))) if H > 1 and T > 1 else (((0, 1), (sh or st, max(H, T))))
-        if (n_low > 1 and low < d) or (n_high > 1 and high < low * (n_low - 1) + d):
-            raise ValueError(f"rows of {name} overlap")
+    if H == 1:
+        sh = 0
+    if T == 1:
+        st = 0
+    if written and not ((H == 1 or sh >= d) and (T == 1 or st >= d)
+                        and (H == 1 or T == 1 or st >= sh * (H - 1) + d or sh >= st * (T - 1) + d)) and t.numel() > 0:
+        raise ValueError(f"rows of {name} overlap")
     return _Rows(t.data_ptr(), sh, st)
 
 
@@ -599,7 +588,7 @@ def _check_tokens(t, name, like=None, T=None):
         raise ValueError(f"{name} must be a [H, T, d] device tensor")
     if T is not None and t.shape[1] != T:
         raise ValueError(f"{name} must have the batch's {T} tokens")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[2] != like.shape[2]):
+    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device() or t.shape[2] != like.shape[2]):
         raise ValueError(f"{name} must share dtype, device and head dimension")
 
 
@@ -650,12 +639,13 @@ class Rotary:
         if layout not in _LAYOUT_CODE:
             raise ValueError(f"unknown layout {layout!r}")
         self.frequencies = frequencies
+        self.device_index = frequencies.get_device()
         self.channels = 2 * frequencies.numel()
         self._desc = _RotaryDesc(ctypes.sizeof(_RotaryDesc), _LAYOUT_CODE[layout], self.channels, float(magnitude),
                                  frequencies.data_ptr())
 
     def _check(self, t):
-        if self.frequencies.device != t.device:
+        if self.device_index != t.get_device():
             raise ValueError("the rotary frequencies are on another device")
 
 
@@ -665,18 +655,20 @@ def rotary(X, rotary, positions=None, first=0, inverse=False, out=None):
     _check_tokens(X, "X")
     rotary._check(X)
     H, L, d = X.shape
-    if positions is not None and (str(positions.dtype) != "torch.int64" or positions.shape != (L,)
-                                  or not positions.is_contiguous() or positions.device != X.device):
-        raise ValueError("positions must be contiguous int64 [L] on X's device")
+    index = X.get_device()
+    at = None
+    if positions is not None:
+        if str(positions.dtype) != "torch.int64" or positions.shape != (L,) or not positions.is_contiguous() \
+                or positions.get_device() != index:
+            raise ValueError("positions must be contiguous int64 [L] on X's device")
+        at = positions.data_ptr()
     if out is None:
         import torch
         out = torch.empty_like(X)
-    elif out.shape != X.shape or out.dtype != X.dtype or out.device != X.device:
+    elif out.shape != X.shape or out.dtype != X.dtype or out.get_device() != index:
         raise ValueError("out must match X in shape, dtype and device")
-    x, y, code = _strides(X, "X"), _strides(out, "out", written=True), _serving_code(X.dtype)
-    with _here(X.device) as stream:
-        st = sga_rotary(x, y, positions.data_ptr() if positions is not None else None, int(first), L, H, d, rotary._desc,
-                        int(bool(inverse)), code, stream)
+    st = _enqueue(index, sga_rotary, _strides(X, "X"), _strides(out, "out", written=True), at, int(first), L, H, d, rotary._desc,
+                  1 if inverse else 0, _serving_code(X.dtype))
     if st != 0:
         raise SgaError(st, "sga_rotary")
     return out
@@ -706,6 +698,7 @@ class PagedBatch:
         self.page_table, self.seq_ptr, self.seq_len = page_table, seq_ptr, seq_len
         self.n_tokens, self.page_size, self.n_pages = int(n_tokens), int(page_size), int(n_pages)
         self.device = page_table.device
+        self.device_index = page_table.get_device()
         self._structs = {}
 
     def _struct(self, page_stride):
@@ -719,21 +712,26 @@ class PagedBatch:
 
     def _caches(self, like, cache_k, cache_v):
         """The batch's record for these caches, and their key heads."""
-        if like.device != self.device:
+        if like.get_device() != self.device_index:
             raise ValueError("the batch is on another device")
-        d, page = like.shape[2], self.page_size
+        d, page, n_pages = like.shape[2], self.page_size, self.n_pages
+        shape = cache_k.shape
+        if len(shape) != 4 or cache_v.shape != shape or shape[0] != n_pages or shape[2] != page or shape[3] != d:
+            raise ValueError("the caches must both be [n_pages, Hkv, page_size, d]")
+        Hkv = shape[1]
+        apart = 0
         for t in (cache_k, cache_v):
-            if t.dim() != 4 or t.shape != cache_k.shape or t.shape[0] != self.n_pages or t.shape[2] != page or t.shape[3] != d:
-                raise ValueError("the caches must both be [n_pages, Hkv, page_size, d]")
-            if t.dtype != like.dtype or t.device != like.device:
+            if t.dtype != like.dtype or t.get_device() != self.device_index:
                 raise ValueError("the caches must share dtype and device with the tokens")
             sp, sh, st, sc = t.stride()
-            if sc != 1 or (page > 1 and st != d) or (t.shape[1] > 1 and sh != page * d):
+            if sc != 1 or (st != d and page > 1) or (sh != page * d and Hkv > 1):
                 raise ValueError("every page of a cache must be contiguous")
-            if self.n_pages > 1 and (sp != cache_k.stride(0) or sp < t.shape[1] * page * d):
+            if n_pages == 1:
+                sp = Hkv * page * d
+            if sp < Hkv * page * d or sp != (apart or sp):
                 raise ValueError("the pages of a cache must not overlap, and both caches must have them at one distance")
-        Hkv = cache_k.shape[1]
-        return self._struct(cache_k.stride(0) if self.n_pages > 1 else Hkv * page * d), Hkv
+            apart = sp
+        return self._struct(apart), Hkv
 
 
 def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None):
@@ -762,10 +760,9 @@ def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None)
         q, q_out, Hq = _strides(Q, "Q"), _strides(Q_out, "Q_out", written=True), Q.shape[0]
     elif Q_out is not None:
         raise ValueError("Q_out without Q")
-    k, v, code = _strides(K, "K"), _strides(V, "V"), _serving_code(K.dtype)
-    with _here(K.device) as stream:
-        st = sga_cache_append(k, v, cache_k.data_ptr(), cache_v.data_ptr(), struct, Hkv, K.shape[2],
-                              rotary._desc if rotary is not None else None, q, q_out, Hq, code, stream)
+    st = _enqueue(batch.device_index, sga_cache_append, _strides(K, "K"), _strides(V, "V"), cache_k.data_ptr(),
+                  cache_v.data_ptr(), struct, Hkv, K.shape[2], rotary._desc if rotary is not None else None, q, q_out, Hq,
+                  _serving_code(K.dtype))
     if st != 0:
         raise SgaError(st, "sga_cache_append")
     return Q_out
@@ -789,28 +786,29 @@ def attention_paged(Q, cache_k, cache_v, batch, spec: MaskSpec, scale, causal=Tr
     """Attention of the batch's new tokens, Q [Hq, n_tokens, d], over the paged cache under a sliding or global + local mask
     of spec.L tokens (window >= L: every token), of earlier tokens only if causal.  Consecutive Hq / Hkv query heads share
     a key head.  Returns O (and lse [Hq, n_tokens] if requested); a token that sees nothing has O = 0, lse = -inf."""
-    import torch
     _check_tokens(Q, "Q", T=batch.n_tokens)
     struct, Hkv = batch._caches(Q, cache_k, cache_v)
     Hq, T, d = Q.shape
+    index = batch.device_index
     if O is None:
+        import torch
         O = torch.empty_like(Q)
-    elif O.shape != Q.shape or O.dtype != Q.dtype or O.device != Q.device:
+    elif O.shape != Q.shape or O.dtype != Q.dtype or O.get_device() != index:
         raise ValueError("O must match Q in shape, dtype and device")
     if want_lse and lse is None:
+        import torch
         lse = torch.empty((Hq, T), dtype=torch.float32, device=Q.device)
-    if lse is not None and (lse.shape != (Hq, T) or lse.dtype != torch.float32 or not lse.is_contiguous()
-                            or lse.device != Q.device):
+    if lse is not None and (lse.shape != (Hq, T) or str(lse.dtype) != "torch.float32" or not lse.is_contiguous()
+                            or lse.get_device() != index):
         raise ValueError("lse must be contiguous float32 [Hq, n_tokens] on Q's device")
     ws_ptr, ws_n = None, 0
     if workspace is not None and workspace.numel() > 0:
-        if workspace.device != Q.device or not workspace.is_contiguous():
+        if workspace.get_device() != index or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on Q's device")
         ws_ptr, ws_n = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    q, o, code = _strides(Q, "Q"), _strides(O, "O", written=True), _serving_code(Q.dtype)
-    with _here(Q.device) as stream:
-        st = sga_attention_paged(q, cache_k.data_ptr(), cache_v.data_ptr(), struct, spec, int(bool(causal)), o, Hq, Hkv, d,
-                                 float(scale), code, lse.data_ptr() if lse is not None else None, ws_ptr, ws_n, stream)
+    st = _enqueue(index, sga_attention_paged, _strides(Q, "Q"), cache_k.data_ptr(), cache_v.data_ptr(), struct, spec,
+                  1 if causal else 0, _strides(O, "O", written=True), Hq, Hkv, d, float(scale), _serving_code(Q.dtype),
+                  lse.data_ptr() if lse is not None else None, ws_ptr, ws_n)
     if st != 0:
         raise SgaError(st, "sga_attention_paged")
     return (O, lse) if lse is not None else O

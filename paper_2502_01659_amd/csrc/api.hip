@@ -613,9 +613,13 @@ sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const voi
   a.tile_rows = plan.tile_rows;
   a.page_pieces = (uint32_t)(batch->page_stride / (16 / element_bytes(dtype)));
   a.groups = plan.groups;
-  a.partials = plan.bytes > 0 && workspace_bytes >= plan.bytes ? static_cast<float*>(workspace) : nullptr;
+  a.splits = 1;
   a.slots = plan.slots;
-  a.splits = a.partials ? plan.splits : 1;
+  if (plan.bytes > 0 && workspace_bytes >= plan.bytes) {
+    a.splits = plan.splits;
+    a.notes = workspace;
+    a.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + (size_t)plan.groups * kNoteBytes);
+  }
   a.stream = static_cast<hipStream_t>(stream);
   return launch_paged(a);
 }

@@ -26,8 +26,8 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kBlock = 32;            // keys of a block
 constexpr int kRows = 16;             // rows of a tile
 constexpr int kWaves = 4;             // wavefronts of a workgroup, which take its blocks in turn
-constexpr int kPieceBlocks = 16;      // fewest blocks of a piece of a split tile of 128 rows
-constexpr int kChunkPieces = 2048;
+constexpr int kChunkPieces = 1024;    // pieces of tiles of 128 rows that a call is cut into
+
 constexpr int kTokenRows = 64;        // sequences with more rows than this on average take tiles of 128 rows
 
 __device__ __forceinline__ int64_t uniform64(int64_t v) {
@@ -122,7 +122,7 @@ __device__ __forceinline__ Tile tile_of(const PagedAttention& a, int32_t seq, in
 // Lengths are estimates (a tile's blocks are counted when it is met; a cut goes to the block in proportion) that follow from
 // the sequence alone: tile u < t1 is a0 + u * step long, the others a1.  Causal, the keys grow with the tiles until the
 // window is full; otherwise the tiles of global rows see everything and the others a window.
-constexpr uint32_t kTileCost = 64;
+constexpr uint32_t kTileCost = 256;
 constexpr uint32_t kLeastShare = 512;      // keys of the smallest share
 constexpr uint32_t kWholeTiles = 32;       // tiles shorter than this part of a share are not cut
 
@@ -217,15 +217,15 @@ struct Share {
     const SequenceWork w = work_of<kTileRows>(a, from + l);
     const uint64_t own = w.per_head * (uint64_t)a.Hkv;
     uint64_t sum = own;
-#pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
+    for (int off = 1; off < kWave && off < a.batch.n_seqs; off <<= 1) {
       const uint64_t below = (uint64_t)__shfl_up((unsigned long long)sum, off, kWave);
       if (l >= off) sum += below;
     }
     work[l] = w;
-    start[l] = base + sum - own;
     chunk = from;
-    behind = base + from_lane(sum, kWave - 1);
+    const int32_t here = min(a.batch.n_seqs - from, kWave);
+    behind = base + from_lane(sum, here - 1);
+    start[l] = l < here ? base + sum - own : behind;
     __builtin_amdgcn_wave_barrier();
   }
   __device__ __forceinline__ void take_sequence() {
@@ -346,33 +346,58 @@ template <int D>
 __device__ __forceinline__ float* record_of_share(const PagedAttention& a, uint32_t share, bool begins_within) {
   return record_of<D, kRows>(a, (int64_t)share * 2 + (begins_within ? 0 : 1));
 }
-
-// The tile of slot i (tiles of 128 rows): sequence s owns the slots from seq_ptr[s] * group / kTileRows + s, which are
-// enough for it and follow from seq_ptr alone.  False: an empty slot.  All lanes call it.
-template <int kTileRows>
-__device__ __forceinline__ bool tile_of_slot(const PagedAttention& a, int32_t slot, Tile& t) {
-  const PagedArgs& b = a.batch;
-  const int64_t group = a.group.value;
-  auto first_slot = [&](int32_t s) { return (int64_t)row_of_sequence(b, s) * group / kTileRows + s; };
-  const int32_t seq = __builtin_amdgcn_readfirstlane(last_not_above(b.n_seqs, slot, first_slot));
-  const int32_t begin = __builtin_amdgcn_readfirstlane(row_of_sequence(b, seq));
-  const int32_t end = __builtin_amdgcn_readfirstlane(row_of_sequence(b, seq + 1));
-  const int32_t length = __builtin_amdgcn_readfirstlane(b.seq_len[seq]);
-  const int32_t n_new = end > begin ? end - begin : 0;
-  const int64_t index = (int64_t)slot - (begin * group / kTileRows + seq);
-  if (index < 0 || index * kTileRows >= n_new * group) return false;
-  t = tile_of<kTileRows>(a, seq, begin, n_new, length, (int32_t)index);
-  return true;
-}
-
-// Its pieces, at least kPieceBlocks blocks each.
-struct Pieces {
-  int32_t count, blocks;
+// What a workgroup leaves for the kernel that joins: a tile and its parts.
+struct alignas(16) Note {
+  int32_t count;             // parts of the tile; 0: nothing to join here
+  int32_t first;             // the first one's share or record
+  int32_t seq, begin, n_new, length, tile, head;
 };
-__device__ __forceinline__ Pieces pieces_of(int32_t blocks, int32_t splits) {
-  const int32_t even = (blocks + splits - 1) / splits, each = even > kPieceBlocks ? even : kPieceBlocks;
-  const int32_t n = (blocks + each - 1) / each;
-  return {n > 0 ? n : 1, each};
+static_assert(sizeof(Note) == kNoteBytes, "the plan counts on this");
+__device__ __forceinline__ Note* notes_of(const PagedAttention& a) { return reinterpret_cast<Note*>(a.notes); }
+
+// Which piece of which tile of 128 rows workgroup `rest` of a key head has.  A sequence's tiles are all cut into as many pieces as
+// its longest one needs to have pieces of about the size at which the call has kChunkPieces of them (as far as the
+// lengths say; 512 keys at least), so that uneven sequences keep the chip evenly busy.  The pieces lie in the order
+// sequence, piece, tile.  False: there is no such piece.  All lanes call it.
+template <int kTileRows>
+__device__ __forceinline__ bool piece_of(const PagedAttention& a, int32_t rest, Tile& tile, int32_t& index, int32_t& piece,
+                                         int32_t& pieces) {
+  const int l = threadIdx.x & (kWave - 1);
+  const int32_t n = a.batch.n_seqs;
+  SequenceWork w{};
+  auto longest = [&]() { return (float)max(w.a1, w.t1 > 0 ? w.length_of(w.t1 - 1, step_of<kTileRows>(a)) : 0u); };
+  float total = 0.f;
+  for (int32_t c = 0; c < n; c += kWave) {
+    w = work_of<kTileRows>(a, c + l);
+    total += (float)w.tiles * longest();
+  }
+#pragma unroll
+  for (int off = 1; off < kWave; off <<= 1) total += __shfl_xor(total, off, kWave);
+  const float size = fmaxf((float)kLeastShare, total * (float)a.Hkv * (1.f / kChunkPieces));
+  int32_t behind = 0;
+  for (int32_t c = 0; c < n; c += kWave) {
+    if (n > kWave) w = work_of<kTileRows>(a, c + l);
+    const int32_t cut = a.splits > 1 ? max(1, (int32_t)(longest() / size + 0.5f)) : 1, own = (int32_t)w.tiles * cut;
+    int32_t sum = own;
+    for (int off = 1; off < kWave && off < n; off <<= 1) {
+      const int32_t below = __shfl_up(sum, off, kWave);
+      if (l >= off) sum += below;
+    }
+    const uint64_t begun = __ballot(own > 0 && behind + sum - own <= rest && rest < behind + sum);
+    if (begun) {
+      const int lane = __builtin_ctzll(begun);
+      const uint32_t place = (uint32_t)(rest - behind - __builtin_amdgcn_readlane(sum - own, lane));
+      const uint32_t tiles = __builtin_amdgcn_readlane(w.tiles, lane);
+      pieces = __builtin_amdgcn_readlane(cut, lane);
+      piece = (int32_t)(place / tiles);
+      index = (int32_t)(place - piece * tiles);
+      tile = tile_of<kTileRows>(a, c + lane, __builtin_amdgcn_readlane(w.begin, lane), __builtin_amdgcn_readlane(w.n_new, lane),
+                                __builtin_amdgcn_readlane(w.length, lane), index);
+      return true;
+    }
+    behind += __builtin_amdgcn_readlane(sum, min(n - c, kWave) - 1);
+  }
+  return false;
 }
 
 __device__ __forceinline__ int32_t first_key(const Tile& t, int32_t block) {
@@ -536,6 +561,13 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
   __shared__ Share<kRows> share;
   for (bool first_part = true;; first_part = false) {
   const Part here = share.next(a, blockIdx.x, first_part);
+  if (first_part && a.partials && threadIdx.x == 0) {
+    // the tile that ends in this share and began in an earlier one
+    const bool ends = here.there && here.from > 0 && here.to == here.extent;
+    const int32_t first = ends ? (int32_t)quotient64(share.size * blockIdx.x - here.from, share.size) : 0;
+    notes_of(a)[blockIdx.x] = Note{ends ? (int32_t)blockIdx.x - first + 1 : 0, first, here.seq, here.begin, here.n_new, here.length,
+                                   here.tile, here.head};
+  }
   if (!here.there) return;
   const int tid = thread_again(), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int m = lane & 15, g = lane >> 4;
@@ -828,10 +860,10 @@ paged_chunk_kernel(PagedAttention a) {
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = lane & 31, h = lane >> 5;
   // Workgroup i runs on XCD i % 8: a key head stays on one XCD, or on 8 / Hkv of them, whose L2 then holds the keys that
-  // its tiles share.  Late tiles first: causal, they have the most keys.
+  // its tiles share.
   int32_t head_kv, rest;
   {
-    const uint32_t id = blockIdx.x, per_head = (uint32_t)a.slots * a.splits, heads = a.Hkv;
+    const uint32_t id = blockIdx.x, per_head = (uint32_t)a.slots, heads = a.Hkv;
     if (heads % 8 == 0) {
       const uint32_t turn = (id / 8) / per_head;
       head_kv = id % 8 + 8 * turn;
@@ -845,15 +877,19 @@ paged_chunk_kernel(PagedAttention a) {
     }
     if ((uint32_t)rest >= per_head) return;
   }
-  const int32_t piece = rest / a.slots, slot = a.slots - 1 - (rest - piece * a.slots);
+  const int64_t record = (int64_t)head_kv * a.slots + rest;
   Tile tile;
-  if (!tile_of_slot<kChunkRows>(a, slot, tile)) return;
-  const Pieces pieces = pieces_of(tile.blocks, a.splits);
-  if (piece >= pieces.count) return;
+  int32_t index = 0, piece = 0, pieces = 1;
+  const bool any = piece_of<kChunkRows>(a, rest, tile, index, piece, pieces);
+  if (a.partials && tid == 0) {
+    const bool cut = any && pieces > 1 && piece == 0;
+    notes_of(a)[record] = cut ? Note{pieces, (int32_t)record, tile.seq, tile.begin, tile.n_new, tile.length, index, head_kv} : Note{};
+  }
+  if (!any) return;
   const int32_t group = (int32_t)a.group.value;
   const PagedArgs& b = a.batch;
-  const int32_t first_block = piece * pieces.blocks;
-  const int32_t end_block = min(first_block + pieces.blocks, tile.blocks);
+  const int32_t first_block = (int32_t)((int64_t)tile.blocks * piece / pieces);
+  const int32_t end_block = (int32_t)((int64_t)tile.blocks * (piece + 1) / pieces);
 
   // this lane's row
   const int32_t own_first = 32 * wave, row = own_first + n;
@@ -1131,8 +1167,7 @@ paged_chunk_kernel(PagedAttention a) {
   }
   if (own_first >= tile.count) return;
   const int own_count = min(tile.count - own_first, 32);
-  float* const part = pieces.count > 1
-                          ? record_of<D, kChunkRows>(a, ((int64_t)slot * a.Hkv + head_kv) * a.splits + piece) : nullptr;
+  float* const part = pieces > 1 ? record_of<D, kChunkRows>(a, record) : nullptr;
   auto place_out = [&](int32_t r, int32_t& h_out, int32_t& row_out) {
     const int32_t f = tile.first + own_first + r, tok = (int32_t)quotient((uint32_t)f, a.group);
     h_out = head_kv * group + (f - tok * group);
@@ -1210,61 +1245,59 @@ paged_chunk_kernel(PagedAttention a) {
   if (a.lse && h == 0 && exists) a.lse[(int64_t)head * b.n_tokens + tile.begin + token] = (top + __builtin_amdgcn_logf(total)) * kLn2;
 }
 
-// Joins parts of a tile, in their order: record(i) for i < count; 16 rows from row0 on.
+// Joins the parts of a tile, in their order.  The records of four parts are loaded at a time.
 template <typename T, int D, int kTileRows, typename Record>
-__device__ __forceinline__ void join_parts(const PagedAttention& a, const Tile& tile, int32_t head_kv, int32_t row0, int32_t count,
-                                           Record record) {
-  constexpr int kPer = D / 16;
+__device__ __forceinline__ void join_parts(const PagedAttention& a, const Note& note, int32_t row0, Record record) {
+  constexpr int kPer = D / 16, kAtOnce = 4;
+  const Tile tile = tile_of<kTileRows>(a, note.seq, note.begin, note.n_new, note.length, note.tile);
   const int row = row0 + threadIdx.x / 16, channel = threadIdx.x % 16 * kPer;
   if (row >= tile.count) return;
-  float high = -INFINITY;
-  for (int32_t i = 0; i < count; ++i) high = fmaxf(high, record(i)[kTileRows * D + row]);
-  const float against = high > -INFINITY ? high : 0.f;
-  float total = 0.f, x[kPer];
+  float high = -INFINITY, total = 0.f, x[kPer];
 #pragma unroll
   for (int c = 0; c < kPer; ++c) x[c] = 0.f;
-  for (int32_t i = 0; i < count; ++i) {
-    const float* const p = record(i);
-    if (p[kTileRows * (D + 1) + row] == 0.f) continue;      // no key seen
-    const float weight = __builtin_amdgcn_exp2f(p[kTileRows * D + row] - against);
-    total += weight * p[kTileRows * (D + 1) + row];
+  for (int32_t i = 0; i < note.count; i += kAtOnce) {
+    float top[kAtOnce], sum[kAtOnce];
+    vec_t<float, kPer> o[kAtOnce];
 #pragma unroll
-    for (int c = 0; c < kPer; ++c) x[c] += weight * p[row * D + channel + c];
+    for (int k = 0; k < kAtOnce; ++k) {
+      const float* const p = record(min(i + k, note.count - 1));
+      top[k] = p[kTileRows * D + row];
+      sum[k] = p[kTileRows * (D + 1) + row];
+      o[k] = *reinterpret_cast<const vec_t<float, kPer>*>(p + row * D + channel);
+    }
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (i + k >= note.count || sum[k] == 0.f) continue;   // no key seen
+      const float best = fmaxf(high, top[k]), against = best > -INFINITY ? best : 0.f;
+      const float keep = __builtin_amdgcn_exp2f(high - against), weight = __builtin_amdgcn_exp2f(top[k] - against);
+      high = best;
+      const float kept = total == 0.f ? 0.f : keep;          // (nothing yet: not 0 times what an infinity leaves)
+      total = kept * total + weight * sum[k];
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) x[c] = kept * x[c] + weight * o[k][c];
+    }
   }
-  store_row<T, D>(a, tile, head_kv, row, channel, x, high, total);
+  store_row<T, D>(a, tile, note.head, row, channel, x, high, total);
 }
 
-// ... of the tile that ends in share i and begins in an earlier one
+// ... tiles that end in a share and begin in an earlier one
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves* kWave) void paged_join_kernel(PagedAttention a) {
-  const uint32_t index = blockIdx.x + 1;
-  __shared__ Share<kRows> share;
-  if (threadIdx.x < kWave) {
-    // (an uncut tile is no part; one that goes on behind this share is joined by a later one)
-    share.part.there = 0;
-    if (share.begin(a, index) && share.offset > 0 && !share.whole() && share.at - share.offset + share.extent <= share.end)
-      share.take_part(a);
-  }
-  __syncthreads();
-  const Part here = share.part;
-  if (!here.there) return;
-  const Tile tile = tile_of<kRows>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
-  const uint32_t from = (uint32_t)quotient64(share.size * index - here.from, share.size);
-  join_parts<T, D, kRows>(a, tile, here.head, 0, index - from + 1,
-                          [&](int32_t i) { return record_of_share<D>(a, from + i, i > 0); });
+  const Note note = notes_of(a)[blockIdx.x];
+  if (note.count == 0) return;
+  join_parts<T, D, kRows>(a, note, 0, [&](int32_t i) { return record_of_share<D>(a, note.first + i, i > 0); });
 }
 
-// ... of a slot's tile of 128 rows that is split
+// ... tiles of 128 rows in pieces, whose records lie as far apart as the sequence has tiles
+constexpr int kJoinRows = 64;
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves* kWave) void paged_chunk_join_kernel(PagedAttention a) {
-  const int32_t slot = blockIdx.x / (kChunkRows / 16), head_kv = blockIdx.y;
-  Tile tile;
-  if (!tile_of_slot<kChunkRows>(a, slot, tile)) return;
-  const Pieces pieces = pieces_of(tile.blocks, a.splits);
-  if (pieces.count <= 1) return;
-  const int64_t first = ((int64_t)slot * a.Hkv + head_kv) * a.splits;
-  join_parts<T, D, kChunkRows>(a, tile, head_kv, blockIdx.x % (kChunkRows / 16) * 16, pieces.count,
-                               [&](int32_t i) { return record_of<D, kChunkRows>(a, first + i); });
+  const Note note = notes_of(a)[blockIdx.x];
+  if (note.count == 0) return;
+  const int32_t tiles = (int32_t)(((int64_t)note.n_new * a.group.value + kChunkRows - 1) / kChunkRows);
+  for (int32_t row0 = blockIdx.y * kJoinRows; row0 < (int32_t)(blockIdx.y + 1) * kJoinRows; row0 += 16)
+    join_parts<T, D, kChunkRows>(a, note, row0,
+                                 [&](int32_t i) { return record_of<D, kChunkRows>(a, note.first + (int64_t)i * tiles); });
 }
 
 template <typename T, int D>
@@ -1272,14 +1305,12 @@ sga_status launch_paged_as(const PagedAttention& a) {
   const dim3 block(kWaves * kWave);
   if (a.tile_rows == kChunkRows) {
     if constexpr (sizeof(T) == 2 && D >= 64) {
-      const int64_t per_head = (int64_t)a.slots * a.splits;
-      int64_t groups = per_head * a.Hkv;
-      if (a.Hkv < 8 && 8 % a.Hkv == 0) groups = (per_head + 8 / a.Hkv - 1) / (8 / a.Hkv) * 8;
+      int64_t groups = (int64_t)a.slots * a.Hkv;
+      if (a.Hkv < 8 && 8 % a.Hkv == 0) groups = (int64_t)(a.slots + 8 / a.Hkv - 1) / (8 / a.Hkv) * 8;
       profile_mark_begin(a.stream, "paged_chunk_kernel");
       paged_chunk_kernel<T, D><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
       profile_mark_end(a.stream);
-      if (a.splits > 1)
-        paged_chunk_join_kernel<T, D><<<dim3((unsigned)a.slots * (kChunkRows / 16), (unsigned)a.Hkv), block, 0, a.stream>>>(a);
+      if (a.partials) paged_chunk_join_kernel<T, D><<<dim3((unsigned)a.groups, kChunkRows / kJoinRows), block, 0, a.stream>>>(a);
     }
     return hip_status(hipGetLastError());
   }
@@ -1287,7 +1318,7 @@ sga_status launch_paged_as(const PagedAttention& a) {
   if (a.batch.page.value % 16 == 0) paged_kernel<T, D, true><<<dim3(a.groups), block, 0, a.stream>>>(a);
   else paged_kernel<T, D, false><<<dim3(a.groups), block, 0, a.stream>>>(a);
   profile_mark_end(a.stream);
-  if (a.partials && a.groups > 1) paged_join_kernel<T, D><<<dim3(a.groups - 1), block, 0, a.stream>>>(a);
+  if (a.partials) paged_join_kernel<T, D><<<dim3(a.groups), block, 0, a.stream>>>(a);
   return hip_status(hipGetLastError());
 }
 
@@ -1316,14 +1347,13 @@ PagedPlan plan_paged(const PagedAttention& a) {
   const int64_t window = (a.causal ? 1 : 2) * (int64_t)a.window + step + 1 + a.n_global;
   if (window < keys && !(a.n_global > 0 && !a.causal)) keys = window;
   if (p.tile_rows == kChunkRows) {
-    // pieces of tiles until the chip has four rounds of them, so that uneven sequences come out even
-    const int64_t blocks = (keys + kBlock - 1) / kBlock + 2, most = (blocks + kPieceBlocks - 1) / kPieceBlocks;
-    const int64_t wanted = (kChunkPieces + tiles * a.Hkv - 1) / (tiles * a.Hkv);
-    p.splits = (int32_t)(most < wanted ? most : wanted);
-    if (tiles * p.splits * a.Hkv + 8 >= int64_t(1) << 24) return p;         // (a grid holds fewer than 2^32 threads)
-    p.groups = (int32_t)(tiles * p.splits * a.Hkv);
-    p.slots = (int32_t)tiles;
-    if (p.splits > 1) p.bytes = (size_t)p.groups * kChunkRows * (a.d + 2) * sizeof(float);
+    // cut where the chip would have less than four rounds of tiles; see piece_of for how many pieces that can be
+    p.splits = tiles * a.Hkv < 2048 && keys > kLeastShare ? 2 : 1;
+    const int64_t slots = tiles + (p.splits > 1 ? (kChunkPieces + a.Hkv - 1) / a.Hkv + 1 : 0);
+    if (slots * a.Hkv + 8 >= int64_t(1) << 24) return p;                    // (a grid holds fewer than 2^32 threads)
+    p.slots = (int32_t)slots;
+    p.groups = (int32_t)(slots * a.Hkv);
+    if (p.splits > 1) p.bytes = (size_t)p.groups * (kNoteBytes + kChunkRows * (a.d + 2) * sizeof(float));
     return p;
   }
   // workgroups that the chip holds at once, and that have the least share to do if every tile met all the keys that it can
@@ -1331,7 +1361,7 @@ PagedPlan plan_paged(const PagedAttention& a) {
   const int64_t groups = wide > 256 ? 256 : wide > 64 ? 512 : 1024;
   const int64_t work = (tiles * a.Hkv * (keys + kTileCost) + kLeastShare - 1) / kLeastShare;
   p.groups = (int32_t)(work < groups ? (work > 1 ? work : 1) : groups);
-  if (p.groups > 1) p.bytes = (size_t)p.groups * 2 * kRows * (a.d + 2) * sizeof(float);
+  if (p.groups > 1) p.bytes = (size_t)p.groups * (kNoteBytes + 2 * kRows * (a.d + 2) * sizeof(float));
   return p;
 }
 

@@ -89,6 +89,8 @@ struct RotateArgs {
 };
 sga_status launch_rotate(const RotateArgs& a);
 
+constexpr size_t kNoteBytes = 32;          // (see Note in attention_paged.hip)
+
 struct PagedAttention {
   const void* Q;
   void* O;
@@ -103,6 +105,7 @@ struct PagedAttention {
   float scale;
   uint32_t page_pieces;      // 16-byte pieces from page to page
   float* partials;           // partial states of tiles that are cut; null: none is
+  void* notes;               // ... and what is to be joined, one for each workgroup, ahead of them
   int32_t tile_rows, groups, splits, slots;      // the plan's
   int32_t d, dtype;
   hipStream_t stream;
@@ -111,7 +114,7 @@ struct PagedAttention {
 struct PagedPlan {
   int32_t tile_rows;         // rows of a tile: which kernel takes the call
   int32_t groups;            // workgroups (tiles of 16 rows: each with an equal share of the work); 0: the call is too large
-  int32_t slots, splits;     // tiles of 128 rows: of a key head, some of them empty, and the most pieces of one
+  int32_t slots, splits;     // tiles of 128 rows: pieces of a key head at most, and more than 1 if tiles may be cut
   size_t bytes;
 };
 PagedPlan plan_paged(const PagedAttention& a);
