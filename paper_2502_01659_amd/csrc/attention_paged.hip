@@ -24,9 +24,9 @@ typedef float float4v __attribute__((ext_vector_type(4)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kBlock = 32;            // keys of a block
-constexpr int kRows = 16;             // rows of a tile
+constexpr int kRows = 16;             // rows of a tile, or twice as many where a sequence brings more
 constexpr int kWaves = 4;             // wavefronts of a workgroup, which take its blocks in turn
-constexpr int kChunkPieces = 1024;    // pieces of tiles of 128 rows that a call is cut into
+constexpr int kChunkPieces = 1536;    // pieces of tiles of 128 rows that a call is cut into
 
 constexpr int kTokenRows = 64;        // sequences with more rows than this on average take tiles of 128 rows
 
@@ -196,7 +196,7 @@ __device__ __forceinline__ int thread_again() {
 struct Part {
   int32_t seq, begin, n_new, length, tile, head;
   uint32_t from, to, extent;
-  int32_t there;             // 0: the share is done
+  int32_t there;             // 2: a wavefront's work, 1: the workgroup's
 };
 
 // A workgroup's walk along its share.  It lies in LDS, since it is needed between the parts only; the first wavefront
@@ -209,7 +209,9 @@ struct Share {
   uint64_t at, end, size;    // what is left of the share, and a whole one
   int32_t chunk, lane;       // the current sequence is chunk + lane
   uint32_t head, tile, offset, extent;     // current tile, the place in it, its length
-  Part part;
+  Part part[kWaves];         // what the workgroup does next: one part, or a whole tile for each wavefront
+  int32_t parts, pending;    // how many; and whether the current tile's part is found but not done (it is `ahead`)
+  Part ahead;
 
   // 64 sequences from `from` on, which begins at `base` on the line
   __device__ __forceinline__ void load(const PagedAttention& a, int32_t from, uint64_t base) {
@@ -273,25 +275,26 @@ struct Share {
     locate(a, step_of<kTileRows>(a));
     return true;
   }
-  // The part of the current tile that is in the share.
-  __device__ __forceinline__ void take_part(const PagedAttention& a) {
+  // The part of the current tile that is in the share, if any.
+  __device__ __forceinline__ void find_part(const PagedAttention& a) {
     const bool uncut = !a.partials || whole();
     if (uncut && offset > 0) {              // the share begins inside a tile that is not cut: with its beginning
       at -= offset;
       offset = 0;
     }
-    part.there = 0;
+    pending = 0;
     if (at >= end) return;
     const uint64_t left = end - at;
     const uint32_t to = offset + left < extent ? offset + (uint32_t)left : extent;
     if (uncut && to < extent) return;
     const SequenceWork& now = work[lane];
     if (tile >= now.tiles || head >= (uint32_t)a.Hkv) return;          // (lengths that change while the call runs)
-    part = Part{chunk + lane, now.begin, now.n_new, now.length, (int32_t)tile, (int32_t)head, offset, to, extent, 1};
+    ahead = Part{chunk + lane, now.begin, now.n_new, now.length, (int32_t)tile, (int32_t)head, offset, to, extent, 1};
+    pending = 1;
   }
-  // Goes on behind the part.
+  // Goes on behind the part found.
   __device__ __forceinline__ void advance(const PagedAttention& a) {
-    at += part.to - offset;
+    at += ahead.to - offset;
     offset = 0;
     if (at < end) {
       if (++tile == work[lane].tiles) {
@@ -304,27 +307,46 @@ struct Share {
       }
       extent = work[lane].length_of(tile, step_of<kTileRows>(a));
     }
-    take_part(a);
+    find_part(a);
   }
-  // The first part of share i, or the next one; all wavefronts call it.
-  __device__ __forceinline__ Part next(const PagedAttention& a, uint32_t i, bool first) {
+  // A whole tile that is short against the share is one wavefront's work: four of them then wait for memory and for their
+  // first keys at the same time, and none waits for the others' keys.
+  __device__ __forceinline__ bool alone() const {
+    return ahead.from == 0 && ahead.to == extent && (uint64_t)extent * kWaves <= size;
+  }
+  // What the workgroup with share i does first, or next; all wavefronts call it.  False: nothing is left.
+  __device__ __forceinline__ bool next(const PagedAttention& a, uint32_t i, bool first) {
     if (threadIdx.x < kWave) {
-      if (!first) advance(a);
-      else if (begin(a, i)) take_part(a);
-      else part.there = 0;
+      pending = first ? 0 : pending;
+      parts = 0;
+      if (first && begin(a, i)) find_part(a);
+      bool more = true;
+      while (more && pending) {
+        const bool single = alone();
+        if (parts > 0 && !single) break;
+        part[parts] = ahead;
+        part[parts].there = single ? 2 : 1;
+        ++parts;
+        more = single && parts < kWaves;
+        advance(a);
+      }
     }
     __syncthreads();
+    return parts > 0;
+  }
+  __device__ __forceinline__ Part mine(int i) const {
+    const Part& q = part[i];
     Part p;
-    p.seq = __builtin_amdgcn_readfirstlane(part.seq);
-    p.begin = __builtin_amdgcn_readfirstlane(part.begin);
-    p.n_new = __builtin_amdgcn_readfirstlane(part.n_new);
-    p.length = __builtin_amdgcn_readfirstlane(part.length);
-    p.tile = __builtin_amdgcn_readfirstlane(part.tile);
-    p.head = __builtin_amdgcn_readfirstlane(part.head);
-    p.from = __builtin_amdgcn_readfirstlane(part.from);
-    p.to = __builtin_amdgcn_readfirstlane(part.to);
-    p.extent = __builtin_amdgcn_readfirstlane(part.extent);
-    p.there = __builtin_amdgcn_readfirstlane(part.there);
+    p.seq = __builtin_amdgcn_readfirstlane(q.seq);
+    p.begin = __builtin_amdgcn_readfirstlane(q.begin);
+    p.n_new = __builtin_amdgcn_readfirstlane(q.n_new);
+    p.length = __builtin_amdgcn_readfirstlane(q.length);
+    p.tile = __builtin_amdgcn_readfirstlane(q.tile);
+    p.head = __builtin_amdgcn_readfirstlane(q.head);
+    p.from = __builtin_amdgcn_readfirstlane(q.from);
+    p.to = __builtin_amdgcn_readfirstlane(q.to);
+    p.extent = __builtin_amdgcn_readfirstlane(q.extent);
+    p.there = __builtin_amdgcn_readfirstlane(q.there);
     return p;
   }
 };
@@ -342,9 +364,9 @@ __device__ __forceinline__ float* record_of(const PagedAttention& a, int64_t i) 
   return a.partials + i * (kTileRows * (D + 2));
 }
 // Each share has two, of the tile that it begins within and of the one that it ends within.
-template <int D>
+template <int D, int kTileRows>
 __device__ __forceinline__ float* record_of_share(const PagedAttention& a, uint32_t share, bool begins_within) {
-  return record_of<D, kRows>(a, (int64_t)share * 2 + (begins_within ? 0 : 1));
+  return record_of<D, kTileRows>(a, (int64_t)share * 2 + (begins_within ? 0 : 1));
 }
 // What a workgroup leaves for the kernel that joins: a tile and its parts.
 struct alignas(16) Note {
@@ -413,67 +435,74 @@ __device__ __forceinline__ int64_t place_of(const PagedArgs& b, int32_t seq, int
 }
 
 // Operands of 16-bit storage: eight values of a lane per product of 32.
-template <typename T, int D>
+template <typename T, int D, int N>
 struct Core {
   static constexpr int kSteps = D / 32;      // products over the channels of a 16-key tile
   static constexpr int kRun = D / 16;        // channels of V per lane
   using Piece = vec_t<T, 8>;
   using Run = vec_t<T, kRun>;
   static constexpr int kPieceElems = 8;
-  Piece q[kSteps];
+  Piece q[N][kSteps];
   Piece k[2][kSteps];
   Run v[8];
 
-  __device__ __forceinline__ float4v scores(int t) const {
+  __device__ __forceinline__ float4v scores(int t, int n) const {
     float4v s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) s = matrix(k[t][i], q[i], s);
+    for (int i = 0; i < kSteps; ++i) s = matrix(k[t][i], q[n][i], s);
     return s;
   }
   // P as the sum of two numbers of the storage type: one alone would add an error as large as the
   // rounding of O to O, and the matrix cores wait for memory here.
-  __device__ __forceinline__ void mix(const float (&p)[8], float4v (&o)[kRun]) const {
-    Piece high, low;
+  __device__ __forceinline__ void mix(const float (&p)[N][8], float4v (&o)[N][kRun]) const {
+    Piece high[N], low[N];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      high[e] = (T)p[e];
-      low[e] = (T)(p[e] - (float)high[e]);
-    }
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        high[n][e] = (T)p[n][e];
+        low[n][e] = (T)(p[n][e] - (float)high[n][e]);
+      }
 #pragma unroll
     for (int c = 0; c < kRun; ++c) {
       Piece column;
 #pragma unroll
       for (int e = 0; e < 8; ++e) column[e] = v[e][c];
-      o[c] = matrix(column, high, o[c]);
-      o[c] = matrix(column, low, o[c]);
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        o[n][c] = matrix(column, high[n], o[n][c]);
+        o[n][c] = matrix(column, low[n], o[n][c]);
+      }
     }
   }
 };
 // fp32 storage: products of four, every operand used whole.
-template <int D>
-struct Core<float, D> {
+template <int D, int N>
+struct Core<float, D, N> {
   static constexpr int kSteps = D / 16;      // 16-byte pieces of a key per lane
   static constexpr int kRun = D / 16;
   using Piece = vec_t<float, 4>;
   using Run = vec_t<float, kRun>;
   static constexpr int kPieceElems = 4;
-  Piece q[kSteps];
+  Piece q[N][kSteps];
   Piece k[2][kSteps];
   Run v[8];
 
-  __device__ __forceinline__ float4v scores(int t) const {
+  __device__ __forceinline__ float4v scores(int t, int n) const {
     float4v s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = matrix(k[t][i][e], q[i][e], s);
+      for (int e = 0; e < 4; ++e) s = matrix(k[t][i][e], q[n][i][e], s);
     return s;
   }
-  __device__ __forceinline__ void mix(const float (&p)[8], float4v (&o)[kRun]) const {
+  __device__ __forceinline__ void mix(const float (&p)[N][8], float4v (&o)[N][kRun]) const {
 #pragma unroll
-    for (int c = 0; c < kRun; ++c)
+    for (int n = 0; n < N; ++n)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) o[c] = matrix(v[e][c], p[e], o[c]);
+      for (int c = 0; c < kRun; ++c)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[n][c] = matrix(v[e][c], p[n][e], o[n][c]);
   }
 };
 
@@ -549,45 +578,61 @@ struct Places {
   int64_t key[2], value[8];  // else: of the lane's keys
   uint32_t held;             // bit t: tile t has a page; else bit j: key j of the block has one
 };
+struct Asked {
+  int32_t page, in_page;     // of a key: its page table entry (-1 behind the last column) and the row in that page
+};
 
-template <typename T, int D, bool kWholeTiles>
-__global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) {
-  using C = Core<T, D>;
-  constexpr int kRun = C::kRun;
+// N: 16-row groups of a tile, which share the keys that a wavefront loads.
+template <typename T, int D, int N, bool kWholeTiles>
+__global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1 : 2))) void paged_kernel(
+    PagedAttention a) {
+  using C = Core<T, D, N>;
+  constexpr int kRun = C::kRun, kTileRows = 16 * N;
   constexpr int kStride = D + 4;                          // floats of a row in LDS
-  __shared__ __align__(16) float out[kWaves][kRows][kStride];
-  __shared__ float tops[kWaves][kRows], sums[kWaves][kRows];
+  __shared__ __align__(16) float out[kWaves][kTileRows][kStride];
+  __shared__ float tops[kWaves][kTileRows], sums[kWaves][kTileRows];
   const int32_t group = (int32_t)a.group.value;
-  __shared__ Share<kRows> share;
+  __shared__ Share<kTileRows> share;
   for (bool first_part = true;; first_part = false) {
-  const Part here = share.next(a, blockIdx.x, first_part);
+  const bool any = share.next(a, blockIdx.x, first_part);
   if (first_part && a.partials && threadIdx.x == 0) {
     // the tile that ends in this share and began in an earlier one
-    const bool ends = here.there && here.from > 0 && here.to == here.extent;
-    const int32_t first = ends ? (int32_t)quotient64(share.size * blockIdx.x - here.from, share.size) : 0;
-    notes_of(a)[blockIdx.x] = Note{ends ? (int32_t)blockIdx.x - first + 1 : 0, first, here.seq, here.begin, here.n_new, here.length,
-                                   here.tile, here.head};
+    const Part& p = share.part[0];
+    const bool ends = any && p.from > 0 && p.to == p.extent;
+    const int32_t first = ends ? (int32_t)quotient64(share.size * blockIdx.x - p.from, share.size) : 0;
+    notes_of(a)[blockIdx.x] = Note{ends ? (int32_t)blockIdx.x - first + 1 : 0, first, p.seq, p.begin, p.n_new, p.length,
+                                   p.tile, p.head};
   }
-  if (!here.there) return;
+  if (!any) return;
   const int tid = thread_again(), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int m = lane & 15, g = lane >> 4;
+  const int parts = __builtin_amdgcn_readfirstlane(share.parts);
+  const bool alone = __builtin_amdgcn_readfirstlane(share.part[0].there) == 2;      // this wavefront has a tile to itself
+  if (!alone || wave < parts) {
+  const Part here = share.mine(alone ? wave : 0);
   const int32_t head_kv = here.head;
-  const Tile tile = tile_of<kRows>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
-  float* const part = here.from == 0 && here.to == here.extent ? nullptr : record_of_share<D>(a, blockIdx.x, here.from > 0);
+  const Tile tile = tile_of<kTileRows>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
 
-  // this lane's row
-  const int32_t flat = tile.first + (m < tile.count ? m : 0);
-  const int32_t token = (int32_t)quotient((uint32_t)flat, a.group), head = head_kv * group + (flat - token * group);
-  const Sight sight = sight_of(a, tile.length - tile.n_new + token, tile.kept);
+  // this lane's rows
+  Sight sight[N];
   C core;
-  {
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int32_t flat = tile.first + (16 * n + m < tile.count ? 16 * n + m : 0);
+    const int32_t token = (int32_t)quotient((uint32_t)flat, a.group), head = head_kv * group + (flat - token * group);
+    sight[n] = sight_of(a, tile.length - tile.n_new + token, tile.kept);
     const T* q = static_cast<const T*>(a.Q) + (int64_t)head * a.q_head + (int64_t)(tile.begin + token) * a.q_row;
 #pragma unroll
     for (int i = 0; i < C::kSteps; ++i)
-      core.q[i] = *reinterpret_cast<const typename C::Piece*>(q + (g + 4 * i) * C::kPieceElems);
+      core.q[n][i] = *reinterpret_cast<const typename C::Piece*>(q + (g + 4 * i) * C::kPieceElems);
   }
   // keys that every row sees
-  int32_t lo_max = sight.lo, hi_min = sight.hi;
+  int32_t lo_max = sight[0].lo, hi_min = sight[0].hi;
+#pragma unroll
+  for (int n = 1; n < N; ++n) {
+    lo_max = max(lo_max, sight[n].lo);
+    hi_min = min(hi_min, sight[n].hi);
+  }
 #pragma unroll
   for (int off = 1; off < 16; off <<= 1) {
     lo_max = max(lo_max, __shfl_xor(lo_max, off, kWave));
@@ -600,25 +645,30 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
   const int64_t in_head = (int64_t)head_kv * b.page.value * D;
   const T* const cache_k = static_cast<const T*>(a.cache_k) + in_head;
   const T* const cache_v = static_cast<const T*>(a.cache_v) + in_head;
-  auto find = [&](int32_t block) {
+  const int32_t* const table = b.page_table + (int64_t)tile.seq * b.pages_per_seq;
+  // Lane l asks for key l % 32 of a block, a block ahead of the loads that need the answer.
+  auto ask = [&](int32_t block) {
+    const uint32_t j = (uint32_t)(first_key(tile, block) + (lane & 31)), column = quotient(j, b.page);
+    Asked q;
+    q.in_page = (int32_t)(j - column * b.page.value);
+    q.page = column < (uint32_t)b.pages_per_seq ? table[column] : -1;
+    return q;
+  };
+  auto find = [&](const Asked& q) {
+    const bool there = (uint32_t)q.page < b.n_pages;
+    const int64_t o = there ? (int64_t)q.page * b.page_stride + (int64_t)q.in_page * D : 0;
+    const uint32_t held = (uint32_t)__ballot(there);
     Places at;
-    const int32_t j0 = first_key(tile, block);
-    at.held = 0;
     if constexpr (kWholeTiles) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int64_t o = uniform64(place_of(b, tile.seq, j0 + 16 * t, D));
-        at.held |= (o >= 0 ? 1u : 0u) << t;
-        at.tile[t] = o >= 0 ? o : 0;
-      }
+      at.held = (held & 1) | (held >> 15 & 2);
+      at.tile[0] = (int64_t)from_lane((uint64_t)o, 0);
+      at.tile[1] = (int64_t)from_lane((uint64_t)o, 16);
     } else {
-      const int64_t o = place_of(b, tile.seq, j0 + (lane & 31), D);
-      at.held = (uint32_t)__ballot(o >= 0);
-      const int64_t safe = o >= 0 ? o : 0;
+      at.held = held;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) at.key[t] = __shfl(safe, 16 * t + m, kWave);
+      for (int t = 0; t < 2; ++t) at.key[t] = __shfl(o, 16 * t + m, kWave);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) at.value[e] = __shfl(safe, (e < 4 ? 4 * g + e : 12 + 4 * g + e), kWave);
+      for (int e = 0; e < 8; ++e) at.value[e] = __shfl(o, (e < 4 ? 4 * g + e : 12 + 4 * g + e), kWave);
     }
     return at;
   };
@@ -639,136 +689,162 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_kernel(PagedAttention a) 
     }
   };
 
-  const int32_t first_block = block_at(here.from, here.extent, tile.blocks);
-  const int32_t end_block = block_at(here.to, here.extent, tile.blocks);
-  float top, sum;
-  float4v o[kRun];
-
-  // one walk over the wavefront's blocks
-  auto walk = [&]() {
-    top = -INFINITY;
-    sum = 0.f;
+  const int32_t first_block = block_at(here.from, here.extent, tile.blocks) + (alone ? 0 : wave);
+  const int32_t end_block = block_at(here.to, here.extent, tile.blocks), step = alone ? 1 : kWaves;
+  float top[N], sum[N];
+  float4v o[N][kRun];
 #pragma unroll
-    for (int c = 0; c < kRun; ++c) o[c] = float4v{0.f, 0.f, 0.f, 0.f};
-    int32_t block = first_block + wave;
-    if (block >= end_block) return;
-    Places at = find(block);
+  for (int n = 0; n < N; ++n) {
+    top[n] = -INFINITY;
+    sum[n] = 0.f;
+#pragma unroll
+    for (int c = 0; c < kRun; ++c) o[n][c] = float4v{0.f, 0.f, 0.f, 0.f};
+  }
+  Places at;
+  Asked asked{};
+  if (first_block < end_block) {
+    at = find(ask(first_block));
+    asked = ask(first_block + step);      // (behind the last block: a place in the page table's row, or none)
     load_k(at);
     load_v(at);
-    for (; block < end_block; block += kWaves) {
-      const int32_t j0 = first_key(tile, block);
-      const uint32_t held = at.held;
-      const bool more = block + kWaves < end_block;
-      float4v s[2] = {core.scores(0), core.scores(1)};
-      if (more) {
-        at = find(block + kWaves);
-        load_k(at);
-      }
-      const bool all_held = held == (kWholeTiles ? 3u : ~0u);
-      const bool whole = all_held && j0 >= lo_max && j0 + kBlock - 1 <= hi_min;
-      float p[8];
+  }
+  for (int32_t block = first_block; block < end_block; block += step) {
+    const int32_t j0 = first_key(tile, block);
+    const uint32_t held = at.held;
+    const bool more = block + step < end_block;
+    float4v s[N][2];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) p[e] = s[e / 4][e % 4] * (a.scale * kLog2e);
+    for (int n = 0; n < N; ++n) {
+      s[n][0] = core.scores(0, n);
+      s[n][1] = core.scores(1, n);
+    }
+    if (more) {
+      at = find(asked);
+      asked = ask(block + 2 * step);
+      load_k(at);
+    }
+    const bool all_held = held == (kWholeTiles ? 3u : ~0u);
+    const bool whole = all_held && j0 >= lo_max && j0 + kBlock - 1 <= hi_min;
+    float p[N][8];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) p[n][e] = s[n][e / 4][e % 4] * (a.scale * kLog2e);
       if (!whole) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
           const int in_block = 16 * (e / 4) + 4 * g + e % 4, j = j0 + in_block;
           const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
-          p[e] = there && ((j >= sight.lo && j <= sight.hi) || j < sight.lead) ? p[e] : -INFINITY;
+          p[n][e] = there && ((j >= sight[n].lo && j <= sight[n].hi) || j < sight[n].lead) ? p[n][e] : -INFINITY;
         }
       }
-      float best = p[0];
+      float best = p[n][0];
 #pragma unroll
-      for (int e = 1; e < 8; ++e) best = fmaxf(best, p[e]);
-      best = fmaxf(row_max(best), top);
-      if (__any(best > top)) {
-        const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top - best) : 1.f;
-        sum *= keep;
+      for (int e = 1; e < 8; ++e) best = fmaxf(best, p[n][e]);
+      best = fmaxf(row_max(best), top[n]);
+      if (__any(best > top[n])) {
+        const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top[n] - best) : 1.f;
+        sum[n] *= keep;
 #pragma unroll
-        for (int c = 0; c < kRun; ++c) o[c] *= keep;
-        top = best;
+        for (int c = 0; c < kRun; ++c) o[n][c] *= keep;
+        top[n] = best;
       }
-      const float against = top > -INFINITY ? top : 0.f;
+      const float against = top[n] > -INFINITY ? top[n] : 0.f;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(p[e] - against);
-        sum += p[e];
+        p[n][e] = __builtin_amdgcn_exp2f(p[n][e] - against);
+        sum[n] += p[n][e];
       }
-      // values of keys that no row sees (behind the last token, without a page) may be anything
-      if (!all_held || j0 + kBlock > tile.kept) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int in_block = 16 * (e / 4) + 4 * g + e % 4;
-          const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
-          const bool use = there && j0 + in_block < tile.kept;
-#pragma unroll
-          for (int c = 0; c < kRun; ++c) core.v[e][c] = use ? core.v[e][c] : (T)0.f;
-        }
-      }
-      core.mix(p, o);
-      if (more) load_v(at);
     }
-  };
-  walk();
+    // values of keys that no row sees (behind the last token, without a page) may be anything
+    if (!all_held || j0 + kBlock > tile.kept) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int in_block = 16 * (e / 4) + 4 * g + e % 4;
+        const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
+        const bool use = there && j0 + in_block < tile.kept;
+#pragma unroll
+        for (int c = 0; c < kRun; ++c) core.v[e][c] = use ? core.v[e][c] : (T)0.f;
+      }
+    }
+    core.mix(p, o);
+    if (more) load_v(at);
+  }
   bool finite = true;
 #pragma unroll
-  for (int c = 0; c < kRun; ++c)
+  for (int n = 0; n < N; ++n)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) finite = finite && __builtin_isfinite(o[c][r]);
+    for (int c = 0; c < kRun; ++c)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) finite = finite && __builtin_isfinite(o[n][c][r]);
   if (__all(finite)) {
-    const float total = row_sum(sum);
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int n = 0; n < N; ++n) {
+      const float total = row_sum(sum[n]);
 #pragma unroll
-      for (int c = 0; c < kRun; ++c) out[wave][m][(4 * g + r) * kRun + c] = o[c][r];
-    if (g == 0) {
-      tops[wave][m] = top;
-      sums[wave][m] = total;
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int c = 0; c < kRun; ++c) out[wave][16 * n + m][(4 * g + r) * kRun + c] = o[n][c][r];
+      if (g == 0) {
+        tops[wave][16 * n + m] = top[n];
+        sums[wave][16 * n + m] = total;
+      }
     }
   } else {
     for (int row = 0; row < tile.count; ++row) {
-      float x[(D + 63) / 64];
-      attend_row<T, D>(a, tile, head_kv, tile.first + row, first_block + wave, end_block, kWaves, top, sum, x);
+      float x[(D + 63) / 64], row_top, row_total;
+      attend_row<T, D>(a, tile, head_kv, tile.first + row, first_block, end_block, step, row_top, row_total, x);
 #pragma unroll
       for (int c = 0; c < (D + 63) / 64; ++c)
         if (lane + 64 * c < D) out[wave][row][lane + 64 * c] = x[c];
       if (lane == 0) {
-        tops[wave][row] = top;
-        sums[wave][row] = sum;
+        tops[wave][row] = row_top;
+        sums[wave][row] = row_total;
       }
     }
   }
-  __syncthreads();
-
-  // the wavefronts' states of a row, added in their order
-  constexpr int kPer = D * kRows / (kWaves * kWave);       // channels of a thread: D / 16
-  const int row = tid / (D / kPer), channel = tid % (D / kPer) * kPer;
-  if (row < tile.count) {
-    float high = -INFINITY;
+  constexpr int kPer = D / 16;                             // channels of a thread
+  if (alone) {
+    __builtin_amdgcn_wave_barrier();
+    for (int i = lane; i < 16 * tile.count; i += kWave) {
+      float x[kPer];
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) high = fmaxf(high, tops[w][row]);
-    const float against = high > -INFINITY ? high : 0.f;
-    float total = 0.f, x[kPer];
-#pragma unroll
-    for (int c = 0; c < kPer; ++c) x[c] = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      if (sums[w][row] == 0.f) continue;                   // no key seen
-      const float weight = __builtin_amdgcn_exp2f(tops[w][row] - against);
-      total += weight * sums[w][row];
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) x[c] += weight * out[w][row][channel + c];
+      for (int c = 0; c < kPer; ++c) x[c] = out[wave][i / 16][i % 16 * kPer + c];
+      store_row<T, D>(a, tile, head_kv, i / 16, i % 16 * kPer, x, tops[wave][i / 16], sums[wave][i / 16]);
     }
-    if (part) {
+  } else {
+    __syncthreads();
+    // the wavefronts' states of a row, added in their order
+    float* const part = here.from == 0 && here.to == here.extent ? nullptr : record_of_share<D, kTileRows>(a, blockIdx.x, here.from > 0);
+    const int channel = tid % 16 * kPer;
+    for (int row = tid / 16; row < tile.count; row += kWaves * kWave / 16) {
+      float high = -INFINITY;
 #pragma unroll
-      for (int c = 0; c < kPer; ++c) part[row * D + channel + c] = x[c];
-      if (channel == 0) {
-        part[kRows * D + row] = high;
-        part[kRows * (D + 1) + row] = total;
+      for (int w = 0; w < kWaves; ++w) high = fmaxf(high, tops[w][row]);
+      const float against = high > -INFINITY ? high : 0.f;
+      float total = 0.f, x[kPer];
+#pragma unroll
+      for (int c = 0; c < kPer; ++c) x[c] = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        if (sums[w][row] == 0.f) continue;                 // no key seen
+        const float weight = __builtin_amdgcn_exp2f(tops[w][row] - against);
+        total += weight * sums[w][row];
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) x[c] += weight * out[w][row][channel + c];
       }
-    } else {
-      store_row<T, D>(a, tile, head_kv, row, channel, x, high, total);
+      if (part) {
+#pragma unroll
+        for (int c = 0; c < kPer; ++c) part[row * D + channel + c] = x[c];
+        if (channel == 0) {
+          part[kTileRows * D + row] = high;
+          part[kTileRows * (D + 1) + row] = total;
+        }
+      } else {
+        store_row<T, D>(a, tile, head_kv, row, channel, x, high, total);
+      }
     }
+  }
   }
   __syncthreads();                                         // the next part's states take the same space
   }
@@ -1281,11 +1357,12 @@ __device__ __forceinline__ void join_parts(const PagedAttention& a, const Note& 
 }
 
 // ... tiles that end in a share and begin in an earlier one
-template <typename T, int D>
+template <typename T, int D, int kTileRows>
 __global__ __launch_bounds__(kWaves* kWave) void paged_join_kernel(PagedAttention a) {
   const Note note = notes_of(a)[blockIdx.x];
   if (note.count == 0) return;
-  join_parts<T, D, kRows>(a, note, 0, [&](int32_t i) { return record_of_share<D>(a, note.first + i, i > 0); });
+  join_parts<T, D, kTileRows>(a, note, blockIdx.y * 16,
+                              [&](int32_t i) { return record_of_share<D, kTileRows>(a, note.first + i, i > 0); });
 }
 
 // ... tiles of 128 rows in pieces, whose records lie as far apart as the sequence has tiles
@@ -1298,6 +1375,17 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_chunk_join_kernel(PagedAt
   for (int32_t row0 = blockIdx.y * kJoinRows; row0 < (int32_t)(blockIdx.y + 1) * kJoinRows; row0 += 16)
     join_parts<T, D, kChunkRows>(a, note, row0,
                                  [&](int32_t i) { return record_of<D, kChunkRows>(a, note.first + (int64_t)i * tiles); });
+}
+
+template <typename T, int D, int N>
+sga_status launch_paged_rows(const PagedAttention& a) {
+  const dim3 block(kWaves * kWave);
+  profile_mark_begin(a.stream, "paged_kernel");
+  if (a.batch.page.value % 16 == 0) paged_kernel<T, D, N, true><<<dim3(a.groups), block, 0, a.stream>>>(a);
+  else paged_kernel<T, D, N, false><<<dim3(a.groups), block, 0, a.stream>>>(a);
+  profile_mark_end(a.stream);
+  if (a.partials) paged_join_kernel<T, D, 16 * N><<<dim3(a.groups, N), block, 0, a.stream>>>(a);
+  return hip_status(hipGetLastError());
 }
 
 template <typename T, int D>
@@ -1314,12 +1402,9 @@ sga_status launch_paged_as(const PagedAttention& a) {
     }
     return hip_status(hipGetLastError());
   }
-  profile_mark_begin(a.stream, "paged_kernel");
-  if (a.batch.page.value % 16 == 0) paged_kernel<T, D, true><<<dim3(a.groups), block, 0, a.stream>>>(a);
-  else paged_kernel<T, D, false><<<dim3(a.groups), block, 0, a.stream>>>(a);
-  profile_mark_end(a.stream);
-  if (a.partials) paged_join_kernel<T, D><<<dim3(a.groups), block, 0, a.stream>>>(a);
-  return hip_status(hipGetLastError());
+  if constexpr (!(sizeof(T) == 4 && D == 256))      // (the registers do not hold two groups of such rows)
+    if (a.tile_rows != kRows) return launch_paged_rows<T, D, 2>(a);
+  return launch_paged_rows<T, D, 1>(a);
 }
 
 template <typename T>
@@ -1339,6 +1424,8 @@ PagedPlan plan_paged(const PagedAttention& a) {
   const int64_t all_rows = (int64_t)a.batch.n_tokens * a.group.value;
   if (a.dtype != SGA_F32 && a.d >= 64 && a.batch.page.value % 16 == 0 && all_rows > (int64_t)kTokenRows * a.batch.n_seqs)
     p.tile_rows = kChunkRows;
+  else if (all_rows > (int64_t)kRows * a.batch.n_seqs && !(a.dtype == SGA_F32 && a.d == 256))
+    p.tile_rows = 2 * kRows;
   const int64_t tiles = all_rows / p.tile_rows + a.batch.n_seqs;
   if (tiles >= int64_t(1) << 24) return p;                 // (rows of a sequence are counted in 31 bits)
   // keys that a tile meets at most
@@ -1357,11 +1444,11 @@ PagedPlan plan_paged(const PagedAttention& a) {
     return p;
   }
   // workgroups that the chip holds at once, and that have the least share to do if every tile met all the keys that it can
-  const int wide = a.d * (a.dtype == SGA_F32 ? 2 : 1);
-  const int64_t groups = wide > 256 ? 256 : wide > 64 ? 512 : 1024;
+  const int64_t row_bytes = (int64_t)a.d * (a.dtype == SGA_F32 ? 4 : 2) * (p.tile_rows / kRows);
+  const int64_t groups = a.d == 256 ? 256 : row_bytes > 128 ? 512 : 768;
   const int64_t work = (tiles * a.Hkv * (keys + kTileCost) + kLeastShare - 1) / kLeastShare;
   p.groups = (int32_t)(work < groups ? (work > 1 ? work : 1) : groups);
-  if (p.groups > 1) p.bytes = (size_t)p.groups * (kNoteBytes + 2 * kRows * (a.d + 2) * sizeof(float));
+  if (p.groups > 1) p.bytes = (size_t)p.groups * (kNoteBytes + 2 * p.tile_rows * (a.d + 2) * sizeof(float));
   return p;
 }
 
