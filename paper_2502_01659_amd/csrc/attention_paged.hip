@@ -26,9 +26,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kBlock = 32;            // keys of a block
 constexpr int kRows = 16;             // rows of a tile, or twice as many where a sequence brings more
 constexpr int kWaves = 4;             // wavefronts of a workgroup, which take its blocks in turn
+constexpr int kLeastPiece = 1024;
 constexpr int kChunkPieces = 1536;    // pieces of tiles of 128 rows that a call is cut into
 
-constexpr int kTokenRows = 64;        // sequences with more rows than this on average take tiles of 128 rows
+constexpr int kTokenRows = 32;        // sequences with more rows than this on average take tiles of 128 rows
 
 __device__ __forceinline__ int64_t uniform64(int64_t v) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
@@ -395,7 +396,7 @@ __device__ __forceinline__ bool piece_of(const PagedAttention& a, int32_t rest, 
   }
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) total += __shfl_xor(total, off, kWave);
-  const float size = fmaxf((float)kLeastShare, total * (float)a.Hkv * (1.f / kChunkPieces));
+  const float size = fmaxf((float)kLeastPiece, total * (float)a.Hkv * (1.f / kChunkPieces));
   int32_t behind = 0;
   for (int32_t c = 0; c < n; c += kWave) {
     if (n > kWave) w = work_of<kTileRows>(a, c + l);
@@ -446,11 +447,14 @@ struct Core {
   Piece k[2][kSteps];
   Run v[8];
 
-  __device__ __forceinline__ float4v scores(int t, int n) const {
-    float4v s = {0.f, 0.f, 0.f, 0.f};
+  // (a product waits for the one before it on the same sum: the sums take turns)
+  __device__ __forceinline__ void scores(float4v (&s)[N][2]) const {
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) s = matrix(k[t][i], q[n][i], s);
-    return s;
+    for (int i = 0; i < kSteps; ++i)
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int t = 0; t < 2; ++t) s[n][t] = matrix(k[t][i], q[n][i], i ? s[n][t] : float4v{0.f, 0.f, 0.f, 0.f});
   }
   // P as the sum of two numbers of the storage type: one alone would add an error as large as the
   // rounding of O to O, and the matrix cores wait for memory here.
@@ -469,10 +473,9 @@ struct Core {
 #pragma unroll
       for (int e = 0; e < 8; ++e) column[e] = v[e][c];
 #pragma unroll
-      for (int n = 0; n < N; ++n) {
-        o[n][c] = matrix(column, high[n], o[n][c]);
-        o[n][c] = matrix(column, low[n], o[n][c]);
-      }
+      for (int n = 0; n < N; ++n) o[n][c] = matrix(column, high[n], o[n][c]);
+#pragma unroll
+      for (int n = 0; n < N; ++n) o[n][c] = matrix(column, low[n], o[n][c]);
     }
   }
 };
@@ -488,21 +491,24 @@ struct Core<float, D, N> {
   Piece k[2][kSteps];
   Run v[8];
 
-  __device__ __forceinline__ float4v scores(int t, int n) const {
-    float4v s = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void scores(float4v (&s)[N][2]) const {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s = matrix(k[t][i][e], q[n][i][e], s);
-    return s;
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int n = 0; n < N; ++n)
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            s[n][t] = matrix(k[t][i][e], q[n][i][e], i || e ? s[n][t] : float4v{0.f, 0.f, 0.f, 0.f});
   }
   __device__ __forceinline__ void mix(const float (&p)[N][8], float4v (&o)[N][kRun]) const {
 #pragma unroll
-    for (int n = 0; n < N; ++n)
+    for (int e = 0; e < 8; ++e)
 #pragma unroll
       for (int c = 0; c < kRun; ++c)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[n][c] = matrix(v[e][c], p[n][e], o[n][c]);
+        for (int n = 0; n < N; ++n) o[n][c] = matrix(v[e][c], p[n][e], o[n][c]);
   }
 };
 
@@ -575,7 +581,7 @@ __device__ __forceinline__ void store_row(const PagedAttention& a, const Tile& t
 // Where the rows of a block's keys are.  kWholeTiles: pages hold multiples of 16 tokens, so a 16-key tile lies in one.
 struct Places {
   int64_t tile[2];           // kWholeTiles: element offset of the tile's first row (wave-uniform)
-  int64_t key[2], value[8];  // else: of the lane's keys
+  int64_t key;               // else: of key lane % 32
   uint32_t held;             // bit t: tile t has a page; else bit j: key j of the block has one
 };
 struct Asked {
@@ -665,17 +671,14 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
       at.tile[1] = (int64_t)from_lane((uint64_t)o, 16);
     } else {
       at.held = held;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) at.key[t] = __shfl(o, 16 * t + m, kWave);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) at.value[e] = __shfl(o, (e < 4 ? 4 * g + e : 12 + 4 * g + e), kWave);
+      at.key = o;
     }
     return at;
   };
   auto load_k = [&](const Places& at) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const T* row = kWholeTiles ? cache_k + at.tile[t] + m * D : cache_k + at.key[t];
+      const T* row = kWholeTiles ? cache_k + at.tile[t] + m * D : cache_k + __shfl(at.key, 16 * t + m, kWave);
 #pragma unroll
       for (int i = 0; i < C::kSteps; ++i)
         core.k[t][i] = *reinterpret_cast<const typename C::Piece*>(row + (g + 4 * i) * C::kPieceElems);
@@ -684,7 +687,8 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
   auto load_v = [&](const Places& at) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-      const T* row = kWholeTiles ? cache_v + at.tile[e / 4] + (4 * g + e % 4) * D : cache_v + at.value[e];
+      const T* row = kWholeTiles ? cache_v + at.tile[e / 4] + (4 * g + e % 4) * D
+                                 : cache_v + __shfl(at.key, 16 * (e / 4) + 4 * g + e % 4, kWave);
       core.v[e] = *reinterpret_cast<const typename C::Run*>(row + m * kRun);
     }
   };
@@ -713,11 +717,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
     const uint32_t held = at.held;
     const bool more = block + step < end_block;
     float4v s[N][2];
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-      s[n][0] = core.scores(0, n);
-      s[n][1] = core.scores(1, n);
-    }
+    core.scores(s);
     if (more) {
       at = find(asked);
       asked = ask(block + 2 * step);
@@ -851,7 +851,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
 }
 
 // ---- many new tokens: tiles of 128 rows ---------------------------------------------------------------------
-// 16-bit storage, pages of multiples of 16 tokens.  Four wavefronts own 32 rows each and share every block of keys: K and V
+// 16-bit storage.  Four wavefronts own 32 rows each and share every block of keys: K and V
 // are copied global -> LDS without registers, once per workgroup, into a ring of four blocks, three ahead; the
 // barrier that opens a block also frees the one before it.  Products of 32 x 32 x 16: S^T = K Q^T and O^T += V^T P^T, a lane's
 // row is lane % 32 in both, and the keys that it holds of S^T are those that it feeds as P.  The scores of the
@@ -915,6 +915,18 @@ __device__ __forceinline__ void copy_pieces(const char* k, uint32_t k_offset, co
   }
 }
 
+// The same from an address of each lane's own.
+template <int kCopies, int kStep, int kApart>
+__device__ __forceinline__ void copy_pieces_from(const char* k, const char* v, uint32_t to) {
+  uint32_t kept;
+#pragma unroll
+  for (int i = 0; i < kCopies; ++i)
+    asm volatile(
+        "s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off\n\t"
+        "s_add_u32 m0, m0, %4\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, off\n\ts_mov_b32 m0, %0"
+        : "=&s"(kept) : "v"(k + 64 * i), "v"(v + 64 * i), "s"(to + i * kStep), "i"(kApart) : "memory", "scc");
+}
+
 // A block of 32 keys in LDS: groups of 32 channels, in a group the 32 keys' rows of 64 bytes.  What the products read then
 // differs by constants from one or two addresses per lane, and 16 lanes' pieces (K: four rows apart they would share
 // banks, so a row's four pieces are permuted; V: eight rows in a row) meet every bank once.
@@ -925,7 +937,7 @@ struct ChunkBlock {
   static __device__ __forceinline__ int k_turn(int row) { return row >> 2 & 3; }
 };
 
-template <typename T, int D>
+template <typename T, int D, bool kWholeTiles>
 __global__ __attribute__((amdgpu_waves_per_eu(D > 128 ? 1 : 2, D > 128 ? 1 : 2))) __launch_bounds__(kWaves* kWave) void
 paged_chunk_kernel(PagedAttention a) {
   using B = ChunkBlock<D>;
@@ -933,6 +945,10 @@ paged_chunk_kernel(PagedAttention a) {
   constexpr int kSlotBytes = 2 * B::kBytes, kPer = 2 * B::kCopies;    // copies of a wavefront per block
   constexpr int kSteps = D / 16, kTiles = D / 32;
   __shared__ __align__(16) char ring[kChunkSlots * kSlotBytes];
+  // Pages that do not hold multiples of 16 tokens: the page of every key of the next kAskBlocks blocks, asked for at once.  (A
+  // load into registers between the copies would make its reader wait for all of them.)
+  constexpr int kAskBlocks = 64;
+  __shared__ int32_t page_of_key[kWholeTiles ? 1 : kAskBlocks * kBlock];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = lane & 31, h = lane >> 5;
   // Workgroup i runs on XCD i % 8: a key head stays on one XCD, or on 8 / Hkv of them, whose L2 then holds the keys that
@@ -1012,8 +1028,9 @@ paged_chunk_kernel(PagedAttention a) {
   // Wavefront w copies 16-key tile w / 2, half of the groups: lane l 16 bytes of row l / 4.  (Bytes from the tile's first row on;
   // the groups follow at 64 bytes.)
   const int copy_row = 16 * (wave / 2) + lane / 4;
-  const uint32_t copy_from = (lane / 4) * B::kRowBytes + (wave % 2) * (B::kCopies * 64);
-  const uint32_t k_from = copy_from + ((lane & 3) ^ B::k_turn(copy_row)) * 16, v_from = copy_from + (lane & 3) * 16;
+  const uint32_t k_in_row = (wave % 2) * (B::kCopies * 64) + ((lane & 3) ^ B::k_turn(copy_row)) * 16;
+  const uint32_t v_in_row = (wave % 2) * (B::kCopies * 64) + (lane & 3) * 16;
+  const uint32_t k_from = (lane / 4) * B::kRowBytes + k_in_row, v_from = (lane / 4) * B::kRowBytes + v_in_row;
   const uint32_t own_part = (wave % 2) * (B::kCopies * B::kGroupBytes) + (wave / 2) * 1024;
   const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(char __attribute__((address_space(3)))*)ring);
   // The place of this wavefront's rows in the block that is copied next: its page's column and the row within it follow each
@@ -1030,11 +1047,27 @@ paged_chunk_kernel(PagedAttention a) {
     in_page = j - column * page;
     look_up();
   };
+  auto ask = [&]() {                     // (every wavefront: all have issued the blocks before)
+    for (int i = tid; i < kAskBlocks * kBlock; i += kWaves * kWave) {
+      const int32_t block = next_block + i / kBlock;
+      const uint32_t c = quotient((uint32_t)(first_key(tile, block < end_block ? block : end_block - 1) + i % kBlock), b.page);
+      page_of_key[i] = b.page_table[(int64_t)tile.seq * b.pages_per_seq + min(c, last_column)];
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  };
   auto issue = [&]() {                   // copies next_block, or the last one again
-    const uint64_t at = ((uint64_t)min(entry, last_page) * a.page_pieces << 4) + in_page * B::kRowBytes;
-    copy_pieces<B::kCopies, B::kGroupBytes, B::kBytes>(cache_k + at, k_from, cache_v + at, v_from, next_at);
+    if constexpr (kWholeTiles) {
+      const uint64_t at = ((uint64_t)min(entry, last_page) * a.page_pieces << 4) + in_page * B::kRowBytes;
+      copy_pieces<B::kCopies, B::kGroupBytes, B::kBytes>(cache_k + at, k_from, cache_v + at, v_from, next_at);
+    } else {
+      const int32_t block = next_block < end_block ? next_block : end_block - 1;
+      const uint32_t j = (uint32_t)(first_key(tile, block) + copy_row), in_page = j - quotient(j, b.page) * page;
+      const uint32_t held_by = min((uint32_t)page_of_key[(block - first_block) % kAskBlocks * kBlock + copy_row], last_page);
+      const uint64_t at = ((uint64_t)held_by * a.page_pieces << 4) + in_page * B::kRowBytes;
+      copy_pieces_from<B::kCopies, B::kGroupBytes, B::kBytes>(cache_k + at + k_in_row, cache_v + at + v_in_row, next_at);
+    }
     next_at = ring_at + ((next_at - ring_at + kSlotBytes) & (kChunkSlots * kSlotBytes - 1));
-    if (++next_block < end_block) {
+    if (++next_block < end_block && kWholeTiles) {
       if (next_block == tile.lead) {
         start_at(next_block);
       } else {
@@ -1053,6 +1086,8 @@ paged_chunk_kernel(PagedAttention a) {
   auto publish = [&]() {
     wait_loads_except<kPer*(kChunkAhead - 2)>();
     asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    if constexpr (!kWholeTiles)
+      if ((next_block - first_block) % kAskBlocks == 0 && next_block < end_block) ask();
     issue();
   };
 
@@ -1131,19 +1166,10 @@ paged_chunk_kernel(PagedAttention a) {
     }
   };
 
-  // Does any of the workgroup's keys miss its page?  Where none does, and that is nearly always, no block asks again.
+  // which keys of the block at key j0 have a page (missing: some key of the workgroup's has none)
   bool missing = false;
-  auto held_of = [&](int32_t j0) {      // bit t: the 16-key tile t of the block at key j0 has a page
-    uint32_t held = 3u;
-    if (missing) {
-      held = 0;
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const uint32_t c = quotient((uint32_t)(j0 + 16 * t), b.page);
-        if (c < (uint32_t)b.pages_per_seq && (uint32_t)table[c] < b.n_pages) held |= 1u << t;
-      }
-    }
-    return held;
+  auto held_of = [&](int32_t j0) {
+    return missing ? (uint32_t)__ballot(place_of(b, tile.seq, j0 + (lane & 31), D) >= 0) : ~0u;
   };
   // A block that some row of the wavefront does not see whole.
   auto edge = [&](int32_t block) {
@@ -1153,7 +1179,7 @@ paged_chunk_kernel(PagedAttention a) {
       // values that are no token's: 0, whatever memory held, each wavefront in its own rows (every wavefront is here)
       const uint32_t held = held_of(j0);
       char* const dst = ring + slot_of(block) + B::kBytes + own_part;
-      if (!(held >> (wave / 2) & 1) || j0 + copy_row >= tile.kept) {
+      if (!(held >> copy_row & 1) || j0 + copy_row >= tile.kept) {
 #pragma unroll
         for (int i = 0; i < B::kCopies; ++i) *reinterpret_cast<uint4*>(dst + i * B::kGroupBytes + lane * 16) = uint4{0, 0, 0, 0};
       }
@@ -1168,7 +1194,7 @@ paged_chunk_kernel(PagedAttention a) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int in_block = 8 * (r / 4) + 4 * h + r % 4, j = j0 + in_block;
-      const bool sees = (held >> (r / 8) & 1) && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
+      const bool sees = (held >> in_block & 1) && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
       s[r] = sees ? s[r] : -INFINITY;
     }
     const float total = numerators(s, top, p);
@@ -1187,16 +1213,20 @@ paged_chunk_kernel(PagedAttention a) {
   };
 
   if (first_block < end_block) {
-#pragma unroll
-    for (int i = 0; i < kSteps; ++i) asm volatile("" : "+v"(qf[i]));   // Q has arrived: from here on only the copies are counted
-    start_at(first_block);
-    for (int i = 0; i < kChunkAhead; ++i) issue();
-    for (int32_t i = first_block + (int32_t)tid; i < end_block; i += kWaves * kWave) {
-      const int32_t j0 = first_key(tile, i);
-#pragma unroll
-      for (int t = 0; t < 2; ++t) missing = missing || place_of(b, tile.seq, j0 + 16 * t, D) < 0;
+    // Does a token's key miss its page?  Asked while Q is on its way: where none does, and that is nearly always, no block
+    // asks again.
+    const int apart = kWholeTiles ? 16 : 1;
+    for (int32_t i = tid; i < (end_block - first_block) * (kBlock / apart); i += kWaves * kWave) {
+      const int32_t j = first_key(tile, first_block + i / (kBlock / apart)) + i % (kBlock / apart) * apart;
+      const uint32_t c = quotient((uint32_t)j, b.page);
+      missing |= (uint32_t)b.page_table[(int64_t)tile.seq * b.pages_per_seq + min(c, last_column)] >= b.n_pages && j < tile.kept;
     }
     missing = __syncthreads_or(missing);
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) asm volatile("" : "+v"(qf[i]));   // Q has arrived: from here on only the copies are counted
+    if constexpr (kWholeTiles) start_at(first_block);
+    else ask();
+    for (int i = 0; i < kChunkAhead; ++i) issue();
     // blocks [inner, outer) are seen whole by every row (none where pages are missing)
     int32_t inner = end_block, outer = end_block;
     if (!missing) {
@@ -1396,13 +1426,14 @@ sga_status launch_paged_as(const PagedAttention& a) {
       int64_t groups = (int64_t)a.slots * a.Hkv;
       if (a.Hkv < 8 && 8 % a.Hkv == 0) groups = (int64_t)(a.slots + 8 / a.Hkv - 1) / (8 / a.Hkv) * 8;
       profile_mark_begin(a.stream, "paged_chunk_kernel");
-      paged_chunk_kernel<T, D><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
+      if (a.batch.page.value % 16 == 0) paged_chunk_kernel<T, D, true><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
+      else paged_chunk_kernel<T, D, false><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
       profile_mark_end(a.stream);
       if (a.partials) paged_chunk_join_kernel<T, D><<<dim3((unsigned)a.groups, kChunkRows / kJoinRows), block, 0, a.stream>>>(a);
     }
     return hip_status(hipGetLastError());
   }
-  if constexpr (!(sizeof(T) == 4 && D == 256))      // (the registers do not hold two groups of such rows)
+  if constexpr (!(sizeof(T) == 4 && D > 64))        // (the registers do not hold two groups of such rows)
     if (a.tile_rows != kRows) return launch_paged_rows<T, D, 2>(a);
   return launch_paged_rows<T, D, 1>(a);
 }
@@ -1422,9 +1453,9 @@ sga_status launch_paged_type(const PagedAttention& a) {
 PagedPlan plan_paged(const PagedAttention& a) {
   PagedPlan p{kRows, 0, 0, 1, 0};
   const int64_t all_rows = (int64_t)a.batch.n_tokens * a.group.value;
-  if (a.dtype != SGA_F32 && a.d >= 64 && a.batch.page.value % 16 == 0 && all_rows > (int64_t)kTokenRows * a.batch.n_seqs)
+  if (a.dtype != SGA_F32 && a.d >= 64 && all_rows > (int64_t)kTokenRows * a.batch.n_seqs)
     p.tile_rows = kChunkRows;
-  else if (all_rows > (int64_t)kRows * a.batch.n_seqs && !(a.dtype == SGA_F32 && a.d == 256))
+  else if (all_rows > (int64_t)kRows * a.batch.n_seqs && !(a.dtype == SGA_F32 && a.d > 64))
     p.tile_rows = 2 * kRows;
   const int64_t tiles = all_rows / p.tile_rows + a.batch.n_seqs;
   if (tiles >= int64_t(1) << 24) return p;                 // (rows of a sequence are counted in 31 bits)

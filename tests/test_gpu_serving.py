@@ -205,8 +205,8 @@ def test_append_passes_over_missing_pages():
 
 # ---- attention ------------------------------------------------------------------------------------
 def long_chunks(dtype, T, n_seqs, group, d, page):
-    """Calls whose sequences bring more than 64 rows on average take tiles of 128 rows."""
-    return dtype != "f32" and d >= 64 and page % 16 == 0 and T * group > 64 * n_seqs
+    """Calls whose sequences bring more than 32 rows on average take tiles of 128 rows."""
+    return dtype != "f32" and d >= 64 and T * group > 32 * n_seqs
 
 
 def check_attention(dtype, new, length, page, Hq, Hkv, d, spec, causal=True, padding=0, memory="token", missing=(), scale=None,
@@ -349,6 +349,16 @@ def test_attention_long_chunks(dtype, d, causal):
     check_attention(dtype, [130], [1000], 32, 2, 2, d, full(1000), causal=causal, missing=[(0, 3, -1), (0, 17, 10 ** 6), (0, 31, -9)])
     check_attention(dtype, [200], [150], 16, 2, 1, d, full(160), causal=causal)      # the first 50 lie before position 0
     check_attention(dtype, [100], [100], 16, 5, 5, d, MaskSpec(KIND_SLIDING, 80, window=0), causal=causal, workspace=False)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16"), (256, "f16")])
+@pytest.mark.parametrize("page", [1, 5, 24, 100])
+def test_attention_long_chunks_pages_of_any_size(d, dtype, page):
+    check_attention(dtype, [129, 1, 300], [129, 40, 700], page, 2, 2, d, full(704), padding=5)
+    check_attention(dtype, [60], [2500], page, 2, 1, d, full(2500), causal=False)          # more blocks than are asked for at once
+    check_attention(dtype, [70, 0, 65], [3000, 7, 65], page, 4, 1, d, MaskSpec(KIND_GLOBAL_LOCAL, 3008, window=1200, n_global=70))
+    last = (1000 - 1) // page
+    check_attention(dtype, [130], [1000], page, 2, 2, d, full(1000), missing=[(0, 3, -1), (0, last // 2, 10 ** 6), (0, last, -9)])
 
 
 @pytest.mark.parametrize("dtype", ["f16", "bf16"])
