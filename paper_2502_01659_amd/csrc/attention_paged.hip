@@ -258,22 +258,41 @@ struct Share {
 
   // Share i of the call.  False: there is nothing in it.
   __device__ __forceinline__ bool begin(const PagedAttention& a, uint32_t i) {
-    uint64_t total = 0;
-    for (int32_t c = 0; c < a.batch.n_seqs; c += kWave) {
-      load(a, c, total);
-      total = behind;
+    // once over the sequences for the line's length, and if they are not all at hand then, again up to the place
+    const int32_t n = a.batch.n_seqs;
+    uint64_t base = 0;
+    bool counted = false;
+    for (int32_t c = 0;;) {
+      load(a, c, base);
+      base = behind;
+      c += kWave;
+      if (!counted) {
+        if (c < n) continue;
+        const uint64_t total = base;
+        uint64_t each = total;
+        if (a.groups > 1) {
+          each = quotient64(total + a.groups - 1, a.groups);
+          each = each > kLeastShare ? each : kLeastShare;
+        }
+        size = each;
+        at = each * i;
+        end = at + each < total ? at + each : total;
+        if (at >= total) return false;
+        if (n <= kWave) break;
+        counted = true;
+        base = 0;
+        c = 0;
+      } else if (base > at || c >= n) {
+        break;
+      }
     }
-    uint64_t each = quotient64(total + a.groups - 1, a.groups);
-    each = each > kLeastShare ? each : kLeastShare;
-    size = each;
-    at = each * i;
-    end = at + each < total ? at + each : total;
-    if (at >= total) return false;
-    if (a.batch.n_seqs > kWave) {
-      load(a, 0, 0);
-      while (behind <= at && chunk + kWave < a.batch.n_seqs) load(a, chunk + kWave, behind);
+    if (i > 0) {
+      locate(a, step_of<kTileRows>(a));
+    } else {
+      take_sequence();
+      head = tile = offset = 0;
+      extent = work[lane].length_of(0, step_of<kTileRows>(a));
     }
-    locate(a, step_of<kTileRows>(a));
     return true;
   }
   // The part of the current tile that is in the share, if any.
@@ -938,7 +957,7 @@ struct ChunkBlock {
 };
 
 template <typename T, int D, bool kWholeTiles>
-__global__ __attribute__((amdgpu_waves_per_eu(D > 128 ? 1 : 2, D > 128 ? 1 : 2))) __launch_bounds__(kWaves* kWave) void
+__global__ __attribute__((amdgpu_waves_per_eu(D > 128 ? 1 : D > 64 ? 2 : 3, D > 128 ? 1 : D > 64 ? 2 : 3))) __launch_bounds__(kWaves* kWave) void
 paged_chunk_kernel(PagedAttention a) {
   using B = ChunkBlock<D>;
   using Piece = vec_t<T, 8>;

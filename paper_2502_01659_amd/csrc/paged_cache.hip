@@ -11,7 +11,9 @@ namespace sga {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kMaxTokens = 8;      // tokens of a workgroup
+// tokens of a workgroup at most (us, 8 / 4 / 2: queries of 65,536 tokens, 32 heads of 128, bf16 204 / 193 / 187; prompts of 33,000
+// tokens into pages, 32 + 8 + 8 heads, fp16 192 / 187 / 189; 100,003 tokens, 8 heads of 64, fp32 76 / 73 / 76)
+constexpr int kMaxTokens = 4;
 constexpr int kMaxGroups = 1 << 20;  // workgroups along the tokens (a grid holds fewer than 2^32 threads); they stride
 
 // cos t and sin t for t = position * f.  The product is held as a rounded part and its error, and multiples of pi / 2
