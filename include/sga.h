@@ -430,7 +430,8 @@ typedef struct {
  * Writes the keys and values of new tokens into their pages, the keys rotated by their
  * positions (rotary NULL: as they are), and in the same pass rotates the queries beside them.
  *   K, V       read, [Hkv][n_tokens][d]
- *   cache_k, cache_v   device, written at the new tokens' places only
+ *   cache_k, cache_v   device, written at the new tokens' places only; two caches, whose pages may take turns in one
+ *              buffer (page_stride)
  *   Q, Q_out   both NULL, or read and written, [Hq][n_tokens][d] (Q_out may be Q); Q_out is
  *              written for every token of a sequence, also where its page is missing.
  *              A call with Q needs rotary.
@@ -456,6 +457,7 @@ sga_status sga_cache_append(const sga_rows* K, const sga_rows* V, void* cache_k,
  *   workspace  device, 256-byte aligned, optional: partial states of split sequences.  With one of
  *              sga_paged_workspace_bytes a few long sequences spread over the chip; without one, or
  *              with a smaller one, each group of queries and key head is one workgroup's work.
+ *              Its contents need not be preserved; calls that overlap in time need one each.
  * A token that sees nothing gets O = 0, lse = -inf.  Tokens that a query does not see have no
  * influence on it, whatever their keys and values hold (infinities, NaN, memory never written).
  * Supported: d = 32, 64, 128, 256.  Addresses and strides are multiples of 16 bytes.  Results do not

@@ -583,13 +583,11 @@ def _strides(t, name, written=False):
     return _Rows(t.data_ptr(), sh, st)
 
 
-def _check_tokens(t, name, like=None, T=None):
+def _check_tokens(t, name, T=None):
     if t.dim() != 3 or not t.is_cuda:
         raise ValueError(f"{name} must be a [H, T, d] device tensor")
     if T is not None and t.shape[1] != T:
         raise ValueError(f"{name} must have the batch's {T} tokens")
-    if like is not None and (t.dtype != like.dtype or t.get_device() != like.get_device() or t.shape[2] != like.shape[2]):
-        raise ValueError(f"{name} must share dtype, device and head dimension")
 
 
 def rotary_frequencies(channels, base=10000.0, scaling=None, factor=1.0, original_length=0, slow_turns=1.0, fast_turns=32.0,
@@ -738,10 +736,10 @@ def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None)
     """Write the batch's new keys (rotated) and values, [Hkv, n_tokens, d], into their pages, and rotate the queries Q
     beside them.  Returns Q_out (which may be Q) if Q is given."""
     _check_tokens(K, "K", T=batch.n_tokens)
-    _check_tokens(V, "V", like=K, T=batch.n_tokens)
     struct, Hkv = batch._caches(K, cache_k, cache_v)
-    if K.shape[0] != Hkv or V.shape[0] != Hkv:
-        raise ValueError("K and V must have the caches' heads")
+    index, shape, dtype = batch.device_index, K.shape, K.dtype
+    if shape[0] != Hkv or V.shape != shape or V.dtype != dtype or V.get_device() != index:
+        raise ValueError("K and V must be alike and have the caches' heads")
     q = q_out = None
     Hq = 0
     if rotary is not None:
@@ -749,20 +747,19 @@ def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None)
     if Q is not None:
         if rotary is None:
             raise ValueError("queries are rotated: a call with Q needs rotary")
-        _check_tokens(Q, "Q", like=K, T=batch.n_tokens)
+        if Q.dim() != 3 or Q.shape[1:] != shape[1:] or Q.dtype != dtype or Q.get_device() != index:
+            raise ValueError("Q must be [Hq, n_tokens, d] and share dtype and device with K")
         if Q_out is None:
             import torch
             Q_out = torch.empty_like(Q)
-        else:
-            _check_tokens(Q_out, "Q_out", like=Q, T=batch.n_tokens)
-            if Q_out.shape != Q.shape:
-                raise ValueError("Q_out must match Q")
+        elif Q_out.shape != Q.shape or Q_out.dtype != dtype or Q_out.get_device() != index:
+            raise ValueError("Q_out must match Q")
         q, q_out, Hq = _strides(Q, "Q"), _strides(Q_out, "Q_out", written=True), Q.shape[0]
     elif Q_out is not None:
         raise ValueError("Q_out without Q")
-    st = _enqueue(batch.device_index, sga_cache_append, _strides(K, "K"), _strides(V, "V"), cache_k.data_ptr(),
-                  cache_v.data_ptr(), struct, Hkv, K.shape[2], rotary._desc if rotary is not None else None, q, q_out, Hq,
-                  _serving_code(K.dtype))
+    st = _enqueue(index, sga_cache_append, _strides(K, "K"), _strides(V, "V"), cache_k.data_ptr(),
+                  cache_v.data_ptr(), struct, Hkv, shape[2], rotary._desc if rotary is not None else None, q, q_out, Hq,
+                  _serving_code(dtype))
     if st != 0:
         raise SgaError(st, "sga_cache_append")
     return Q_out

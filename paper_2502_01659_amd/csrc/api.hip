@@ -552,7 +552,7 @@ sga_status sga_cache_append(const sga_rows* K, const sga_rows* V, void* cache_k,
   if ((rotary && !valid_rotary(rotary, d)) || !valid_batch(batch, Hkv, d)) return SGA_ERR_INVALID_ARG;
   if ((Q != nullptr) != (Q_out != nullptr) || (Q && (!rotary || Hq < 1 || Hq > 65535))) return SGA_ERR_INVALID_ARG;
   if (batch->n_tokens == 0 || batch->n_seqs == 0) return SGA_OK;
-  if (!valid_rows(K, dtype) || !valid_rows(V, dtype) || !cache_k || !cache_v) return SGA_ERR_INVALID_ARG;
+  if (!valid_rows(K, dtype) || !valid_rows(V, dtype) || !cache_k || !cache_v || cache_k == cache_v) return SGA_ERR_INVALID_ARG;
   if (!aligned_to(cache_k, element_bytes(dtype)) || !aligned_to(cache_v, element_bytes(dtype))) return SGA_ERR_INVALID_ARG;
   if (Q && (!valid_rows(Q, dtype) || !valid_rows(Q_out, dtype) || !apart_or_same(*Q, *Q_out))) return SGA_ERR_INVALID_ARG;
   (void)hipGetLastError();

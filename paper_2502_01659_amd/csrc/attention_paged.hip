@@ -158,7 +158,7 @@ __device__ __forceinline__ SequenceWork work_of(const PagedAttention& a, int32_t
   if (s >= b.n_seqs) return w;
   w.begin = row_of_sequence(b, s);
   const int32_t end = row_of_sequence(b, s + 1);
-  w.length = b.seq_len[s];
+  w.length = max(b.seq_len[s], 0);
   w.n_new = end > w.begin ? end - w.begin : 0;
   w.tiles = (uint32_t)(((int64_t)w.n_new * a.group.value + kTileRows - 1) / kTileRows);
   const int64_t kept = kept_of(a, w.length), old = (int64_t)w.length - w.n_new, step = kTileRows / a.group.value;

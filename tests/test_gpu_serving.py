@@ -392,6 +392,113 @@ def test_attention_far_pages():
     assert within(sga.attention_paged(Q, ck, cv, batch, spec, 0.1), want, bar)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("seed", range(3))
+def test_attention_of_many_sequences(dtype, seed):
+    """More sequences than a wavefront looks at at a time, some without new tokens, tiles that are cut and tiles that are not."""
+    rng = np.random.default_rng(seed)
+    n = [150, 70, 200][seed]
+    new = rng.integers(0, 3, n).tolist()
+    length = [int(a + b) for a, b in zip(new, np.where(rng.random(n) < 0.03, 1500, rng.integers(0, 60, n)))]
+    new[0] = new[-1] = 0
+    check_attention(dtype, new, length, 16, 4, 2, 64, full(1600), seed=seed)
+    check_attention(dtype, new, length, 7, 6, 2, 64, MaskSpec(KIND_GLOBAL_LOCAL, 1600, window=25, n_global=2), seed=seed, workspace=False)
+    new = [x * 17 for x in new]
+    length = [a + b for a, b in zip(new, length)]
+    check_attention(dtype, new, length, 16, 4, 2, 64, full(1600), seed=seed, padding=3)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_attention_drawn(seed):
+    """Drawn sizes over the whole range of what a call may be."""
+    rng = np.random.default_rng(1000 + seed)
+    dtype, d = rng.choice(["f32", "f16", "bf16"]), int(rng.choice([32, 64, 128, 256]))
+    Hkv, G, S = int(rng.integers(1, 4)), int(rng.choice([1, 1, 2, 3, 5, 8, 17])), int(rng.integers(1, 9))
+    page = int(rng.choice([1, 3, 16, 17, 32, 48, 64, 200]))
+    most = int(rng.choice([1, 4, 40, 150]))
+    new = rng.integers(0, most + 1, S).tolist()
+    length = [int(a + b) for a, b in zip(new, rng.integers(0, int(rng.choice([1, 50, 900])), S))]
+    if rng.random() < 0.2:
+        length[0] = max(0, new[0] - 3)                       # tokens before position 0
+    L = max(1, max(length) - int(rng.choice([0, 0, 5])))
+    w = int(rng.choice([0, 5, 40, 300, 10 ** 6]))
+    spec = MaskSpec(KIND_SLIDING, L, window=w) if rng.random() < 0.5 else MaskSpec(KIND_GLOBAL_LOCAL, L, window=w, n_global=min(L, int(rng.choice([0, 1, 33, 70]))))
+    missing = [(int(rng.integers(S)), int(rng.integers(max(1, -(-max(length) // page)))), int(rng.choice([-1, 1 << 30, -(1 << 31)])))
+               for _ in range(int(rng.choice([0, 0, 3])))]
+    check_attention(dtype, new, length, page, Hkv * G, Hkv, d, spec, causal=bool(rng.random() < 0.7), padding=int(rng.integers(3)),
+                    memory=str(rng.choice(["head", "token", "slice"])), missing=missing, workspace=bool(rng.random() < 0.7),
+                    seed=seed, scale=float(rng.choice([0.1, 1 / math.sqrt(d), -0.2])))
+
+
+def test_attention_results_do_not_change():
+    """The same call twice, and after another call has used the workspace, gives the same bits."""
+    for new, length in (([1] * 5, [3000, 20, 700, 1, 1500]), ([100, 30, 1], [900, 500, 2000])):
+        batch, table, ptr, lens, n_pages, T = batch_of(new, length, 16)
+        ck, cv = caches(n_pages, 2, 16, 128, "bf16", 3)
+        Q, spec = tokens(8, T, 128, "bf16", 4), full(3000)
+        ws = sga.alloc_paged_workspace(batch, spec, 8, 2, 128, "bf16")
+        a = sga.attention_paged(Q, ck, cv, batch, spec, 0.09, workspace=ws, want_lse=True)
+        sga.attention_paged(Q * 2, ck, cv, batch, MaskSpec(KIND_SLIDING, 3000, window=100), 0.2, causal=False, workspace=ws)
+        ws.fill_(255)
+        b = sga.attention_paged(Q, ck, cv, batch, spec, 0.09, workspace=ws, want_lse=True)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_two_captured_graphs_share_a_workspace():
+    batch, table, ptr, lens, n_pages, T = batch_of([1, 40, 1], [2500, 700, 64], 16)
+    ck, cv = caches(n_pages, 2, 16, 64, "f16", 3)
+    Q, spec = tokens(4, T, 64, "f16", 4), full(2500)
+    ws = sga.alloc_paged_workspace(batch, spec, 4, 2, 64, "f16")
+    want = [sga.attention_paged(Q * k, ck, cv, batch, spec, 0.125) for k in (1, 2)]
+    X, out, graphs = [Q * 1, Q * 2], [torch.zeros_like(Q) for _ in range(2)], []
+    torch.cuda.synchronize()
+    for k in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            sga.attention_paged(X[k], ck, cv, batch, spec, 0.125, O=out[k], workspace=ws)
+        graphs.append(g)
+    eager = [sga.attention_paged(X[k], ck, cv, batch, spec, 0.125, workspace=ws) for k in range(2)]
+    for _ in range(3):
+        for k in (0, 1, 1, 0):
+            out[k].zero_()
+            graphs[k].replay()
+            assert torch.equal(out[k], eager[k])
+            # without a workspace no tile is cut: the same sums in another order
+            assert ((out[k].float() - want[k].float()).abs() <= 2e-3 * (1 + want[k].float().abs())).all()
+            sga.attention_paged(X[1 - k], ck, cv, batch, spec, 0.125, workspace=ws)
+
+
+def test_refusals_of_device_tensors():
+    batch, table, ptr, lens, n_pages, T = batch_of([2, 3], [20, 30], 16)
+    ck, cv = caches(n_pages, 2, 16, 64, "f16", 3)
+    Q, K = tokens(4, T, 64, "f16", 4), tokens(2, T, 64, "f16", 5)
+    rot = sga.Rotary(sga.rotary_frequencies(64)[0])
+    spec = full(32)
+    for bad in (lambda: sga.attention_paged(Q[:, :4], ck, cv, batch, spec, 0.1), lambda: sga.attention_paged(Q.float(), ck, cv, batch, spec, 0.1),
+                lambda: sga.attention_paged(Q, ck[:, :, :8], cv, batch, spec, 0.1), lambda: sga.attention_paged(Q, ck.transpose(1, 2), cv, batch, spec, 0.1),
+                lambda: sga.attention_paged(Q, ck[:-1], cv[:-1], batch, spec, 0.1), lambda: sga.attention_paged(Q, ck, cv, batch, spec, 0.1, O=K),
+                lambda: sga.attention_paged(Q, ck, cv, batch, spec, 0.1, lse=torch.empty(4, T, device="cuda", dtype=torch.float64)),
+                lambda: sga.attention_paged(Q, ck, cv, batch, spec, 0.1, O=torch.empty(4, 1, 64, dtype=torch.float16, device="cuda").expand(4, T, 64)),
+                lambda: sga.attention_paged(Q, ck, cv.float(), batch, spec, 0.1), lambda: sga.attention_paged(Q.cpu(), ck, cv, batch, spec, 0.1),
+                lambda: sga.attention_paged(Q, ck, cv, batch, spec, 0.1, workspace=torch.empty(1000)),
+                lambda: sga.cache_append(K[:1], K, ck, cv, batch), lambda: sga.cache_append(K, K, ck, cv, batch, Q=Q),
+                lambda: sga.cache_append(K, K, ck, cv, batch, rotary=rot, Q_out=Q), lambda: sga.cache_append(K, Q, ck, cv, batch),
+                lambda: sga.rotary(Q, rot, positions=torch.arange(T, device="cuda", dtype=torch.int32)),
+                lambda: sga.rotary(Q, rot, positions=torch.arange(T + 1, device="cuda")), lambda: sga.rotary(Q, rot, out=Q[:, :-1]),
+                lambda: sga.rotary(Q[..., ::2], rot), lambda: sga.Rotary(sga.rotary_frequencies(64)[0].float()),
+                lambda: sga.Rotary(sga.rotary_frequencies(64)[0], layout="other")):
+        with pytest.raises((ValueError, TypeError)):
+            bad()
+    with pytest.raises(sga.SgaError):                        # more channels than the head has
+        sga.rotary(Q[..., :32], rot)
+    with pytest.raises(sga.SgaError):                        # an address off 16 bytes
+        sga.attention_paged(torch.empty(4 * T * 64 + 1, dtype=torch.float16, device="cuda")[1:].view(4, T, 64), ck, cv, batch, spec, 0.1)
+    with pytest.raises(TypeError):
+        sga.rotary(Q.double(), rot)
+    with pytest.raises(sga.SgaError):                        # the other calls know nothing of bf16
+        sga.attention_forward_implicit(*(torch.zeros(1, 8, 48, device="cuda"),) * 3, MaskSpec(KIND_SLIDING, 8, window=1), 0.1)
+
+
 def test_attention_without_tokens():
     batch, *_ = batch_of([0, 0], [5, 9], 16)
     ck, cv = caches(batch.n_pages, 2, 16, 64, "f16", 1)

@@ -47,11 +47,12 @@ def test_rotary_argument_errors():
 
 
 def test_append_argument_errors():
-    def call(K=rows(), V=rows(), ck=OK, cv=OK, b=batch(), Hkv=2, d=64, r=desc(), Q=None, Q_out=None, Hq=0, dtype=1):
+    def call(K=rows(), V=rows(), ck=OK, cv=0x4000, b=batch(), Hkv=2, d=64, r=desc(), Q=None, Q_out=None, Hq=0, dtype=1):
         return sga.sga_cache_append(K, V, ck, cv, b, Hkv, d, r, Q, Q_out, Hq, dtype, None)
     assert call(b=batch(n_tokens=0)) == 0 and call(b=batch(n_seqs=0)) == 0
     assert call(b=batch(n_tokens=0, page_table=None, seq_ptr=None, seq_len=None), K=rows(None), V=rows(None)) == 0
     assert call(K=None) == -1 and call(V=rows(None)) == -1 and call(ck=None) == -1 and call(cv=OK + 1) == -1
+    assert call(cv=OK) == -1                                  # keys and values in one place
     assert call(b=None) == -1 and call(Hkv=0) == -1 and call(d=1) == -1 and call(dtype=5) == -1
     for bad in (dict(struct_bytes=0), dict(n_seqs=-1), dict(n_tokens=-1), dict(n_tokens=1 << 31), dict(n_pages=0),
                 dict(n_pages=1 << 31), dict(page_size=0), dict(page_size=65537), dict(pages_per_seq=0),
