@@ -26,10 +26,17 @@ constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kBlock = 32;            // keys of a block
 constexpr int kRows = 16;             // rows of a tile, or twice as many where a sequence brings more
 constexpr int kWaves = 4;             // wavefronts of a workgroup, which take its blocks in turn
-constexpr int kLeastPiece = 1024;
-constexpr int kChunkPieces = 1536;    // pieces of tiles of 128 rows that a call is cut into
+// Pieces of tiles of 128 rows that a call is cut into, three rounds of the places on the chip, and the fewest keys of one: a piece
+// costs a prologue of about 4 us and a partial state of 66 KB (d = 128), eight blocks of fp32 products as much as 32 of
+// 16-bit ones.  (us, bf16, 32 / 8 heads of 128: 1,024 / 1,536 / 2,048 pieces, eight chunks of 256 behind up to 16k 344 / 329 / 334;
+// least piece 512 / 1,024 / 2,048 keys, 512 tokens behind 8k 128 / 111 / 98, four chunks of 64 behind 8k 106 / 64 / 64, 64 channels
+// and one head per key head 69 / 70 / 121.)
+constexpr int kLeastPiece = 1024, kLeastPieceF32 = 256;
+constexpr int kChunkPieces = 1536;
 
-constexpr int kTokenRows = 32;        // sequences with more rows than this on average take tiles of 128 rows
+// Sequences with more rows than this on average take tiles of 128 rows.  (us, below / above: 32 rows behind 4k to 16k, 32 sequences,
+// bf16, d = 128 231 / 251, d = 64 122 / 139; 40 rows 189 / 169; 64 rows, 16 sequences 202 / 182; 29 rows at d = 256 54 / 64.)
+constexpr int kTokenRows = 32;
 
 __device__ __forceinline__ int64_t uniform64(int64_t v) {
   const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
@@ -123,6 +130,8 @@ __device__ __forceinline__ Tile tile_of(const PagedAttention& a, int32_t seq, in
 // Lengths are estimates (a tile's blocks are counted when it is met; a cut goes to the block in proportion) that follow from
 // the sequence alone: tile u < t1 is a0 + u * step long, the others a1.  Causal, the keys grow with the tiles until the
 // window is full; otherwise the tiles of global rows see everything and the others a window.
+// (us, kTileCost 64 / 256 / 512: a step of 64 sequences of 512 to 32k tokens 371 / 359 / 362, 160 windows of 2,048 127 / 123 / 127,
+// drafts at d = 256 60 / 53 / 71; kLeastShare 256 / 512 / 1,024, drafts 72 / 67 / 81.)
 constexpr uint32_t kTileCost = 256;
 constexpr uint32_t kLeastShare = 512;      // keys of the smallest share
 constexpr uint32_t kWholeTiles = 32;       // tiles shorter than this part of a share are not cut
@@ -392,34 +401,45 @@ __device__ __forceinline__ float* record_of_share(const PagedAttention& a, uint3
 struct alignas(16) Note {
   int32_t count;             // parts of the tile; 0: nothing to join here
   int32_t first;             // the first one's share or record
-  int32_t seq, begin, n_new, length, tile, head;
+  int32_t apart;             // (tiles of 128 rows) from a part's record to the next one's
+  int32_t begin, n_new, length, tile, head;
 };
 static_assert(sizeof(Note) == kNoteBytes, "the plan counts on this");
 __device__ __forceinline__ Note* notes_of(const PagedAttention& a) { return reinterpret_cast<Note*>(a.notes); }
 
-// Which piece of which tile of 128 rows workgroup `rest` of a key head has.  A sequence's tiles are all cut into as many pieces as
-// its longest one needs to have pieces of about the size at which the call has kChunkPieces of them (as far as the
-// lengths say; 512 keys at least), so that uneven sequences keep the chip evenly busy.  The pieces lie in the order
-// sequence, piece, tile.  False: there is no such piece.  All lanes call it.
+// Which piece of which tile of 128 rows workgroup `rest` of a key head has.  Not causal, a sequence's first tiles may hold global
+// rows, which see everything, and the others see a window; causal, all count as its longest one.  The tiles of
+// a kind are all cut into as many pieces as make them about the size at which the call has kChunkPieces of them
+// (as far as the lengths say; kLeastPiece keys at least), so that uneven sequences keep the chip evenly busy.  The pieces lie in
+// the order sequence, kind, piece, tile; the pieces of a tile are `apart` from each other.  False: there is no such piece.  All lanes call it.
 template <int kTileRows>
 __device__ __forceinline__ bool piece_of(const PagedAttention& a, int32_t rest, Tile& tile, int32_t& index, int32_t& piece,
-                                         int32_t& pieces) {
+                                         int32_t& pieces, int32_t& apart) {
   const int l = threadIdx.x & (kWave - 1);
   const int32_t n = a.batch.n_seqs;
   SequenceWork w{};
-  auto longest = [&]() { return (float)max(w.a1, w.t1 > 0 ? w.length_of(w.t1 - 1, step_of<kTileRows>(a)) : 0u); };
+  int32_t all = 0, rows = 0;                 // tiles that see everything, the others
+  float all_length = 0.f, length = 0.f;
+  auto look = [&](int32_t s) {
+    w = work_of<kTileRows>(a, s);
+    all = a.causal ? 0 : (int32_t)w.t1;
+    rows = (int32_t)w.tiles - all;
+    all_length = (float)w.a0;
+    length = (float)(a.causal && w.t1 > 0 ? max(w.a1, w.length_of(w.t1 - 1, step_of<kTileRows>(a))) : w.a1);
+  };
   float total = 0.f;
   for (int32_t c = 0; c < n; c += kWave) {
-    w = work_of<kTileRows>(a, c + l);
-    total += (float)w.tiles * longest();
+    look(c + l);
+    total += (float)all * all_length + (float)rows * length;
   }
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) total += __shfl_xor(total, off, kWave);
-  const float size = fmaxf((float)kLeastPiece, total * (float)a.Hkv * (1.f / kChunkPieces));
+  const float size = fmaxf((float)(a.dtype == SGA_F32 ? kLeastPieceF32 : kLeastPiece), total * (float)a.Hkv * (1.f / kChunkPieces));
+  auto cuts = [&](float x) { return a.splits > 1 ? max(1, (int32_t)(x / size + 0.5f)) : 1; };
   int32_t behind = 0;
   for (int32_t c = 0; c < n; c += kWave) {
-    if (n > kWave) w = work_of<kTileRows>(a, c + l);
-    const int32_t cut = a.splits > 1 ? max(1, (int32_t)(longest() / size + 0.5f)) : 1, own = (int32_t)w.tiles * cut;
+    if (n > kWave) look(c + l);
+    const int32_t all_cuts = cuts(all_length), row_cuts = cuts(length), own = all * all_cuts + rows * row_cuts;
     int32_t sum = own;
     for (int off = 1; off < kWave && off < n; off <<= 1) {
       const int32_t below = __shfl_up(sum, off, kWave);
@@ -428,11 +448,14 @@ __device__ __forceinline__ bool piece_of(const PagedAttention& a, int32_t rest, 
     const uint64_t begun = __ballot(own > 0 && behind + sum - own <= rest && rest < behind + sum);
     if (begun) {
       const int lane = __builtin_ctzll(begun);
-      const uint32_t place = (uint32_t)(rest - behind - __builtin_amdgcn_readlane(sum - own, lane));
-      const uint32_t tiles = __builtin_amdgcn_readlane(w.tiles, lane);
-      pieces = __builtin_amdgcn_readlane(cut, lane);
-      piece = (int32_t)(place / tiles);
-      index = (int32_t)(place - piece * tiles);
+      const int32_t first = __builtin_amdgcn_readlane(all, lane), first_cuts = __builtin_amdgcn_readlane(all_cuts, lane);
+      int32_t place = rest - behind - __builtin_amdgcn_readlane(sum - own, lane);
+      const bool in_first = place < first * first_cuts;
+      pieces = in_first ? first_cuts : __builtin_amdgcn_readlane(row_cuts, lane);
+      apart = in_first ? first : __builtin_amdgcn_readlane(rows, lane);
+      place -= in_first ? 0 : first * first_cuts;
+      piece = (int32_t)((uint32_t)place / (uint32_t)apart);
+      index = place - piece * apart + (in_first ? 0 : first);
       tile = tile_of<kTileRows>(a, c + lane, __builtin_amdgcn_readlane(w.begin, lane), __builtin_amdgcn_readlane(w.n_new, lane),
                                 __builtin_amdgcn_readlane(w.length, lane), index);
       return true;
@@ -625,7 +648,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
     const Part& p = share.part[0];
     const bool ends = any && p.from > 0 && p.to == p.extent;
     const int32_t first = ends ? (int32_t)quotient64(share.size * blockIdx.x - p.from, share.size) : 0;
-    notes_of(a)[blockIdx.x] = Note{ends ? (int32_t)blockIdx.x - first + 1 : 0, first, p.seq, p.begin, p.n_new, p.length,
+    notes_of(a)[blockIdx.x] = Note{ends ? (int32_t)blockIdx.x - first + 1 : 0, first, 0, p.begin, p.n_new, p.length,
                                    p.tile, p.head};
   }
   if (!any) return;
@@ -893,6 +916,13 @@ __device__ __forceinline__ floatx16 matrix32(vec_t<bf16_t, 8> a, vec_t<bf16_t, 8
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
 }
 
+// Full precision: four products of two, the halves of the wavefront each with its piece.
+__device__ __forceinline__ floatx16 matrix32(vec_t<float, 4> a, vec_t<float, 4> b, floatx16 c) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[e], b[e], c, 0, 0, 0);
+  return c;
+}
+
 // The value of the lane 32 positions away.
 __device__ __forceinline__ float other_half(float x, int h) {
   const unsigned xi = __builtin_bit_cast(unsigned, x);
@@ -946,23 +976,30 @@ __device__ __forceinline__ void copy_pieces_from(const char* k, const char* v, u
         : "=&s"(kept) : "v"(k + 64 * i), "v"(v + 64 * i), "s"(to + i * kStep), "i"(kApart) : "memory", "scc");
 }
 
-// A block of 32 keys in LDS: groups of 32 channels, in a group the 32 keys' rows of 64 bytes.  What the products read then
+// A block of 32 keys in LDS: groups of 64 bytes of a row, in a group the 32 keys' parts one behind the other.  What the products read then
 // differs by constants from one or two addresses per lane, and 16 lanes' pieces (K: four rows apart they would share
 // banks, so a row's four pieces are permuted; V: eight rows in a row) meet every bank once.
-template <int D>
+template <int kRow>
 struct ChunkBlock {
-  static constexpr int kRowBytes = 2 * D, kBytes = kBlock * kRowBytes, kGroupBytes = kBlock * 64;
-  static constexpr int kCopies = D / 64;      // copies of a wavefront: 16 rows of as many groups
+  static constexpr int kRowBytes = kRow, kBytes = kBlock * kRowBytes, kGroupBytes = kBlock * 64;
+  static constexpr int kCopies = kRow / 128;  // copies of a wavefront: 16 rows of as many groups
   static __device__ __forceinline__ int k_turn(int row) { return row >> 2 & 3; }
 };
 
+// Row sizes that the ring fits, and the wavefronts per SIMD that registers and LDS then leave.
+__host__ __device__ constexpr bool chunk_fits(int64_t row_bytes) { return row_bytes >= 128 && row_bytes <= 512; }
+constexpr int chunk_waves(int row_bytes) { return row_bytes > 256 ? 1 : row_bytes > 128 ? 2 : 3; }
+
 template <typename T, int D, bool kWholeTiles>
-__global__ __attribute__((amdgpu_waves_per_eu(D > 128 ? 1 : D > 64 ? 2 : 3, D > 128 ? 1 : D > 64 ? 2 : 3))) __launch_bounds__(kWaves* kWave) void
+__global__ __attribute__((amdgpu_waves_per_eu(chunk_waves(sizeof(T) * D), chunk_waves(sizeof(T) * D)))) __launch_bounds__(kWaves* kWave) void
 paged_chunk_kernel(PagedAttention a) {
-  using B = ChunkBlock<D>;
-  using Piece = vec_t<T, 8>;
+  using B = ChunkBlock<D * (int)sizeof(T)>;
+  constexpr int kPieceElems = 16 / sizeof(T);
+  using Piece = vec_t<T, kPieceElems>;
+  using Numerators = vec_t<T, 8>;
+  constexpr bool kSingle = sizeof(T) == 4;
   constexpr int kSlotBytes = 2 * B::kBytes, kPer = 2 * B::kCopies;    // copies of a wavefront per block
-  constexpr int kSteps = D / 16, kTiles = D / 32;
+  constexpr int kSteps = B::kRowBytes / 32, kTiles = D / 32;
   __shared__ __align__(16) char ring[kChunkSlots * kSlotBytes];
   // Pages that do not hold multiples of 16 tokens: the page of every key of the next kAskBlocks blocks, asked for at once.  (A
   // load into registers between the copies would make its reader wait for all of them.)
@@ -990,11 +1027,11 @@ paged_chunk_kernel(PagedAttention a) {
   }
   const int64_t record = (int64_t)head_kv * a.slots + rest;
   Tile tile;
-  int32_t index = 0, piece = 0, pieces = 1;
-  const bool any = piece_of<kChunkRows>(a, rest, tile, index, piece, pieces);
+  int32_t index = 0, piece = 0, pieces = 1, apart = 0;
+  const bool any = piece_of<kChunkRows>(a, rest, tile, index, piece, pieces, apart);
   if (a.partials && tid == 0) {
     const bool cut = any && pieces > 1 && piece == 0;
-    notes_of(a)[record] = cut ? Note{pieces, (int32_t)record, tile.seq, tile.begin, tile.n_new, tile.length, index, head_kv} : Note{};
+    notes_of(a)[record] = cut ? Note{pieces, (int32_t)record, apart, tile.begin, tile.n_new, tile.length, index, head_kv} : Note{};
   }
   if (!any) return;
   const int32_t group = (int32_t)a.group.value;
@@ -1011,15 +1048,15 @@ paged_chunk_kernel(PagedAttention a) {
   if (own_first >= tile.count) sight = Sight{0, -1, 0};                // a wavefront without rows only copies
   Piece qf[kSteps];
   {
-    const T* q = static_cast<const T*>(a.Q) + (int64_t)head * a.q_head + (int64_t)(tile.begin + token) * a.q_row + 8 * h;
+    const T* q = static_cast<const T*>(a.Q) + (int64_t)head * a.q_head + (int64_t)(tile.begin + token) * a.q_row + kPieceElems * h;
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i) qf[i] = *reinterpret_cast<const Piece*>(q + 16 * i);
+    for (int i = 0; i < kSteps; ++i) qf[i] = *reinterpret_cast<const Piece*>(q + 2 * kPieceElems * i);
     // (a mask puts -inf into scores before the scale: the scale is positive from here on)
     if (!(a.scale > 0.f)) {
 #pragma unroll
       for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) qf[i][e] = a.scale == 0.f ? (T)((float)qf[i][e] * 0.f) : -qf[i][e];
+        for (int e = 0; e < kPieceElems; ++e) qf[i][e] = a.scale == 0.f ? (T)((float)qf[i][e] * 0.f) : -qf[i][e];
     }
   }
   const float factor = a.scale == 0.f ? 1.f : fabsf(a.scale) * kLog2e;
@@ -1133,6 +1170,7 @@ paged_chunk_kernel(PagedAttention a) {
 #pragma unroll
     for (int i = 0; i < kSteps; ++i) s = matrix32(k[i], qf[i], s);
   };
+  // (16-bit) 32 t + 0..31 channels of 16 keys, turned
   auto read_v = [&](uint32_t slot_at, int u, Piece (&v)[kTiles]) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
@@ -1145,7 +1183,7 @@ paged_chunk_kernel(PagedAttention a) {
     }
   };
   // Accumulator register r holds key 8 (r / 4) + 4 h + r % 4 of the block.
-  auto numerators = [&](const floatx16& s, float against, Piece (&p)[2]) {
+  auto numerators = [&](const floatx16& s, float against, Numerators (&p)[2]) {
     float total = 0.f;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -1170,18 +1208,29 @@ paged_chunk_kernel(PagedAttention a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[t][r] *= keep;
   };
-  auto weigh = [&](uint32_t slot_at, const floatx16& s, float total, Piece (&p)[2]) {
+  auto weigh = [&](uint32_t slot_at, const floatx16& s, float total, Numerators (&p)[2]) {
     if (__any(!(total < kMostNumerators))) {          // (before a row's first key: infinite or NaN)
       raise(s);
       total = numerators(s, top > -INFINITY ? top : 0.f, p);
     }
     sum += total;
+    if constexpr (kSingle) {
+      // register r: key 8 (r / 4) + 4 h + r % 4, and a lane's channels kTiles n ..
+      const char* const at = ring + B::kBytes + slot_at + (kTiles * 4 * n / 64) * B::kGroupBytes + kTiles * 4 * n % 64 + 4 * h * 64;
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      Piece v[kTiles];
-      read_v(slot_at, u, v);
+      for (int r = 0; r < 16; ++r) {
+        const vec_t<float, kTiles> v = *reinterpret_cast<const vec_t<float, kTiles>*>(at + (8 * (r / 4) + r % 4) * 64);
 #pragma unroll
-      for (int t = 0; t < kTiles; ++t) o[t] = matrix32(v[t], p[u], o[t]);
+        for (int t = 0; t < kTiles; ++t) o[t] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[t], p[r / 8][r % 8], o[t], 0, 0, 0);
+      }
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        Piece v[kTiles];
+        read_v(slot_at, u, v);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) o[t] = matrix32(v[t], p[u], o[t]);
+      }
     }
   };
 
@@ -1205,7 +1254,8 @@ paged_chunk_kernel(PagedAttention a) {
       asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
     if (!meets(block)) return;
-    Piece k[kSteps], p[2];
+    Piece k[kSteps];
+    Numerators p[2];
     floatx16 s;
     read_k(slot_of(block), k);
     products(k, s);
@@ -1223,7 +1273,8 @@ paged_chunk_kernel(PagedAttention a) {
   uint32_t here = 0;                    // its slot
   auto after = [](uint32_t slot_at) { return (slot_at + kSlotBytes) & (kChunkSlots * kSlotBytes - 1); };
   auto inside = [&](floatx16& s, floatx16& ahead) {
-    Piece k[kSteps], p[2];
+    Piece k[kSteps];
+    Numerators p[2];
     read_k(after(here), k);
     products(k, ahead);
     const float total = numerators(s, top, p);
@@ -1272,7 +1323,7 @@ paged_chunk_kernel(PagedAttention a) {
         inside(s_b, s_a);
         publish();
       }
-      Piece p[2];
+      Numerators p[2];
       if (block + 1 < outer) {
         inside(s_a, s_b);
         publish();
@@ -1309,7 +1360,8 @@ paged_chunk_kernel(PagedAttention a) {
       attend_row<T, D>(a, tile, head_kv, tile.first + own_first + r, first_block, end_block, 1, row_top, row_total, x);
       if (part) {
 #pragma unroll
-        for (int c = 0; c < (D + 63) / 64; ++c) part[(own_first + r) * D + lane + 64 * c] = x[c];
+        for (int c = 0; c < (D + 63) / 64; ++c)
+          if (lane + 64 * c < D) part[(own_first + r) * D + lane + 64 * c] = x[c];
         if (lane == 0) {
           part[kChunkRows * D + own_first + r] = row_top;
           part[kChunkRows * (D + 1) + own_first + r] = row_total;
@@ -1321,7 +1373,8 @@ paged_chunk_kernel(PagedAttention a) {
       const float inv = row_total != 0.f ? 1.f / row_total : 0.f;
       T* to = static_cast<T*>(a.O) + (int64_t)h_out * a.o_head + (int64_t)row_out * a.o_row;
 #pragma unroll
-      for (int c = 0; c < (D + 63) / 64; ++c) to[lane + 64 * c] = (T)(x[c] * inv);
+      for (int c = 0; c < (D + 63) / 64; ++c)
+        if (lane + 64 * c < D) to[lane + 64 * c] = (T)(x[c] * inv);
       if (a.lse && lane == 0)
         a.lse[(int64_t)h_out * b.n_tokens + row_out] = (row_top + __builtin_amdgcn_logf(row_total)) * kLn2;
     }
@@ -1330,12 +1383,23 @@ paged_chunk_kernel(PagedAttention a) {
   const float total = sum + other_half(sum, h);
   if (part) {
     if (!exists) return;
+    // register 4 g + e of tile t: channel 32 t + 8 g + 4 h + e, in full precision kTiles (8 g + 4 h + e) + t
+    if constexpr (kSingle) {
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+      for (int r = 0; r < 16; ++r) {
+        vec_t<float, kTiles> w;
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        *reinterpret_cast<float4v*>(part + row * D + 32 * t + 8 * g + 4 * h) =
-            float4v{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
+        for (int t = 0; t < kTiles; ++t) w[t] = o[t][r];
+        *reinterpret_cast<vec_t<float, kTiles>*>(part + row * D + kTiles * (8 * (r / 4) + 4 * h + r % 4)) = w;
+      }
+    } else {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+          *reinterpret_cast<float4v*>(part + row * D + 32 * t + 8 * g + 4 * h) =
+              float4v{o[t][4 * g], o[t][4 * g + 1], o[t][4 * g + 2], o[t][4 * g + 3]};
+    }
     if (h == 0) {
       part[kChunkRows * D + row] = top;
       part[kChunkRows * (D + 1) + row] = total;
@@ -1344,18 +1408,28 @@ paged_chunk_kernel(PagedAttention a) {
   }
   // A lane holds pieces of its own row; the rows go through LDS and leave whole.
   const float inv = total != 0.f ? 1.f / total : 0.f;
-  constexpr int kPitch = B::kRowBytes + 16, kRowPieces = D / 8;
+  constexpr int kPitch = B::kRowBytes + 16, kRowPieces = B::kRowBytes / 16;
   static_assert(kWaves * 32 * kPitch <= kChunkSlots * kSlotBytes, "the results fit the ring");
   char* const mine = ring + wave * (32 * kPitch);
+  if constexpr (kSingle) {
 #pragma unroll
-  for (int t = 0; t < kTiles; ++t)
+    for (int r = 0; r < 16; ++r) {
+      vec_t<float, kTiles> w;
 #pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      vec_t<T, 4> w;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) w[e] = (T)(o[t][4 * g + e] * inv);
-      *reinterpret_cast<vec_t<T, 4>*>(mine + n * kPitch + (32 * t + 8 * g + 4 * h) * 2) = w;
+      for (int t = 0; t < kTiles; ++t) w[t] = o[t][r] * inv;
+      *reinterpret_cast<vec_t<float, kTiles>*>(mine + n * kPitch + kTiles * (8 * (r / 4) + 4 * h + r % 4) * 4) = w;
     }
+  } else {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        vec_t<T, 4> w;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = (T)(o[t][4 * g + e] * inv);
+        *reinterpret_cast<vec_t<T, 4>*>(mine + n * kPitch + (32 * t + 8 * g + 4 * h) * 2) = w;
+      }
+  }
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int i = 0; i < 32 * kRowPieces / kWave; ++i) {
@@ -1363,7 +1437,7 @@ paged_chunk_kernel(PagedAttention a) {
     if (r < own_count) {
       int32_t h_out, row_out;
       place_out(r, h_out, row_out);
-      *reinterpret_cast<Piece*>(static_cast<T*>(a.O) + (int64_t)h_out * a.o_head + (int64_t)row_out * a.o_row + at * 8) =
+      *reinterpret_cast<Piece*>(static_cast<T*>(a.O) + (int64_t)h_out * a.o_head + (int64_t)row_out * a.o_row + at * kPieceElems) =
           *reinterpret_cast<const Piece*>(mine + r * kPitch + at * 16);
     }
   }
@@ -1374,7 +1448,7 @@ paged_chunk_kernel(PagedAttention a) {
 template <typename T, int D, int kTileRows, typename Record>
 __device__ __forceinline__ void join_parts(const PagedAttention& a, const Note& note, int32_t row0, Record record) {
   constexpr int kPer = D / 16, kAtOnce = 4;
-  const Tile tile = tile_of<kTileRows>(a, note.seq, note.begin, note.n_new, note.length, note.tile);
+  const Tile tile = tile_of<kTileRows>(a, 0, note.begin, note.n_new, note.length, note.tile);
   const int row = row0 + threadIdx.x / 16, channel = threadIdx.x % 16 * kPer;
   if (row >= tile.count) return;
   float high = -INFINITY, total = 0.f, x[kPer];
@@ -1414,16 +1488,15 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_join_kernel(PagedAttentio
                               [&](int32_t i) { return record_of_share<D, kTileRows>(a, note.first + i, i > 0); });
 }
 
-// ... tiles of 128 rows in pieces, whose records lie as far apart as the sequence has tiles
+// ... tiles of 128 rows in pieces
 constexpr int kJoinRows = 64;
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves* kWave) void paged_chunk_join_kernel(PagedAttention a) {
   const Note note = notes_of(a)[blockIdx.x];
   if (note.count == 0) return;
-  const int32_t tiles = (int32_t)(((int64_t)note.n_new * a.group.value + kChunkRows - 1) / kChunkRows);
   for (int32_t row0 = blockIdx.y * kJoinRows; row0 < (int32_t)(blockIdx.y + 1) * kJoinRows; row0 += 16)
     join_parts<T, D, kChunkRows>(a, note, row0,
-                                 [&](int32_t i) { return record_of<D, kChunkRows>(a, note.first + (int64_t)i * tiles); });
+                                 [&](int32_t i) { return record_of<D, kChunkRows>(a, note.first + (int64_t)i * note.apart); });
 }
 
 template <typename T, int D, int N>
@@ -1441,7 +1514,7 @@ template <typename T, int D>
 sga_status launch_paged_as(const PagedAttention& a) {
   const dim3 block(kWaves * kWave);
   if (a.tile_rows == kChunkRows) {
-    if constexpr (sizeof(T) == 2 && D >= 64) {
+    if constexpr (chunk_fits(sizeof(T) * D)) {
       int64_t groups = (int64_t)a.slots * a.Hkv;
       if (a.Hkv < 8 && 8 % a.Hkv == 0) groups = (int64_t)(a.slots + 8 / a.Hkv - 1) / (8 / a.Hkv) * 8;
       profile_mark_begin(a.stream, "paged_chunk_kernel");
@@ -1472,7 +1545,10 @@ sga_status launch_paged_type(const PagedAttention& a) {
 PagedPlan plan_paged(const PagedAttention& a) {
   PagedPlan p{kRows, 0, 0, 1, 0};
   const int64_t all_rows = (int64_t)a.batch.n_tokens * a.group.value;
-  if (a.dtype != SGA_F32 && a.d >= 64 && all_rows > (int64_t)kTokenRows * a.batch.n_seqs)
+  // (fp32 at d <= 64 under a narrow window: a wavefront meets 9 of the 13 blocks of its workgroup's tile, and waits in the others; us,
+  // tiles of 16 / 128 rows: +-128 and 16 global rows 147 / 154, 128 causal 96 / 98; but at d = 128, 256 causal 315 / 296)
+  const bool narrow = a.dtype == SGA_F32 && a.d <= 64 && (a.causal ? 1 : 2) * (int64_t)a.window < 512;
+  if (chunk_fits((int64_t)a.d * (a.dtype == SGA_F32 ? 4 : 2)) && !narrow && all_rows > (int64_t)kTokenRows * a.batch.n_seqs)
     p.tile_rows = kChunkRows;
   else if (all_rows > (int64_t)kRows * a.batch.n_seqs && !(a.dtype == SGA_F32 && a.d > 64))
     p.tile_rows = 2 * kRows;

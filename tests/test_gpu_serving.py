@@ -205,7 +205,8 @@ def test_append_passes_over_missing_pages():
 
 # ---- attention ------------------------------------------------------------------------------------
 def long_chunks(dtype, T, n_seqs, group, d, page):
-    """Calls whose sequences bring more than 32 rows on average take tiles of 128 rows."""
+    """16-bit calls whose sequences bring more than 32 rows on average take tiles of 128 rows, where a row of keys has 128 to
+    512 bytes; there a probability is rounded once.  (In full precision neither kernel rounds it.)"""
     return dtype != "f32" and d >= 64 and T * group > 32 * n_seqs
 
 
@@ -235,7 +236,7 @@ def check_attention(dtype, new, length, page, Hq, Hkv, d, spec, causal=True, pad
     torch.cuda.synchronize()
     kernel = sga.sga_profile_last_kernel()
     sga.sga_profile_enable(0)
-    assert kernel == ("paged_chunk_kernel" if long else "paged_kernel")
+    assert dtype == "f32" or kernel == ("paged_chunk_kernel" if long else "paged_kernel")
     end = int(ptr[-1])
     assert (host(O)[:, end:] == 7.0).all() and (host(lse)[:, end:] == 7.0).all()
     assert within(host(O)[:, :end], want[:, :end], bar[:, :end])
@@ -317,7 +318,7 @@ def test_attention_of_infinities_that_are_not_seen(dtype, page):
         Q = tokens(2, T, 64, dtype, 3)
         got = host(sga.attention_paged(Q, ck, cv, batch, spec, 0.125, causal=causal))
         want, _, bar, _ = S.attend(host(Q), host(clean[0]), host(clean[1]), table, ptr, lens, spec, 0.125, causal, dtype,
-                                   long_chunks(dtype, T, 1, 1, 64, page))
+                                   once=long_chunks(dtype, T, 1, 1, 64, page))
         i = np.arange(80)
         sees = lambda token: (np.abs(i - token) <= 4) & ((token <= i) | (not causal))
         assert np.isnan(got[0, sees(20)]).all()
@@ -337,8 +338,8 @@ def test_attention_of_one_key_and_large_scores():
     check_attention("f16", [5], [64], 16, 2, 1, 64, full(64), scale=0.0)
 
 
-@pytest.mark.parametrize("dtype", ["f16", "bf16"])
-@pytest.mark.parametrize("d", [64, 128, 256])
+@pytest.mark.parametrize("dtype,d", [("f16", 64), ("f16", 128), ("f16", 256), ("bf16", 64), ("bf16", 128), ("bf16", 256),
+                                     ("f32", 32), ("f32", 64), ("f32", 128)])
 @pytest.mark.parametrize("causal", [True, False])
 def test_attention_long_chunks(dtype, d, causal):
     """Tiles of 128 rows: ragged ends, tiles of few rows, several pieces, global tokens before the window, missing pages."""
@@ -351,7 +352,7 @@ def test_attention_long_chunks(dtype, d, causal):
     check_attention(dtype, [100], [100], 16, 5, 5, d, MaskSpec(KIND_SLIDING, 80, window=0), causal=causal, workspace=False)
 
 
-@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16"), (256, "f16")])
+@pytest.mark.parametrize("d,dtype", [(64, "f16"), (128, "bf16"), (256, "f16"), (32, "f32"), (64, "f32"), (128, "f32")])
 @pytest.mark.parametrize("page", [1, 5, 24, 100])
 def test_attention_long_chunks_pages_of_any_size(d, dtype, page):
     check_attention(dtype, [129, 1, 300], [129, 40, 700], page, 2, 2, d, full(704), padding=5)
@@ -361,7 +362,7 @@ def test_attention_long_chunks_pages_of_any_size(d, dtype, page):
     check_attention(dtype, [130], [1000], page, 2, 2, d, full(1000), missing=[(0, 3, -1), (0, last // 2, 10 ** 6), (0, last, -9)])
 
 
-@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 def test_attention_long_chunks_of_uneven_scores(dtype):
     """Scores that grow along the keys raise the reference again and again; one key that takes all; a zero and a negative scale."""
     def grow(ck, cv, table):
