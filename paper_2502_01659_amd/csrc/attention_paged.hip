@@ -1,8 +1,10 @@
 // Attention of new tokens over a paged cache (sga_attention_paged).
 //
-// A tile is kRows consecutive rows of one sequence and key head, a row being a new token and one of the query heads
-// that share the key head (row = token * group + head).  Keys are met in blocks of 32 aligned ones: those of the
-// global tokens before the window, then the window's.  Per block, with matrix instructions of 16 x 16 results,
+// Two kernels: paged_kernel for short chunks, which memory bounds, and paged_chunk_kernel (below) for long ones, which the
+// matrix cores bound.  In the first a tile is 16 or 32 consecutive rows of one sequence and key head, a row being a new
+// token and one of the query heads that share the key head (row = token * group + head).  Keys are met in blocks of 32
+// aligned ones: those of the global tokens before the window, then the window's.  Per block, with matrix instructions of
+// 16 x 16 results,
 //     S^T[key][row] = K Q^T          O^T[channel][row] += V^T P^T
 // so that a lane holds one row (lane % 16) in both, its running maximum and sum stay with it, and the
 // probabilities leave the first product in the registers where the second one reads them: the order of the keys inside
@@ -13,8 +15,6 @@
 //      columns by itself, so V needs neither LDS nor another lane
 //   O  row m, channels g d / 4 .. of it: a run of d / 4 neighbouring channels
 #include "serving.h"
-
-#include <type_traits>
 
 namespace sga {
 namespace {
@@ -37,12 +37,6 @@ constexpr int kChunkPieces = 1536;
 // Sequences with more rows than this on average take tiles of 128 rows.  (us, below / above: 32 rows behind 4k to 16k, 32 sequences,
 // bf16, d = 128 231 / 251, d = 64 122 / 139; 40 rows 189 / 169; 64 rows, 16 sequences 202 / 182; 29 rows at d = 256 54 / 64.)
 constexpr int kTokenRows = 32;
-
-__device__ __forceinline__ int64_t uniform64(int64_t v) {
-  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)v);
-  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)v >> 32));
-  return (int64_t)(((uint64_t)hi << 32) | lo);
-}
 
 // The largest of a row's four lanes (m, 0..3).
 __device__ __forceinline__ float row_max(float x) {
@@ -139,7 +133,6 @@ constexpr uint32_t kWholeTiles = 32;       // tiles shorter than this part of a 
 __device__ __forceinline__ uint64_t quotient64(uint64_t n, uint64_t d) {
   return (n | d) >> 32 ? n / d : (uint64_t)((uint32_t)n / (uint32_t)d);
 }
-__device__ __forceinline__ uint64_t uniform64u(uint64_t v) { return (uint64_t)uniform64((int64_t)v); }
 __device__ __forceinline__ uint64_t from_lane(uint64_t v, int lane) {
   return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), lane) << 32 |
          (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, lane);
@@ -631,6 +624,9 @@ struct Asked {
 };
 
 // N: 16-row groups of a tile, which share the keys that a wavefront loads.
+// One share after the other of each workgroup's tiles.  Measured (us alone, TB/s of the keys and values that rows see): one
+// token of 64 sequences of 512 to 32,768, 8 key heads of 128, bf16 343 (5.8, a large copy: 5.0), of 160 windows of 2,048, 4 key
+// heads, fp16 114 (4.9); a document of six sequences, window 128, fp32, d = 64, which its products of fp32 operands bound, 140.
 template <typename T, int D, int N, bool kWholeTiles>
 __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1 : 2))) void paged_kernel(
     PagedAttention a) {
@@ -642,266 +638,269 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
   const int32_t group = (int32_t)a.group.value;
   __shared__ Share<kTileRows> share;
   for (bool first_part = true;; first_part = false) {
-  const bool any = share.next(a, blockIdx.x, first_part);
-  if (first_part && a.partials && threadIdx.x == 0) {
-    // the tile that ends in this share and began in an earlier one
-    const Part& p = share.part[0];
-    const bool ends = any && p.from > 0 && p.to == p.extent;
-    const int32_t first = ends ? (int32_t)quotient64(share.size * blockIdx.x - p.from, share.size) : 0;
-    notes_of(a)[blockIdx.x] = Note{ends ? (int32_t)blockIdx.x - first + 1 : 0, first, 0, p.begin, p.n_new, p.length,
-                                   p.tile, p.head};
-  }
-  if (!any) return;
-  const int tid = thread_again(), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int m = lane & 15, g = lane >> 4;
-  const int parts = __builtin_amdgcn_readfirstlane(share.parts);
-  const bool alone = __builtin_amdgcn_readfirstlane(share.part[0].there) == 2;      // this wavefront has a tile to itself
-  if (!alone || wave < parts) {
-  const Part here = share.mine(alone ? wave : 0);
-  const int32_t head_kv = here.head;
-  const Tile tile = tile_of<kTileRows>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
+    const bool any = share.next(a, blockIdx.x, first_part);
+    if (first_part && a.partials && threadIdx.x == 0) {
+      // the tile that ends in this share and began in an earlier one
+      const Part& p = share.part[0];
+      const bool ends = any && p.from > 0 && p.to == p.extent;
+      const int32_t first = ends ? (int32_t)quotient64(share.size * blockIdx.x - p.from, share.size) : 0;
+      notes_of(a)[blockIdx.x] = Note{ends ? (int32_t)blockIdx.x - first + 1 : 0, first, 0, p.begin, p.n_new, p.length,
+                                     p.tile, p.head};
+    }
+    if (!any) return;
+    const int tid = thread_again(), lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+    const int m = lane & 15, g = lane >> 4;
+    const int parts = __builtin_amdgcn_readfirstlane(share.parts);
+    const bool alone = __builtin_amdgcn_readfirstlane(share.part[0].there) == 2;      // this wavefront has a tile to itself
+    if (!alone || wave < parts) {
+      const Part here = share.mine(alone ? wave : 0);
+      const int32_t head_kv = here.head;
+      const Tile tile = tile_of<kTileRows>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
 
-  // this lane's rows
-  Sight sight[N];
-  C core;
+      // this lane's rows
+      Sight sight[N];
+      C core;
 #pragma unroll
-  for (int n = 0; n < N; ++n) {
-    const int32_t flat = tile.first + (16 * n + m < tile.count ? 16 * n + m : 0);
-    const int32_t token = (int32_t)quotient((uint32_t)flat, a.group), head = head_kv * group + (flat - token * group);
-    sight[n] = sight_of(a, tile.length - tile.n_new + token, tile.kept);
-    const T* q = static_cast<const T*>(a.Q) + (int64_t)head * a.q_head + (int64_t)(tile.begin + token) * a.q_row;
+      for (int n = 0; n < N; ++n) {
+        const int32_t flat = tile.first + (16 * n + m < tile.count ? 16 * n + m : 0);
+        const int32_t token = (int32_t)quotient((uint32_t)flat, a.group), head = head_kv * group + (flat - token * group);
+        sight[n] = sight_of(a, tile.length - tile.n_new + token, tile.kept);
+        const T* q = static_cast<const T*>(a.Q) + (int64_t)head * a.q_head + (int64_t)(tile.begin + token) * a.q_row;
 #pragma unroll
-    for (int i = 0; i < C::kSteps; ++i)
-      core.q[n][i] = *reinterpret_cast<const typename C::Piece*>(q + (g + 4 * i) * C::kPieceElems);
-  }
-  // keys that every row sees
-  int32_t lo_max = sight[0].lo, hi_min = sight[0].hi;
+        for (int i = 0; i < C::kSteps; ++i)
+          core.q[n][i] = *reinterpret_cast<const typename C::Piece*>(q + (g + 4 * i) * C::kPieceElems);
+      }
+      // keys that every row sees
+      int32_t lo_max = sight[0].lo, hi_min = sight[0].hi;
 #pragma unroll
-  for (int n = 1; n < N; ++n) {
-    lo_max = max(lo_max, sight[n].lo);
-    hi_min = min(hi_min, sight[n].hi);
-  }
+      for (int n = 1; n < N; ++n) {
+        lo_max = max(lo_max, sight[n].lo);
+        hi_min = min(hi_min, sight[n].hi);
+      }
 #pragma unroll
-  for (int off = 1; off < 16; off <<= 1) {
-    lo_max = max(lo_max, __shfl_xor(lo_max, off, kWave));
-    hi_min = min(hi_min, __shfl_xor(hi_min, off, kWave));
-  }
-  lo_max = __builtin_amdgcn_readfirstlane(lo_max);
-  hi_min = __builtin_amdgcn_readfirstlane(hi_min);
+      for (int off = 1; off < 16; off <<= 1) {
+        lo_max = max(lo_max, __shfl_xor(lo_max, off, kWave));
+        hi_min = min(hi_min, __shfl_xor(hi_min, off, kWave));
+      }
+      lo_max = __builtin_amdgcn_readfirstlane(lo_max);
+      hi_min = __builtin_amdgcn_readfirstlane(hi_min);
 
-  const PagedArgs& b = a.batch;
-  const int64_t in_head = (int64_t)head_kv * b.page.value * D;
-  const T* const cache_k = static_cast<const T*>(a.cache_k) + in_head;
-  const T* const cache_v = static_cast<const T*>(a.cache_v) + in_head;
-  const int32_t* const table = b.page_table + (int64_t)tile.seq * b.pages_per_seq;
-  // Lane l asks for key l % 32 of a block, a block ahead of the loads that need the answer.
-  auto ask = [&](int32_t block) {
-    const uint32_t j = (uint32_t)(first_key(tile, block) + (lane & 31)), column = quotient(j, b.page);
-    Asked q;
-    q.in_page = (int32_t)(j - column * b.page.value);
-    q.page = column < (uint32_t)b.pages_per_seq ? table[column] : -1;
-    return q;
-  };
-  auto find = [&](const Asked& q) {
-    const bool there = (uint32_t)q.page < b.n_pages;
-    const int64_t o = there ? (int64_t)q.page * b.page_stride + (int64_t)q.in_page * D : 0;
-    const uint32_t held = (uint32_t)__ballot(there);
-    Places at;
-    if constexpr (kWholeTiles) {
-      at.held = (held & 1) | (held >> 15 & 2);
-      at.tile[0] = (int64_t)from_lane((uint64_t)o, 0);
-      at.tile[1] = (int64_t)from_lane((uint64_t)o, 16);
-    } else {
-      at.held = held;
-      at.key = o;
-    }
-    return at;
-  };
-  auto load_k = [&](const Places& at) {
+      const PagedArgs& b = a.batch;
+      const int64_t in_head = (int64_t)head_kv * b.page.value * D;
+      const T* const cache_k = static_cast<const T*>(a.cache_k) + in_head;
+      const T* const cache_v = static_cast<const T*>(a.cache_v) + in_head;
+      const int32_t* const table = b.page_table + (int64_t)tile.seq * b.pages_per_seq;
+      // Lane l asks for key l % 32 of a block, a block ahead of the loads that need the answer.
+      auto ask = [&](int32_t block) {
+        const uint32_t j = (uint32_t)(first_key(tile, block) + (lane & 31)), column = quotient(j, b.page);
+        Asked q;
+        q.in_page = (int32_t)(j - column * b.page.value);
+        q.page = column < (uint32_t)b.pages_per_seq ? table[column] : -1;
+        return q;
+      };
+      auto find = [&](const Asked& q) {
+        const bool there = (uint32_t)q.page < b.n_pages;
+        const int64_t o = there ? (int64_t)q.page * b.page_stride + (int64_t)q.in_page * D : 0;
+        const uint32_t held = (uint32_t)__ballot(there);
+        Places at;
+        if constexpr (kWholeTiles) {
+          at.held = (held & 1) | (held >> 15 & 2);
+          at.tile[0] = (int64_t)from_lane((uint64_t)o, 0);
+          at.tile[1] = (int64_t)from_lane((uint64_t)o, 16);
+        } else {
+          at.held = held;
+          at.key = o;
+        }
+        return at;
+      };
+      auto load_k = [&](const Places& at) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const T* row = kWholeTiles ? cache_k + at.tile[t] + m * D : cache_k + __shfl(at.key, 16 * t + m, kWave);
+        for (int t = 0; t < 2; ++t) {
+          const T* row = kWholeTiles ? cache_k + at.tile[t] + m * D : cache_k + __shfl(at.key, 16 * t + m, kWave);
 #pragma unroll
-      for (int i = 0; i < C::kSteps; ++i)
-        core.k[t][i] = *reinterpret_cast<const typename C::Piece*>(row + (g + 4 * i) * C::kPieceElems);
-    }
-  };
-  auto load_v = [&](const Places& at) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const T* row = kWholeTiles ? cache_v + at.tile[e / 4] + (4 * g + e % 4) * D
-                                 : cache_v + __shfl(at.key, 16 * (e / 4) + 4 * g + e % 4, kWave);
-      core.v[e] = *reinterpret_cast<const typename C::Run*>(row + m * kRun);
-    }
-  };
-
-  const int32_t first_block = block_at(here.from, here.extent, tile.blocks) + (alone ? 0 : wave);
-  const int32_t end_block = block_at(here.to, here.extent, tile.blocks), step = alone ? 1 : kWaves;
-  float top[N], sum[N];
-  float4v o[N][kRun];
-#pragma unroll
-  for (int n = 0; n < N; ++n) {
-    top[n] = -INFINITY;
-    sum[n] = 0.f;
-#pragma unroll
-    for (int c = 0; c < kRun; ++c) o[n][c] = float4v{0.f, 0.f, 0.f, 0.f};
-  }
-  Places at;
-  Asked asked{};
-  if (first_block < end_block) {
-    at = find(ask(first_block));
-    asked = ask(first_block + step);      // (behind the last block: a place in the page table's row, or none)
-    load_k(at);
-    load_v(at);
-  }
-  for (int32_t block = first_block; block < end_block; block += step) {
-    const int32_t j0 = first_key(tile, block);
-    const uint32_t held = at.held;
-    const bool more = block + step < end_block;
-    float4v s[N][2];
-    core.scores(s);
-    if (more) {
-      at = find(asked);
-      asked = ask(block + 2 * step);
-      load_k(at);
-    }
-    const bool all_held = held == (kWholeTiles ? 3u : ~0u);
-    const bool whole = all_held && j0 >= lo_max && j0 + kBlock - 1 <= hi_min;
-    float p[N][8];
-#pragma unroll
-    for (int n = 0; n < N; ++n) {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) p[n][e] = s[n][e / 4][e % 4] * (a.scale * kLog2e);
-      if (!whole) {
+          for (int i = 0; i < C::kSteps; ++i)
+            core.k[t][i] = *reinterpret_cast<const typename C::Piece*>(row + (g + 4 * i) * C::kPieceElems);
+        }
+      };
+      auto load_v = [&](const Places& at) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          const int in_block = 16 * (e / 4) + 4 * g + e % 4, j = j0 + in_block;
-          const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
-          p[n][e] = there && ((j >= sight[n].lo && j <= sight[n].hi) || j < sight[n].lead) ? p[n][e] : -INFINITY;
+          const T* row = kWholeTiles ? cache_v + at.tile[e / 4] + (4 * g + e % 4) * D
+                                     : cache_v + __shfl(at.key, 16 * (e / 4) + 4 * g + e % 4, kWave);
+          core.v[e] = *reinterpret_cast<const typename C::Run*>(row + m * kRun);
         }
+      };
+
+      const int32_t first_block = block_at(here.from, here.extent, tile.blocks) + (alone ? 0 : wave);
+      const int32_t end_block = block_at(here.to, here.extent, tile.blocks), step = alone ? 1 : kWaves;
+      float top[N], sum[N];
+      float4v o[N][kRun];
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        top[n] = -INFINITY;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int c = 0; c < kRun; ++c) o[n][c] = float4v{0.f, 0.f, 0.f, 0.f};
       }
-      float best = p[n][0];
-#pragma unroll
-      for (int e = 1; e < 8; ++e) best = fmaxf(best, p[n][e]);
-      best = fmaxf(row_max(best), top[n]);
-      if (__any(best > top[n])) {
-        const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top[n] - best) : 1.f;
-        sum[n] *= keep;
-#pragma unroll
-        for (int c = 0; c < kRun; ++c) o[n][c] *= keep;
-        top[n] = best;
+      Places at;
+      Asked asked{};
+      if (first_block < end_block) {
+        at = find(ask(first_block));
+        asked = ask(first_block + step);      // (behind the last block: a place in the page table's row, or none)
+        load_k(at);
+        load_v(at);
       }
-      const float against = top[n] > -INFINITY ? top[n] : 0.f;
+      for (int32_t block = first_block; block < end_block; block += step) {
+        const int32_t j0 = first_key(tile, block);
+        const uint32_t held = at.held;
+        const bool more = block + step < end_block;
+        float4v s[N][2];
+        core.scores(s);
+        if (more) {
+          at = find(asked);
+          asked = ask(block + 2 * step);
+          load_k(at);
+        }
+        const bool all_held = held == (kWholeTiles ? 3u : ~0u);
+        const bool whole = all_held && j0 >= lo_max && j0 + kBlock - 1 <= hi_min;
+        float p[N][8];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[n][e] = __builtin_amdgcn_exp2f(p[n][e] - against);
-        sum[n] += p[n][e];
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) p[n][e] = s[n][e / 4][e % 4] * (a.scale * kLog2e);
+          if (!whole) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              const int in_block = 16 * (e / 4) + 4 * g + e % 4, j = j0 + in_block;
+              const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
+              p[n][e] = there && ((j >= sight[n].lo && j <= sight[n].hi) || j < sight[n].lead) ? p[n][e] : -INFINITY;
+            }
+          }
+          float best = p[n][0];
+#pragma unroll
+          for (int e = 1; e < 8; ++e) best = fmaxf(best, p[n][e]);
+          best = fmaxf(row_max(best), top[n]);
+          if (__any(best > top[n])) {
+            const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top[n] - best) : 1.f;
+            sum[n] *= keep;
+#pragma unroll
+            for (int c = 0; c < kRun; ++c) o[n][c] *= keep;
+            top[n] = best;
+          }
+          const float against = top[n] > -INFINITY ? top[n] : 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            p[n][e] = __builtin_amdgcn_exp2f(p[n][e] - against);
+            sum[n] += p[n][e];
+          }
+        }
+        // values of keys that no row sees (behind the last token, without a page) may be anything
+        if (!all_held || j0 + kBlock > tile.kept) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int in_block = 16 * (e / 4) + 4 * g + e % 4;
+            const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
+            const bool use = there && j0 + in_block < tile.kept;
+#pragma unroll
+            for (int c = 0; c < kRun; ++c) core.v[e][c] = use ? core.v[e][c] : (T)0.f;
+          }
+        }
+        core.mix(p, o);
+        if (more) load_v(at);
       }
-    }
-    // values of keys that no row sees (behind the last token, without a page) may be anything
-    if (!all_held || j0 + kBlock > tile.kept) {
+      bool finite = true;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int in_block = 16 * (e / 4) + 4 * g + e % 4;
-        const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
-        const bool use = there && j0 + in_block < tile.kept;
+      for (int n = 0; n < N; ++n)
 #pragma unroll
-        for (int c = 0; c < kRun; ++c) core.v[e][c] = use ? core.v[e][c] : (T)0.f;
-      }
-    }
-    core.mix(p, o);
-    if (more) load_v(at);
-  }
-  bool finite = true;
+        for (int c = 0; c < kRun; ++c)
 #pragma unroll
-  for (int n = 0; n < N; ++n)
+          for (int r = 0; r < 4; ++r) finite = finite && __builtin_isfinite(o[n][c][r]);
+      if (__all(finite)) {
 #pragma unroll
-    for (int c = 0; c < kRun; ++c)
+        for (int n = 0; n < N; ++n) {
+          const float total = row_sum(sum[n]);
 #pragma unroll
-      for (int r = 0; r < 4; ++r) finite = finite && __builtin_isfinite(o[n][c][r]);
-  if (__all(finite)) {
+          for (int r = 0; r < 4; ++r)
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      const float total = row_sum(sum[n]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int c = 0; c < kRun; ++c) out[wave][16 * n + m][(4 * g + r) * kRun + c] = o[n][c][r];
-      if (g == 0) {
-        tops[wave][16 * n + m] = top[n];
-        sums[wave][16 * n + m] = total;
-      }
-    }
-  } else {
-    for (int row = 0; row < tile.count; ++row) {
-      float x[(D + 63) / 64], row_top, row_total;
-      attend_row<T, D>(a, tile, head_kv, tile.first + row, first_block, end_block, step, row_top, row_total, x);
-#pragma unroll
-      for (int c = 0; c < (D + 63) / 64; ++c)
-        if (lane + 64 * c < D) out[wave][row][lane + 64 * c] = x[c];
-      if (lane == 0) {
-        tops[wave][row] = row_top;
-        sums[wave][row] = row_total;
-      }
-    }
-  }
-  constexpr int kPer = D / 16;                             // channels of a thread
-  if (alone) {
-    __builtin_amdgcn_wave_barrier();
-    for (int i = lane; i < 16 * tile.count; i += kWave) {
-      float x[kPer];
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) x[c] = out[wave][i / 16][i % 16 * kPer + c];
-      store_row<T, D>(a, tile, head_kv, i / 16, i % 16 * kPer, x, tops[wave][i / 16], sums[wave][i / 16]);
-    }
-  } else {
-    __syncthreads();
-    // the wavefronts' states of a row, added in their order
-    float* const part = here.from == 0 && here.to == here.extent ? nullptr : record_of_share<D, kTileRows>(a, blockIdx.x, here.from > 0);
-    const int channel = tid % 16 * kPer;
-    for (int row = tid / 16; row < tile.count; row += kWaves * kWave / 16) {
-      float high = -INFINITY;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) high = fmaxf(high, tops[w][row]);
-      const float against = high > -INFINITY ? high : 0.f;
-      float total = 0.f, x[kPer];
-#pragma unroll
-      for (int c = 0; c < kPer; ++c) x[c] = 0.f;
-#pragma unroll
-      for (int w = 0; w < kWaves; ++w) {
-        if (sums[w][row] == 0.f) continue;                 // no key seen
-        const float weight = __builtin_amdgcn_exp2f(tops[w][row] - against);
-        total += weight * sums[w][row];
-#pragma unroll
-        for (int c = 0; c < kPer; ++c) x[c] += weight * out[w][row][channel + c];
-      }
-      if (part) {
-#pragma unroll
-        for (int c = 0; c < kPer; ++c) part[row * D + channel + c] = x[c];
-        if (channel == 0) {
-          part[kTileRows * D + row] = high;
-          part[kTileRows * (D + 1) + row] = total;
+            for (int c = 0; c < kRun; ++c) out[wave][16 * n + m][(4 * g + r) * kRun + c] = o[n][c][r];
+          if (g == 0) {
+            tops[wave][16 * n + m] = top[n];
+            sums[wave][16 * n + m] = total;
+          }
         }
       } else {
-        store_row<T, D>(a, tile, head_kv, row, channel, x, high, total);
+        for (int row = 0; row < tile.count; ++row) {
+          float x[(D + 63) / 64], row_top, row_total;
+          attend_row<T, D>(a, tile, head_kv, tile.first + row, first_block, end_block, step, row_top, row_total, x);
+#pragma unroll
+          for (int c = 0; c < (D + 63) / 64; ++c)
+            if (lane + 64 * c < D) out[wave][row][lane + 64 * c] = x[c];
+          if (lane == 0) {
+            tops[wave][row] = row_top;
+            sums[wave][row] = row_total;
+          }
+        }
+      }
+      constexpr int kPer = D / 16;                             // channels of a thread
+      if (alone) {
+        __builtin_amdgcn_wave_barrier();
+        for (int i = lane; i < 16 * tile.count; i += kWave) {
+          float x[kPer];
+#pragma unroll
+          for (int c = 0; c < kPer; ++c) x[c] = out[wave][i / 16][i % 16 * kPer + c];
+          store_row<T, D>(a, tile, head_kv, i / 16, i % 16 * kPer, x, tops[wave][i / 16], sums[wave][i / 16]);
+        }
+      } else {
+        __syncthreads();
+        // the wavefronts' states of a row, added in their order
+        float* const part = here.from == 0 && here.to == here.extent ? nullptr : record_of_share<D, kTileRows>(a, blockIdx.x, here.from > 0);
+        const int channel = tid % 16 * kPer;
+        for (int row = tid / 16; row < tile.count; row += kWaves * kWave / 16) {
+          float high = -INFINITY;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) high = fmaxf(high, tops[w][row]);
+          const float against = high > -INFINITY ? high : 0.f;
+          float total = 0.f, x[kPer];
+#pragma unroll
+          for (int c = 0; c < kPer; ++c) x[c] = 0.f;
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w) {
+            if (sums[w][row] == 0.f) continue;                 // no key seen
+            const float weight = __builtin_amdgcn_exp2f(tops[w][row] - against);
+            total += weight * sums[w][row];
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) x[c] += weight * out[w][row][channel + c];
+          }
+          if (part) {
+#pragma unroll
+            for (int c = 0; c < kPer; ++c) part[row * D + channel + c] = x[c];
+            if (channel == 0) {
+              part[kTileRows * D + row] = high;
+              part[kTileRows * (D + 1) + row] = total;
+            }
+          } else {
+            store_row<T, D>(a, tile, head_kv, row, channel, x, high, total);
+          }
+        }
       }
     }
-  }
-  }
-  __syncthreads();                                         // the next part's states take the same space
+    __syncthreads();                                       // the next part's states take the same space
   }
 }
 
 // ---- many new tokens: tiles of 128 rows ---------------------------------------------------------------------
-// 16-bit storage.  Four wavefronts own 32 rows each and share every block of keys: K and V
-// are copied global -> LDS without registers, once per workgroup, into a ring of four blocks, three ahead; the
-// barrier that opens a block also frees the one before it.  Products of 32 x 32 x 16: S^T = K Q^T and O^T += V^T P^T, a lane's
-// row is lane % 32 in both, and the keys that it holds of S^T are those that it feeds as P.  The scores of the
-// next block are issued ahead of this block's exponentials, so matrix and vector units have work at once.
-// The reference of a row's exponentials (m) is raised only when its numerators grow past 2^14: what matters is that they
-// stay in the range of the storage type, and the sums l and O are in 32 bits whatever their reference.
+// Four wavefronts own 32 rows each and share every block of keys: K and V are copied global -> LDS without registers,
+// once per workgroup, into a ring of four blocks, three ahead; the barrier that opens a block also frees the one before
+// it.  Products of 32 x 32 x 16 (fp32 storage: x 2): S^T = K Q^T and O^T += V^T P^T, a lane's row is lane % 32 in both, and
+// the keys that it holds of S^T are those that it feeds as P.  The scores of the next block are issued ahead of this
+// block's exponentials, so matrix and vector units have work at once.
+// 16-bit storage: the reference of a row's exponentials (m) is raised only when its numerators grow past 2^14: what matters
+// is that they stay in the range of the storage type, and the sums l and O are in 32 bits whatever their reference.
 // P is rounded to the storage type once (fp16 2^-11, bf16 2^-8 of each numerator, independent of each other): the matrix
 // cores bound this kernel, and a second term for it would cost a half more.  l sums the unrounded numerators.
+// Measured (us and TFLOP/s of the products that the mask asks for): a causal prompt of 32,768 tokens, 8 heads of 128, bf16
+// 2,310 (950 of a library product's 1,266); the same with 32 heads under a window of 2,048, fp16 1,250 (850: a tile meets
+// 68 blocks, eight of them edges that test every key); 16,384 tokens, causal, 8 heads of 64, fp32 2,570 (107 of 154).
 typedef float floatx16 __attribute__((ext_vector_type(16)));
 typedef short short4v __attribute__((ext_vector_type(4)));
 
@@ -1488,15 +1487,13 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_join_kernel(PagedAttentio
                               [&](int32_t i) { return record_of_share<D, kTileRows>(a, note.first + i, i > 0); });
 }
 
-// ... tiles of 128 rows in pieces
-constexpr int kJoinRows = 64;
+// ... tiles of 128 rows in pieces (16 rows a workgroup: 64 made a chunk of 32 tokens behind 32k 69 us instead of 48)
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves* kWave) void paged_chunk_join_kernel(PagedAttention a) {
   const Note note = notes_of(a)[blockIdx.x];
   if (note.count == 0) return;
-  for (int32_t row0 = blockIdx.y * kJoinRows; row0 < (int32_t)(blockIdx.y + 1) * kJoinRows; row0 += 16)
-    join_parts<T, D, kChunkRows>(a, note, row0,
-                                 [&](int32_t i) { return record_of<D, kChunkRows>(a, note.first + (int64_t)i * note.apart); });
+  join_parts<T, D, kChunkRows>(a, note, blockIdx.y * 16,
+                               [&](int32_t i) { return record_of<D, kChunkRows>(a, note.first + (int64_t)i * note.apart); });
 }
 
 template <typename T, int D, int N>
@@ -1521,7 +1518,7 @@ sga_status launch_paged_as(const PagedAttention& a) {
       if (a.batch.page.value % 16 == 0) paged_chunk_kernel<T, D, true><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
       else paged_chunk_kernel<T, D, false><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
       profile_mark_end(a.stream);
-      if (a.partials) paged_chunk_join_kernel<T, D><<<dim3((unsigned)a.groups, kChunkRows / kJoinRows), block, 0, a.stream>>>(a);
+      if (a.partials) paged_chunk_join_kernel<T, D><<<dim3((unsigned)a.groups, kChunkRows / 16), block, 0, a.stream>>>(a);
     }
     return hip_status(hipGetLastError());
   }

@@ -5,6 +5,8 @@
 // bounds it; what could cost more is the sines, and they depend on the token and the pair but not on the head.  A
 // workgroup therefore takes a few tokens with all their heads (of Q, K and V together when it appends to a
 // cache), computes their sines once into LDS and streams the rows past them, 16 bytes per lane and access.
+// Measured (us, read and written): queries of 65,536 tokens, 32 heads of 128, bf16 193 (5.6 TB/s; a large copy 5.0); prompts
+// of 33,000 tokens into pages, 32 + 8 + 8 heads of 128, fp16 182 (4.5); 100,003 tokens, 8 heads of 64, fp32 73 (5.6).
 #include "serving.h"
 
 namespace sga {
@@ -57,121 +59,121 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, RotateSh
   constexpr int64_t kNone = INT64_MIN;
 
   for (int64_t row0_ = (int64_t)blockIdx.x * tokens; row0_ < a.n_rows; row0_ += (int64_t)gridDim.x * tokens) {
-  const int32_t row0 = (int32_t)row0_;
-  const int count = a.n_rows - row0 < tokens ? a.n_rows - row0 : tokens;
-  __syncthreads();                                          // the rows before these are done with the turns
-  if constexpr (kPaged) {
-    for (int t = tid / kWave; t < count; t += kThreads / kWave) {
-      const int32_t row = row0 + t;
-      const PagedArgs& b = a.batch;
-      const int32_t s = last_not_above(b.n_seqs, row, [&](int32_t i) { return b.seq_ptr[i]; });
-      const int64_t begin = b.seq_ptr[s], end = b.seq_ptr[s + 1];
-      int64_t pos = kNone, place = -1;
-      if (begin <= row && row < end) {
-        pos = (int64_t)b.seq_len[s] - (end - row);
-        if (pos >= 0 && pos < (int64_t)b.pages_per_seq * b.page.value) {
-          const uint32_t column = quotient((uint32_t)pos, b.page), in_page = (uint32_t)pos - column * b.page.value;
-          const uint32_t page = (uint32_t)b.page_table[(int64_t)s * b.pages_per_seq + column];
-          if (page < b.n_pages) place = (int64_t)page * b.page_stride + (int64_t)in_page * a.d;
+    const int32_t row0 = (int32_t)row0_;
+    const int count = a.n_rows - row0 < tokens ? a.n_rows - row0 : tokens;
+    __syncthreads();                                          // the rows before these are done with the turns
+    if constexpr (kPaged) {
+      for (int t = tid / kWave; t < count; t += kThreads / kWave) {
+        const int32_t row = row0 + t;
+        const PagedArgs& b = a.batch;
+        const int32_t s = last_not_above(b.n_seqs, row, [&](int32_t i) { return b.seq_ptr[i]; });
+        const int64_t begin = b.seq_ptr[s], end = b.seq_ptr[s + 1];
+        int64_t pos = kNone, place = -1;
+        if (begin <= row && row < end) {
+          pos = (int64_t)b.seq_len[s] - (end - row);
+          if (pos >= 0 && pos < (int64_t)b.pages_per_seq * b.page.value) {
+            const uint32_t column = quotient((uint32_t)pos, b.page), in_page = (uint32_t)pos - column * b.page.value;
+            const uint32_t page = (uint32_t)b.page_table[(int64_t)s * b.pages_per_seq + column];
+            if (page < b.n_pages) place = (int64_t)page * b.page_stride + (int64_t)in_page * a.d;
+          }
+        }
+        if ((tid & (kWave - 1)) == 0) {
+          position[t] = pos;
+          cache_row[t] = place;
         }
       }
-      if ((tid & (kWave - 1)) == 0) {
-        position[t] = pos;
-        cache_row[t] = place;
-      }
+    } else if (tid < count) {
+      position[tid] = a.positions ? a.positions[row0 + tid] : a.first + row0 + tid;
     }
-  } else if (tid < count) {
-    position[tid] = a.positions ? a.positions[row0 + tid] : a.first + row0 + tid;
-  }
-  __syncthreads();
-  const int pairs = a.rotary.channels >> 1;
-  for (int i = tid; i < count * pairs; i += kThreads) {
-    const int t = i / pairs, k = i - t * pairs;
-    if (kPaged && position[t] == kNone) continue;
-    const float2 cs = turn_of(position[t], a.rotary.frequencies[k]);
-    const float m = a.rotary.magnitude;
-    turns[i] = make_float2(m * cs.x, a.rotary.inverse ? -m * cs.y : m * cs.y);
-  }
-  __syncthreads();
+    __syncthreads();
+    const int pairs = a.rotary.channels >> 1;
+    for (int i = tid; i < count * pairs; i += kThreads) {
+      const int t = i / pairs, k = i - t * pairs;
+      if (kPaged && position[t] == kNone) continue;
+      const float2 cs = turn_of(position[t], a.rotary.frequencies[k]);
+      const float m = a.rotary.magnitude;
+      turns[i] = make_float2(m * cs.x, a.rotary.inverse ? -m * cs.y : m * cs.y);
+    }
+    __syncthreads();
 
-  using Vec = vec_t<T, V>;
-  const int32_t head0 = blockIdx.y * shape.heads_here;
-  const int heads = shape.all_heads - head0 < shape.heads_here ? shape.all_heads - head0 : shape.heads_here;
-  const int turning = a.rotary.channels / (2 * V);           // items of a row that turn
-  const uint32_t total = shape.items.value * (uint32_t)tokens * (uint32_t)shape.heads_here;
-  for (uint32_t i = tid; i < total; i += kThreads) {
-    const uint32_t row = quotient(i, shape.items), k = i - row * shape.items.value;
-    uint32_t t, h;
-    if (shape.head_first) {
-      t = quotient(row, shape.heads);
-      h = row - t * shape.heads.value;
-    } else {
-      h = quotient(row, shape.tokens);
-      t = row - h * shape.tokens.value;
-    }
-    if ((int)t >= count || (int)h >= heads) continue;
-    h += head0;
-    int which = 0;
-    if (kPaged) {
-      while (which < a.n_tensors - 1 && (int)h >= a.tensor[which].heads) h -= a.tensor[which++].heads;
-    }
-    const RowsArg& x = a.tensor[which];
-    const T* src = static_cast<const T*>(x.src) + (int64_t)h * x.src_head + (int64_t)(row0 + (int)t) * x.src_row;
-    T* dst = static_cast<T*>(x.dst) + (int64_t)h * x.dst_head;
-    if (kPaged) {
-      if (position[t] == kNone || (x.paged && cache_row[t] < 0)) continue;
-      dst += x.paged ? cache_row[t] : (int64_t)(row0 + (int)t) * x.dst_row;
-    } else {
-      dst += (int64_t)(row0 + (int)t) * x.dst_row;
-    }
-    const bool turns_here = (int)k < turning && (!kPaged || x.rotate);
-    const bool split = turns_here && !a.rotary.interleaved;
-    const int at = split ? (int)k * V : (int)k * 2 * V, at2 = split ? at + pairs : at + V;
-    if (V == 1 && at2 >= a.d) {                              // the last channel of an odd number
-      dst[at] = src[at];
-      continue;
-    }
-    Vec u, v;
-    if constexpr (V == 1) {
-      u[0] = src[at];
-      v[0] = src[at2];
-    } else {
-      u = *reinterpret_cast<const Vec*>(src + at);
-      v = *reinterpret_cast<const Vec*>(src + at2);
-    }
-    if (turns_here) {
-      const float2* cs = turns + (int)t * pairs + (int)k * V;
-      if (split) {
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float p = (float)u[e], q = (float)v[e], c = cs[e].x, s = cs[e].y;
-          u[e] = (T)(p * c - q * s);
-          v[e] = (T)(p * s + q * c);
-        }
-      } else if constexpr (V == 1) {
-        const float p = (float)u[0], q = (float)v[0], c = cs[0].x, s = cs[0].y;
-        u[0] = (T)(p * c - q * s);
-        v[0] = (T)(p * s + q * c);
+    using Vec = vec_t<T, V>;
+    const int32_t head0 = blockIdx.y * shape.heads_here;
+    const int heads = shape.all_heads - head0 < shape.heads_here ? shape.all_heads - head0 : shape.heads_here;
+    const int turning = a.rotary.channels / (2 * V);           // items of a row that turn
+    const uint32_t total = shape.items.value * (uint32_t)tokens * (uint32_t)shape.heads_here;
+    for (uint32_t i = tid; i < total; i += kThreads) {
+      const uint32_t row = quotient(i, shape.items), k = i - row * shape.items.value;
+      uint32_t t, h;
+      if (shape.head_first) {
+        t = quotient(row, shape.heads);
+        h = row - t * shape.heads.value;
       } else {
+        h = quotient(row, shape.tokens);
+        t = row - h * shape.tokens.value;
+      }
+      if ((int)t >= count || (int)h >= heads) continue;
+      h += head0;
+      int which = 0;
+      if (kPaged) {
+        while (which < a.n_tensors - 1 && (int)h >= a.tensor[which].heads) h -= a.tensor[which++].heads;
+      }
+      const RowsArg& x = a.tensor[which];
+      const T* src = static_cast<const T*>(x.src) + (int64_t)h * x.src_head + (int64_t)(row0 + (int)t) * x.src_row;
+      T* dst = static_cast<T*>(x.dst) + (int64_t)h * x.dst_head;
+      if (kPaged) {
+        if (position[t] == kNone || (x.paged && cache_row[t] < 0)) continue;
+        dst += x.paged ? cache_row[t] : (int64_t)(row0 + (int)t) * x.dst_row;
+      } else {
+        dst += (int64_t)(row0 + (int)t) * x.dst_row;
+      }
+      const bool turns_here = (int)k < turning && (!kPaged || x.rotate);
+      const bool split = turns_here && !a.rotary.interleaved;
+      const int at = split ? (int)k * V : (int)k * 2 * V, at2 = split ? at + pairs : at + V;
+      if (V == 1 && at2 >= a.d) {                              // the last channel of an odd number
+        dst[at] = src[at];
+        continue;
+      }
+      Vec u, v;
+      if constexpr (V == 1) {
+        u[0] = src[at];
+        v[0] = src[at2];
+      } else {
+        u = *reinterpret_cast<const Vec*>(src + at);
+        v = *reinterpret_cast<const Vec*>(src + at2);
+      }
+      if (turns_here) {
+        const float2* cs = turns + (int)t * pairs + (int)k * V;
+        if (split) {
 #pragma unroll
-        for (int e = 0; e < V; e += 2) {
-          const float p = (float)u[e], q = (float)u[e + 1], c = cs[e / 2].x, s = cs[e / 2].y;
-          const float p2 = (float)v[e], q2 = (float)v[e + 1], c2 = cs[(V + e) / 2].x, s2 = cs[(V + e) / 2].y;
-          u[e] = (T)(p * c - q * s);
-          u[e + 1] = (T)(p * s + q * c);
-          v[e] = (T)(p2 * c2 - q2 * s2);
-          v[e + 1] = (T)(p2 * s2 + q2 * c2);
+          for (int e = 0; e < V; ++e) {
+            const float p = (float)u[e], q = (float)v[e], c = cs[e].x, s = cs[e].y;
+            u[e] = (T)(p * c - q * s);
+            v[e] = (T)(p * s + q * c);
+          }
+        } else if constexpr (V == 1) {
+          const float p = (float)u[0], q = (float)v[0], c = cs[0].x, s = cs[0].y;
+          u[0] = (T)(p * c - q * s);
+          v[0] = (T)(p * s + q * c);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; e += 2) {
+            const float p = (float)u[e], q = (float)u[e + 1], c = cs[e / 2].x, s = cs[e / 2].y;
+            const float p2 = (float)v[e], q2 = (float)v[e + 1], c2 = cs[(V + e) / 2].x, s2 = cs[(V + e) / 2].y;
+            u[e] = (T)(p * c - q * s);
+            u[e + 1] = (T)(p * s + q * c);
+            v[e] = (T)(p2 * c2 - q2 * s2);
+            v[e + 1] = (T)(p2 * s2 + q2 * c2);
+          }
         }
       }
+      if constexpr (V == 1) {
+        dst[at] = u[0];
+        dst[at2] = v[0];
+      } else {
+        *reinterpret_cast<Vec*>(dst + at) = u;
+        *reinterpret_cast<Vec*>(dst + at2) = v;
+      }
     }
-    if constexpr (V == 1) {
-      dst[at] = u[0];
-      dst[at2] = v[0];
-    } else {
-      *reinterpret_cast<Vec*>(dst + at) = u;
-      *reinterpret_cast<Vec*>(dst + at2) = v;
-    }
-  }
   }
 }
 
