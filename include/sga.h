@@ -463,7 +463,8 @@ sga_status sga_cache_append(const sga_rows* K, const sga_rows* V, void* cache_k,
  * Supported: d = 32, 64, 128, 256.  Addresses and strides are multiples of 16 bytes.  Results do not
  * depend on the order in which the work runs.  Kernels only: nothing is allocated and the host does not wait.
  * Errors: SGA_ERR_INVALID_ARG, SGA_ERR_UNSUPPORTED (d, other mask kinds), SGA_ERR_OVERFLOW
- * (n_tokens * Hq / Hkv / 16 + n_seqs of 2^24 and more: cut such a call by sequences).
+ * (n_tokens * Hq / Hkv / 16 + n_seqs or n_tokens * Hq / 128 + n_seqs * Hkv of about 2^24 and more: cut such a
+ * call by sequences).
  */
 sga_status sga_paged_workspace_bytes(const sga_paged_batch* batch, const sga_mask_desc* mask, int32_t Hq, int32_t Hkv,
                                      int32_t d, int32_t dtype, size_t* bytes_out);

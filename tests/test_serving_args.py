@@ -150,3 +150,12 @@ def test_rotary_frequencies():
                 dict(channels=8, scaling="parts", original_length=100, slow_turns=4.0, fast_turns=2.0)):
         with pytest.raises(ValueError):
             sga.rotary_frequencies(device="cpu", **bad)
+
+
+def test_calls_too_large_for_one_grid():
+    spec = MaskSpec(KIND_SLIDING, 1 << 20, window=1024)
+    def size(n, Hq, Hkv, d, dtype=1, n_seqs=2):
+        return sga.sga_paged_workspace_bytes(batch(n_tokens=n, n_seqs=n_seqs, page_stride=Hkv * 16 * d), spec, Hq, Hkv, d, dtype)[0]
+    assert size(1 << 25, 64, 64, 128) == -4                   # 2^24 tiles of 128 rows over all heads
+    assert size((1 << 25) - (1 << 14), 64, 64, 128) == 0
+    assert size((1 << 31) - 1, 8, 1, 32) == -4 and size((1 << 31) - 1, 1, 1, 64) == -4
