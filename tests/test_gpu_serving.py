@@ -591,3 +591,49 @@ def test_captured_steps_follow_the_lengths():
         side.synchronize()
         assert torch.equal(O, O2) and torch.equal(lse, lse2) and torch.equal(q, q2)
     assert torch.isfinite(O).all()
+
+
+@pytest.mark.parametrize("dtype,d,page,new", [("f16", 128, 16, [1, 3]), ("bf16", 64, 24, [90, 41]), ("f32", 64, 32, [100, 1]),
+                                              ("f32", 32, 8, [2, 1]), ("f16", 256, 5, [70, 70])])
+def test_caches_whose_pages_take_turns(dtype, d, page, new):
+    """Keys and values page by page in one buffer, beside those of other layers: the same results as in two caches, and nothing
+    written beside them."""
+    Hq, Hkv, lens = 4, 2, [700, 300]
+    spec = MaskSpec(KIND_GLOBAL_LOCAL, 768, window=200, n_global=5)
+    batch, table, ptr, _, n_pages, T = batch_of(new, lens, page)
+    ck, cv = caches(n_pages, Hkv, page, d, dtype, 1)
+    whole = torch.full((n_pages, 6, Hkv, page, d), 7.0, dtype=DTYPE[dtype], device="cuda")
+    pk, pv = whole[:, 2], whole[:, 3]
+    pk.copy_(ck)
+    pv.copy_(cv)
+    rot = sga.Rotary(sga.rotary_frequencies(d)[0])
+    Q, K, V = (tokens(h, T, d, dtype, s) for h, s in ((Hq, 1), (Hkv, 2), (Hkv, 3)))
+    ws = sga.alloc_paged_workspace(batch, spec, Hq, Hkv, d, dtype)
+    out = []
+    for k, v in ((ck, cv), (pk, pv)):
+        q = sga.cache_append(K, V, k, v, batch, rotary=rot, Q=Q)
+        out.append((q, *sga.attention_paged(q, k, v, batch, spec, 0.1, workspace=ws, want_lse=True)))
+    assert all(torch.equal(a, b) for a, b in zip(*out))
+    assert torch.equal(pk, ck) and torch.equal(pv, cv)
+    assert (whole[:, [0, 1, 4, 5]] == 7).all()
+
+
+def test_two_streams_at_once():
+    """Calls of two streams that overlap in time, each with a workspace of its own."""
+    spec = MaskSpec(KIND_SLIDING, 4096, window=4096)
+    work = []
+    for s, new in enumerate(([1, 1, 1], [200, 3, 64])):
+        batch, *_, n_pages, T = batch_of(new, [4000, 900, 2500], 16)
+        ck, cv = caches(n_pages, 2, 16, 128, "bf16", s)
+        work.append((tokens(8, T, 128, "bf16", s), ck, cv, batch, spec, 0.09))
+    want = [sga.attention_paged(*w, workspace=sga.alloc_paged_workspace(w[3], spec, 8, 2, 128, "bf16")) for w in work]
+    spaces = [sga.alloc_paged_workspace(w[3], spec, 8, 2, 128, "bf16") for w in work]
+    outs = [[torch.zeros_like(w[0]) for _ in range(8)] for w in work]
+    streams = [torch.cuda.Stream() for _ in work]
+    torch.cuda.synchronize()
+    for i in range(8):
+        for w, space, out, stream in zip(work, spaces, outs, streams):
+            with torch.cuda.stream(stream):
+                sga.attention_paged(*w, O=out[i], workspace=space)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, x) for x, out in zip(want, outs) for o in out)
