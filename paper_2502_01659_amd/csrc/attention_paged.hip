@@ -626,7 +626,8 @@ struct Asked {
 // N: 16-row groups of a tile, which share the keys that a wavefront loads.
 // One share after the other of each workgroup's tiles.  Measured (us alone, TB/s of the keys and values that rows see): one
 // token of 64 sequences of 512 to 32,768, 8 key heads of 128, bf16 343 (5.8, a large copy: 5.0), of 160 windows of 2,048, 4 key
-// heads, fp16 114 (4.9); a document of six sequences, window 128, fp32, d = 64, which its products of fp32 operands bound, 140.
+// heads, fp16 114 (4.9); a document of six sequences, window 128, fp32, d = 64 140 (43 TFLOP/s of 154:
+// short tiles, whose first loads two wavefronts per SIMD do not hide; matrix cores 32 % busy).
 template <typename T, int D, int N, bool kWholeTiles>
 __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1 : 2))) void paged_kernel(
     PagedAttention a) {
