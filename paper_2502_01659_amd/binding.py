@@ -626,9 +626,23 @@ def rotary_frequencies(channels, base=10000.0, scaling=None, factor=1.0, origina
     return f.to(device), magnitude
 
 
-class Rotary:
+class _Fixed:
+    """Attributes are set once.  The records for the library, and what a captured graph has taken from them, hold addresses and
+    sizes: they would not follow an attribute that is replaced (one that is given what it holds, as by `x.seq_len += 1`, is not)."""
+
+    def __setattr__(self, name, value):
+        if name in self.__dict__ and self.__dict__[name] is not value:
+            raise AttributeError(f"{type(self).__name__}.{name} cannot be replaced: write into its tensor, or make a new {type(self).__name__}")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError(f"{type(self).__name__}.{name} cannot be removed")
+
+
+class Rotary(_Fixed):
     """Which channels turn, how fast, and in which layout (sga_rotary_desc).  frequencies: float64 [channels / 2] on the
-    device, radians per position; layout "half" (channels i and i + channels / 2) or "interleaved" (2 i and 2 i + 1)."""
+    device, radians per position; layout "half" (channels i and i + channels / 2) or "interleaved" (2 i and 2 i + 1).
+    New frequencies may be written into the tensor; the attributes cannot be replaced."""
 
     def __init__(self, frequencies, layout="half", magnitude=1.0):
         if str(frequencies.dtype) != "torch.float64" or frequencies.dim() != 1 or frequencies.numel() < 1 \
@@ -672,7 +686,7 @@ def rotary(X, rotary, positions=None, first=0, inverse=False, out=None):
     return out
 
 
-class PagedBatch:
+class PagedBatch(_Fixed):
     """New tokens of several sequences and the pages of their keys and values (sga_paged_batch).
 
     page_table  int32 [S, columns]: page of tokens c * page_size .. of a sequence, -1 where there is none
@@ -680,7 +694,8 @@ class PagedBatch:
     seq_len     int32 [S]: tokens of the sequence, the new ones among them
     n_tokens    rows of the packed tensors (rows behind the last sequence are padding)
     page_size, n_pages   of the caches [n_pages, Hkv, page_size, d]
-    The arrays are read when the calls run, so a program may write new lengths and pages into them.
+    The arrays are read when the calls run, so a program may write new lengths and pages into them (`batch.seq_len += 1`).
+    The attributes themselves cannot be replaced: for other arrays or another number of tokens make a new batch.
     """
 
     def __init__(self, page_table, seq_ptr, seq_len, n_tokens, page_size, n_pages):

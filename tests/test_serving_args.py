@@ -159,3 +159,53 @@ def test_calls_too_large_for_one_grid():
     assert size(1 << 25, 64, 64, 128) == -4                   # 2^24 tiles of 128 rows over all heads
     assert size((1 << 25) - (1 << 14), 64, 64, 128) == 0
     assert size((1 << 31) - 1, 8, 1, 32) == -4 and size((1 << 31) - 1, 1, 1, 64) == -4
+
+
+class OnDevice:
+    """A host tensor that says it lies on device 0: enough to make the records that calls hand to the library."""
+    is_cuda, device = True, torch.device("cuda", 0)
+
+    def __init__(self, t):
+        self.t = t
+
+    def __getattr__(self, name):
+        return getattr(self.t, name)
+
+    def get_device(self):
+        return 0
+
+    def __iadd__(self, x):
+        self.t += x
+        return self
+
+
+def test_a_batch_and_a_rotation_keep_what_they_were_made_of():
+    """The records for the library hold addresses and sizes: nothing that they were made of can be replaced behind them."""
+    table, ptr, length = (OnDevice(torch.zeros(n, dtype=t)) for n, t in (((2, 4), torch.int32), (3, torch.int64), (2, torch.int32)))
+    b = sga.PagedBatch(table, ptr, length, 8, 16, 10)
+    record = b._struct(2048)
+    for name, other in (("page_table", OnDevice(torch.zeros(2, 9, dtype=torch.int32))), ("seq_ptr", OnDevice(torch.zeros(3, dtype=torch.int64))),
+                        ("seq_len", OnDevice(length.t + 1)), ("n_tokens", 7), ("page_size", 32), ("n_pages", 11), ("device", None),
+                        ("device_index", 1)):
+        held = getattr(b, name)
+        with pytest.raises(AttributeError, match=name):
+            setattr(b, name, other)
+        with pytest.raises(AttributeError, match=name):
+            delattr(b, name)
+        assert getattr(b, name) is held
+    b.seq_len += 1                                            # written into: the same array
+    assert b.seq_len is length and length.t.tolist() == [1, 1]
+    for stride in (2048, 4096):
+        r = b._struct(stride)
+        assert (r.page_table, r.seq_ptr, r.seq_len) == (table.data_ptr(), ptr.data_ptr(), length.data_ptr())
+        assert (r.n_tokens, r.n_pages, r.page_size, r.pages_per_seq, r.n_seqs, r.page_stride) == (8, 10, 16, 4, 2, stride)
+    assert b._struct(2048) is record
+
+    f = OnDevice(torch.ones(32, dtype=torch.float64))
+    rot = sga.Rotary(f, magnitude=0.5)
+    for name, other in (("frequencies", OnDevice(torch.ones(16, dtype=torch.float64))), ("channels", 32), ("_desc", None), ("device_index", 1)):
+        with pytest.raises(AttributeError, match=name):
+            setattr(rot, name, other)
+        with pytest.raises(AttributeError, match=name):
+            delattr(rot, name)
+    assert (rot._desc.frequencies, rot._desc.channels, rot.channels) == (f.data_ptr(), 64, 64)
