@@ -594,16 +594,20 @@ __device__ __forceinline__ void attend_row(const PagedAttention& a, const Tile& 
     sum *= keep;
 #pragma unroll
     for (int c = 0; c < (D + 63) / 64; ++c) o[c] *= keep;
+    float total = 0.f, mix[(D + 63) / 64] = {};              // (added up by blocks, see the kernel)
     for (uint32_t left = (uint32_t)__ballot(sees); left; left &= left - 1) {
       const int from = __ffs(left) - 1;
       const float w = __shfl(p, from, kWave);
       const int32_t low = __shfl((int32_t)at, from, kWave), high = __shfl((int32_t)(at >> 32), from, kWave);
       const T* const v = static_cast<const T*>(a.cache_v) + in_head + ((int64_t)high << 32 | (uint32_t)low);
-      sum += w;
+      total += w;
 #pragma unroll
       for (int c = 0; c < (D + 63) / 64; ++c)
-        if (lane + 64 * c < D) o[c] = fmaf(w, (float)v[lane + 64 * c], o[c]);
+        if (lane + 64 * c < D) mix[c] = fmaf(w, (float)v[lane + 64 * c], mix[c]);
     }
+    sum += total;
+#pragma unroll
+    for (int c = 0; c < (D + 63) / 64; ++c) o[c] += mix[c];
   }
 }
 
@@ -796,12 +800,16 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
             for (int c = 0; c < kRun; ++c) o[n][c] *= keep;
             top[n] = best;
           }
+          // (a block's numerators are added up before they join the row's sum: many small ones beside a few large ones would each
+          // be rounded to the sum's step)
           const float against = top[n] > -INFINITY ? top[n] : 0.f;
+          float total = 0.f;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             p[n][e] = __builtin_amdgcn_exp2f(p[n][e] - against);
-            sum[n] += p[n][e];
+            total += p[n][e];
           }
+          sum[n] += total;
         }
         // values of keys that no row sees (behind the last token, without a page) may be anything
         if (!all_held || j0 + kBlock > tile.kept) {

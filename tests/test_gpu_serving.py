@@ -637,3 +637,48 @@ def test_two_streams_at_once():
                 sga.attention_paged(*w, O=out[i], workspace=space)
     torch.cuda.synchronize()
     assert all(torch.equal(o, x) for x, out in zip(want, outs) for o in out)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [1, 20, 64])
+@pytest.mark.parametrize("spoiled", [False, True])           # one value of a token is infinite: its channel is, the others are as they were
+def test_attention_of_many_small_weights(dtype, new, spoiled):
+    """Long contexts often give a few first tokens nearly all of the weight: here tokens 0, 32, 64 and 96, one for each wavefront's first
+    block, whose values are 0, and 32,764 tokens `gap` below them, which alone decide O.  Their weights are far below the smallest
+    number of fp16; together they are not.  Scores are 0 and gap exactly, so O = e^-gap sum(v) / (4 + 32,764 e^-gap)."""
+    n, d, page = 32768, 64, 64
+    long = long_chunks(dtype, new, 1, 1, d, page) or (dtype == "f32" and new > 32)
+    batch, table, ptr, lens, n_pages, T = batch_of([new], [n], page)
+    ck, cv = (torch.zeros(n_pages, 1, page, d, dtype=DTYPE[dtype], device="cuda") for _ in range(2))
+    values = torch.rand(n, d, generator=torch.Generator().manual_seed(1)).add_(0.5).to(DTYPE[dtype])
+    values[[0, 32, 64, 96]] = 0
+    if spoiled:
+        values[1000, 5] = math.inf
+    at = torch.from_numpy(table[0].astype(np.int64)).cuda()
+    cv[at, 0] = values.view(-1, page, d).cuda()
+    for t in (0, 32, 64, 96):
+        ck[at[t // page], 0, t % page, 0] = 1
+    Q = torch.zeros(1, T, d, dtype=DTYPE[dtype], device="cuda")
+    Q[..., 0] = 1
+    total = host(values).sum(0)
+    for gap in (12.0, 14.5, 16.0, 16.75, 17.25, 17.5, 18.5, 20.0):
+        for workspace in (None, sga.alloc_paged_workspace(batch, full(n), 1, 1, d, dtype)):
+            print("small weights", dtype, new, spoiled, gap, flush=True)
+            assert sga.sga_profile_enable(1) == 0
+            O, lse = sga.attention_paged(Q, ck, cv, batch, full(n), gap, causal=False, workspace=workspace, want_lse=True)
+            torch.cuda.synchronize()
+            kernel = sga.sga_profile_last_kernel()
+            sga.sga_profile_enable(0)
+            assert kernel == ("paged_chunk_kernel" if long else "paged_kernel")
+            sums = 4 + (n - 4) * math.exp(-gap)
+            want = math.exp(-gap) * total / sums
+            # The exponent is at most 29 and off by three half steps of it: 2^-17 of a weight.  Sums in 32 bits: an addition is off by
+            # half a step of the sum, that of the four first tokens, and every lane makes at most n / 32 of them to l (2^-24 n / 32 in all),
+            # n / 16 to O (of what O holds: sqrt(n) half steps and to spare).  Numerators enter the products
+            # as two numbers of 16 bits or rounded once, fp16 ones that reach 2^10 at least with an absolute half step of 2^-25.
+            parts = {"f32": 0.0, "f16": 2.0 ** -21, "bf16": 2.0 ** -15}[dtype] if not long else (0.0 if dtype == "f32" else S.HALF_STEP[dtype])
+            relative = 2.0 ** -17 + parts + n / 32 * 2.0 ** -24 + (4 + math.sqrt(n)) * 2.0 ** -23
+            bar = want * (relative + S.HALF_STEP[dtype]) + (2.0 ** -35 * total / sums + 2.0 ** -25 if dtype == "f16" else 0)
+            assert within(O, np.broadcast_to(want, (1, T, d)), np.broadcast_to(bar, (1, T, d)))
+            off = np.abs(host(lse) - (gap + math.log(sums))).max()
+            assert off <= n / 32 * 2.0 ** -24 + 2.0 ** -22 * 32, (gap, off)
