@@ -38,6 +38,16 @@ constexpr int kChunkPieces = 1536;
 // bf16, d = 128 231 / 251, d = 64 122 / 139; 40 rows 189 / 169; 64 rows, 16 sequences 202 / 182; 29 rows at d = 256 54 / 64.)
 constexpr int kTokenRows = 32;
 
+// Numerators of fp16 storage are kept 2^kRaise times as large as against the row's largest score: fp16 ends at 2^-25 (2^-14 with all
+// its bits), and a long context can hold most of its weight in tokens that are each below that beside a few large ones.  The
+// reference is that much lower, lse and sums follow from it, and nothing else changes.  Short chunks raise the reference with every larger score,
+// so the largest numerator is 2^15 and what a pair of fp16 numbers loses begins 2^-40 below it; long chunks leave room for scores that grow, and
+// lose 2^-35 (kMostNumerators).
+template <typename T>
+constexpr float kRaise = sizeof(T) == 2 && !__is_same(T, bf16_t) ? 15.f : 0.f;
+template <typename T>
+constexpr float kChunkRaise = sizeof(T) == 2 && !__is_same(T, bf16_t) ? 10.f : 0.f;
+
 // The largest of a row's four lanes (m, 0..3).
 __device__ __forceinline__ float row_max(float x) {
   x = fmaxf(x, __shfl_xor(x, 16, kWave));
@@ -500,7 +510,8 @@ struct Core {
         for (int t = 0; t < 2; ++t) s[n][t] = matrix(k[t][i], q[n][i], i ? s[n][t] : float4v{0.f, 0.f, 0.f, 0.f});
   }
   // P as the sum of two numbers of the storage type: one alone would add an error as large as the
-  // rounding of O to O, and the matrix cores wait for memory here.
+  // rounding of O to O, and the matrix cores wait for memory here.  What is left is 2^-22 (bf16 2^-16) of a numerator, or 2^-25 (fp16,
+  // whose largest is 2^15).
   __device__ __forceinline__ void mix(const float (&p)[N][8], float4v (&o)[N][kRun]) const {
     Piece high[N], low[N];
 #pragma unroll
@@ -792,7 +803,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
           float best = p[n][0];
 #pragma unroll
           for (int e = 1; e < 8; ++e) best = fmaxf(best, p[n][e]);
-          best = fmaxf(row_max(best), top[n]);
+          best = fmaxf(row_max(best) - kRaise<T>, top[n]);
           if (__any(best > top[n])) {
             const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top[n] - best) : 1.f;
             sum[n] *= keep;
@@ -911,10 +922,11 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
 // it.  Products of 32 x 32 x 16 (fp32 storage: x 2): S^T = K Q^T and O^T += V^T P^T, a lane's row is lane % 32 in both, and
 // the keys that it holds of S^T are those that it feeds as P.  The scores of the next block are issued ahead of this
 // block's exponentials, so matrix and vector units have work at once.
-// 16-bit storage: the reference of a row's exponentials (m) is raised only when its numerators grow past 2^14: what matters
+// The reference of a row's exponentials (m) is raised only when a lane's 16 numerators of a block add up to kMostNumerators: what matters
 // is that they stay in the range of the storage type, and the sums l and O are in 32 bits whatever their reference.
-// P is rounded to the storage type once (fp16 2^-11, bf16 2^-8 of each numerator, independent of each other): the matrix
-// cores bound this kernel, and a second term for it would cost a half more.  l sums the unrounded numerators.
+// P is rounded to the storage type once: fp16 2^-11 of a numerator, and at least 2^-25 where the largest of the row is 2^10 or more; bf16
+// 2^-8.  Scores that differ are rounded independently of each other, equal ones alike, so O is off by at most that part
+// of the weighted mean of |V|.  The matrix cores bound this kernel, and a second term for P would cost a half more.  l sums the unrounded numerators.
 // Measured (us and TFLOP/s of the products that the mask asks for): a causal prompt of 32,768 tokens, 8 heads of 128, bf16
 // 2,310 (950 of a library product's 1,266); the same with 32 heads under a window of 2,048, fp16 1,250 (850: a tile meets
 // 68 blocks, eight of them edges that test every key); 16,384 tokens, causal, 8 heads of 64, fp32 2,570 (107 of 154).
@@ -923,7 +935,10 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 
 constexpr int kChunkRows = 128, kChunkSlots = 4;
 constexpr int kChunkAhead = kChunkSlots - 1;
-constexpr float kMostNumerators = 16384.f;
+// (fp16 ends at 65,504.  From 2^10, the largest right after the reference was raised, 16 equal ones have room for a factor of 3.75 and a
+// single one of 60.)
+template <typename T>
+constexpr float kMostNumerators = kChunkRaise<T> > 0.f ? 61440.f : 16384.f;
 
 __device__ __forceinline__ floatx16 matrix32(vec_t<f16_t, 8> a, vec_t<f16_t, 8> b, floatx16 c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
@@ -1209,12 +1224,12 @@ paged_chunk_kernel(PagedAttention a) {
     }
     return total;
   };
-  // the reference of the rows' numerators becomes their largest score so far
+  // the reference of the rows' numerators becomes their largest score so far, or 2^kChunkRaise below it
   auto raise = [&](const floatx16& s) {
     float best = s[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) best = fmaxf(best, s[r]);
-    best = fmaxf(best, other_half(best, h)) * factor;
+    best = fmaxf(best, other_half(best, h)) * factor - kChunkRaise<T>;
     best = fmaxf(best, top);
     const float keep = best > -INFINITY ? __builtin_amdgcn_exp2f(top - best) : 1.f;
     top = best;
@@ -1225,7 +1240,7 @@ paged_chunk_kernel(PagedAttention a) {
       for (int r = 0; r < 16; ++r) o[t][r] *= keep;
   };
   auto weigh = [&](uint32_t slot_at, const floatx16& s, float total, Numerators (&p)[2]) {
-    if (__any(!(total < kMostNumerators))) {          // (before a row's first key: infinite or NaN)
+    if (__any(!(total < kMostNumerators<T>))) {          // (before a row's first key: infinite or NaN)
       raise(s);
       total = numerators(s, top > -INFINITY ? top : 0.f, p);
     }

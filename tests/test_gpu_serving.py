@@ -639,7 +639,7 @@ def test_two_streams_at_once():
     assert all(torch.equal(o, x) for x, out in zip(want, outs) for o in out)
 
 
-@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("new", [1, 20, 64])
 @pytest.mark.parametrize("spoiled", [False, True])           # one value of a token is infinite: its channel is, the others are as they were
 def test_attention_of_many_small_weights(dtype, new, spoiled):
