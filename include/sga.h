@@ -383,8 +383,8 @@ typedef struct {
  * Rotary positions.  With a, b the channels of pair i and t = position * frequencies[i],
  *   a' = magnitude * (a cos t - b sin t),   b' = magnitude * (a sin t + b cos t)
  * or, with inverse != 0, the same with -t: for the gradient G of the result, the inverse of G
- * is the gradient of the input.  The angles are formed and reduced in 64 bits, without loss at any
- * position; sines and products are taken in 32, and results rounded once.
+ * is the gradient of the input.  The angles are formed and reduced in 64 bits, without loss where
+ * |position| < 2^52 and |t| < 2^62; sines and products are taken in 32, and results rounded once.
  *   X          read, Y written, [H][L][d]; Y may be X (same address and strides), else they must
  *              not overlap
  *   positions  device, int64 [L], or NULL: row t has position first + t.  |position| < 2^52

@@ -19,15 +19,20 @@ constexpr int kMaxTokens = 4;
 constexpr int kMaxGroups = 1 << 20;  // workgroups along the tokens (a grid holds fewer than 2^32 threads); they stride
 
 // cos t and sin t for t = position * f.  The product is held as a rounded part and its error, and multiples of pi / 2
-// are taken off in 64 bits (pi / 2 as the sum of two numbers, 2^-107 off), so that what is left is good to 2^-53 at any position;
-// rounded to 32 bits it is within 2^-25, and the Taylor polynomials of degree 9 and 10 are within 2e-9 up to pi / 4.
+// are taken off in 64 bits (pi / 2 as the sum of two numbers, 2^-107 off), twice: the first time about as many as the rounded part has, whose
+// step alone is many turns at far positions, the second time what that and the product's error leave.  Up to |t| = 2^62 the rest
+// is within pi / 4 and good to 2^-40; rounded to 32 bits it is within 2^-25, and the Taylor polynomials of degree 9 and 10 are within 2e-9 there.
 __device__ __forceinline__ float2 turn_of(int64_t position, double f) {
+  constexpr double kQuarters = 0.63661977236758134308, kHigh = 1.57079632679489655800, kLow = 6.12323399573676603587e-17;
   const double p = (double)position;
   const double x = p * f, x_low = __builtin_fma(p, f, -x);
-  const double n = __builtin_rint(x * 0.63661977236758134308);
-  double r = __builtin_fma(-n, 1.57079632679489655800, x);
-  r = __builtin_fma(-n, 6.12323399573676603587e-17, r) + x_low;
-  const int quarter = (int)((int64_t)n & 3);
+  const double n = __builtin_rint(x * kQuarters);
+  double r = __builtin_fma(-n, kHigh, x);
+  r = __builtin_fma(-n, kLow, r) + x_low;
+  const double rest = __builtin_rint(r * kQuarters);
+  r = __builtin_fma(-rest, kHigh, r);
+  r = __builtin_fma(-rest, kLow, r);
+  const int quarter = (int)(((int64_t)n + (int64_t)rest) & 3);
   const float y = (float)r, z = y * y;
   float s = 2.7557319224e-6f, c = -2.7557319224e-7f;
   s = fmaf(s, z, -1.9841269841e-4f);

@@ -682,3 +682,29 @@ def test_attention_of_many_small_weights(dtype, new, spoiled):
             assert within(O, np.broadcast_to(want, (1, T, d)), np.broadcast_to(bar, (1, T, d)))
             off = np.abs(host(lse) - (gap + math.log(sums))).max()
             assert off <= n / 32 * 2.0 ** -24 + 2.0 ** -22 * 32, (gap, off)
+
+
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+def test_rotary_up_to_the_last_position(layout):
+    """|position| up to 2^52, and angles up to 2^62: the product's error is then hundreds of turns and is reduced too."""
+    pi = 314159265358979323846264338327950288419716939937510582097494459230781640628620899      # 10^80 pi
+    unit = 10 ** 80
+    x = tokens(2, 64, 64, "f32", 5)
+    near, _ = sga.rotary_frequencies(64)
+    for freqs in (near, near * 1000.0, -near * 3.0):
+        for first, step in (((1 << 50) + 12345, 977), ((1 << 51) - 64 * 977, 977), ((1 << 52) - 64 * 977, 977), (1 - (1 << 52), 12345)):
+            at = [first + t * step for t in range(64)]
+            assert max(map(abs, at)) < 1 << 52
+            angle = np.zeros((64, 32))
+            for k, f in enumerate(freqs.cpu().tolist()):
+                num, den = f.as_integer_ratio()
+                angle[:, k] = [float(num * p * unit // den % (2 * pi)) / float(unit) for p in at]
+            a, b = (host(x)[..., :32], host(x)[..., 32:]) if layout == "half" else (host(x)[..., ::2], host(x)[..., 1::2])
+            u, v = a * np.cos(angle) - b * np.sin(angle), a * np.sin(angle) + b * np.cos(angle)
+            size = np.abs(a) + np.abs(b)
+            if layout == "half":
+                want, size = np.concatenate((u, v), -1), np.concatenate((size, size), -1)
+            else:
+                want, size = np.stack((u, v), -1).reshape(2, 64, 64), np.stack((size, size), -1).reshape(2, 64, 64)
+            got = sga.rotary(x, sga.Rotary(freqs, layout=layout), positions=torch.tensor(at, device="cuda"))
+            assert within(got, want, S.rotate_bar(want, size, "f32"))
