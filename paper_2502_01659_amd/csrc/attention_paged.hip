@@ -1062,7 +1062,9 @@ paged_chunk_kernel(PagedAttention a) {
   const bool any = piece_of<kChunkRows>(a, rest, tile, index, piece, pieces, apart);
   if (a.partials && tid == 0) {
     const bool cut = any && pieces > 1 && piece == 0;
-    notes_of(a)[record] = cut ? Note{pieces, (int32_t)record, apart, tile.begin, tile.n_new, tile.length, index, head_kv} : Note{};
+    // (a seq_ptr that decreases can bring more tiles than the plan counts: pieces behind the last workgroup's have no record)
+    const int32_t count = cut ? min(pieces, 1 + (int32_t)((uint32_t)(a.slots - 1 - rest) / (uint32_t)apart)) : 0;
+    notes_of(a)[record] = cut ? Note{count, (int32_t)record, apart, tile.begin, tile.n_new, tile.length, index, head_kv} : Note{};
   }
   if (!any) return;
   const int32_t group = (int32_t)a.group.value;

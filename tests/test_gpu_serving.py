@@ -708,3 +708,26 @@ def test_rotary_up_to_the_last_position(layout):
                 want, size = np.stack((u, v), -1).reshape(2, 64, 64), np.stack((size, size), -1).reshape(2, 64, 64)
             got = sga.rotary(x, sga.Rotary(freqs, layout=layout), positions=torch.tensor(at, device="cuda"))
             assert within(got, want, S.rotate_bar(want, size, "f32"))
+
+
+def test_attention_of_sequences_that_go_back():
+    """A seq_ptr that decreases brings more tiles than the call was planned for.  Rows may be wrong then, but no partial state is read from
+    behind the workspace: that memory holds NaN here.  (Every sequence of tokens is the same one, so no row is NaN by itself.)"""
+    T, d, page, length = 333 * 128, 64, 64, 4096
+    g = torch.Generator(device="cuda").manual_seed(1)
+    table = torch.arange(length // page, dtype=torch.int32, device="cuda").repeat(5, 1)
+    ptr = torch.tensor([0, T, 0, T, 0, T], device="cuda")
+    lens = torch.full((5,), length, dtype=torch.int32, device="cuda")
+    batch = sga.PagedBatch(table, ptr, lens, T, page, length // page)
+    ck, cv = (torch.randn(length // page, 1, page, d, generator=g, device="cuda", dtype=torch.float16) for _ in range(2))
+    Q = torch.randn(1, T, d, generator=g, device="cuda", dtype=torch.float16)
+    n = sga.paged_workspace_bytes(batch, full(length), 1, 1, d, torch.float16)
+    assert n > 0
+    # the tokens lie before position 0 but for the last 4,096: a cut tile of theirs is joined from its own records alone
+    space = torch.full((n + (64 << 20),), 255, dtype=torch.uint8, device="cuda")
+    O, lse = torch.zeros_like(Q), torch.zeros(1, T, device="cuda")
+    sga.attention_paged(Q, ck, cv, batch, full(length), 0.125, O=O, lse=lse, workspace=space[:n])
+    assert torch.isfinite(O).all() and not torch.isnan(lse).any()
+    assert (space[n:] == 255).all()
+    sga.cache_append(Q, Q, ck, cv, batch)
+    assert torch.isfinite(ck).all() and torch.isfinite(cv).all()
