@@ -197,7 +197,7 @@ sga_status launch_rotate_as(const RotateArgs& a) {
   int tokens = kMaxTokens;
   while (tokens > 1 && a.n_rows / tokens < 1024) tokens >>= 1;
   int heads = s.all_heads;
-  const int64_t groups = (a.n_rows + tokens - 1) / tokens;
+  const int64_t groups = ((int64_t)a.n_rows + tokens - 1) / tokens;
   while (heads > 1 && groups * ((s.all_heads + heads - 1) / heads) < 256 && heads * items * tokens > kThreads)
     heads = (heads + 1) / 2;
   s.items = fast_div(items);

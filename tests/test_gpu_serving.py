@@ -731,3 +731,16 @@ def test_attention_of_sequences_that_go_back():
     assert (space[n:] == 255).all()
     sga.cache_append(Q, Q, ck, cv, batch)
     assert torch.isfinite(ck).all() and torch.isfinite(cv).all()
+
+
+def test_rotary_of_the_most_rows():
+    """2^31 - 1 rows, the most that a call takes: the first, the last and some between them."""
+    L = (1 << 31) - 1
+    x = torch.zeros(1, L, 2, dtype=torch.float16, device="cuda")
+    at = torch.tensor([0, 1, 4095, (1 << 22) + 3, (1 << 30) + 5, L - 4, L - 1], device="cuda")
+    x[0, at] = torch.arange(1, 15, device="cuda").view(7, 2).half()
+    rot = sga.Rotary(torch.full((1,), 0.37, dtype=torch.float64, device="cuda"))
+    want, size = S.rotate(host(x[:, at]), at.cpu().numpy() - 7, np.array([0.37]))
+    assert sga.rotary(x, rot, first=-7, out=x) is x
+    assert within(x[:, at], want, S.rotate_bar(want, size, "f16"))
+    assert int(torch.count_nonzero(x[0, :, 0])) <= 7
