@@ -49,7 +49,7 @@ __device__ __forceinline__ int32_t last_not_above(int32_t n, int64_t x, First fi
   const int lane = threadIdx.x & (kWave - 1);
   int32_t lo = 0, hi = n;
   while (hi - lo > 1) {
-    const int32_t step = (hi - lo + kWave - 1) / kWave;
+    const int32_t step = (hi - lo - 1) / kWave + 1;
     const int64_t at = (int64_t)lo + (int64_t)lane * step;
     const int n_below = __popcll(__ballot(at < hi && first((int32_t)(at < hi ? at : hi - 1)) <= x));
     lo += (n_below > 0 ? n_below - 1 : 0) * step;

@@ -744,3 +744,25 @@ def test_rotary_of_the_most_rows():
     assert sga.rotary(x, rot, first=-7, out=x) is x
     assert within(x[:, at], want, S.rotate_bar(want, size, "f16"))
     assert int(torch.count_nonzero(x[0, :, 0])) <= 7
+
+
+def test_append_of_the_most_sequences():
+    """2^31 - 1 sequences, the most that a batch may have, all but three without new tokens; attention refuses as many."""
+    S_, d, page = (1 << 31) - 1, 32, 16
+    who = [5, (1 << 30) + 77, S_ - 1]
+    table = torch.full((S_, 1), -1, dtype=torch.int32, device="cuda")
+    ptr, lens = torch.zeros(S_ + 1, dtype=torch.int64, device="cuda"), torch.zeros(S_, dtype=torch.int32, device="cuda")
+    for i, s in enumerate(who):
+        table[s, 0] = 2 - i
+        ptr[s + 1:] += 1
+        lens[s] = 3 + i
+    batch = sga.PagedBatch(table, ptr, lens, 3, page, 3)
+    ck, cv = caches(3, 1, page, d, "f16", 1)
+    before = [ck.clone(), cv.clone()]
+    K, V = tokens(1, 3, d, "f16", 2), tokens(1, 3, d, "f16", 3)
+    sga.cache_append(K, V, ck, cv, batch)
+    for i in range(3):
+        before[0][2 - i, :, 2 + i], before[1][2 - i, :, 2 + i] = K[:, i], V[:, i]
+    assert torch.equal(ck, before[0]) and torch.equal(cv, before[1])
+    with pytest.raises(sga.SgaError):
+        sga.attention_paged(K, ck, cv, batch, full(16), 0.1)
