@@ -766,3 +766,134 @@ def test_append_of_the_most_sequences():
     assert torch.equal(ck, before[0]) and torch.equal(cv, before[1])
     with pytest.raises(sga.SgaError):
         sga.attention_paged(K, ck, cv, batch, full(16), 0.1)
+
+
+# ---- which kernel takes a call, and calls of many sequences -----------------------------------------
+def kernel_of(dtype, T, n_seqs, group, d, spec, causal):
+    """Rows of keys of 128 to 512 bytes and more than 32 rows per sequence on average take tiles of 128 rows, unless full precision at
+    d <= 64 meets a window of fewer than 512 keys."""
+    row = d * (4 if dtype == "f32" else 2)
+    narrow = dtype == "f32" and d <= 64 and (1 if causal else 2) * spec.window < 512
+    return "paged_chunk_kernel" if 128 <= row <= 512 and not narrow and T * group > 32 * n_seqs else "paged_kernel"
+
+
+def attend_on_device(Q, ck, cv, table, new, length, spec, scale, causal, dtype, once):
+    """serving_oracle.attend for whole sequences at a time, in 64 bits on the device: (O, lse, bar of O, bar of lse) of the real rows."""
+    page, Hkv, d = ck.shape[2], ck.shape[1], ck.shape[3]
+    G, parts = Q.shape[0] // Hkv, {"f32": 0.0, "f16": 2.0 ** -21, "bf16": 2.0 ** -15}[dtype] if not once else S.HALF_STEP[dtype]
+    out = [[], [], [], []]
+    row = 0
+    for s, (n, L) in enumerate(zip(new, length)):
+        if n == 0:
+            continue
+        at = torch.arange(L, device="cuda")
+        where = torch.from_numpy(table[s].astype(np.int64)).cuda()[at // page]
+        k, v = (c[where, :, at % page].double().transpose(0, 1).unsqueeze(1) for c in (ck, cv))              # [Hkv, 1, L, d]
+        q = Q[:, row:row + n].double().reshape(Hkv, G, n, d)
+        i, j = torch.arange(L - n, L, device="cuda")[:, None], at[None]
+        see = (i - j).abs() <= spec.window
+        if spec.kind == KIND_GLOBAL_LOCAL:
+            see |= (j < spec.n_global) | (i < spec.n_global)
+        see &= (i < spec.L) & (j < spec.L)
+        if causal:
+            see &= j <= i
+        z = scale * torch.matmul(q, k.transpose(-1, -2).contiguous())
+        size = torch.matmul(q.abs(), k.abs().transpose(-1, -2).contiguous()).masked_fill_(~see, 0.0).amax(-1)
+        off = d * 2.0 ** -24 * abs(scale) * size + 2.0 ** -22 * (1 + z.abs().masked_fill_(~see, 0.0).amax(-1))
+        z.masked_fill_(~see, -math.inf)
+        lse = torch.logsumexp(z, -1)
+        w = (z - torch.where(lse.isinf(), 0.0, lse).unsqueeze(-1)).exp()
+        O, share = torch.matmul(w, v), torch.matmul(w, v.abs())
+        bar = share * (2 * off + parts + (4 + math.sqrt(L)) * 2.0 ** -23).unsqueeze(-1) + O.abs() * S.HALF_STEP[dtype]
+        if dtype == "f16":
+            bar += 2.0 ** -35 * v.abs().sum(-2, keepdim=True) + 2.0 ** -25        # (the largest numerator of a row is 2^10 or more)
+        for x, y in zip(out, (O, lse, bar, 2 * off + 2.0 ** -22 * (1 + lse.abs()))):
+            x.append(y.reshape(Hkv * G, n, *y.shape[3:]))
+        row += n
+    return [host(torch.cat(x, 1)) for x in out]
+
+
+def check_on_device(dtype, new, length, page, Hq, Hkv, d, spec, causal=True, workspace=True, seed=0):
+    print("attend", dtype, len(new), sum(new), max(length), page, Hq, Hkv, d, spec, causal, flush=True)
+    batch, table, ptr, lens, n_pages, T = batch_of(new, length, page, seed=seed, padding=1)
+    ck, cv = caches(n_pages, Hkv, page, d, dtype, seed + 1)
+    Q, scale = tokens(Hq, T, d, dtype, seed + 3), 1 / math.sqrt(d)
+    want = kernel_of(dtype, T, len(new), Hq // Hkv, d, spec, causal)
+    ws = sga.alloc_paged_workspace(batch, spec, Hq, Hkv, d, dtype) if workspace else None
+    O, lse = torch.full((Hq, T, d), 7.0, dtype=DTYPE[dtype], device="cuda"), torch.full((Hq, T), 7.0, device="cuda")
+    assert sga.sga_profile_enable(1) == 0
+    sga.attention_paged(Q, ck, cv, batch, spec, scale, causal=causal, O=O, lse=lse, workspace=ws)
+    torch.cuda.synchronize()
+    kernel = sga.sga_profile_last_kernel()
+    sga.sga_profile_enable(0)
+    assert kernel == want
+    o, l, bar, l_bar = attend_on_device(Q, ck, cv, table, new, length, spec, scale, causal, dtype, want == "paged_chunk_kernel" and dtype != "f32")
+    assert within(O[:, :T - 1], o, bar) and within(lse[:, :T - 1], l, l_bar)
+    assert (O[:, T - 1:] == 7).all() and (lse[:, T - 1:] == 7).all()
+    return kernel
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("d,window,new,kernel", [
+    (32, 1 << 20, 33, "paged_chunk_kernel"), (64, 1 << 20, 32, "paged_kernel"), (64, 1 << 20, 33, "paged_chunk_kernel"),
+    (128, 1 << 20, 33, "paged_chunk_kernel"), (128, 100, 200, "paged_chunk_kernel"), (256, 1 << 20, 200, "paged_kernel"),
+    (64, 512, 200, "paged_chunk_kernel"), (64, 255, 200, "paged_kernel"), (32, 255, 200, "paged_kernel"), (32, 512, 200, "paged_chunk_kernel"),
+])
+def test_attention_kernels_of_full_precision(d, window, new, kernel, causal):
+    for page in (16, 24):
+        spec = MaskSpec(KIND_SLIDING, 1300, window=window)
+        # (padding counts: the one row of it is left out of the sequences' tokens)
+        assert check_on_device("f32", [2 * new - 1 - new // 2, new // 2], [1300, 900], page, 2, 2, d, spec, causal) == kernel
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_attention_of_single_tokens_beside_prompts(dtype):
+    """What a server sends at once: many single tokens and a prompt.  The kernel goes by the average."""
+    rng = np.random.default_rng(1)
+    behind = [int(x) for x in rng.integers(1, 900, 300)]
+    for n, prompt, kernel in ((300, 4096, "paged_kernel"), (60, 4096, "paged_chunk_kernel")):
+        new, length = [1] * n, behind[:n]
+        new.insert(n // 3, prompt)
+        length.insert(n // 3, prompt + 500)
+        for spec in (full(5000), MaskSpec(KIND_GLOBAL_LOCAL, 5000, window=600, n_global=20)):
+            assert check_on_device(dtype, new, length, 16, 2, 2, 64, spec) == kernel
+    assert check_on_device(dtype, new, length, 24, 8, 2, 128, full(5000), workspace=False) == "paged_chunk_kernel"
+
+
+@pytest.mark.parametrize("dtype,d", [("f16", 64), ("bf16", 128), ("f32", 64)])
+def test_attention_of_thousands_of_sequences(dtype, d):
+    rng = np.random.default_rng(2)
+    length = [int(x) for x in rng.integers(1, 60, 3000)]
+    length[17], length[2999] = 4000, 3000
+    for n in (700, 3000):
+        check_on_device(dtype, [1] * n, length[-n:], 16, 2, 1, d, full(4000))
+    new = [int(x) for x in rng.integers(0, 90, 150)]           # long chunks of more sequences than a wavefront looks at at a time, in pieces
+    length = [a + int(b) for a, b in zip(new, rng.integers(0, 3000, 150))]
+    assert check_on_device(dtype, new, length, 16, 1, 1, d, full(4000)) == "paged_chunk_kernel"
+    assert check_on_device(dtype, new, length, 5, 1, 1, d, MaskSpec(KIND_GLOBAL_LOCAL, 4000, window=1500, n_global=9), causal=False) \
+        == "paged_chunk_kernel"
+
+
+@pytest.mark.parametrize("page", [64, 24])
+@pytest.mark.parametrize("new", [1, 9, 150])
+def test_attention_far_pages_of_every_kernel(new, page):
+    """Offsets of more than 2^31 elements: single tokens, drafts and long chunks, pages of whole 16-key tiles and others."""
+    Hkv, d, length = 8, 128, 150
+    n_pages, columns = (1 << 31) // (page * Hkv * d) + 40, -(-length // page)
+    ck, cv = (torch.empty(n_pages, Hkv, page, d, dtype=torch.float16, device="cuda") for _ in range(2))
+    table = np.array([[n_pages - 1 - 2 * c if c % 2 == 0 else c for c in range(columns)]], dtype=np.int32)
+    assert int(table[0, 0]) * page * Hkv * d > 1 << 31
+    K, V, Q = (tokens(h, length, d, "f16", s) for h, s in ((Hkv, 1), (Hkv, 2), (16, 3)))
+    dev = [torch.from_numpy(x).cuda() for x in (table, np.array([0, length]), np.array([length], dtype=np.int32))]
+    sga.cache_append(K, V, ck, cv, sga.PagedBatch(*dev, length, page, n_pages))
+    for t in range(length):
+        assert torch.equal(ck[int(table[0, t // page]), :, t % page], K[:, t]) and torch.equal(cv[int(table[0, t // page]), :, t % page], V[:, t])
+    dev[1] = torch.tensor([0, new], device="cuda")
+    batch = sga.PagedBatch(*dev, new, page, n_pages)
+    at = torch.from_numpy(table[0].astype(np.int64)).cuda()
+    small = [c[at] for c in (ck, cv)]
+    spec = MaskSpec(KIND_GLOBAL_LOCAL, length, window=100, n_global=3)
+    want, lse, bar, lse_bar = S.attend(host(Q[:, :new]), host(small[0]), host(small[1]), np.arange(columns)[None], np.array([0, new]),
+                                       np.array([length]), spec, 0.1, True, "f16", new * 2 > 32)
+    got = sga.attention_paged(Q[:, :new], ck, cv, batch, spec, 0.1, want_lse=True)
+    assert within(got[0], want, bar) and within(got[1], lse, lse_bar)
