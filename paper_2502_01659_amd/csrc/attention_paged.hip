@@ -34,9 +34,13 @@ constexpr int kWaves = 4;             // wavefronts of a workgroup, which take i
 constexpr int kLeastPiece = 1024, kLeastPieceF32 = 256;
 constexpr int kChunkPieces = 1536;
 
-// Sequences with more rows than this on average take tiles of 128 rows.  (us, below / above: 32 rows behind 4k to 16k, 32 sequences,
-// bf16, d = 128 231 / 251, d = 64 122 / 139; 40 rows 189 / 169; 64 rows, 16 sequences 202 / 182; 29 rows at d = 256 54 / 64.)
-constexpr int kTokenRows = 32;
+// Sequences with more rows than this on average take tiles of 128 rows.  (us, short tiles / tiles of 128 rows, 8 heads, behind 4k to 16k; bf16, 32
+// sequences: 29 rows d = 64 123 / 137, d = 128 232 / 252, d = 256 427 / 504; 33 rows 191 / 142, 391 / 255, 854 / 511.  Full precision, 8 sequences, where
+// a tile of 128 rows costs the same however few rows it has, since the matrix cores bound it: 33 rows d = 32 79 / 104, d = 64 123 / 191, d = 128 284 / 380;
+// 64 rows d = 128 370 / 391; 80 rows 451 / 402; 96 rows d = 32 105 / 121, d = 64 169 / 199; 128 rows 127 / 118, 222 / 210; but where all of a
+// sequence is 256 tokens or fewer a short tile's chain of loads is what counts: 16 sequences of 80 tokens d = 32 26 / 15, d = 64 30 / 19, the last 80 of
+// 256 32 / 22, 42 / 30, of 512 32 / 31, 45 / 47.)
+constexpr int token_rows(bool single, int d, int64_t tokens) { return !single || (d <= 64 && tokens <= 256) ? 32 : d > 64 ? 64 : 96; }
 
 // Numerators of fp16 storage are kept 2^kRaise times as large as against the row's largest score: fp16 ends at 2^-25 (2^-14 with all
 // its bits), and a long context can hold most of its weight in tokens that are each below that beside a few large ones.  The
@@ -1576,18 +1580,20 @@ sga_status launch_paged_type(const PagedAttention& a) {
 PagedPlan plan_paged(const PagedAttention& a) {
   PagedPlan p{kRows, 0, 0, 1, 0};
   const int64_t all_rows = (int64_t)a.batch.n_tokens * a.group.value;
-  // (fp32 at d <= 64 under a narrow window: a wavefront meets 9 of the 13 blocks of its workgroup's tile, and waits in the others; us,
-  // tiles of 16 / 128 rows: +-128 and 16 global rows 147 / 154, 128 causal 96 / 98; but at d = 128, 256 causal 315 / 296)
-  const bool narrow = a.dtype == SGA_F32 && a.d <= 64 && (a.causal ? 1 : 2) * (int64_t)a.window < 512;
-  if (chunk_fits((int64_t)a.d * (a.dtype == SGA_F32 ? 4 : 2)) && !narrow && all_rows > (int64_t)kTokenRows * a.batch.n_seqs)
+  // (fp32 at d = 64 under a narrow window: a wavefront meets 9 of the 13 blocks of its workgroup's tile, and waits in the others; us,
+  // short tiles / tiles of 128 rows, documents of 900 to 4,096 tokens, 8 heads: 128 causal 79 / 90, +-64 80 / 92, +-128 118 / 120, with 16 global
+  // rows and pages of 24 139 / 148; 300 causal 120 / 125, 400 156 / 141, +-200 174 / 151.  At d = 32 128 causal 53 / 42, +-64 53 / 42; at d = 128, 256 causal 315 / 296.)
+  const bool single = a.dtype == SGA_F32, narrow = single && a.d == 64 && (a.causal ? 1 : 2) * (int64_t)a.window <= 256;
+  const int64_t room = (int64_t)a.batch.pages_per_seq * a.batch.page.value, tokens = a.L < room ? a.L : room;      // of a sequence at most
+  if (chunk_fits((int64_t)a.d * (single ? 4 : 2)) && !narrow && all_rows > (int64_t)token_rows(single, a.d, tokens) * a.batch.n_seqs)
     p.tile_rows = kChunkRows;
   else if (all_rows > (int64_t)kRows * a.batch.n_seqs && !(a.dtype == SGA_F32 && a.d > 64))
     p.tile_rows = 2 * kRows;
   const int64_t tiles = all_rows / p.tile_rows + a.batch.n_seqs;
   if (tiles >= int64_t(1) << 24) return p;                 // (rows of a sequence are counted in 31 bits)
   // keys that a tile meets at most
-  const int64_t room = (int64_t)a.batch.pages_per_seq * a.batch.page.value, step = p.tile_rows / (int64_t)a.group.value;
-  int64_t keys = a.L < room ? a.L : room;
+  const int64_t step = p.tile_rows / (int64_t)a.group.value;
+  int64_t keys = tokens;
   const int64_t window = (a.causal ? 1 : 2) * (int64_t)a.window + step + 1 + a.n_global;
   if (window < keys && !(a.n_global > 0 && !a.causal)) keys = window;
   if (p.tile_rows == kChunkRows) {

@@ -640,14 +640,14 @@ def test_two_streams_at_once():
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
-@pytest.mark.parametrize("new", [1, 20, 64])
+@pytest.mark.parametrize("new", [1, 20, 100])
 @pytest.mark.parametrize("spoiled", [False, True])           # one value of a token is infinite: its channel is, the others are as they were
 def test_attention_of_many_small_weights(dtype, new, spoiled):
     """Long contexts often give a few first tokens nearly all of the weight: here tokens 0, 32, 64 and 96, one for each wavefront's first
     block, whose values are 0, and 32,764 tokens `gap` below them, which alone decide O.  Their weights are far below the smallest
     number of fp16; together they are not.  Scores are 0 and gap exactly, so O = e^-gap sum(v) / (4 + 32,764 e^-gap)."""
     n, d, page = 32768, 64, 64
-    long = long_chunks(dtype, new, 1, 1, d, page) or (dtype == "f32" and new > 32)
+    long = kernel_of(dtype, new, 1, 1, d, full(n), False, n) == "paged_chunk_kernel"
     batch, table, ptr, lens, n_pages, T = batch_of([new], [n], page)
     ck, cv = (torch.zeros(n_pages, 1, page, d, dtype=DTYPE[dtype], device="cuda") for _ in range(2))
     values = torch.rand(n, d, generator=torch.Generator().manual_seed(1)).add_(0.5).to(DTYPE[dtype])
@@ -769,12 +769,13 @@ def test_append_of_the_most_sequences():
 
 
 # ---- which kernel takes a call, and calls of many sequences -----------------------------------------
-def kernel_of(dtype, T, n_seqs, group, d, spec, causal):
-    """Rows of keys of 128 to 512 bytes and more than 32 rows per sequence on average take tiles of 128 rows, unless full precision at
-    d <= 64 meets a window of fewer than 512 keys."""
+def kernel_of(dtype, T, n_seqs, group, d, spec, causal, most):
+    """Rows of keys of 128 to 512 bytes and more than 32 rows per sequence on average (full precision 96, 64 at d = 128, 32 up to d = 64 where a
+    sequence has 256 tokens at most) take tiles of 128 rows, unless full precision at d = 64 meets a window of 256 keys or fewer."""
     row = d * (4 if dtype == "f32" else 2)
-    narrow = dtype == "f32" and d <= 64 and (1 if causal else 2) * spec.window < 512
-    return "paged_chunk_kernel" if 128 <= row <= 512 and not narrow and T * group > 32 * n_seqs else "paged_kernel"
+    narrow = dtype == "f32" and d == 64 and (1 if causal else 2) * spec.window <= 256
+    rows = 32 if dtype != "f32" or (d <= 64 and min(spec.L, most) <= 256) else 64 if d > 64 else 96
+    return "paged_chunk_kernel" if 128 <= row <= 512 and not narrow and T * group > rows * n_seqs else "paged_kernel"
 
 
 def attend_on_device(Q, ck, cv, table, new, length, spec, scale, causal, dtype, once):
@@ -818,7 +819,7 @@ def check_on_device(dtype, new, length, page, Hq, Hkv, d, spec, causal=True, wor
     batch, table, ptr, lens, n_pages, T = batch_of(new, length, page, seed=seed, padding=1)
     ck, cv = caches(n_pages, Hkv, page, d, dtype, seed + 1)
     Q, scale = tokens(Hq, T, d, dtype, seed + 3), 1 / math.sqrt(d)
-    want = kernel_of(dtype, T, len(new), Hq // Hkv, d, spec, causal)
+    want = kernel_of(dtype, T, len(new), Hq // Hkv, d, spec, causal, table.shape[1] * page)
     ws = sga.alloc_paged_workspace(batch, spec, Hq, Hkv, d, dtype) if workspace else None
     O, lse = torch.full((Hq, T, d), 7.0, dtype=DTYPE[dtype], device="cuda"), torch.full((Hq, T), 7.0, device="cuda")
     assert sga.sga_profile_enable(1) == 0
@@ -835,15 +836,19 @@ def check_on_device(dtype, new, length, page, Hq, Hkv, d, spec, causal=True, wor
 
 @pytest.mark.parametrize("causal", [True, False])
 @pytest.mark.parametrize("d,window,new,kernel", [
-    (32, 1 << 20, 33, "paged_chunk_kernel"), (64, 1 << 20, 32, "paged_kernel"), (64, 1 << 20, 33, "paged_chunk_kernel"),
-    (128, 1 << 20, 33, "paged_chunk_kernel"), (128, 100, 200, "paged_chunk_kernel"), (256, 1 << 20, 200, "paged_kernel"),
-    (64, 512, 200, "paged_chunk_kernel"), (64, 255, 200, "paged_kernel"), (32, 255, 200, "paged_kernel"), (32, 512, 200, "paged_chunk_kernel"),
+    (32, 1 << 20, 96, "paged_kernel"), (32, 1 << 20, 97, "paged_chunk_kernel"), (64, 1 << 20, 96, "paged_kernel"),
+    (64, 1 << 20, 97, "paged_chunk_kernel"), (128, 1 << 20, 64, "paged_kernel"), (128, 1 << 20, 65, "paged_chunk_kernel"),
+    (128, 100, 200, "paged_chunk_kernel"), (256, 1 << 20, 200, "paged_kernel"), (64, 257, 200, "paged_chunk_kernel"),
+    (64, 128, 200, "paged_kernel"), (32, 20, 200, "paged_chunk_kernel"),
 ])
 def test_attention_kernels_of_full_precision(d, window, new, kernel, causal):
     for page in (16, 24):
         spec = MaskSpec(KIND_SLIDING, 1300, window=window)
         # (padding counts: the one row of it is left out of the sequences' tokens)
         assert check_on_device("f32", [2 * new - 1 - new // 2, new // 2], [1300, 900], page, 2, 2, d, spec, causal) == kernel
+    for length, short in ((256, "paged_chunk_kernel"), (257, "paged_kernel")):
+        if d <= 64 and new <= 97:
+            assert check_on_device("f32", [40, 50], [length, 60], 1, 2, 2, d, full(1300), causal) == short
 
 
 @pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
@@ -851,7 +856,7 @@ def test_attention_of_single_tokens_beside_prompts(dtype):
     """What a server sends at once: many single tokens and a prompt.  The kernel goes by the average."""
     rng = np.random.default_rng(1)
     behind = [int(x) for x in rng.integers(1, 900, 300)]
-    for n, prompt, kernel in ((300, 4096, "paged_kernel"), (60, 4096, "paged_chunk_kernel")):
+    for n, prompt, kernel in ((300, 4096, "paged_kernel"), (30, 4096, "paged_chunk_kernel")):
         new, length = [1] * n, behind[:n]
         new.insert(n // 3, prompt)
         length.insert(n // 3, prompt + 500)
@@ -867,7 +872,7 @@ def test_attention_of_thousands_of_sequences(dtype, d):
     length[17], length[2999] = 4000, 3000
     for n in (700, 3000):
         check_on_device(dtype, [1] * n, length[-n:], 16, 2, 1, d, full(4000))
-    new = [int(x) for x in rng.integers(0, 90, 150)]           # long chunks of more sequences than a wavefront looks at at a time, in pieces
+    new = [int(x) for x in rng.integers(0, 90 if dtype != "f32" else 250, 150)]           # long chunks of more sequences than a wavefront looks at at a time, in pieces
     length = [a + int(b) for a, b in zip(new, rng.integers(0, 3000, 150))]
     assert check_on_device(dtype, new, length, 16, 1, 1, d, full(4000)) == "paged_chunk_kernel"
     assert check_on_device(dtype, new, length, 5, 1, 1, d, MaskSpec(KIND_GLOBAL_LOCAL, 4000, window=1500, n_global=9), causal=False) \
