@@ -1597,8 +1597,10 @@ PagedPlan plan_paged(const PagedAttention& a) {
   const int64_t window = (a.causal ? 1 : 2) * (int64_t)a.window + step + 1 + a.n_global;
   if (window < keys && !(a.n_global > 0 && !a.causal)) keys = window;
   if (p.tile_rows == kChunkRows) {
-    // cut where the chip would have less than four rounds of tiles; see piece_of for how many pieces that can be
-    p.splits = tiles * a.Hkv < 2048 && keys > kLeastShare ? 2 : 1;
+    // cut where the chip would have less than four rounds of tiles, and where a tile can be long enough for two pieces (see piece_of; full
+    // precision would cut from 128 keys on, for which a join does not pay)
+    const int64_t least = single ? kLeastPieceF32 : kLeastPiece;
+    p.splits = tiles * a.Hkv < 2048 && keys > kLeastShare && 2 * (keys + kTileCost) >= 3 * least ? 2 : 1;
     const int64_t slots = tiles + (p.splits > 1 ? (kChunkPieces + a.Hkv - 1) / a.Hkv + 1 : 0);
     if (slots * a.Hkv + 8 >= int64_t(1) << 24) return p;                    // (a grid holds fewer than 2^32 threads)
     p.slots = (int32_t)slots;

@@ -209,3 +209,15 @@ def test_a_batch_and_a_rotation_keep_what_they_were_made_of():
         with pytest.raises(AttributeError, match=name):
             delattr(rot, name)
     assert (rot._desc.frequencies, rot._desc.channels, rot.channels) == (f.data_ptr(), 64, 64)
+
+
+def test_workspace_of_long_chunks_that_are_not_cut():
+    """A tile of 128 rows is cut into pieces of at least 1,024 keys and their cost: up to 1,279 keys there is nothing to join."""
+    def size(keys, dtype, window=None):
+        b = batch(n_seqs=2, n_tokens=400, pages_per_seq=-(-keys // 16), page_stride=8 * 16 * 128)
+        st, n = sga.sga_paged_workspace_bytes(b, MaskSpec(KIND_SLIDING, keys, window=keys if window is None else window), 8, 8, 128, dtype)
+        assert st == 0
+        return n
+    assert size(1279, 2) == 0 and size(1280, 2) > 0 and size(1279, 1) == 0
+    assert size(65536, 2, window=500) == 0 and size(65536, 2, window=1200) > 0
+    assert size(512, 0) == 0 and size(513, 0) > 0             # full precision: pieces of 256, from 513 keys on
