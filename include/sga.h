@@ -457,9 +457,15 @@ sga_status sga_cache_append(const sga_rows* K, const sga_rows* V, void* cache_k,
  *   workspace  device, 256-byte aligned, optional: partial states of split sequences.  With one of
  *              sga_paged_workspace_bytes a few long sequences spread over the chip; without one, or
  *              with a smaller one, each group of queries and key head is one workgroup's work.
- *              Its contents need not be preserved; calls that overlap in time need one each.
+ *              Its contents need not be preserved; calls that overlap in time need one each.  (Its size belongs to
+ *              the batch's sizes and the mask: ask again for another mask.)
  * A token that sees nothing gets O = 0, lse = -inf.  Tokens that a query does not see have no
  * influence on it, whatever their keys and values hold (infinities, NaN, memory never written).
+ * Rounding: scores, sums and lse are in 32 bits.  16-bit storage: where the sequences of a call have more than 32
+ * rows on average (n_tokens * Hq / Hkv / n_seqs, padding and sequences without new tokens counted; d >= 64),
+ * softmax weights are rounded to the storage type once before they meet V, which moves O by at most 2^-11 (fp16) or 2^-8 (bf16) of
+ * the weighted mean of |V|; else they are held as two such numbers.  Calls that must not differ by that are kept on one side of the line.
+ * fp16 weights below 2^-35 (in the second case 2^-40) of a row's largest are lost.
  * Supported: d = 32, 64, 128, 256.  Addresses and strides are multiples of 16 bytes.  Results do not
  * depend on the order in which the work runs.  Kernels only: nothing is allocated and the host does not wait.
  * Errors: SGA_ERR_INVALID_ARG, SGA_ERR_UNSUPPORTED (d, other mask kinds), SGA_ERR_OVERFLOW

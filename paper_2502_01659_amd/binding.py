@@ -602,6 +602,9 @@ def rotary_frequencies(channels, base=10000.0, scaling=None, factor=1.0, origina
              "parts"     by the turns that a pair makes over original_length: from fast_turns on its frequency
                          stays, up to slow_turns it is divided by factor, between them in proportion; the magnitude
                          is 1 + ln(factor) / 10
+
+    The formulas are published: "linear" is the position interpolation of Chen et al. (2023, arXiv 2306.15595), "base" and "parts"
+    with its magnitude are the scaled base and the interpolation by parts of Peng et al. (2023, arXiv 2309.00071).
     """
     import math
     import torch
@@ -663,7 +666,8 @@ class Rotary(_Fixed):
 
 def rotary(X, rotary, positions=None, first=0, inverse=False, out=None):
     """Rotate [H, L, d] by position: row t has positions[t] (int64 [L]), or first + t.  inverse=True turns back: of a
-    gradient, that is the gradient of the input.  out may be X."""
+    gradient, that is the gradient of the input.  (Like the package's other calls it records no history: a backward pass calls it
+    again with inverse=True.)  out may be X."""
     _check_tokens(X, "X")
     rotary._check(X)
     H, L, d = X.shape
@@ -749,7 +753,7 @@ class PagedBatch(_Fixed):
 
 def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None):
     """Write the batch's new keys (rotated) and values, [Hkv, n_tokens, d], into their pages, and rotate the queries Q
-    beside them.  Returns Q_out (which may be Q) if Q is given."""
+    beside them.  Returns Q_out (which may be Q) if Q is given; one that is made here holds nothing in padding rows."""
     _check_tokens(K, "K", T=batch.n_tokens)
     struct, Hkv = batch._caches(K, cache_k, cache_v)
     index, shape, dtype = batch.device_index, K.shape, K.dtype
@@ -788,7 +792,8 @@ def paged_workspace_bytes(batch, spec: MaskSpec, Hq, Hkv, d, dtype) -> int:
 
 
 def alloc_paged_workspace(batch, spec: MaskSpec, Hq, Hkv, d, dtype):
-    """Workspace for attention_paged calls of this batch and mask (calls that overlap in time need one each)."""
+    """Workspace for attention_paged calls of this batch and mask (calls that overlap in time need one each).  A call under another
+    mask may need more; with a smaller one than its own it runs without cutting long sequences, which is slower and as right."""
     import torch
     return torch.empty(paged_workspace_bytes(batch, spec, Hq, Hkv, d, dtype), dtype=torch.uint8, device=batch.device)
 
@@ -797,7 +802,8 @@ def attention_paged(Q, cache_k, cache_v, batch, spec: MaskSpec, scale, causal=Tr
                     want_lse=False):
     """Attention of the batch's new tokens, Q [Hq, n_tokens, d], over the paged cache under a sliding or global + local mask
     of spec.L tokens (window >= L: every token), of earlier tokens only if causal.  Consecutive Hq / Hkv query heads share
-    a key head.  Returns O (and lse [Hq, n_tokens] if requested); a token that sees nothing has O = 0, lse = -inf."""
+    a key head.  Returns O (and lse [Hq, n_tokens] if requested); a token that sees nothing has O = 0, lse = -inf; padding rows
+    are left as they were, in tensors that are made here with whatever memory held."""
     _check_tokens(Q, "Q", T=batch.n_tokens)
     struct, Hkv = batch._caches(Q, cache_k, cache_v)
     Hq, T, d = Q.shape

@@ -652,9 +652,10 @@ struct Asked {
 
 // N: 16-row groups of a tile, which share the keys that a wavefront loads.
 // One share after the other of each workgroup's tiles.  Measured (us alone, TB/s of the keys and values that rows see): one
-// token of 64 sequences of 512 to 32,768, 8 key heads of 128, bf16 343 (5.8, a large copy: 5.0), of 160 windows of 2,048, 4 key
-// heads, fp16 114 (4.9); a document of six sequences, window 128, fp32, d = 64 140 (43 TFLOP/s of 154:
-// short tiles, whose first loads two wavefronts per SIMD do not hide; matrix cores 32 % busy).
+// token of 64 sequences of 512 to 32,768, 8 key heads of 128, bf16 349 (5.7, a large copy: 5.0), of 160 windows of 2,048, 4 key
+// heads, fp16 116 (4.8); a document of six sequences, window 128, fp32, d = 64 137 (43 TFLOP/s of 154: matrix cores 32 % busy.  445 of the 512
+// workgroups get five or six tiles, four in a first pass and one or two in a second, so a third of the wavefronts' time passes at the barrier behind it;
+// and first loads of short tiles, which two wavefronts per SIMD do not hide).
 template <typename T, int D, int N, bool kWholeTiles>
 __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1 : 2))) void paged_kernel(
     PagedAttention a) {
@@ -940,7 +941,8 @@ typedef short short4v __attribute__((ext_vector_type(4)));
 constexpr int kChunkRows = 128, kChunkSlots = 4;
 constexpr int kChunkAhead = kChunkSlots - 1;
 // (fp16 ends at 65,504.  From 2^10, the largest right after the reference was raised, 16 equal ones have room for a factor of 3.75 and a
-// single one of 60.)
+// single one of 60, where 2^14 against a largest of 1 left 2^10 and 2^14: us, a prompt of 32,768 tokens under a window of 2,048, 32 heads of 128,
+// scores of deviation 1 / 3 / 6 / 12 1,230 / 1,300 / 1,345 / 1,355 against 1,225 / 1,240 / 1,245 / 1,265.)
 template <typename T>
 constexpr float kMostNumerators = kChunkRaise<T> > 0.f ? 61440.f : 16384.f;
 
