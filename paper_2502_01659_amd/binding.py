@@ -712,11 +712,9 @@ class PagedBatch(_Fixed):
             raise ValueError("seq_len must be contiguous int32 [S]")
         if not page_table.is_cuda or seq_ptr.device != page_table.device or seq_len.device != page_table.device:
             raise ValueError("page_table, seq_ptr and seq_len must be tensors of one device")
-        self.page_table, self.seq_ptr, self.seq_len = page_table, seq_ptr, seq_len
-        self.n_tokens, self.page_size, self.n_pages = int(n_tokens), int(page_size), int(n_pages)
-        self.device = page_table.device
-        self.device_index = page_table.get_device()
-        self._structs = {}
+        # (one update: the check of __setattr__ for each would cost 2 us, and a program may make a batch per step)
+        self.__dict__.update(page_table=page_table, seq_ptr=seq_ptr, seq_len=seq_len, n_tokens=int(n_tokens), page_size=int(page_size),
+                             n_pages=int(n_pages), device=page_table.device, device_index=page_table.get_device(), _structs={})
 
     def _struct(self, page_stride):
         s = self._structs.get(page_stride)
