@@ -46,7 +46,8 @@ constexpr int token_rows(bool single, int d, int64_t tokens) { return !single ||
 // its bits), and a long context can hold most of its weight in tokens that are each below that beside a few large ones.  The
 // reference is that much lower, lse and sums follow from it, and nothing else changes.  Short chunks raise the reference with every larger score,
 // so the largest numerator is 2^15 and what a pair of fp16 numbers loses begins 2^-40 below it; long chunks leave room for scores that grow, and
-// lose 2^-35 (kMostNumerators).
+// lose 2^-35 (kMostNumerators).  (Scores from 2^24 on, whose own step is as large, may pass the end of fp16: such rows are not finite then and are
+// redone in 32 bits, see attend_row.)
 template <typename T>
 constexpr float kRaise = sizeof(T) == 2 && !__is_same(T, bf16_t) ? 15.f : 0.f;
 template <typename T>

@@ -902,3 +902,29 @@ def test_attention_far_pages_of_every_kernel(new, page):
                                        np.array([length]), spec, 0.1, True, "f16", new * 2 > 32)
     got = sga.attention_paged(Q[:, :new], ck, cv, batch, spec, 0.1, want_lse=True)
     assert within(got[0], want, bar) and within(got[1], lse, lse_bar)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("new", [1, 20, 100])
+def test_attention_of_huge_scores(dtype, new):
+    """Scores so large that a step of theirs is more than what numerators are raised by: the tokens that share the largest one have the
+    mean of their values as O, the others nothing."""
+    n, d, page = 300, 64, 16
+    batch, table, ptr, lens, n_pages, T = batch_of([new], [n], page)
+    ck, cv = caches(n_pages, 1, page, d, dtype, 3)
+    ck.zero_()
+    at = torch.from_numpy(table[0].astype(np.int64)).cuda()
+    seen = np.arange(n) % 3 == 1
+    for t in np.nonzero(seen)[0]:
+        ck[at[t // page], 0, t % page, 0] = 1
+    v = host(cv[at, 0].reshape(-1, d)[:n])[seen]
+    Q = torch.zeros(1, T, d, dtype=DTYPE[dtype], device="cuda")
+    Q[..., 0] = 1
+    long = kernel_of(dtype, T, 1, 1, d, full(n), False, n_pages * page) == "paged_chunk_kernel"
+    parts = {"f32": 0.0, "f16": 2.0 ** -21, "bf16": 2.0 ** -15}[dtype] if not long else (0.0 if dtype == "f32" else S.HALF_STEP[dtype])
+    for scale in [2.0 ** k * m for k in (10, 20, 22, 23, 24, 25, 26, 27, 28, 29, 30, 40) for m in (1.0, 1.4)]:
+        print("huge scores", dtype, new, scale, flush=True)
+        O, lse = sga.attention_paged(Q, ck, cv, batch, full(n), scale, causal=False, want_lse=True)
+        bar = np.abs(v.mean(0)) * S.HALF_STEP[dtype] + np.abs(v).mean(0) * (parts + 16 * 2.0 ** -23) + 2.0 ** -25
+        assert within(O, np.broadcast_to(v.mean(0), (1, T, d)), np.broadcast_to(bar, (1, T, d)))
+        assert within(lse, np.full((1, T), scale + math.log(seen.sum())), np.full((1, T), 2.0 ** -21 * scale))
