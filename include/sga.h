@@ -55,8 +55,8 @@ typedef enum {
 } sga_status;
 
 /* Storage type of Q, K, V and O.  Accumulation is always fp32.  SGA_BF16 is taken by the entry
-   points of serving alone (sga_rotary, sga_cache_append, sga_attention_paged); the others refuse
-   it as an unknown type. */
+   points of serving and of generation with drafted tokens alone; the others refuse it as an unknown
+   type. */
 typedef enum { SGA_F32 = 0, SGA_F16 = 1, SGA_BF16 = 2 } sga_dtype;
 
 /* Mask families of Section II-C. */
@@ -478,6 +478,149 @@ sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const voi
                                const sga_mask_desc* mask, int32_t causal, const sga_rows* O, int32_t Hq, int32_t Hkv,
                                int32_t d, float scale, int32_t dtype, float* lse, void* workspace, size_t workspace_bytes,
                                void* stream);
+
+/*
+ * ---- Generation with drafted tokens --------------------------------------------------------------
+ *
+ * A step of generation with drafts: pages for the tokens that come, the tokens' tree, then for every layer keys and queries
+ * normalised, rotated and written, and attention of the tree's tokens over the cache; after the program has chosen
+ * which drafts stay, their keys and values move into place:
+ *   sga_pages_advance, sga_draft_tree_build, { sga_cache_append_normed, sga_attention_tree } per layer, sga_cache_keep,
+ * and again sga_pages_advance, which is told how many stayed.  Arrays are read on the device, so a captured step follows them.
+ */
+
+/*
+ * Free pages: a ring of n_pages entries, of which `count` from place `first` on (around the end) are free pages.
+ *   pages      device, int32 [n_pages], read and written
+ *   state      device, int64 [2]: first, count (brought into 0 .. n_pages - 1 and 0 .. n_pages if they are not)
+ * A page is free, or stands in one place of one sequence's row of the page table.
+ */
+typedef struct {
+  uint32_t struct_bytes;      /* = sizeof(sga_page_pool)                                      */
+  int32_t reserved;           /* 0                                                            */
+  int32_t* pages;
+  int64_t* state;
+} sga_page_pool;
+
+/*
+ * The next step's page tables, packed rows and lengths, from the last step's and what the sequences ask for.
+ * Sequence s has l = seq_len[s] - rows + kept[s] tokens, rows = seq_ptr[s+1] - seq_ptr[s] (kept NULL: l = seq_len[s]; seq_ptr is not
+ * read then).  ask[s] >= 0 tokens more are asked for; ask[s] < 0: the sequence ends (l = 0, it gets no rows).
+ *   Back   go the pages of sequences that end, pages behind the last column that l + ask tokens need, and, with a mask, those that lie
+ *          wholly behind the window of a token at position l and hold no global token.  Their entries become -1.
+ *   Taken  are pages for the entries that are no page among columns ceil(l / page_size) .. ceil((l + ask) / page_size) - 1.
+ *   Granted is a request if it fits the page table's columns, if all such requests up to its sequence's (granted or not) fit n_tokens, and
+ *          if it needs no page or all pages needed up to its sequence are no more than `count`.  A sequence whose request is not
+ *          granted gets no rows and keeps its l tokens (and pages).  Pages that go back are free from the next call on.
+ * Results: page_table, seq_ptr, seq_len = l + granted tokens, the pool's state; pages that go back are put behind the ring's last, in
+ * the order (sequence, column).  The same arrays give the same results whatever runs when.
+ *   batch      read: the last step's.  next: written, alike in sizes; its arrays may be batch's.  (page_stride is not looked at.)
+ *   pool       read; its ring is written.  state_out: device, int64 [2], written; may be pool's state.
+ *   ask        device, int32 [n_seqs].  kept: device, int32 [n_seqs] (brought into 0 .. rows), or NULL
+ *   mask       host, SGA_MASK_SLIDING or SGA_MASK_GLOBAL_LOCAL (L is not looked at), or NULL: nothing goes back behind a window
+ *   positions  device, int64 [n_tokens], or NULL: written, the place in its sequence of every new token's row
+ *   slots      device, int64 [n_tokens], or NULL: written, page * page_size + row in the page of every new token, -1 without a page
+ *   workspace  device, 256-byte aligned, sga_pages_workspace_bytes; calls that overlap in time need one each
+ * Rows behind the last sequence are left as they were.  n_seqs up to 65,536.
+ * Errors: SGA_ERR_INVALID_ARG, SGA_ERR_UNSUPPORTED (other masks), SGA_ERR_WORKSPACE.
+ */
+sga_status sga_pages_workspace_bytes(const sga_paged_batch* batch, size_t* bytes_out);
+sga_status sga_pages_advance(const sga_paged_batch* batch, const sga_paged_batch* next, const sga_page_pool* pool, int64_t* state_out,
+                             const int32_t* ask, const int32_t* kept, const sga_mask_desc* mask, int64_t* positions, int64_t* slots,
+                             void* workspace, size_t workspace_bytes, void* stream);
+
+/* Norm of a head's row x over its d channels: x_c * (mean x^2 + epsilon)^-1/2 * (weight_c + offset).  The sum of squares is in 32 bits. */
+typedef struct {
+  uint32_t struct_bytes;      /* = sizeof(sga_norm_desc)                                      */
+  int32_t weight_dtype;       /* sga_dtype                                                    */
+  const void* weight;         /* device, [d]; NULL: no weights (offset is not looked at)      */
+  float epsilon;              /* > 0                                                          */
+  float offset;               /* 1 where a model stores its weights' difference from 1        */
+} sga_norm_desc;
+
+/*
+ * Norms every head's row and turns it by its position (sga_rotary), of queries and keys in one pass; results are rounded once.
+ *   Q      read, Q_out written, [Hq][L][d]; K, K_out both NULL, or read and written, [Hkv][L][d].  Each out may be its input
+ *          (same address and strides), else no two may overlap.
+ *   q_norm, k_norm   NULL: not normed.  rotary NULL: not turned.  (A call has to do something: not all are NULL.)
+ *   positions, first, L, d, H, dtype   as for sga_rotary
+ * The gradient: dQ_out is that of the result, dQ that of Q, and dq_weight float32 [d] that of the weights, summed over all rows
+ * (NULL: not asked for; without weights or norm there is none).  dQ may be dQ_out or Q (same address and strides).
+ *   workspace  device, 256-byte aligned, sga_norm_workspace_bytes: needed where a gradient of weights is asked for
+ * The sums run in a fixed order: the same call gives the same bits.
+ * Errors: SGA_ERR_INVALID_ARG as for sga_rotary, SGA_ERR_WORKSPACE.
+ */
+sga_status sga_norm_rotary(const sga_rows* Q, const sga_rows* Q_out, const sga_norm_desc* q_norm, int32_t Hq, const sga_rows* K,
+                           const sga_rows* K_out, const sga_norm_desc* k_norm, int32_t Hkv, const int64_t* positions, int64_t first,
+                           int64_t L, int32_t d, const sga_rotary_desc* rotary, int32_t dtype, void* stream);
+sga_status sga_norm_workspace_bytes(int64_t L, int32_t Hq, int32_t Hkv, int32_t d, size_t* bytes_out);
+sga_status sga_norm_rotary_backward(const sga_rows* Q, const sga_rows* dQ_out, const sga_rows* dQ, const sga_norm_desc* q_norm,
+                                    float* dq_weight, int32_t Hq, const sga_rows* K, const sga_rows* dK_out, const sga_rows* dK,
+                                    const sga_norm_desc* k_norm, float* dk_weight, int32_t Hkv, const int64_t* positions, int64_t first,
+                                    int64_t L, int32_t d, const sga_rotary_desc* rotary, int32_t dtype, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
+/*
+ * A tree of drafted tokens for every sequence of a batch: new token t follows new token parent[t] < t of its sequence, or the last
+ * token before the new ones.  Its keys and values are at place base + t of the cache, base = seq_len - new, but its position is
+ * base + depth[t], depth = its ancestors among the new tokens.
+ *   depth   device, int32 [n_tokens].  Below 0: the row is no token of the tree: nothing is appended for it, and it sees nothing.
+ *   seen    device, [n_tokens][words]: bit t of a row: it sees new token t of its sequence (itself among them)
+ * Tokens from 32 * words on are not seen.  A program may also write both by itself: any bits.
+ */
+typedef struct {
+  uint32_t struct_bytes;      /* = sizeof(sga_draft_tree)                                     */
+  int32_t words;              /* 32-bit words of a row of `seen`, 1 .. 16                     */
+  int32_t* depth;
+  uint32_t* seen;
+} sga_draft_tree;
+
+/*
+ * Writes depth and seen of the batch's rows from their parents: a token sees itself and those of its ancestors that the mask shows
+ * its position.  Rows from 32 * words on of a sequence get depth -1 and no bits; rows behind the last sequence are left as they were.
+ *   parent  device, int32 [n_tokens]: index among the sequence's new tokens; an entry that is none of 0 .. t - 1 stands for the last
+ *           token before them
+ *   mask    host, SGA_MASK_SLIDING or SGA_MASK_GLOBAL_LOCAL
+ * Errors: SGA_ERR_INVALID_ARG, SGA_ERR_UNSUPPORTED (other masks).
+ */
+sga_status sga_draft_tree_build(const int32_t* parent, const sga_paged_batch* batch, const sga_mask_desc* mask,
+                                const sga_draft_tree* tree, void* stream);
+
+/*
+ * sga_cache_append with norms and a tree: keys and queries are normed (k_norm, q_norm; NULL: not) before they are turned (rotary NULL:
+ * not), and with a tree (NULL: none) turned by the tree's positions.  A call with Q needs rotary or q_norm.  Rows that the tree does not
+ * have are left out: nothing is written for them, Q_out neither.
+ */
+sga_status sga_cache_append_normed(const sga_rows* K, const sga_rows* V, void* cache_k, void* cache_v, const sga_paged_batch* batch,
+                                   int32_t Hkv, int32_t d, const sga_rotary_desc* rotary, const sga_norm_desc* k_norm, const sga_rows* Q,
+                                   const sga_rows* Q_out, int32_t Hq, const sga_norm_desc* q_norm, const sga_draft_tree* tree,
+                                   int32_t dtype, void* stream);
+
+/*
+ * sga_attention_paged for the tokens of a tree: of the context, the tokens before the new ones, a token at position
+ * p = base + depth sees what the mask shows it (causally), and of the new tokens those whose bits are set.  Everything else
+ * (empty rows, missing pages, rounding, sizes, workspace, errors) is as there; the workspace's size has its own call.
+ */
+sga_status sga_tree_workspace_bytes(const sga_paged_batch* batch, const sga_mask_desc* mask, const sga_draft_tree* tree, int32_t Hq,
+                                    int32_t Hkv, int32_t d, int32_t dtype, size_t* bytes_out);
+sga_status sga_attention_tree(const sga_rows* Q, const void* cache_k, const void* cache_v, const sga_paged_batch* batch,
+                              const sga_draft_tree* tree, const sga_mask_desc* mask, const sga_rows* O, int32_t Hq, int32_t Hkv,
+                              int32_t d, float scale, int32_t dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The new tokens that stay move into place: of sequence s, the keys and values at place base + path[s][k] of the cache go to place
+ * base + k, for k < count[s], base = seq_len - new.  (A path down a tree of tokens that were appended at their positions: what
+ * moves has been turned as its new place asks.)  Lengths are not changed: sga_pages_advance takes the counts.
+ *   cache_k, cache_v   device, read and written: n_layers caches each, layer_stride elements apart (n_layers 1: not looked at)
+ *   path    device, int32 [n_seqs][path_columns]; an entry outside k .. new - 1 moves nothing.  (Rising paths are never
+ *           below k.)  All moves are of what the cache held before the call.
+ *   count   device, int32 [n_seqs]; no more than path_columns are looked at
+ * Nothing moves from or to a place without a page.  d 2..1024, any dtype of serving.
+ * Errors: SGA_ERR_INVALID_ARG, SGA_ERR_OVERFLOW (layers * Hkv * d of 2^29 and more).
+ */
+sga_status sga_cache_keep(void* cache_k, void* cache_v, const sga_paged_batch* batch, int32_t Hkv, int32_t d, int32_t n_layers,
+                          int64_t layer_stride, const int32_t* path, int32_t path_columns, const int32_t* count, int32_t dtype,
+                          void* stream);
 
 /*
  * Benchmark hook: timing of the dominant attention kernel of each forward call.

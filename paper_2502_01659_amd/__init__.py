@@ -19,7 +19,11 @@ from .binding import (SgaError, PATH_AUTO, PATH_GATHER, PATH_TILE, PATH_TILE_SPL
                       sga_static_scratch_init, sga_static_scratch_bytes, sga_attention_forward_static,
                       sga_rotary, sga_cache_append, sga_paged_workspace_bytes, sga_attention_paged,
                       Rotary, rotary_frequencies, rotary, PagedBatch, cache_append,
-                      paged_workspace_bytes, alloc_paged_workspace, attention_paged)
+                      paged_workspace_bytes, alloc_paged_workspace, attention_paged,
+                      sga_pages_workspace_bytes, sga_pages_advance, sga_norm_rotary, sga_norm_workspace_bytes, sga_norm_rotary_backward,
+                      sga_draft_tree_build, sga_cache_append_normed, sga_tree_workspace_bytes, sga_attention_tree, sga_cache_keep,
+                      PagePool, alloc_pages_workspace, pages_advance, Norm, norm_rotary, norm_workspace_bytes, alloc_norm_workspace,
+                      norm_rotary_backward, DraftTree, build_draft_tree, cache_keep)
 
 __all__ = [
     "SgaError", "PATH_AUTO", "PATH_GATHER", "PATH_TILE", "PATH_TILE_SPLIT", "load", "lib_path",
@@ -37,4 +41,8 @@ __all__ = [
     "sga_rotary", "sga_cache_append", "sga_paged_workspace_bytes", "sga_attention_paged",
     "Rotary", "rotary_frequencies", "rotary", "PagedBatch", "cache_append",
     "paged_workspace_bytes", "alloc_paged_workspace", "attention_paged",
+    "sga_pages_workspace_bytes", "sga_pages_advance", "sga_norm_rotary", "sga_norm_workspace_bytes", "sga_norm_rotary_backward",
+    "sga_draft_tree_build", "sga_cache_append_normed", "sga_tree_workspace_bytes", "sga_attention_tree", "sga_cache_keep",
+    "PagePool", "alloc_pages_workspace", "pages_advance", "Norm", "norm_rotary", "norm_workspace_bytes", "alloc_norm_workspace",
+    "norm_rotary_backward", "DraftTree", "build_draft_tree", "cache_keep",
 ]

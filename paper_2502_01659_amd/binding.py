@@ -64,6 +64,19 @@ class _PagedBatch(ctypes.Structure):
                 ("seq_len", ctypes.c_void_p)]
 
 
+class _PagePool(ctypes.Structure):
+    _fields_ = [("struct_bytes", ctypes.c_uint32), ("reserved", ctypes.c_int32), ("pages", ctypes.c_void_p), ("state", ctypes.c_void_p)]
+
+
+class _NormDesc(ctypes.Structure):
+    _fields_ = [("struct_bytes", ctypes.c_uint32), ("weight_dtype", ctypes.c_int32), ("weight", ctypes.c_void_p),
+                ("epsilon", ctypes.c_float), ("offset", ctypes.c_float)]
+
+
+class _DraftTree(ctypes.Structure):
+    _fields_ = [("struct_bytes", ctypes.c_uint32), ("words", ctypes.c_int32), ("depth", ctypes.c_void_p), ("seen", ctypes.c_void_p)]
+
+
 GRAPH_TILES_COVER_ALL, GRAPH_TILE_PARTS_FIT, GRAPH_ROW_CHUNKS_FIT, GRAPH_ROWS_SHARE_KEYS, GRAPH_ROWS_EVEN = 1, 2, 4, 8, 16
 
 
@@ -129,6 +142,28 @@ def load():
     lib.sga_attention_paged.restype = ctypes.c_int
     lib.sga_attention_paged.argtypes = [rows, vp, vp, batch, P(_MaskDesc), i32, rows, i32, i32, i32, f32, i32, vp, vp,
                                         ctypes.c_size_t, vp]
+    pool, norm, tree, mask, size = P(_PagePool), P(_NormDesc), P(_DraftTree), P(_MaskDesc), P(ctypes.c_size_t)
+    lib.sga_pages_workspace_bytes.restype = ctypes.c_int
+    lib.sga_pages_workspace_bytes.argtypes = [batch, size]
+    lib.sga_pages_advance.restype = ctypes.c_int
+    lib.sga_pages_advance.argtypes = [batch, batch, pool, vp, vp, vp, mask, vp, vp, vp, ctypes.c_size_t, vp]
+    lib.sga_norm_rotary.restype = ctypes.c_int
+    lib.sga_norm_rotary.argtypes = [rows, rows, norm, i32, rows, rows, norm, i32, vp, i64, i64, i32, rotary_desc, i32, vp]
+    lib.sga_norm_workspace_bytes.restype = ctypes.c_int
+    lib.sga_norm_workspace_bytes.argtypes = [i64, i32, i32, i32, size]
+    lib.sga_norm_rotary_backward.restype = ctypes.c_int
+    lib.sga_norm_rotary_backward.argtypes = [rows, rows, rows, norm, vp, i32, rows, rows, rows, norm, vp, i32, vp, i64, i64, i32,
+                                             rotary_desc, i32, vp, ctypes.c_size_t, vp]
+    lib.sga_draft_tree_build.restype = ctypes.c_int
+    lib.sga_draft_tree_build.argtypes = [vp, batch, mask, tree, vp]
+    lib.sga_cache_append_normed.restype = ctypes.c_int
+    lib.sga_cache_append_normed.argtypes = [rows, rows, vp, vp, batch, i32, i32, rotary_desc, norm, rows, rows, i32, norm, tree, i32, vp]
+    lib.sga_tree_workspace_bytes.restype = ctypes.c_int
+    lib.sga_tree_workspace_bytes.argtypes = [batch, mask, tree, i32, i32, i32, i32, size]
+    lib.sga_attention_tree.restype = ctypes.c_int
+    lib.sga_attention_tree.argtypes = [rows, vp, vp, batch, tree, mask, rows, i32, i32, i32, f32, i32, vp, vp, ctypes.c_size_t, vp]
+    lib.sga_cache_keep.restype = ctypes.c_int
+    lib.sga_cache_keep.argtypes = [vp, vp, batch, i32, i32, i32, i64, vp, i32, vp, i32, vp]
     lib.sga_profile_last_kernel.restype = ctypes.c_char_p
     lib.sga_profile_last_kernel.argtypes = []
     _lib = lib
@@ -273,6 +308,61 @@ def sga_attention_paged(Q, cache_k, cache_v, batch, spec, causal, O, Hq, Hkv, d,
                         workspace_bytes_, stream):
     return load().sga_attention_paged(Q, cache_k, cache_v, batch, _desc(spec), causal, O, Hq, Hkv, d, scale, dtype_code, lse,
                                       workspace, workspace_bytes_, stream)
+
+
+def sga_pages_workspace_bytes(batch):
+    """-> (status, bytes)"""
+    out = ctypes.c_size_t(0)
+    st = load().sga_pages_workspace_bytes(batch, ctypes.byref(out))
+    return st, out.value
+
+
+def sga_pages_advance(batch, next_batch, pool, state_out, ask, kept, spec, positions, slots, workspace, workspace_bytes_, stream):
+    """spec: MaskSpec or None"""
+    return load().sga_pages_advance(batch, next_batch, pool, state_out, ask, kept, _desc(spec) if spec is not None else None, positions,
+                                    slots, workspace, workspace_bytes_, stream)
+
+
+def sga_norm_rotary(Q, Q_out, q_norm, Hq, K, K_out, k_norm, Hkv, positions, first, L, d, rotary_desc, dtype_code, stream):
+    return load().sga_norm_rotary(Q, Q_out, q_norm, Hq, K, K_out, k_norm, Hkv, positions, first, L, d, rotary_desc, dtype_code, stream)
+
+
+def sga_norm_workspace_bytes(L, Hq, Hkv, d):
+    """-> (status, bytes)"""
+    out = ctypes.c_size_t(0)
+    st = load().sga_norm_workspace_bytes(L, Hq, Hkv, d, ctypes.byref(out))
+    return st, out.value
+
+
+def sga_norm_rotary_backward(Q, dQ_out, dQ, q_norm, dq_weight, Hq, K, dK_out, dK, k_norm, dk_weight, Hkv, positions, first, L, d,
+                             rotary_desc, dtype_code, workspace, workspace_bytes_, stream):
+    return load().sga_norm_rotary_backward(Q, dQ_out, dQ, q_norm, dq_weight, Hq, K, dK_out, dK, k_norm, dk_weight, Hkv, positions, first,
+                                           L, d, rotary_desc, dtype_code, workspace, workspace_bytes_, stream)
+
+
+def sga_draft_tree_build(parent, batch, spec, tree, stream):
+    return load().sga_draft_tree_build(parent, batch, _desc(spec), tree, stream)
+
+
+def sga_cache_append_normed(K, V, cache_k, cache_v, batch, Hkv, d, rotary_desc, k_norm, Q, Q_out, Hq, q_norm, tree, dtype_code, stream):
+    return load().sga_cache_append_normed(K, V, cache_k, cache_v, batch, Hkv, d, rotary_desc, k_norm, Q, Q_out, Hq, q_norm, tree,
+                                          dtype_code, stream)
+
+
+def sga_tree_workspace_bytes(batch, spec, tree, Hq, Hkv, d, dtype_code):
+    """-> (status, bytes)"""
+    out = ctypes.c_size_t(0)
+    st = load().sga_tree_workspace_bytes(batch, _desc(spec), tree, Hq, Hkv, d, dtype_code, ctypes.byref(out))
+    return st, out.value
+
+
+def sga_attention_tree(Q, cache_k, cache_v, batch, tree, spec, O, Hq, Hkv, d, scale, dtype_code, lse, workspace, workspace_bytes_, stream):
+    return load().sga_attention_tree(Q, cache_k, cache_v, batch, tree, _desc(spec), O, Hq, Hkv, d, scale, dtype_code, lse, workspace,
+                                     workspace_bytes_, stream)
+
+
+def sga_cache_keep(cache_k, cache_v, batch, Hkv, d, n_layers, layer_stride, path, path_columns, count, dtype_code, stream):
+    return load().sga_cache_keep(cache_k, cache_v, batch, Hkv, d, n_layers, layer_stride, path, path_columns, count, dtype_code, stream)
 
 
 # ---- tensor-level helpers ---------------------------------------------------------
@@ -749,9 +839,11 @@ class PagedBatch(_Fixed):
         return self._struct(apart), Hkv
 
 
-def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None):
+def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None, q_norm=None, k_norm=None, tree=None):
     """Write the batch's new keys (rotated) and values, [Hkv, n_tokens, d], into their pages, and rotate the queries Q
-    beside them.  Returns Q_out (which may be Q) if Q is given; one that is made here holds nothing in padding rows."""
+    beside them.  Returns Q_out (which may be Q) if Q is given; one that is made here holds nothing in padding rows.
+    q_norm, k_norm (Norm): queries and keys are normed first.  tree (DraftTree): the new tokens are drafts, at the tree's
+    positions; rows that are none of its tokens are passed over."""
     _check_tokens(K, "K", T=batch.n_tokens)
     struct, Hkv = batch._caches(K, cache_k, cache_v)
     index, shape, dtype = batch.device_index, K.shape, K.dtype
@@ -761,9 +853,17 @@ def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None)
     Hq = 0
     if rotary is not None:
         rotary._check(K)
+    normed = q_norm is not None or k_norm is not None or tree is not None
+    if normed:
+        _check_norm(k_norm, K)
+        _check_norm(q_norm, K)
+        if q_norm is not None and Q is None:
+            raise ValueError("q_norm without Q")
+        if tree is not None:
+            tree._check(batch)
     if Q is not None:
-        if rotary is None:
-            raise ValueError("queries are rotated: a call with Q needs rotary")
+        if rotary is None and q_norm is None:
+            raise ValueError("queries are rotated: a call with Q needs rotary" if not normed else "a call with Q needs rotary or q_norm")
         if Q.dim() != 3 or Q.shape[1:] != shape[1:] or Q.dtype != dtype or Q.get_device() != index:
             raise ValueError("Q must be [Hq, n_tokens, d] and share dtype and device with K")
         if Q_out is None:
@@ -774,6 +874,13 @@ def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None)
         q, q_out, Hq = _strides(Q, "Q"), _strides(Q_out, "Q_out", written=True), Q.shape[0]
     elif Q_out is not None:
         raise ValueError("Q_out without Q")
+    if normed:
+        st = _enqueue(index, sga_cache_append_normed, _strides(K, "K"), _strides(V, "V"), cache_k.data_ptr(), cache_v.data_ptr(), struct,
+                      Hkv, shape[2], rotary._desc if rotary is not None else None, k_norm._desc if k_norm is not None else None, q, q_out,
+                      Hq, q_norm._desc if q_norm is not None else None, tree._desc if tree is not None else None, _serving_code(dtype))
+        if st != 0:
+            raise SgaError(st, "sga_cache_append_normed")
+        return Q_out
     st = _enqueue(index, sga_cache_append, _strides(K, "K"), _strides(V, "V"), cache_k.data_ptr(),
                   cache_v.data_ptr(), struct, Hkv, shape[2], rotary._desc if rotary is not None else None, q, q_out, Hq,
                   _serving_code(dtype))
@@ -782,26 +889,34 @@ def cache_append(K, V, cache_k, cache_v, batch, rotary=None, Q=None, Q_out=None)
     return Q_out
 
 
-def paged_workspace_bytes(batch, spec: MaskSpec, Hq, Hkv, d, dtype) -> int:
+def paged_workspace_bytes(batch, spec: MaskSpec, Hq, Hkv, d, dtype, tree=None) -> int:
+    if tree is not None:
+        tree._check(batch)
+        st, n = sga_tree_workspace_bytes(batch._struct(Hkv * batch.page_size * d), spec, tree._desc, Hq, Hkv, d, _serving_code(dtype))
+        if st != 0:
+            raise SgaError(st, "sga_tree_workspace_bytes")
+        return n
     st, n = sga_paged_workspace_bytes(batch._struct(Hkv * batch.page_size * d), spec, Hq, Hkv, d, _serving_code(dtype))
     if st != 0:
         raise SgaError(st, "sga_paged_workspace_bytes")
     return n
 
 
-def alloc_paged_workspace(batch, spec: MaskSpec, Hq, Hkv, d, dtype):
+def alloc_paged_workspace(batch, spec: MaskSpec, Hq, Hkv, d, dtype, tree=None):
     """Workspace for attention_paged calls of this batch and mask (calls that overlap in time need one each).  A call under another
     mask may need more; with a smaller one than its own it runs without cutting long sequences, which is slower and as right."""
     import torch
-    return torch.empty(paged_workspace_bytes(batch, spec, Hq, Hkv, d, dtype), dtype=torch.uint8, device=batch.device)
+    return torch.empty(paged_workspace_bytes(batch, spec, Hq, Hkv, d, dtype, tree), dtype=torch.uint8, device=batch.device)
 
 
 def attention_paged(Q, cache_k, cache_v, batch, spec: MaskSpec, scale, causal=True, O=None, lse=None, workspace=None,
-                    want_lse=False):
+                    want_lse=False, tree=None):
     """Attention of the batch's new tokens, Q [Hq, n_tokens, d], over the paged cache under a sliding or global + local mask
     of spec.L tokens (window >= L: every token), of earlier tokens only if causal.  Consecutive Hq / Hkv query heads share
     a key head.  Returns O (and lse [Hq, n_tokens] if requested); a token that sees nothing has O = 0, lse = -inf; padding rows
-    are left as they were, in tensors that are made here with whatever memory held."""
+    are left as they were, in tensors that are made here with whatever memory held.
+    tree (DraftTree): the new tokens are drafts.  Each sees what the mask shows its position of the tokens before them, and of them those
+    whose bits are set."""
     _check_tokens(Q, "Q", T=batch.n_tokens)
     struct, Hkv = batch._caches(Q, cache_k, cache_v)
     Hq, T, d = Q.shape
@@ -822,9 +937,293 @@ def attention_paged(Q, cache_k, cache_v, batch, spec: MaskSpec, scale, causal=Tr
         if workspace.get_device() != index or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on Q's device")
         ws_ptr, ws_n = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    if tree is not None:
+        tree._check(batch)
+        if not causal:
+            raise ValueError("a tree's tokens see what is before them: causal=False makes no sense")
+        st = _enqueue(index, sga_attention_tree, _strides(Q, "Q"), cache_k.data_ptr(), cache_v.data_ptr(), struct, tree._desc, spec,
+                      _strides(O, "O", written=True), Hq, Hkv, d, float(scale), _serving_code(Q.dtype),
+                      lse.data_ptr() if lse is not None else None, ws_ptr, ws_n)
+        if st != 0:
+            raise SgaError(st, "sga_attention_tree")
+        return (O, lse) if lse is not None else O
     st = _enqueue(index, sga_attention_paged, _strides(Q, "Q"), cache_k.data_ptr(), cache_v.data_ptr(), struct, spec,
                   1 if causal else 0, _strides(O, "O", written=True), Hq, Hkv, d, float(scale), _serving_code(Q.dtype),
                   lse.data_ptr() if lse is not None else None, ws_ptr, ws_n)
     if st != 0:
         raise SgaError(st, "sga_attention_paged")
     return (O, lse) if lse is not None else O
+
+
+# ---- generation with drafted tokens ----------------------------------------------------------------
+def _check_ints(t, name, dtype, shape, index):
+    if str(t.dtype) != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda or t.get_device() != index:
+        raise ValueError(f"{name} must be contiguous {dtype[6:]} {list(shape)} on the batch's device")
+
+
+def _workspace_of(workspace, index):
+    if workspace is None or workspace.numel() == 0:
+        return None, 0
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the inputs' device")
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+class PagePool(_Fixed):
+    """Free pages of a cache (sga_page_pool): a ring.
+
+    pages   int32 [n_pages]; the `count` entries from `first` on, around the end, are free pages
+    state   int64 [2]: first, count
+    PagePool.full(n_pages) makes one whose pages are all free.  The attributes cannot be replaced."""
+
+    def __init__(self, pages, state):
+        if str(pages.dtype) != "torch.int32" or pages.dim() != 1 or pages.numel() < 1 or not pages.is_contiguous() or not pages.is_cuda:
+            raise ValueError("pages must be a contiguous int32 device tensor [n_pages]")
+        if str(state.dtype) != "torch.int64" or state.shape != (2,) or not state.is_contiguous() or state.device != pages.device:
+            raise ValueError("state must be contiguous int64 [2] on the device of pages")
+        self.__dict__.update(pages=pages, state=state, device_index=pages.get_device(),
+                             _desc=_PagePool(ctypes.sizeof(_PagePool), 0, pages.data_ptr(), state.data_ptr()))
+
+    @classmethod
+    def full(cls, n_pages, device="cuda"):
+        import torch
+        return cls(torch.arange(n_pages, dtype=torch.int32, device=device), torch.tensor([0, n_pages], device=device))
+
+
+def alloc_pages_workspace(batch):
+    """Workspace for pages_advance calls of batches of these sizes (calls that overlap in time need one each)."""
+    import torch
+    st, n = sga_pages_workspace_bytes(batch._struct(batch.page_size))
+    if st != 0:
+        raise SgaError(st, "sga_pages_workspace_bytes")
+    return torch.empty(n, dtype=torch.uint8, device=batch.device)
+
+
+def pages_advance(batch, pool, ask, kept=None, spec=None, positions=None, slots=None, out=None, workspace=None):
+    """The next step's page table, packed rows and lengths, written into the batch's arrays and the pool, or into
+    out = (batch, pool), a batch alike in sizes and a pool on the same ring (a program that plans a step while the last one runs).
+
+    ask        int32 [S]: tokens that a sequence asks for, below 0 where it ends
+    kept       int32 [S]: how many of the last step's rows stay (None: all)
+    spec       a sliding or global + local mask: pages behind its window go back (None: none does)
+    positions  int64 [n_tokens], slots int64 [n_tokens]: written, the place in its sequence of every new token, and
+               page * page_size + row where it lies in the cache
+    A sequence whose request does not fit gets no rows (seq_ptr tells) and keeps what it has.  Returns the batch written."""
+    index = batch.device_index
+    S = batch.seq_len.shape[0]
+    to, to_pool = out if out is not None else (batch, pool)
+    if to.page_table.shape != batch.page_table.shape or to.device_index != index or to.n_tokens != batch.n_tokens \
+            or to.page_size != batch.page_size or to.n_pages != batch.n_pages:
+        raise ValueError("out's batch must be like the batch")
+    if pool.device_index != index or to_pool.device_index != index or pool.pages.numel() != batch.n_pages \
+            or to_pool.pages.data_ptr() != pool.pages.data_ptr() or to_pool.pages.numel() != pool.pages.numel():
+        raise ValueError("the pool must have the batch's pages, and out's pool the same ring")
+    _check_ints(ask, "ask", "torch.int32", (S,), index)
+    if kept is not None:
+        _check_ints(kept, "kept", "torch.int32", (S,), index)
+    for t, name in ((positions, "positions"), (slots, "slots")):
+        if t is not None:
+            _check_ints(t, name, "torch.int64", (batch.n_tokens,), index)
+    if workspace is None:
+        workspace = alloc_pages_workspace(batch)
+    ws_ptr, ws_n = _workspace_of(workspace, index)
+    st = _enqueue(index, sga_pages_advance, batch._struct(batch.page_size), to._struct(to.page_size), pool._desc, to_pool.state.data_ptr(),
+                  ask.data_ptr() or None, kept.data_ptr() or None if kept is not None else None, spec,
+                  positions.data_ptr() or None if positions is not None else None, slots.data_ptr() or None if slots is not None else None,
+                  ws_ptr, ws_n)
+    if st != 0:
+        raise SgaError(st, "sga_pages_advance")
+    return to
+
+
+class Norm(_Fixed):
+    """Norm of a head's row: x * (mean x^2 + epsilon)^-1/2 * (weight + offset) (sga_norm_desc).  weight: [d] on the device in fp32, fp16
+    or bf16, or None for none.  New weights may be written into the tensor; the attributes cannot be replaced."""
+
+    def __init__(self, weight=None, epsilon=1e-6, offset=0.0):
+        code = 0
+        if weight is not None:
+            if weight.dim() != 1 or not weight.is_contiguous() or not weight.is_cuda:
+                raise ValueError("weight must be a contiguous device tensor [d]")
+            code = _serving_code(weight.dtype)
+        if not 0 < epsilon < float("inf"):
+            raise ValueError("epsilon must be positive")
+        self.__dict__.update(weight=weight, epsilon=float(epsilon), offset=float(offset), _desc=_NormDesc(
+            ctypes.sizeof(_NormDesc), code, weight.data_ptr() if weight is not None else None, float(epsilon), float(offset)))
+
+
+def _check_norm(norm, t):
+    if norm is not None and norm.weight is not None and (norm.weight.shape[0] != t.shape[2] or norm.weight.get_device() != t.get_device()):
+        raise ValueError("a norm's weight must be [d] on the tokens' device")
+
+
+def _check_norm_call(Q, K, rotary, q_norm, k_norm, positions):
+    _check_tokens(Q, "Q")
+    H, L, d = Q.shape
+    index = Q.get_device()
+    if K is not None and (K.dim() != 3 or K.shape[1:] != Q.shape[1:] or K.dtype != Q.dtype or K.get_device() != index):
+        raise ValueError("K must be [Hkv, L, d] and share dtype and device with Q")
+    if K is None and k_norm is not None:
+        raise ValueError("k_norm without K")
+    if rotary is None and q_norm is None and k_norm is None:
+        raise ValueError("neither norms nor rotary: there is nothing to do")
+    if rotary is not None:
+        rotary._check(Q)
+    _check_norm(q_norm, Q)
+    _check_norm(k_norm, Q)
+    if positions is not None:
+        if str(positions.dtype) != "torch.int64" or positions.shape != (L,) or not positions.is_contiguous() or positions.get_device() != index:
+            raise ValueError("positions must be contiguous int64 [L] on Q's device")
+    return index, positions.data_ptr() if positions is not None else None
+
+
+def _like(out, t, name):
+    if out is None:
+        import torch
+        return torch.empty_like(t)
+    if out.shape != t.shape or out.dtype != t.dtype or out.get_device() != t.get_device():
+        raise ValueError(f"{name} must match its input in shape, dtype and device")
+    return out
+
+
+def norm_rotary(Q, K=None, rotary=None, q_norm=None, k_norm=None, positions=None, first=0, Q_out=None, K_out=None):
+    """Norm every head's row of Q [Hq, L, d] (and K [Hkv, L, d]) and rotate it by position, in one pass: row t has positions[t] (int64
+    [L]), or first + t.  Each out may be its input.  Returns Q_out, or (Q_out, K_out).  (No history is recorded: a backward pass
+    calls norm_rotary_backward.)"""
+    index, at = _check_norm_call(Q, K, rotary, q_norm, k_norm, positions)
+    Q_out = _like(Q_out, Q, "Q_out")
+    if K is not None:
+        K_out = _like(K_out, K, "K_out")
+    elif K_out is not None:
+        raise ValueError("K_out without K")
+    st = _enqueue(index, sga_norm_rotary, _strides(Q, "Q"), _strides(Q_out, "Q_out", written=True), q_norm._desc if q_norm is not None else None,
+                  Q.shape[0], _strides(K, "K") if K is not None else None, _strides(K_out, "K_out", written=True) if K is not None else None,
+                  k_norm._desc if k_norm is not None else None, K.shape[0] if K is not None else 0, at, int(first), Q.shape[1], Q.shape[2],
+                  rotary._desc if rotary is not None else None, _serving_code(Q.dtype))
+    if st != 0:
+        raise SgaError(st, "sga_norm_rotary")
+    return Q_out if K is None else (Q_out, K_out)
+
+
+def norm_workspace_bytes(L, Hq, Hkv, d) -> int:
+    st, n = sga_norm_workspace_bytes(L, Hq, Hkv, d)
+    if st != 0:
+        raise SgaError(st, "sga_norm_workspace_bytes")
+    return n
+
+
+def alloc_norm_workspace(L, Hq, Hkv, d, device="cuda"):
+    """Workspace for norm_rotary_backward calls of these sizes (Hkv 0: of Q alone)."""
+    import torch
+    return torch.empty(norm_workspace_bytes(L, Hq, Hkv, d), dtype=torch.uint8, device=device)
+
+
+def norm_rotary_backward(Q, dQ_out, K=None, dK_out=None, rotary=None, q_norm=None, k_norm=None, positions=None, first=0, dQ=None, dK=None,
+                         dq_weight=None, dk_weight=None, workspace=None):
+    """The gradient of norm_rotary(Q, K, ...) from those of its results: (dQ, dq_weight), or (dQ, dq_weight, dK, dk_weight).  Weights' gradients
+    are float32 [d], summed over all rows, None where a norm has no weights; they are written into dq_weight and dk_weight if given.  dQ may be
+    dQ_out or Q, dK likewise."""
+    index, at = _check_norm_call(Q, K, rotary, q_norm, k_norm, positions)
+    if (K is None) != (dK_out is None) or (K is None and dK is not None):
+        raise ValueError("K, its result's gradient and dK go together")
+    for x, g, name in ((Q, dQ_out, "dQ_out"), (K, dK_out, "dK_out")):
+        if x is not None and (g.shape != x.shape or g.dtype != x.dtype or g.get_device() != index):
+            raise ValueError(f"{name} must match the input in shape, dtype and device")
+    import torch
+    dQ = _like(dQ, Q, "dQ")
+    dK = _like(dK, K, "dK") if K is not None else None
+    d = Q.shape[2]
+    dw = []
+    for norm, given, name in ((q_norm, dq_weight, "dq_weight"), (k_norm, dk_weight, "dk_weight")):
+        if norm is None or norm.weight is None:
+            if given is not None:
+                raise ValueError(f"{name} without weights")
+            dw.append(None)
+        elif given is None:
+            dw.append(torch.empty(d, dtype=torch.float32, device=Q.device))
+        elif given.shape != (d,) or str(given.dtype) != "torch.float32" or not given.is_contiguous() or given.get_device() != index:
+            raise ValueError(f"{name} must be contiguous float32 [d] on Q's device")
+        else:
+            dw.append(given)
+    if workspace is None and (dw[0] is not None or dw[1] is not None):
+        workspace = alloc_norm_workspace(Q.shape[1], Q.shape[0], K.shape[0] if K is not None else 0, d, Q.device)
+    ws_ptr, ws_n = _workspace_of(workspace, index)
+    k = (_strides(K, "K"), _strides(dK_out, "dK_out"), _strides(dK, "dK", written=True)) if K is not None else (None, None, None)
+    st = _enqueue(index, sga_norm_rotary_backward, _strides(Q, "Q"), _strides(dQ_out, "dQ_out"), _strides(dQ, "dQ", written=True),
+                  q_norm._desc if q_norm is not None else None, dw[0].data_ptr() if dw[0] is not None else None, Q.shape[0], *k,
+                  k_norm._desc if k_norm is not None else None, dw[1].data_ptr() if dw[1] is not None else None,
+                  K.shape[0] if K is not None else 0, at, int(first), Q.shape[1], d, rotary._desc if rotary is not None else None,
+                  _serving_code(Q.dtype), ws_ptr, ws_n)
+    if st != 0:
+        raise SgaError(st, "sga_norm_rotary_backward")
+    return (dQ, dw[0]) if K is None else (dQ, dw[0], dK, dw[1])
+
+
+class DraftTree(_Fixed):
+    """A tree of drafted tokens for every sequence of a batch (sga_draft_tree).
+
+    depth   int32 [n_tokens]: a token's position is its sequence's tokens before the new ones + depth; below 0: no token of the tree
+    seen    int32 [n_tokens, words]: bit t (of word t / 32): the token sees new token t of its sequence, itself among them; up to 16 words
+    build_draft_tree fills both from the tokens' parents; a program may write them itself.  The attributes cannot be replaced."""
+
+    def __init__(self, depth, seen):
+        if str(depth.dtype) != "torch.int32" or depth.dim() != 1 or not depth.is_contiguous() or not depth.is_cuda:
+            raise ValueError("depth must be a contiguous int32 device tensor [n_tokens]")
+        if str(seen.dtype) != "torch.int32" or seen.dim() != 2 or seen.shape[0] != depth.shape[0] or not 1 <= seen.shape[1] <= 16 \
+                or not seen.is_contiguous() or seen.device != depth.device:
+            raise ValueError("seen must be contiguous int32 [n_tokens, 1 to 16 words] on the device of depth")
+        self.__dict__.update(depth=depth, seen=seen, device_index=depth.get_device(), _desc=_DraftTree(
+            ctypes.sizeof(_DraftTree), seen.shape[1], depth.data_ptr(), seen.data_ptr()))
+
+    def _check(self, batch):
+        if self.depth.shape[0] != batch.n_tokens or self.device_index != batch.device_index:
+            raise ValueError("the tree must have the batch's n_tokens and device")
+
+
+def build_draft_tree(parent, batch, spec: MaskSpec, tree=None, most=64):
+    """Depths and visible ancestors of the batch's new tokens under a sliding or global + local mask, from their parents: int32 [n_tokens], index
+    among the sequence's new tokens, -1 for the last token before them.  Writes into `tree`, or makes one for up to `most` tokens (512 at
+    most) a sequence; later ones are none of it (depth -1)."""
+    index = batch.device_index
+    _check_ints(parent, "parent", "torch.int32", (batch.n_tokens,), index)
+    if tree is None:
+        import torch
+        if not 1 <= most <= 512:
+            raise ValueError("a tree has 1 to 512 tokens")
+        tree = DraftTree(torch.empty(batch.n_tokens, dtype=torch.int32, device=batch.device),
+                         torch.empty(batch.n_tokens, -(-most // 32), dtype=torch.int32, device=batch.device))
+    tree._check(batch)
+    st = _enqueue(index, sga_draft_tree_build, parent.data_ptr(), batch._struct(batch.page_size), spec, tree._desc)
+    if st != 0:
+        raise SgaError(st, "sga_draft_tree_build")
+    return tree
+
+
+def cache_keep(cache_k, cache_v, batch, path, count):
+    """Move the batch's accepted tokens into place: keys and values of new token path[s, k] of sequence s to the place of new token k, k <
+    count[s].  path: int32 [S, columns], rising; count: int32 [S].  The caches are [n_pages, Hkv, page_size, d], or [layers, n_pages,
+    Hkv, page_size, d] for all layers at once.  Lengths stay: pages_advance takes the counts as `kept`."""
+    layers, apart = 1, 0
+    if cache_k.dim() == 5:
+        if cache_v.shape != cache_k.shape or cache_v.stride(0) != cache_k.stride(0):
+            raise ValueError("the caches of all layers must be alike")
+        layers, apart = cache_k.shape[0], cache_k.stride(0)
+        if layers < 1:
+            raise ValueError("no layer")
+        if layers > 1 and apart < cache_k.stride(1) * (cache_k.shape[1] - 1) + cache_k[0, 0].numel():
+            # layers may take turns page by page, as pages of keys and values may
+            if apart < cache_k[0, 0].numel() or cache_k.stride(1) < apart * (layers - 1) + cache_k[0, 0].numel():
+                raise ValueError("the caches of different layers overlap")
+        cache_k, cache_v = cache_k[0], cache_v[0]
+    if cache_k.dim() != 4 or not cache_k.is_cuda:
+        raise ValueError("the caches must both be [n_pages, Hkv, page_size, d], or of several layers")
+    struct, Hkv = batch._caches(cache_k[0], cache_k, cache_v)
+    index, S = batch.device_index, batch.seq_len.shape[0]
+    if path.dim() != 2:
+        raise ValueError("path must be int32 [S, columns]")
+    _check_ints(path, "path", "torch.int32", (S, path.shape[1]), index)
+    _check_ints(count, "count", "torch.int32", (S,), index)
+    st = _enqueue(index, sga_cache_keep, cache_k.data_ptr(), cache_v.data_ptr(), struct, Hkv, cache_k.shape[3], layers, apart, path.data_ptr(),
+                  path.shape[1], count.data_ptr(), _serving_code(cache_k.dtype))
+    if st != 0:
+        raise SgaError(st, "sga_cache_keep")

@@ -522,6 +522,53 @@ sga_status paged_shape(const sga_paged_batch* batch, const sga_mask_desc* mask, 
   return SGA_OK;
 }
 
+bool valid_tree(const sga_draft_tree* t) {
+  return t->depth && t->seen && aligned_to(t->depth, 4) && aligned_to(t->seen, 4);
+}
+
+sga_status run_paged(const sga_rows* Q, const void* cache_k, const void* cache_v, const sga_paged_batch* batch, const sga_draft_tree* tree,
+                     const sga_mask_desc* mask, int32_t causal, const sga_rows* O, int32_t Hq, int32_t Hkv, int32_t d, float scale,
+                     int32_t dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!Q || !O) return SGA_ERR_INVALID_ARG;
+  PagedAttention a{};
+  const sga_status st = paged_shape(batch, mask, causal, Hq, Hkv, d, dtype, a);
+  if (st != SGA_OK) return st;
+  if (tree) {
+    if (tree->struct_bytes != sizeof(sga_draft_tree) || tree->words < 1 || tree->words > 16) return SGA_ERR_INVALID_ARG;
+    a.words = tree->words;
+  }
+  if (workspace ? (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 : workspace_bytes != 0) return SGA_ERR_INVALID_ARG;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return SGA_OK;
+  if (!wide_rows(Q, dtype) || !wide_rows(O, dtype) || Q->data == O->data) return SGA_ERR_INVALID_ARG;
+  if (!cache_k || !cache_v || !aligned16(cache_k) || !aligned16(cache_v)) return SGA_ERR_INVALID_ARG;
+  if (batch->page_stride % (16 / element_bytes(dtype)) != 0 || !aligned_to(lse, 4)) return SGA_ERR_INVALID_ARG;
+  if (tree && !valid_tree(tree)) return SGA_ERR_INVALID_ARG;
+  const PagedPlan plan = plan_paged(a);
+  if (plan.groups == 0) return SGA_ERR_OVERFLOW;
+  (void)hipGetLastError();
+  a.Q = Q->data; a.q_head = Q->head_stride; a.q_row = Q->row_stride;
+  a.O = O->data; a.o_head = O->head_stride; a.o_row = O->row_stride;
+  a.cache_k = cache_k; a.cache_v = cache_v;
+  a.lse = lse;
+  if (tree) {
+    a.depth = tree->depth;
+    a.seen = tree->seen;
+  }
+  a.scale = scale;
+  a.tile_rows = plan.tile_rows;
+  a.page_pieces = (uint32_t)(batch->page_stride / (16 / element_bytes(dtype)));
+  a.groups = plan.groups;
+  a.splits = 1;
+  a.slots = plan.slots;
+  if (plan.bytes > 0 && workspace_bytes >= plan.bytes) {
+    a.splits = plan.splits;
+    a.notes = workspace;
+    a.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + (size_t)plan.groups * kNoteBytes);
+  }
+  a.stream = static_cast<hipStream_t>(stream);
+  return launch_paged(a);
+}
+
 }  // namespace
 
 extern "C" {
@@ -593,35 +640,287 @@ sga_status sga_attention_paged(const sga_rows* Q, const void* cache_k, const voi
                                const sga_mask_desc* mask, int32_t causal, const sga_rows* O, int32_t Hq, int32_t Hkv,
                                int32_t d, float scale, int32_t dtype, float* lse, void* workspace, size_t workspace_bytes,
                                void* stream) {
-  if (!Q || !O) return SGA_ERR_INVALID_ARG;
-  PagedAttention a{};
-  const sga_status st = paged_shape(batch, mask, causal, Hq, Hkv, d, dtype, a);
+  return run_paged(Q, cache_k, cache_v, batch, nullptr, mask, causal, O, Hq, Hkv, d, scale, dtype, lse, workspace, workspace_bytes,
+                   stream);
+}
+
+}  // extern "C"
+
+// ---- generation with drafted tokens ---------------------------------------------------------------
+namespace {
+
+bool valid_norm(const sga_norm_desc* n) {
+  return !n || (n->struct_bytes == sizeof(sga_norm_desc) && serving_dtype(n->weight_dtype) && n->epsilon > 0.f &&
+                n->epsilon < INFINITY && aligned_to(n->weight, element_bytes(n->weight_dtype)));
+}
+
+NormArg norm_arg(const sga_norm_desc* n) {
+  if (!n) return NormArg{nullptr, 0.f, 0.f, 0, 0};
+  return NormArg{n->weight, n->epsilon, n->offset, n->weight_dtype, 1};
+}
+
+// What a batch's arrays have to be where they are read whatever n_tokens is.
+bool valid_arrays(const sga_paged_batch* b) {
+  if (!b->seq_ptr || !aligned_to(b->seq_ptr, 8)) return false;
+  if (b->n_seqs == 0) return true;
+  return b->page_table && b->seq_len && aligned_to(b->page_table, 4) && aligned_to(b->seq_len, 4);
+}
+
+sga_status window_of(const sga_mask_desc* mask) {
+  const sga_status st = mask_validate(mask);
   if (st != SGA_OK) return st;
-  if (workspace ? (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 : workspace_bytes != 0) return SGA_ERR_INVALID_ARG;
-  if (batch->n_tokens == 0 || batch->n_seqs == 0) return SGA_OK;
-  if (!wide_rows(Q, dtype) || !wide_rows(O, dtype) || Q->data == O->data) return SGA_ERR_INVALID_ARG;
-  if (!cache_k || !cache_v || !aligned16(cache_k) || !aligned16(cache_v)) return SGA_ERR_INVALID_ARG;
-  if (batch->page_stride % (16 / element_bytes(dtype)) != 0 || !aligned_to(lse, 4)) return SGA_ERR_INVALID_ARG;
-  const PagedPlan plan = plan_paged(a);
-  if (plan.groups == 0) return SGA_ERR_OVERFLOW;
-  (void)hipGetLastError();
-  a.Q = Q->data; a.q_head = Q->head_stride; a.q_row = Q->row_stride;
-  a.O = O->data; a.o_head = O->head_stride; a.o_row = O->row_stride;
-  a.cache_k = cache_k; a.cache_v = cache_v;
-  a.lse = lse;
-  a.scale = scale;
-  a.tile_rows = plan.tile_rows;
-  a.page_pieces = (uint32_t)(batch->page_stride / (16 / element_bytes(dtype)));
-  a.groups = plan.groups;
-  a.splits = 1;
-  a.slots = plan.slots;
-  if (plan.bytes > 0 && workspace_bytes >= plan.bytes) {
-    a.splits = plan.splits;
-    a.notes = workspace;
-    a.partials = reinterpret_cast<float*>(static_cast<char*>(workspace) + (size_t)plan.groups * kNoteBytes);
+  return mask->kind == SGA_MASK_SLIDING || mask->kind == SGA_MASK_GLOBAL_LOCAL ? SGA_OK : SGA_ERR_UNSUPPORTED;
+}
+
+constexpr int32_t kMostSequences = 65536;
+
+}  // namespace
+
+extern "C" {
+
+sga_status sga_pages_workspace_bytes(const sga_paged_batch* batch, size_t* bytes_out) {
+  if (!bytes_out || !valid_batch(batch, 0, 0) || batch->n_seqs > kMostSequences) return SGA_ERR_INVALID_ARG;
+  PagesArgs a{};
+  a.from = batch_args(*batch);
+  plan_pages(a);
+  *bytes_out = pages_workspace(a);
+  return SGA_OK;
+}
+
+sga_status sga_pages_advance(const sga_paged_batch* batch, const sga_paged_batch* next, const sga_page_pool* pool, int64_t* state_out,
+                             const int32_t* ask, const int32_t* kept, const sga_mask_desc* mask, int64_t* positions, int64_t* slots,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+  if (!valid_batch(batch, 0, 0) || !valid_batch(next, 0, 0) || batch->n_seqs > kMostSequences) return SGA_ERR_INVALID_ARG;
+  if (next->n_seqs != batch->n_seqs || next->n_tokens != batch->n_tokens || next->n_pages != batch->n_pages ||
+      next->page_size != batch->page_size || next->pages_per_seq != batch->pages_per_seq)
+    return SGA_ERR_INVALID_ARG;
+  if (!pool || pool->struct_bytes != sizeof(sga_page_pool) || pool->reserved != 0 || !pool->pages || !aligned_to(pool->pages, 4) || !pool->state ||
+      !aligned_to(pool->state, 8) || !state_out || !aligned_to(state_out, 8))
+    return SGA_ERR_INVALID_ARG;
+  if (!valid_arrays(batch) || !valid_arrays(next)) return SGA_ERR_INVALID_ARG;
+  if ((batch->n_seqs > 0 && !ask) || !aligned_to(ask, 4) || !aligned_to(kept, 4) || !aligned_to(positions, 8) || !aligned_to(slots, 8))
+    return SGA_ERR_INVALID_ARG;
+  if (mask) {
+    const sga_status st = window_of(mask);
+    if (st != SGA_OK) return st;
   }
+  if (workspace ? (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 : workspace_bytes != 0) return SGA_ERR_INVALID_ARG;
+  PagesArgs a{};
+  a.from = batch_args(*batch);
+  plan_pages(a);
+  if (workspace_bytes < pages_workspace(a)) return SGA_ERR_WORKSPACE;
+  a.page_table = const_cast<int32_t*>(next->page_table);
+  a.seq_ptr = const_cast<int64_t*>(next->seq_ptr);
+  a.seq_len = const_cast<int32_t*>(next->seq_len);
+  a.ring = pool->pages;
+  a.state = pool->state;
+  a.state_out = state_out;
+  a.ask = ask;
+  a.kept = kept;
+  a.positions = positions;
+  a.slots = slots;
+  if (mask) {
+    a.give_back = 1;
+    a.window = mask->window;
+    a.n_global = mask->kind == SGA_MASK_GLOBAL_LOCAL ? mask->n_global : 0;
+  }
+  a.workspace = workspace;
   a.stream = static_cast<hipStream_t>(stream);
-  return launch_paged(a);
+  (void)hipGetLastError();
+  return launch_pages(a);
+}
+
+sga_status sga_norm_rotary(const sga_rows* Q, const sga_rows* Q_out, const sga_norm_desc* q_norm, int32_t Hq, const sga_rows* K,
+                           const sga_rows* K_out, const sga_norm_desc* k_norm, int32_t Hkv, const int64_t* positions, int64_t first,
+                           int64_t L, int32_t d, const sga_rotary_desc* rotary, int32_t dtype, void* stream) {
+  if (!Q || !Q_out || (K != nullptr) != (K_out != nullptr) || !serving_dtype(dtype) || L < 0 || L >= (int64_t(1) << 31)) return SGA_ERR_INVALID_ARG;
+  if (Hq < 1 || Hq > 65535 || (K && (Hkv < 1 || Hkv > 65535)) || d < 2 || d > kMaxRotaryDim) return SGA_ERR_INVALID_ARG;
+  if ((rotary && !valid_rotary(rotary, d)) || !valid_norm(q_norm) || !valid_norm(k_norm) || (!K && k_norm) || (!rotary && !q_norm && !k_norm))
+    return SGA_ERR_INVALID_ARG;
+  if (L == 0) return SGA_OK;
+  if (!valid_rows(Q, dtype) || !valid_rows(Q_out, dtype) || !apart_or_same(*Q, *Q_out)) return SGA_ERR_INVALID_ARG;
+  if (K && (!valid_rows(K, dtype) || !valid_rows(K_out, dtype) || !apart_or_same(*K, *K_out) || K_out->data == Q_out->data)) return SGA_ERR_INVALID_ARG;
+  if (!aligned_to(positions, 8)) return SGA_ERR_INVALID_ARG;
+  (void)hipGetLastError();
+  NormRotateArgs a{};
+  int n = 0;
+  a.norm[n] = norm_arg(q_norm);
+  a.r.tensor[n++] = rows_arg(*Q, *Q_out, Hq, rotary != nullptr);
+  if (K) {
+    a.norm[n] = norm_arg(k_norm);
+    a.r.tensor[n++] = rows_arg(*K, *K_out, Hkv, rotary != nullptr);
+  }
+  a.r.n_tensors = n;
+  a.r.n_rows = (int32_t)L; a.r.d = d;
+  a.r.positions = positions; a.r.first = first;
+  a.r.rotary = rotary_args(rotary, 0);
+  a.r.dtype = dtype;
+  a.r.stream = static_cast<hipStream_t>(stream);
+  return launch_norm_rotate(a);
+}
+
+sga_status sga_norm_workspace_bytes(int64_t L, int32_t Hq, int32_t Hkv, int32_t d, size_t* bytes_out) {
+  if (!bytes_out || L < 0 || L >= (int64_t(1) << 31) || Hq < 1 || Hq > 65535 || Hkv < 0 || Hkv > 65535 || d < 2 || d > kMaxRotaryDim)
+    return SGA_ERR_INVALID_ARG;
+  *bytes_out = norm_partial_bytes(L, Hq, Hkv, d);
+  return SGA_OK;
+}
+
+sga_status sga_norm_rotary_backward(const sga_rows* Q, const sga_rows* dQ_out, const sga_rows* dQ, const sga_norm_desc* q_norm,
+                                    float* dq_weight, int32_t Hq, const sga_rows* K, const sga_rows* dK_out, const sga_rows* dK,
+                                    const sga_norm_desc* k_norm, float* dk_weight, int32_t Hkv, const int64_t* positions, int64_t first,
+                                    int64_t L, int32_t d, const sga_rotary_desc* rotary, int32_t dtype, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  const bool two = dK_out != nullptr;
+  if (!dQ_out || !dQ || two != (dK != nullptr) || !serving_dtype(dtype) || L < 0 || L >= (int64_t(1) << 31)) return SGA_ERR_INVALID_ARG;
+  if (Hq < 1 || Hq > 65535 || (two && (Hkv < 1 || Hkv > 65535)) || d < 2 || d > kMaxRotaryDim) return SGA_ERR_INVALID_ARG;
+  if ((rotary && !valid_rotary(rotary, d)) || !valid_norm(q_norm) || !valid_norm(k_norm) || (!two && (K || k_norm || dk_weight)) ||
+      (!rotary && !q_norm && !k_norm))
+    return SGA_ERR_INVALID_ARG;
+  // a gradient of weights needs weights, a norm its input
+  if ((dq_weight && (!q_norm || !q_norm->weight)) || (dk_weight && (!k_norm || !k_norm->weight))) return SGA_ERR_INVALID_ARG;
+  if (!aligned_to(dq_weight, 4) || !aligned_to(dk_weight, 4) || (dq_weight && dq_weight == dk_weight)) return SGA_ERR_INVALID_ARG;
+  if ((q_norm && !Q) || (k_norm && !K) || !aligned_to(positions, 8)) return SGA_ERR_INVALID_ARG;
+  if (workspace ? (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 : workspace_bytes != 0) return SGA_ERR_INVALID_ARG;
+  const bool sums = dq_weight || dk_weight;
+  if (sums && workspace_bytes < norm_partial_bytes(L, Hq, two ? Hkv : 0, d)) return SGA_ERR_WORKSPACE;
+  if (L == 0 && !sums) return SGA_OK;
+  NormGradArgs a{};
+  auto add = [&](const sga_rows* x, const sga_rows* g, const sga_rows* dx, const sga_norm_desc* norm, float* dw, int32_t heads) {
+    if (L > 0) {
+      if (!valid_rows(g, dtype) || !valid_rows(dx, dtype) || !apart_or_same(*g, *dx)) return false;
+      if (norm && (!valid_rows(x, dtype) || !apart_or_same(*x, *dx))) return false;
+    }
+    NormGradRows& t = a.tensor[a.n_tensors++];
+    t.x = norm ? x->data : g->data;
+    t.x_head = norm ? x->head_stride : g->head_stride;
+    t.x_row = norm ? x->row_stride : g->row_stride;
+    t.g = g->data; t.g_head = g->head_stride; t.g_row = g->row_stride;
+    t.dx = dx->data; t.dx_head = dx->head_stride; t.dx_row = dx->row_stride;
+    t.dw = dw;
+    t.norm = norm_arg(norm);
+    t.heads = heads;
+    return true;
+  };
+  if (!add(Q, dQ_out, dQ, q_norm, dq_weight, Hq)) return SGA_ERR_INVALID_ARG;
+  if (two && (!add(K, dK_out, dK, k_norm, dk_weight, Hkv) || (L > 0 && dK->data == dQ->data))) return SGA_ERR_INVALID_ARG;
+  a.n_rows = (int32_t)L; a.d = d;
+  a.positions = positions; a.first = first;
+  a.rotary = rotary_args(rotary, 1);
+  a.partials = sums ? static_cast<float*>(workspace) : nullptr;
+  a.dtype = dtype;
+  a.stream = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  return launch_norm_grad(a);
+}
+
+sga_status sga_draft_tree_build(const int32_t* parent, const sga_paged_batch* batch, const sga_mask_desc* mask,
+                                const sga_draft_tree* tree, void* stream) {
+  if (!valid_batch(batch, 0, 0)) return SGA_ERR_INVALID_ARG;
+  const sga_status st = window_of(mask);
+  if (st != SGA_OK) return st;
+  if (!tree || tree->struct_bytes != sizeof(sga_draft_tree) || tree->words < 1 || tree->words > 16) return SGA_ERR_INVALID_ARG;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return SGA_OK;
+  if (!parent || !aligned_to(parent, 4) || !valid_tree(tree)) return SGA_ERR_INVALID_ARG;
+  TreeArgs a{};
+  a.batch = batch_args(*batch);
+  a.parent = parent;
+  a.depth = tree->depth;
+  a.seen = tree->seen;
+  a.words = tree->words;
+  a.L = (int32_t)mask->L;
+  a.window = mask->window;
+  a.n_global = mask->kind == SGA_MASK_GLOBAL_LOCAL ? mask->n_global : 0;
+  a.stream = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  return launch_tree(a);
+}
+
+sga_status sga_cache_append_normed(const sga_rows* K, const sga_rows* V, void* cache_k, void* cache_v, const sga_paged_batch* batch,
+                                   int32_t Hkv, int32_t d, const sga_rotary_desc* rotary, const sga_norm_desc* k_norm, const sga_rows* Q,
+                                   const sga_rows* Q_out, int32_t Hq, const sga_norm_desc* q_norm, const sga_draft_tree* tree,
+                                   int32_t dtype, void* stream) {
+  if (!K || !V || !serving_dtype(dtype) || Hkv < 1 || Hkv > 65535 || d < 2 || d > kMaxRotaryDim) return SGA_ERR_INVALID_ARG;
+  if ((rotary && !valid_rotary(rotary, d)) || !valid_norm(q_norm) || !valid_norm(k_norm) || !valid_batch(batch, Hkv, d)) return SGA_ERR_INVALID_ARG;
+  if ((Q != nullptr) != (Q_out != nullptr) || (Q && ((!rotary && !q_norm) || Hq < 1 || Hq > 65535)) || (!Q && q_norm)) return SGA_ERR_INVALID_ARG;
+  if (tree && (tree->struct_bytes != sizeof(sga_draft_tree) || tree->words < 1 || tree->words > 16)) return SGA_ERR_INVALID_ARG;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return SGA_OK;
+  if (tree && !valid_tree(tree)) return SGA_ERR_INVALID_ARG;
+  if (!valid_rows(K, dtype) || !valid_rows(V, dtype) || !cache_k || !cache_v || cache_k == cache_v) return SGA_ERR_INVALID_ARG;
+  if (!aligned_to(cache_k, element_bytes(dtype)) || !aligned_to(cache_v, element_bytes(dtype))) return SGA_ERR_INVALID_ARG;
+  if (Q && (!valid_rows(Q, dtype) || !valid_rows(Q_out, dtype) || !apart_or_same(*Q, *Q_out))) return SGA_ERR_INVALID_ARG;
+  (void)hipGetLastError();
+  NormRotateArgs a{};
+  const int64_t head = (int64_t)batch->page_size * d;      // from head to head within a page
+  int n = 0;
+  if (Q) {
+    a.norm[n] = norm_arg(q_norm);
+    a.r.tensor[n++] = rows_arg(*Q, *Q_out, Hq, rotary != nullptr);
+  }
+  a.norm[n] = norm_arg(k_norm);
+  a.r.tensor[n] = rows_arg(*K, sga_rows{cache_k, head, 0}, Hkv, rotary != nullptr);
+  a.r.tensor[n++].paged = 1;
+  a.r.tensor[n] = rows_arg(*V, sga_rows{cache_v, head, 0}, Hkv, false);
+  a.r.tensor[n++].paged = 1;
+  a.r.n_tensors = n;
+  a.r.n_rows = (int32_t)batch->n_tokens; a.r.d = d;
+  a.r.rotary = rotary_args(rotary, 0);
+  a.r.batch = batch_args(*batch);
+  a.depth = tree ? tree->depth : nullptr;
+  a.r.dtype = dtype;
+  a.r.stream = static_cast<hipStream_t>(stream);
+  return launch_norm_rotate(a);
+}
+
+sga_status sga_tree_workspace_bytes(const sga_paged_batch* batch, const sga_mask_desc* mask, const sga_draft_tree* tree, int32_t Hq,
+                                    int32_t Hkv, int32_t d, int32_t dtype, size_t* bytes_out) {
+  if (!bytes_out || !tree || tree->struct_bytes != sizeof(sga_draft_tree) || tree->words < 1 || tree->words > 16) return SGA_ERR_INVALID_ARG;
+  PagedAttention a{};
+  const sga_status st = paged_shape(batch, mask, 1, Hq, Hkv, d, dtype, a);
+  if (st != SGA_OK) return st;
+  a.words = tree->words;
+  *bytes_out = 0;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0) return SGA_OK;
+  const PagedPlan p = plan_paged(a);
+  if (p.groups == 0) return SGA_ERR_OVERFLOW;
+  *bytes_out = p.bytes;
+  return SGA_OK;
+}
+
+sga_status sga_attention_tree(const sga_rows* Q, const void* cache_k, const void* cache_v, const sga_paged_batch* batch,
+                              const sga_draft_tree* tree, const sga_mask_desc* mask, const sga_rows* O, int32_t Hq, int32_t Hkv,
+                              int32_t d, float scale, int32_t dtype, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!tree) return SGA_ERR_INVALID_ARG;
+  return run_paged(Q, cache_k, cache_v, batch, tree, mask, 1, O, Hq, Hkv, d, scale, dtype, lse, workspace, workspace_bytes, stream);
+}
+
+sga_status sga_cache_keep(void* cache_k, void* cache_v, const sga_paged_batch* batch, int32_t Hkv, int32_t d, int32_t n_layers,
+                          int64_t layer_stride, const int32_t* path, int32_t path_columns, const int32_t* count, int32_t dtype,
+                          void* stream) {
+  if (!serving_dtype(dtype) || Hkv < 1 || Hkv > 65535 || d < 2 || d > kMaxRotaryDim || n_layers < 1 || path_columns < 0) return SGA_ERR_INVALID_ARG;
+  if (!valid_batch(batch, Hkv, d)) return SGA_ERR_INVALID_ARG;
+  if ((int64_t)n_layers * Hkv * d >= int64_t(1) << 29) return SGA_ERR_OVERFLOW;
+  if (batch->n_tokens == 0 || batch->n_seqs == 0 || path_columns == 0) return SGA_OK;
+  const int e = element_bytes(dtype);
+  if (!cache_k || !cache_v || cache_k == cache_v || !aligned_to(cache_k, e) || !aligned_to(cache_v, e)) return SGA_ERR_INVALID_ARG;
+  if (!path || !count || !aligned_to(path, 4) || !aligned_to(count, 4) || (n_layers > 1 && layer_stride < (int64_t)Hkv * batch->page_size * d))
+    return SGA_ERR_INVALID_ARG;
+  KeepArgs a{};
+  a.batch = batch_args(*batch);
+  a.cache_k = static_cast<char*>(cache_k);
+  a.cache_v = static_cast<char*>(cache_v);
+  a.path = path;
+  a.count = count;
+  a.path_columns = path_columns;
+  a.Hkv = Hkv;
+  a.layers = n_layers;
+  a.layer_bytes = n_layers > 1 ? layer_stride * e : 0;
+  a.page_bytes = batch->page_stride * e;
+  a.head_bytes = (int64_t)batch->page_size * d * e;
+  a.row_bytes = (int64_t)d * e;
+  a.stream = static_cast<hipStream_t>(stream);
+  (void)hipGetLastError();
+  return launch_keep(a);
 }
 
 }  // extern "C"

@@ -93,16 +93,52 @@ __device__ __forceinline__ Sight sight_of(const PagedAttention& a, int32_t p, in
   return {p > a.window ? p - a.window : 0, far < last ? (int32_t)far : last, a.n_global < last + 1 ? a.n_global : last + 1};
 }
 
-// Tokens of a sequence that can be seen.
+// Tokens of a sequence that can be seen.  (Of a draft tree: by their places.  A new token's place may lie behind its position, so what the
+// mask's L hides is left out of the tree's bits and of the context instead.)
+template <bool kTree>
 __device__ __forceinline__ int32_t kept_of(const PagedAttention& a, int32_t length) {
   const int64_t room = (int64_t)a.batch.pages_per_seq * a.batch.page.value;
   int64_t kept = length < 0 ? 0 : length;
   kept = kept < room ? kept : room;
-  return (int32_t)(kept < a.L ? kept : a.L);
+  return (int32_t)(kTree || kept < a.L ? kept : a.L);
+}
+
+// Drafted tokens.  New token t of a sequence lies at place base + t of the cache, base = length - n_new, but at position base + depth(t), and
+// sees of the context, the tokens before base, what the mask shows that position, and of the new tokens those whose bits are set in
+// its row of `seen`.  Both kernels meet the context's keys as they do others', and the blocks that reach base as blocks at an edge, in which every key is
+// tested: the bits of a block's 32 keys are two words of the row, put together.  All rows of a sequence meet the same keys.
+__device__ __forceinline__ Sight context_sight(const PagedAttention& a, const Tile& t, int32_t token) {
+  const int32_t base = t.length - t.n_new, depth = a.depth[t.begin + token];
+  const int64_t p = (int64_t)base + depth;
+  if (depth < 0 || p < 0 || p >= a.L) return {0, -1, 0};
+  const int32_t context = base < t.kept ? base : t.kept, last = (context < a.L ? context : a.L) - 1;
+  if (p < a.n_global) return {0, last, 0};
+  return {p > a.window ? (int32_t)(p - a.window) : 0, last, a.n_global < last + 1 ? a.n_global : last + 1};
+}
+// The row of `seen` of a token, -1 where it is none of the tree or outside the mask.
+__device__ __forceinline__ int32_t tree_row(const PagedAttention& a, const Tile& t, int32_t token) {
+  const int32_t depth = a.depth[t.begin + token];
+  const int64_t p = (int64_t)(t.length - t.n_new) + depth;
+  return depth < 0 || p < 0 || p >= a.L ? -1 : t.begin + token;
+}
+// Which of the keys j0 .. j0 + 31 a row sees as new tokens.
+__device__ __forceinline__ uint32_t new_tokens_seen(const PagedAttention& a, const Tile& t, int32_t row, int32_t j0) {
+  const int32_t start = j0 - (t.length - t.n_new), word = start >> 5, shift = start & 31;
+  if (row < 0 || start <= -kBlock || word >= a.words || j0 >= t.kept) return 0;
+  const uint32_t* const seen = a.seen + (int64_t)row * a.words;
+  const uint32_t low = word >= 0 ? seen[word] : 0, high = shift && word + 1 < a.words ? seen[word + 1] : 0;
+  const uint32_t bits = shift ? low >> shift | high << (32 - shift) : low;
+  return t.kept - j0 < kBlock ? bits & ((1u << (t.kept - j0)) - 1) : bits;
+}
+
+template <bool kTree>
+__device__ __forceinline__ Sight row_sight(const PagedAttention& a, const Tile& t, int32_t token) {
+  if constexpr (kTree) return context_sight(a, t, token);
+  return sight_of(a, t.length - t.n_new + token, t.kept);
 }
 
 // Tile t of a sequence.
-template <int kTileRows>
+template <int kTileRows, bool kTree>
 __device__ __forceinline__ Tile tile_of(const PagedAttention& a, int32_t seq, int32_t begin, int32_t n_new, int32_t length,
                                         int32_t index) {
   Tile t;
@@ -113,7 +149,14 @@ __device__ __forceinline__ Tile tile_of(const PagedAttention& a, int32_t seq, in
   const int64_t left = (int64_t)n_new * a.group.value - (int64_t)index * kTileRows;
   t.first = index * kTileRows;
   t.count = left < kTileRows ? (int32_t)left : kTileRows;
-  t.kept = kept_of(a, length);
+  t.kept = kept_of<kTree>(a, length);
+  if constexpr (kTree) {
+    const int32_t start = max(length - n_new, 0), context = min(start, min(t.kept, a.L));
+    t.base = (start < a.n_global || start <= a.window ? 0 : start - a.window) & ~(kBlock - 1);
+    t.lead = (min(min(a.n_global, context), t.base) + kBlock - 1) / kBlock;
+    t.blocks = t.lead + (t.kept > t.base ? (t.kept - 1 - t.base) / kBlock + 1 : 0);
+    return t;
+  }
   // the rows' keys: positions grow with the rows, and so do both ends of what they see
   const int32_t p0 = t.length - t.n_new + (int32_t)quotient((uint32_t)t.first, a.group);
   const int32_t p1 = t.length - t.n_new + (int32_t)quotient((uint32_t)(t.first + t.count - 1), a.group);
@@ -173,7 +216,7 @@ struct SequenceWork {
 template <int kTileRows>
 __device__ __forceinline__ uint32_t step_of(const PagedAttention& a) { return a.causal ? kTileRows / a.group.value : 0; }
 
-template <int kTileRows>
+template <int kTileRows, bool kTree>
 __device__ __forceinline__ SequenceWork work_of(const PagedAttention& a, int32_t s) {
   SequenceWork w{};
   const PagedArgs& b = a.batch;
@@ -183,7 +226,13 @@ __device__ __forceinline__ SequenceWork work_of(const PagedAttention& a, int32_t
   w.length = max(b.seq_len[s], 0);
   w.n_new = end > w.begin ? end - w.begin : 0;
   w.tiles = (uint32_t)(((int64_t)w.n_new * a.group.value + kTileRows - 1) / kTileRows);
-  const int64_t kept = kept_of(a, w.length), old = (int64_t)w.length - w.n_new, step = kTileRows / a.group.value;
+  if constexpr (kTree) {                     // all tiles meet the same keys
+    const int64_t kept = kept_of<true>(a, w.length), reach = (int64_t)a.window + w.n_new + 1 + a.n_global;
+    w.a0 = w.a1 = (uint32_t)(reach < kept ? reach : kept) + kTileCost;
+    w.per_head = (uint64_t)w.tiles * w.a1;
+    return w;
+  }
+  const int64_t kept = kept_of<kTree>(a, w.length), old = (int64_t)w.length - w.n_new, step = kTileRows / a.group.value;
   int64_t window = (a.causal ? 1 : 2) * (int64_t)a.window + step + 1 + a.n_global;
   window = window < kept ? window : kept;
   w.a1 = (uint32_t)window + kTileCost;
@@ -224,7 +273,7 @@ struct Part {
 
 // A workgroup's walk along its share.  It lies in LDS, since it is needed between the parts only; the first wavefront
 // walks, all its lanes with the same values but where they load a sequence each.
-template <int kTileRows>
+template <int kTileRows, bool kTree>
 struct Share {
   SequenceWork work[kWave];  // sequences chunk ..
   uint64_t start[kWave];     // where each begins on the line
@@ -239,7 +288,7 @@ struct Share {
   // 64 sequences from `from` on, which begins at `base` on the line
   __device__ __forceinline__ void load(const PagedAttention& a, int32_t from, uint64_t base) {
     const int l = threadIdx.x & (kWave - 1);
-    const SequenceWork w = work_of<kTileRows>(a, from + l);
+    const SequenceWork w = work_of<kTileRows, kTree>(a, from + l);
     const uint64_t own = w.per_head * (uint64_t)a.Hkv;
     uint64_t sum = own;
     for (int off = 1; off < kWave && off < a.batch.n_seqs; off <<= 1) {
@@ -428,7 +477,7 @@ __device__ __forceinline__ Note* notes_of(const PagedAttention& a) { return rein
 // a kind are all cut into as many pieces as make them about the size at which the call has kChunkPieces of them
 // (as far as the lengths say; kLeastPiece keys at least), so that uneven sequences keep the chip evenly busy.  The pieces lie in
 // the order sequence, kind, piece, tile; the pieces of a tile are `apart` from each other.  False: there is no such piece.  All lanes call it.
-template <int kTileRows>
+template <int kTileRows, bool kTree>
 __device__ __forceinline__ bool piece_of(const PagedAttention& a, int32_t rest, Tile& tile, int32_t& index, int32_t& piece,
                                          int32_t& pieces, int32_t& apart) {
   const int l = threadIdx.x & (kWave - 1);
@@ -437,7 +486,7 @@ __device__ __forceinline__ bool piece_of(const PagedAttention& a, int32_t rest, 
   int32_t all = 0, rows = 0;                 // tiles that see everything, the others
   float all_length = 0.f, length = 0.f;
   auto look = [&](int32_t s) {
-    w = work_of<kTileRows>(a, s);
+    w = work_of<kTileRows, kTree>(a, s);
     all = a.causal ? 0 : (int32_t)w.t1;
     rows = (int32_t)w.tiles - all;
     all_length = (float)w.a0;
@@ -472,7 +521,7 @@ __device__ __forceinline__ bool piece_of(const PagedAttention& a, int32_t rest, 
       place -= in_first ? 0 : first * first_cuts;
       piece = (int32_t)((uint32_t)place / (uint32_t)apart);
       index = place - piece * apart + (in_first ? 0 : first);
-      tile = tile_of<kTileRows>(a, c + lane, __builtin_amdgcn_readlane(w.begin, lane), __builtin_amdgcn_readlane(w.n_new, lane),
+      tile = tile_of<kTileRows, kTree>(a, c + lane, __builtin_amdgcn_readlane(w.begin, lane), __builtin_amdgcn_readlane(w.n_new, lane),
                                 __builtin_amdgcn_readlane(w.length, lane), index);
       return true;
     }
@@ -574,14 +623,14 @@ struct Core<float, D, N> {
 // Walks the blocks [block, end) in steps of `step` for one row, key by key, and adds nothing for a key that it does not see:
 // the products above cannot leave a key out, and 0 times an infinity or NaN in it is NaN.  Only where a tile's result is not
 // finite.  A lane ends with channels lane, lane + 64, ...; top and sum are the wavefront's.
-template <typename T, int D>
+template <typename T, int D, bool kTree>
 __device__ __forceinline__ void attend_row(const PagedAttention& a, const Tile& tile, int32_t head_kv, int32_t flat,
                                            int32_t block, int32_t end, int32_t step, float& top, float& sum,
                                            float (&o)[(D + 63) / 64]) {
   const int lane = threadIdx.x & (kWave - 1);
   const PagedArgs& b = a.batch;
   const int32_t group = (int32_t)a.group.value, token = (int32_t)quotient((uint32_t)flat, a.group);
-  const Sight sight = sight_of(a, tile.length - tile.n_new + token, tile.kept);
+  const Sight sight = row_sight<kTree>(a, tile, token);
   const T* const q = static_cast<const T*>(a.Q) + (int64_t)(head_kv * group + (flat - token * group)) * a.q_head +
                      (int64_t)(tile.begin + token) * a.q_row;
   const int64_t in_head = (int64_t)head_kv * b.page.value * D;
@@ -592,7 +641,10 @@ __device__ __forceinline__ void attend_row(const PagedAttention& a, const Tile& 
   for (; block < end; block += step) {
     const int32_t j = first_key(tile, block) + (lane & (kBlock - 1));
     const int64_t at = place_of(b, tile.seq, j, D);
-    const bool sees = at >= 0 && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
+    bool sees = (j >= sight.lo && j <= sight.hi) || j < sight.lead;
+    if constexpr (kTree)
+      sees |= new_tokens_seen(a, tile, tree_row(a, tile, token), first_key(tile, block)) >> (lane & (kBlock - 1)) & 1;
+    sees = sees && at >= 0;
     float s = -INFINITY;
     if (sees) {
       const T* const k = static_cast<const T*>(a.cache_k) + in_head + at;
@@ -657,7 +709,7 @@ struct Asked {
 // heads, fp16 116 (4.8); a document of six sequences, window 128, fp32, d = 64 137 (43 TFLOP/s of 154: matrix cores 32 % busy.  445 of the 512
 // workgroups get five or six tiles, four in a first pass and one or two in a second, so a third of the wavefronts' time passes at the barrier behind it;
 // and first loads of short tiles, which two wavefronts per SIMD do not hide).
-template <typename T, int D, int N, bool kWholeTiles>
+template <typename T, int D, int N, bool kWholeTiles, bool kTree>
 __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D == 256 ? 1 : 2))) void paged_kernel(
     PagedAttention a) {
   using C = Core<T, D, N>;
@@ -666,7 +718,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
   __shared__ __align__(16) float out[kWaves][kTileRows][kStride];
   __shared__ float tops[kWaves][kTileRows], sums[kWaves][kTileRows];
   const int32_t group = (int32_t)a.group.value;
-  __shared__ Share<kTileRows> share;
+  __shared__ Share<kTileRows, kTree> share;
   for (bool first_part = true;; first_part = false) {
     const bool any = share.next(a, blockIdx.x, first_part);
     if (first_part && a.partials && threadIdx.x == 0) {
@@ -685,16 +737,18 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
     if (!alone || wave < parts) {
       const Part here = share.mine(alone ? wave : 0);
       const int32_t head_kv = here.head;
-      const Tile tile = tile_of<kTileRows>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
+      const Tile tile = tile_of<kTileRows, kTree>(a, here.seq, here.begin, here.n_new, here.length, here.tile);
 
       // this lane's rows
       Sight sight[N];
+      int32_t seen_row[N];                                   // (of a draft tree)
       C core;
 #pragma unroll
       for (int n = 0; n < N; ++n) {
         const int32_t flat = tile.first + (16 * n + m < tile.count ? 16 * n + m : 0);
         const int32_t token = (int32_t)quotient((uint32_t)flat, a.group), head = head_kv * group + (flat - token * group);
-        sight[n] = sight_of(a, tile.length - tile.n_new + token, tile.kept);
+        sight[n] = row_sight<kTree>(a, tile, token);
+        if constexpr (kTree) seen_row[n] = tree_row(a, tile, token);
         const T* q = static_cast<const T*>(a.Q) + (int64_t)head * a.q_head + (int64_t)(tile.begin + token) * a.q_row;
 #pragma unroll
         for (int i = 0; i < C::kSteps; ++i)
@@ -799,11 +853,14 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
 #pragma unroll
           for (int e = 0; e < 8; ++e) p[n][e] = s[n][e / 4][e % 4] * (a.scale * kLog2e);
           if (!whole) {
+            uint32_t drafted = 0;
+            if constexpr (kTree) drafted = new_tokens_seen(a, tile, seen_row[n], j0);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
               const int in_block = 16 * (e / 4) + 4 * g + e % 4, j = j0 + in_block;
               const bool there = kWholeTiles ? (held >> (e / 4)) & 1 : (held >> in_block) & 1;
-              p[n][e] = there && ((j >= sight[n].lo && j <= sight[n].hi) || j < sight[n].lead) ? p[n][e] : -INFINITY;
+              const bool sees = (j >= sight[n].lo && j <= sight[n].hi) || j < sight[n].lead || (kTree && (drafted >> in_block & 1));
+              p[n][e] = there && sees ? p[n][e] : -INFINITY;
             }
           }
           float best = p[n][0];
@@ -865,7 +922,7 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
       } else {
         for (int row = 0; row < tile.count; ++row) {
           float x[(D + 63) / 64], row_top, row_total;
-          attend_row<T, D>(a, tile, head_kv, tile.first + row, first_block, end_block, step, row_top, row_total, x);
+          attend_row<T, D, kTree>(a, tile, head_kv, tile.first + row, first_block, end_block, step, row_top, row_total, x);
 #pragma unroll
           for (int c = 0; c < (D + 63) / 64; ++c)
             if (lane + 64 * c < D) out[wave][row][lane + 64 * c] = x[c];
@@ -1029,7 +1086,7 @@ struct ChunkBlock {
 __host__ __device__ constexpr bool chunk_fits(int64_t row_bytes) { return row_bytes >= 128 && row_bytes <= 512; }
 constexpr int chunk_waves(int row_bytes) { return row_bytes > 256 ? 1 : row_bytes > 128 ? 2 : 3; }
 
-template <typename T, int D, bool kWholeTiles>
+template <typename T, int D, bool kWholeTiles, bool kTree>
 __global__ __attribute__((amdgpu_waves_per_eu(chunk_waves(sizeof(T) * D), chunk_waves(sizeof(T) * D)))) __launch_bounds__(kWaves* kWave) void
 paged_chunk_kernel(PagedAttention a) {
   using B = ChunkBlock<D * (int)sizeof(T)>;
@@ -1067,7 +1124,7 @@ paged_chunk_kernel(PagedAttention a) {
   const int64_t record = (int64_t)head_kv * a.slots + rest;
   Tile tile;
   int32_t index = 0, piece = 0, pieces = 1, apart = 0;
-  const bool any = piece_of<kChunkRows>(a, rest, tile, index, piece, pieces, apart);
+  const bool any = piece_of<kChunkRows, kTree>(a, rest, tile, index, piece, pieces, apart);
   if (a.partials && tid == 0) {
     const bool cut = any && pieces > 1 && piece == 0;
     // (a seq_ptr that decreases can bring more tiles than the plan counts: pieces behind the last workgroup's have no record)
@@ -1085,7 +1142,9 @@ paged_chunk_kernel(PagedAttention a) {
   const bool exists = row < tile.count;
   const int32_t flat = tile.first + (exists ? row : tile.count - 1);
   const int32_t token = (int32_t)quotient((uint32_t)flat, a.group), head = head_kv * group + (flat - token * group);
-  Sight sight = sight_of(a, tile.length - tile.n_new + token, tile.kept);
+  Sight sight = row_sight<kTree>(a, tile, token);
+  int32_t seen_row = -1;                                               // (of a draft tree)
+  if constexpr (kTree) seen_row = tree_row(a, tile, token);
   if (own_first >= tile.count) sight = Sight{0, -1, 0};                // a wavefront without rows only copies
   Piece qf[kSteps];
   {
@@ -1199,6 +1258,8 @@ paged_chunk_kernel(PagedAttention a) {
   auto slot_of = [&](int32_t block) { return (uint32_t)(block - first_block) % kChunkSlots * kSlotBytes; };
   auto meets = [&](int32_t block) {
     const int32_t j0 = first_key(tile, block);
+    if constexpr (kTree)
+      if (j0 + kBlock > tile.length - tile.n_new && own_first < tile.count) return true;
     return (j0 <= hi_max && j0 + kBlock - 1 >= lo_min) || j0 < lead_max;
   };
   auto read_k = [&](uint32_t slot_at, Piece (&k)[kSteps]) {
@@ -1301,11 +1362,13 @@ paged_chunk_kernel(PagedAttention a) {
     read_k(slot_of(block), k);
     products(k, s);
     const uint32_t held = held_of(j0);
+    uint32_t drafted = 0;
+    if constexpr (kTree) drafted = new_tokens_seen(a, tile, seen_row, j0);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int in_block = 8 * (r / 4) + 4 * h + r % 4, j = j0 + in_block;
-      const bool sees = (held >> in_block & 1) && ((j >= sight.lo && j <= sight.hi) || j < sight.lead);
-      s[r] = sees ? s[r] : -INFINITY;
+      const bool sees = (j >= sight.lo && j <= sight.hi) || j < sight.lead || (kTree && (drafted >> in_block & 1));
+      s[r] = (held >> in_block & 1) && sees ? s[r] : -INFINITY;
     }
     const float total = numerators(s, top, p);
     weigh(slot_of(block), s, total, p);
@@ -1398,7 +1461,7 @@ paged_chunk_kernel(PagedAttention a) {
   if (!__all(finite)) {
     for (int r = 0; r < own_count; ++r) {
       float x[(D + 63) / 64], row_top, row_total;
-      attend_row<T, D>(a, tile, head_kv, tile.first + own_first + r, first_block, end_block, 1, row_top, row_total, x);
+      attend_row<T, D, kTree>(a, tile, head_kv, tile.first + own_first + r, first_block, end_block, 1, row_top, row_total, x);
       if (part) {
 #pragma unroll
         for (int c = 0; c < (D + 63) / 64; ++c)
@@ -1489,7 +1552,7 @@ paged_chunk_kernel(PagedAttention a) {
 template <typename T, int D, int kTileRows, typename Record>
 __device__ __forceinline__ void join_parts(const PagedAttention& a, const Note& note, int32_t row0, Record record) {
   constexpr int kPer = D / 16, kAtOnce = 4;
-  const Tile tile = tile_of<kTileRows>(a, 0, note.begin, note.n_new, note.length, note.tile);
+  const Tile tile = tile_of<kTileRows, false>(a, 0, note.begin, note.n_new, note.length, note.tile);
   const int row = row0 + threadIdx.x / 16, channel = threadIdx.x % 16 * kPer;
   if (row >= tile.count) return;
   float high = -INFINITY, total = 0.f, x[kPer];
@@ -1538,18 +1601,18 @@ __global__ __launch_bounds__(kWaves* kWave) void paged_chunk_join_kernel(PagedAt
                                [&](int32_t i) { return record_of<D, kChunkRows>(a, note.first + (int64_t)i * note.apart); });
 }
 
-template <typename T, int D, int N>
+template <typename T, int D, int N, bool kTree>
 sga_status launch_paged_rows(const PagedAttention& a) {
   const dim3 block(kWaves * kWave);
   profile_mark_begin(a.stream, "paged_kernel");
-  if (a.batch.page.value % 16 == 0) paged_kernel<T, D, N, true><<<dim3(a.groups), block, 0, a.stream>>>(a);
-  else paged_kernel<T, D, N, false><<<dim3(a.groups), block, 0, a.stream>>>(a);
+  if (a.batch.page.value % 16 == 0) paged_kernel<T, D, N, true, kTree><<<dim3(a.groups), block, 0, a.stream>>>(a);
+  else paged_kernel<T, D, N, false, kTree><<<dim3(a.groups), block, 0, a.stream>>>(a);
   profile_mark_end(a.stream);
   if (a.partials) paged_join_kernel<T, D, 16 * N><<<dim3(a.groups, N), block, 0, a.stream>>>(a);
   return hip_status(hipGetLastError());
 }
 
-template <typename T, int D>
+template <typename T, int D, bool kTree>
 sga_status launch_paged_as(const PagedAttention& a) {
   const dim3 block(kWaves * kWave);
   if (a.tile_rows == kChunkRows) {
@@ -1557,25 +1620,25 @@ sga_status launch_paged_as(const PagedAttention& a) {
       int64_t groups = (int64_t)a.slots * a.Hkv;
       if (a.Hkv < 8 && 8 % a.Hkv == 0) groups = (int64_t)(a.slots + 8 / a.Hkv - 1) / (8 / a.Hkv) * 8;
       profile_mark_begin(a.stream, "paged_chunk_kernel");
-      if (a.batch.page.value % 16 == 0) paged_chunk_kernel<T, D, true><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
-      else paged_chunk_kernel<T, D, false><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
+      if (a.batch.page.value % 16 == 0) paged_chunk_kernel<T, D, true, kTree><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
+      else paged_chunk_kernel<T, D, false, kTree><<<dim3((unsigned)groups), block, 0, a.stream>>>(a);
       profile_mark_end(a.stream);
       if (a.partials) paged_chunk_join_kernel<T, D><<<dim3((unsigned)a.groups, kChunkRows / 16), block, 0, a.stream>>>(a);
     }
     return hip_status(hipGetLastError());
   }
   if constexpr (!(sizeof(T) == 4 && D > 64))        // (the registers do not hold two groups of such rows)
-    if (a.tile_rows != kRows) return launch_paged_rows<T, D, 2>(a);
-  return launch_paged_rows<T, D, 1>(a);
+    if (a.tile_rows != kRows) return launch_paged_rows<T, D, 2, kTree>(a);
+  return launch_paged_rows<T, D, 1, kTree>(a);
 }
 
-template <typename T>
+template <typename T, bool kTree>
 sga_status launch_paged_type(const PagedAttention& a) {
   switch (a.d) {
-    case 32: return launch_paged_as<T, 32>(a);
-    case 64: return launch_paged_as<T, 64>(a);
-    case 128: return launch_paged_as<T, 128>(a);
-    default: return launch_paged_as<T, 256>(a);
+    case 32: return launch_paged_as<T, 32, kTree>(a);
+    case 64: return launch_paged_as<T, 64, kTree>(a);
+    case 128: return launch_paged_as<T, 128, kTree>(a);
+    default: return launch_paged_as<T, 256, kTree>(a);
   }
 }
 
@@ -1598,7 +1661,8 @@ PagedPlan plan_paged(const PagedAttention& a) {
   // keys that a tile meets at most
   const int64_t step = p.tile_rows / (int64_t)a.group.value;
   int64_t keys = tokens;
-  const int64_t window = (a.causal ? 1 : 2) * (int64_t)a.window + step + 1 + a.n_global;
+  if (a.words > 0) keys = (int64_t)a.L + 32 * a.words < room ? (int64_t)a.L + 32 * a.words : room;      // (new tokens by their places)
+  const int64_t window = (a.causal ? 1 : 2) * (int64_t)a.window + step + 1 + a.n_global + 32 * a.words;
   if (window < keys && !(a.n_global > 0 && !a.causal)) keys = window;
   if (p.tile_rows == kChunkRows) {
     // cut where the chip would have less than four rounds of tiles, and where a tile can be long enough for two pieces (see piece_of; full
@@ -1622,10 +1686,11 @@ PagedPlan plan_paged(const PagedAttention& a) {
 }
 
 sga_status launch_paged(const PagedAttention& a) {
+  const bool tree = a.depth != nullptr;
   switch (a.dtype) {
-    case SGA_F32: return launch_paged_type<float>(a);
-    case SGA_F16: return launch_paged_type<f16_t>(a);
-    default: return launch_paged_type<bf16_t>(a);
+    case SGA_F32: return tree ? launch_paged_type<float, true>(a) : launch_paged_type<float, false>(a);
+    case SGA_F16: return tree ? launch_paged_type<f16_t, true>(a) : launch_paged_type<f16_t, false>(a);
+    default: return tree ? launch_paged_type<bf16_t, true>(a) : launch_paged_type<bf16_t, false>(a);
   }
 }
 

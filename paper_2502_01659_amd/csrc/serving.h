@@ -1,5 +1,5 @@
-// Shared by the serving kernels (paged_cache.hip, attention_paged.hip): storage types, division by a
-// number that the host knows, and the search for a row's sequence.
+// Shared by the serving kernels (paged_cache.hip, norm_rotary.hip, drafts.hip, attention_paged.hip): storage types, division by a
+// number that the host knows, the search for a row's sequence, and the sines of a position.
 #pragma once
 
 #include "sga_internal.h"
@@ -58,6 +58,36 @@ __device__ __forceinline__ int32_t last_not_above(int32_t n, int64_t x, First fi
   return lo;
 }
 
+// cos t and sin t for t = position * f.  The product is held as a rounded part and its error, and multiples of pi / 2
+// are taken off in 64 bits (pi / 2 as the sum of two numbers, 2^-107 off), twice: the first time about as many as the rounded part has, whose
+// step alone is many turns at far positions, the second time what that and the product's error leave.  Up to |t| = 2^62 the rest
+// is within pi / 4 and good to 2^-40; rounded to 32 bits it is within 2^-25, and the Taylor polynomials of degree 9 and 10 are within 2e-9 there.
+__device__ __forceinline__ float2 turn_of(int64_t position, double f) {
+  constexpr double kQuarters = 0.63661977236758134308, kHigh = 1.57079632679489655800, kLow = 6.12323399573676603587e-17;
+  const double p = (double)position;
+  const double x = p * f, x_low = __builtin_fma(p, f, -x);
+  const double n = __builtin_rint(x * kQuarters);
+  double r = __builtin_fma(-n, kHigh, x);
+  r = __builtin_fma(-n, kLow, r) + x_low;
+  const double rest = __builtin_rint(r * kQuarters);
+  r = __builtin_fma(-rest, kHigh, r);
+  r = __builtin_fma(-rest, kLow, r);
+  const int quarter = (int)(((int64_t)n + (int64_t)rest) & 3);
+  const float y = (float)r, z = y * y;
+  float s = 2.7557319224e-6f, c = -2.7557319224e-7f;
+  s = fmaf(s, z, -1.9841269841e-4f);
+  s = fmaf(s, z, 8.3333333333e-3f);
+  s = fmaf(s, z, -1.6666666667e-1f);
+  s = fmaf(s * z, y, y);
+  c = fmaf(c, z, 2.4801587302e-5f);
+  c = fmaf(c, z, -1.3888888889e-3f);
+  c = fmaf(c, z, 4.1666666667e-2f);
+  c = fmaf(c, z, -0.5f);
+  c = fmaf(c, z, 1.0f);
+  const float cos_t = (quarter & 1) ? s : c, sin_t = (quarter & 1) ? c : s;
+  return make_float2(quarter == 1 || quarter == 2 ? -cos_t : cos_t, quarter >= 2 ? -sin_t : sin_t);
+}
+
 struct RotaryArgs {
   const double* frequencies;
   float magnitude;
@@ -89,6 +119,85 @@ struct RotateArgs {
 };
 sga_status launch_rotate(const RotateArgs& a);
 
+// Norm of every head's row before it turns.
+struct NormArg {
+  const void* weight;        // null: all 1
+  float epsilon, offset;
+  int32_t dtype;             // the weight's
+  int32_t on;
+};
+struct NormRotateArgs {
+  RotateArgs r;
+  NormArg norm[3];           // r.tensor's
+  const int32_t* depth;      // a draft tree's depths: positions count from the sequence's first new token; null: a row's own place
+};
+sga_status launch_norm_rotate(const NormRotateArgs& a);
+
+// One tensor of the backward pass.
+struct NormGradRows {
+  const void *x, *g;
+  void* dx;
+  int64_t x_head, x_row, g_head, g_row, dx_head, dx_row;
+  float* dw;                 // null: not asked for
+  NormArg norm;
+  int32_t heads;
+};
+struct NormGradArgs {
+  NormGradRows tensor[2];
+  int32_t n_tensors, n_rows, d;
+  const int64_t* positions;
+  int64_t first;
+  RotaryArgs rotary;         // inverse
+  float* partials;           // [workgroups][d], null: no dw is asked for
+  int32_t dtype;
+  hipStream_t stream;
+};
+size_t norm_partial_bytes(int64_t n_rows, int32_t Hq, int32_t Hkv, int32_t d);
+sga_status launch_norm_grad(const NormGradArgs& a);
+
+// The next step's pages (sga_pages_advance).
+struct PagesArgs {
+  PagedArgs from;                    // as it was
+  int32_t* page_table;               // as it becomes (may be the same arrays)
+  int64_t* seq_ptr;
+  int32_t* seq_len;
+  int32_t* ring;
+  const int64_t* state;
+  int64_t* state_out;
+  const int32_t* ask;
+  const int32_t* kept;               // null: all rows are
+  int64_t *positions, *slots;        // null: not asked for
+  int32_t give_back, window, n_global;     // give_back: pages behind the window go back
+  int32_t segments, per_segment;     // wavefronts of a sequence, columns of each
+  void* workspace;
+  hipStream_t stream;
+};
+void plan_pages(PagesArgs& a);
+size_t pages_workspace(const PagesArgs& a);
+sga_status launch_pages(const PagesArgs& a);
+
+struct TreeArgs {
+  PagedArgs batch;
+  const int32_t* parent;
+  int32_t* depth;
+  uint32_t* seen;
+  int32_t words;
+  int32_t L, window, n_global;
+  hipStream_t stream;
+};
+sga_status launch_tree(const TreeArgs& a);
+
+struct KeepArgs {
+  PagedArgs batch;
+  char *cache_k, *cache_v;
+  const int32_t *path, *count;
+  int32_t path_columns;
+  int32_t Hkv, layers;
+  int64_t layer_bytes, page_bytes, head_bytes, row_bytes;
+  hipStream_t stream;
+};
+sga_status launch_keep(const KeepArgs& a);
+
 constexpr size_t kNoteBytes = 32;          // (see Note in attention_paged.hip)
 
 struct PagedAttention {
@@ -108,6 +217,9 @@ struct PagedAttention {
   void* notes;               // ... and what is to be joined, one for each workgroup, ahead of them
   int32_t tile_rows, groups, splits, slots;      // the plan's
   int32_t d, dtype;
+  const int32_t* depth;      // a draft tree (null: none): the rows' depths and which new tokens they see
+  const uint32_t* seen;
+  int32_t words;
   hipStream_t stream;
 };
 // The kernel, the workgroups and the partial states of a call.
