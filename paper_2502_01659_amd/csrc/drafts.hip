@@ -8,6 +8,10 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 
+__device__ __forceinline__ uint64_t from_lane64(uint64_t v, int lane) {
+  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, lane);
+}
+
 // ---- the next step's pages ---------------------------------------------------------------------------
 // Sequence s had rows(s) = seq_ptr[s + 1] - seq_ptr[s] new tokens, of which kept[s] stay: l = seq_len - rows + kept.  It asks for
 // want tokens more, so it needs columns ceil(l / page) .. ceil((l + want) / page) - 1 of the table; held pages from there on, wholly
@@ -16,15 +20,17 @@ constexpr int kWaves = kThreads / kWave;
 // sequences take from its front, in their order, and what goes back is put behind its end, in the order (sequence, column), so no
 // place that is read is written and neither order nor result depends on how the work runs.
 // A call is small: what it costs is launches and chains of dependent loads.  Two kernels: the first counts, a wavefront for each segment
-// of a sequence's columns; the second sums what the first counted up to its own sequences (a few kilobytes, from L2), and then goes over the same columns
-// again and writes.  It reads nothing but its own columns, the ring's front and what the first one left, so the arrays may be updated in place.
-struct SequenceNote {
-  int32_t length, want;      // tokens kept, tokens asked for and possible (0 otherwise)
+// of a sequence's columns; in the second each wavefront sums up what the first has left of the sequences up to its own (16 bytes for each, from L2, four a lane
+// at a time), and then goes over the same columns again, which it has asked for before that, and writes.  It reads nothing but its own columns, the
+// ring's front and what the first one left, so the arrays may be updated in place.
+struct alignas(16) SequenceNote {
+  int32_t length, want;      // tokens kept; tokens asked for and possible (0 otherwise), -1 where the sequence ends
+  int32_t need, give;        // pages
 };
-struct SegmentNote {
+struct alignas(8) SegmentNote {
   int32_t need, give;
 };
-struct PoolNote {
+struct alignas(16) PoolNote {
   int64_t first, count;
 };
 
@@ -33,20 +39,24 @@ __device__ __forceinline__ SequenceNote* sequence_notes(const PagesArgs& a) { re
 __device__ __forceinline__ SegmentNote* segment_notes(const PagesArgs& a) {
   return reinterpret_cast<SegmentNote*>(sequence_notes(a) + a.from.n_seqs);
 }
+__device__ __forceinline__ PoolNote read_pool(const PagesArgs& a) {
+  const int64_t n = a.from.n_pages;
+  const int64_t first = a.state[0] % n, count = a.state[1];
+  return PoolNote{first < 0 ? first + n : first, count < 0 ? 0 : count < n ? count : n};
+}
 
 // What becomes of a sequence's columns.
 struct Columns {
-  int64_t length, behind;    // tokens; tokens that lie behind the window
+  int64_t behind;            // tokens that lie behind the window
   int32_t first_new, end;    // columns that new tokens begin, and the first that none is in
   bool ended;
-  __device__ __forceinline__ Columns(const PagesArgs& a, int32_t length_, int32_t want, bool ended_) {
+  __device__ __forceinline__ Columns(const PagesArgs& a, int32_t length, int32_t want) {
     const int64_t page = a.from.page.value;
-    length = length_;
-    ended = ended_;
-    const int64_t top = a.from.pages_per_seq, f = (length + page - 1) / page, e = (length + want + page - 1) / page;
+    ended = want < 0;
+    const int64_t top = a.from.pages_per_seq, f = (length + page - 1) / page, e = ((int64_t)length + (ended ? 0 : want) + page - 1) / page;
     first_new = (int32_t)(f < top ? f : top);
     end = (int32_t)(e < top ? e : top);
-    behind = a.give_back ? length - a.window : INT64_MIN;
+    behind = a.give_back ? (int64_t)length - a.window : INT64_MIN;
   }
   // an entry's fate: it goes back, or (want > 0 is what makes end > first_new) its column needs a page
   __device__ __forceinline__ bool gives(const PagesArgs& a, int32_t column, bool held) const {
@@ -56,23 +66,35 @@ struct Columns {
   __device__ __forceinline__ bool needs(int32_t column, bool held) const { return !held && column >= first_new && column < end; }
 };
 
-__device__ __forceinline__ int32_t entry_of(const PagesArgs& a, int32_t s, int32_t column) {
-  return a.from.page_table[(int64_t)s * a.from.pages_per_seq + column];
+__device__ __forceinline__ const int32_t* row_of(const PagesArgs& a, int32_t s) {
+  return a.from.page_table + (int64_t)s * a.from.pages_per_seq;
 }
 
-__global__ __launch_bounds__(kThreads) void pages_count_kernel(PagesArgs a) {
-  const int lane = threadIdx.x & (kWave - 1);
-  if (blockIdx.x == 0 && threadIdx.x == 0) {
-    const int64_t n = a.from.n_pages;
-    int64_t first = a.state[0] % n, count = a.state[1];
-    first = first < 0 ? first + n : first;
-    count = count < 0 ? 0 : count < n ? count : n;
-    *pool_note(a) = PoolNote{first, count};
-  }
-  const int64_t units = (int64_t)a.from.n_seqs * a.segments;
-  for (int64_t unit = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave; unit < units; unit += (int64_t)gridDim.x * kWaves) {
-    const int32_t s = (int32_t)(unit / a.segments), segment = (int32_t)(unit - (int64_t)s * a.segments);
-    int64_t length = a.from.seq_len[s];
+constexpr int kAsked = 8;              // columns of a lane that are asked for at once
+constexpr int kMostSegments = 16;
+
+// A workgroup has 4 or more wavefronts: the segments of a sequence, or of several.
+__global__ __launch_bounds__(kWave* kMostSegments) void pages_count_kernel(PagesArgs a) {
+  __shared__ SegmentNote notes[kMostSegments];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int32_t here = blockDim.x / kWave / a.segments, s = blockIdx.x * here + wave / a.segments, segment = wave % a.segments;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *pool_note(a) = read_pool(a);
+  const bool there = s < a.from.n_seqs;
+  int64_t length = 0;
+  int32_t want = 0, need = 0, give = 0;
+  if (there) {
+    const int32_t begin = segment * a.per_segment, end = min(begin + a.per_segment, a.from.pages_per_seq);
+    const int32_t* const row = row_of(a, s);
+    int32_t entry[kAsked];
+    auto ask = [&](int32_t from) {
+#pragma unroll
+      for (int i = 0; i < kAsked; ++i) {
+        const int32_t c = from + i * kWave + lane;
+        entry[i] = c < end ? row[c] : -1;
+      }
+    };
+    ask(begin);
+    length = a.from.seq_len[s];
     length = length < 0 ? 0 : length;
     if (a.kept) {
       int64_t rows = a.from.seq_ptr[s + 1] - a.from.seq_ptr[s], kept = a.kept[s];
@@ -80,153 +102,182 @@ __global__ __launch_bounds__(kThreads) void pages_count_kernel(PagesArgs a) {
       kept = kept < 0 ? 0 : kept < rows ? kept : rows;
       length += kept - rows;
     }
-    const int32_t ask = a.ask[s];
-    const bool ended = ask < 0;
-    if (ended) length = 0;
-    const int32_t want = ask > 0 && length + ask <= (int64_t)a.from.pages_per_seq * a.from.page.value ? ask : 0;
-    const Columns columns(a, (int32_t)length, want, ended);
-    const int32_t begin = segment * a.per_segment, end = min(begin + a.per_segment, a.from.pages_per_seq);
-    int32_t need = 0, give = 0;
-#pragma unroll 4
-    for (int32_t c = begin + lane; c < end; c += kWave) {
-      const bool held = (uint32_t)entry_of(a, s, c) < a.from.n_pages;
-      need += columns.needs(c, held);
-      give += columns.gives(a, c, held);
-    }
+    const int32_t ask_for = a.ask[s];
+    if (ask_for < 0) length = 0;
+    want = ask_for < 0 ? -1 : length + ask_for <= (int64_t)a.from.pages_per_seq * a.from.page.value ? ask_for : 0;
+    const Columns columns(a, (int32_t)length, want);
+    for (int32_t c0 = begin; c0 < end; c0 += kAsked * kWave) {
+      int32_t now[kAsked];
 #pragma unroll
-    for (int off = 1; off < kWave; off <<= 1) {
-      need += __shfl_xor(need, off, kWave);
-      give += __shfl_xor(give, off, kWave);
+      for (int i = 0; i < kAsked; ++i) now[i] = entry[i];
+      if (c0 + kAsked * kWave < end) ask(c0 + kAsked * kWave);
+#pragma unroll
+      for (int i = 0; i < kAsked; ++i) {
+        const int32_t c = c0 + i * kWave + lane;
+        const bool held = (uint32_t)now[i] < a.from.n_pages;
+        need += __popcll(__ballot(c < end && columns.needs(c, held)));
+        give += __popcll(__ballot(columns.gives(a, c, held)));
+      }
     }
-    if (lane == 0) {
-      segment_notes(a)[unit] = SegmentNote{need, give};
-      if (segment == 0) sequence_notes(a)[s] = SequenceNote{(int32_t)length, ended ? -1 : want};
+    if (lane == 0) notes[wave] = segment_notes(a)[(int64_t)s * a.segments + segment] = SegmentNote{need, give};
+  }
+  __syncthreads();
+  if (there && segment == 0 && lane == 0) {
+    for (int i = 1; i < a.segments; ++i) {
+      need += notes[wave + i].need;
+      give += notes[wave + i].give;
     }
+    sequence_notes(a)[s] = SequenceNote{(int32_t)length, want, need, give};
   }
 }
 
-__device__ __forceinline__ int64_t sum_up(int64_t x, int64_t (&parts)[kWaves], int64_t& all) {
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+// The wavefront's lanes' sums up to each lane; all: the last one's.
+__device__ __forceinline__ int64_t sum_up(int64_t x, int64_t& all) {
+  const int lane = threadIdx.x & (kWave - 1);
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
     const int64_t below = (int64_t)__shfl_up((unsigned long long)x, off, kWave);
     if (lane >= off) x += below;
   }
-  __syncthreads();                    // the last sum's readers are done
-  if (lane == kWave - 1) parts[wave] = x;
-  __syncthreads();
-  all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) x += parts[w];
-    all += parts[w];
-  }
+  all = (int64_t)from_lane64((uint64_t)x, kWave - 1);
   return x;
 }
 
-__global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int32_t units_per_group) {
-  __shared__ int64_t parts[kWaves];
-  struct Place {
-    int64_t rows, pages, given;       // before the sequence
-    int32_t granted;
-  };
-  __shared__ Place places[kThreads];  // of the sequences of the current chunk
-  const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = tid / kWave;
-  const PoolNote pool = *pool_note(a);
+constexpr int kEach = 4;               // sequences of a lane at a time
+
+__global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(PagesArgs a, int32_t seqs_per_wave) {
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int32_t groups = blockDim.x / kWave / a.segments, S = a.from.n_seqs, segment = wave % a.segments;
+  // this wavefront's sequences, all in the same segment of their columns
+  const int32_t s0 = (int32_t)min((int64_t)(blockIdx.x * groups + wave / a.segments) * seqs_per_wave, (int64_t)S), s1 = min(s0 + seqs_per_wave, S);
+  if (s0 >= s1) return;
   const int64_t n = a.from.n_pages, page = a.from.page.value;
-  const int64_t units = (int64_t)a.from.n_seqs * a.segments;
-  const int64_t unit0 = (int64_t)blockIdx.x * units_per_group, unit1 = min(unit0 + units_per_group, units);
-  if (unit0 >= units) return;
-  const bool last = unit1 == units;
-  const int32_t last_seq = (int32_t)((unit1 - 1) / a.segments);
-  int64_t rows = 0, wanted = 0, pages = 0, taken = 0, given = 0;       // over the chunks before
-  int64_t unit = unit0;
-  for (int32_t chunk = 0; chunk <= last_seq; chunk += kThreads) {
-    const int32_t s = chunk + tid;
-    SequenceNote note{0, 0};
-    int64_t need = 0, give = 0;
-    if (s < a.from.n_seqs) {
-      note = sequence_notes(a)[s];
-      for (int i = 0; i < a.segments; ++i) {
-        const SegmentNote x = segment_notes(a)[(int64_t)s * a.segments + i];
-        need += x.need;
-        give += x.give;
-      }
+  const int32_t begin = segment * a.per_segment, end = min(begin + a.per_segment, a.from.pages_per_seq);
+  // (a lane keeps what it has asked for in LDS: it is met in a loop)
+  __shared__ int32_t asked_for[kMostSegments][kAsked][kWave];
+  int32_t (*const entries)[kWave] = asked_for[wave];
+  auto ask = [&](int32_t s, int32_t from) {
+    const int32_t* const row = row_of(a, s);
+    int32_t entry[kAsked];
+#pragma unroll
+    for (int i = 0; i < kAsked; ++i) {
+      const int32_t c = from + i * kWave + lane;
+      entry[i] = c < end ? row[c] : -1;
     }
-    const int64_t want = note.want > 0 ? note.want : 0;
-    int64_t all_need, all_want, all_rows, all_taken, all_give;
-    const int64_t need_up = pages + sum_up(need, parts, all_need), want_up = wanted + sum_up(want, parts, all_want);
-    const bool granted = want > 0 && want_up <= a.from.n_tokens && (need == 0 || need_up <= pool.count);
-    const int64_t rows_up = rows + sum_up(granted ? want : 0, parts, all_rows);
-    const int64_t taken_up = taken + sum_up(granted ? need : 0, parts, all_taken);
-    const int64_t give_up = given + sum_up(give, parts, all_give);
-    places[tid] = Place{rows_up - (granted ? want : 0), taken_up - (granted ? need : 0), give_up - give, granted};
-    __syncthreads();
-    // the workgroup's units of these sequences, a wavefront each
-    for (int64_t u = unit + wave; u < unit1 && u < (int64_t)(chunk + kThreads) * a.segments; u += kWaves) {
-      const int32_t seq = (int32_t)(u / a.segments), segment = (int32_t)(u - (int64_t)seq * a.segments);
-      const Place at = places[seq - chunk];
-      const SequenceNote mine = sequence_notes(a)[seq];
-      const int32_t want_here = mine.want > 0 ? mine.want : 0;
-      const Columns columns(a, mine.length, want_here, mine.want < 0);
-      int64_t take = at.pages, back = at.given;
+#pragma unroll
+    for (int i = 0; i < kAsked; ++i) entries[i][lane] = entry[i];
+  };
+  ask(s0, begin);
+  const PoolNote pool = *pool_note(a);
+  int64_t rows = 0, wanted = 0, pages = 0, taken = 0, given = 0;       // over the chunks before
+  for (int32_t chunk = 0; chunk < s1; chunk += kEach * kWave) {
+    SequenceNote note[kEach];
+    int64_t want = 0, need = 0, give = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      const int32_t s = chunk + lane * kEach + i;
+      note[i] = s < S ? sequence_notes(a)[s] : SequenceNote{0, 0, 0, 0};
+      want += max(note[i].want, 0);
+      need += note[i].need;
+      give += note[i].give;
+    }
+    int64_t all_want, all_need, all_give, all_rows, all_taken;
+    int64_t want_up = wanted + sum_up(want, all_want) - want, need_up = pages + sum_up(need, all_need) - need;
+    const int64_t give_up = given + sum_up(give, all_give) - give;
+    bool granted[kEach];
+    int64_t own_rows = 0, own_taken = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      want_up += max(note[i].want, 0);
+      need_up += note[i].need;
+      granted[i] = note[i].want > 0 && want_up <= a.from.n_tokens && (note[i].need == 0 || need_up <= pool.count);
+      own_rows += granted[i] ? note[i].want : 0;
+      own_taken += granted[i] ? note[i].need : 0;
+    }
+    const int64_t rows_up = rows + sum_up(own_rows, all_rows) - own_rows, taken_up = taken + sum_up(own_taken, all_taken) - own_taken;
+    for (int32_t s = max(s0, chunk); s < s1 && s < chunk + kEach * kWave; ++s) {
+      const int owner = (s - chunk) / kEach, which = (s - chunk) % kEach;
+      SequenceNote mine{};
+      int64_t before_rows = rows_up, take = taken_up, back = give_up;
+      bool has = false;
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) {
+        if (i == which) {
+          mine = note[i];
+          has = granted[i];
+        } else if (i < which) {
+          before_rows += granted[i] ? note[i].want : 0;
+          take += granted[i] ? note[i].need : 0;
+          back += note[i].give;
+        }
+      }
+      before_rows = (int64_t)from_lane64((uint64_t)before_rows, owner);
+      take = (int64_t)from_lane64((uint64_t)take, owner);
+      back = (int64_t)from_lane64((uint64_t)back, owner);
+      const int32_t length = __builtin_amdgcn_readlane(mine.length, owner), asked = __builtin_amdgcn_readlane(mine.want, owner);
+      has = __builtin_amdgcn_readlane(has ? 1 : 0, owner);
       for (int i = 0; i < segment; ++i) {
-        const SegmentNote x = segment_notes(a)[(int64_t)seq * a.segments + i];
+        const SegmentNote x = segment_notes(a)[(int64_t)s * a.segments + i];
         take += x.need;
         back += x.give;
       }
+      const Columns columns(a, length, asked);
+      const int32_t new_rows = has ? asked : 0;
       if (segment == 0 && lane == 0) {
-        a.seq_ptr[seq] = at.rows;
-        a.seq_len[seq] = mine.length + (at.granted ? want_here : 0);
+        a.seq_ptr[s] = before_rows;
+        a.seq_len[s] = length + new_rows;
       }
-      const int32_t begin = segment * a.per_segment, end = min(begin + a.per_segment, a.from.pages_per_seq);
-      for (int32_t c0 = begin; c0 < end; c0 += kWave) {
-        const int32_t c = c0 + lane;
-        int32_t entry = c < end ? entry_of(a, seq, c) : -1;
-        const bool held = c < end && (uint32_t)entry < a.from.n_pages;
-        const bool gives = columns.gives(a, c, held), needs = c < end && columns.needs(c, held);
-        const uint64_t giving = __ballot(gives), needing = __ballot(needs), below = (uint64_t(1) << lane) - 1;
-        if (gives) {
-          const int64_t r = pool.count + back + __popcll(giving & below);
-          if (r < n) {                                 // (a page that stands in two tables comes back twice)
-            int64_t where = pool.first + r;
-            a.ring[where < n ? where : where - n] = entry;
+      if (s > s0) ask(s, begin);
+      for (int32_t c0 = begin; c0 < end; c0 += kAsked * kWave) {
+        if (c0 > begin) ask(s, c0);
+#pragma unroll 1
+        for (int i = 0; i < kAsked; ++i) {
+          const int32_t first = c0 + i * kWave, c = first + lane;
+          if (first >= end) break;
+          int32_t to = entries[i][lane];
+          const bool held = (uint32_t)to < a.from.n_pages;
+          const bool gives = columns.gives(a, c, held), needs = c < end && columns.needs(c, held);
+          const uint64_t giving = __ballot(gives), needing = __ballot(needs), below = (uint64_t(1) << lane) - 1;
+          if (gives) {
+            const int64_t r = pool.count + back + __popcll(giving & below);
+            if (r < n) {                               // (a page that stands in two tables comes back twice)
+              const int64_t where = pool.first + r;
+              a.ring[where < n ? where : where - n] = to;
+            }
+            to = -1;
           }
-          entry = -1;
-        }
-        if (needs && at.granted) {
-          int64_t where = pool.first + take + __popcll(needing & below);
-          entry = a.ring[where < n ? where : where - n];
-        }
-        if (c < end) a.page_table[(int64_t)seq * a.from.pages_per_seq + c] = entry;
-        back += __popcll(giving);
-        take += __popcll(needing);
-        if (at.granted && (a.positions || a.slots)) {
-          // the new tokens in these columns
-          const int64_t from = max((int64_t)mine.length, c0 * page), to = min((int64_t)mine.length + want_here, min((int64_t)c0 + kWave, (int64_t)end) * page);
-          for (int64_t p0 = from; p0 < to; p0 += kWave) {
-            const int64_t p = p0 + lane;
-            const uint32_t column = quotient((uint32_t)p, a.from.page);
-            const int32_t held_by = __shfl(entry, (int)(column - (uint32_t)c0) & (kWave - 1), kWave);
-            if (p < to) {
-              const int64_t row = at.rows + p - mine.length;
-              if (a.positions) a.positions[row] = p;
-              if (a.slots) a.slots[row] = (uint32_t)held_by < a.from.n_pages ? (int64_t)held_by * page + (p - (int64_t)column * page) : -1;
+          if (needs && has) {
+            const int64_t where = pool.first + take + __popcll(needing & below);
+            to = a.ring[where < n ? where : where - n];
+          }
+          if (c < end) a.page_table[(int64_t)s * a.from.pages_per_seq + c] = to;
+          back += __popcll(giving);
+          take += __popcll(needing);
+          if (has && (a.positions || a.slots)) {
+            // the new tokens in these columns
+            const int64_t from = max((int64_t)length, first * page), stop = min((int64_t)length + new_rows, min((int64_t)first + kWave, (int64_t)end) * page);
+            for (int64_t p0 = from; p0 < stop; p0 += kWave) {
+              const int64_t p = p0 + lane;
+              const uint32_t column = quotient((uint32_t)p, a.from.page);
+              const int32_t held_by = __shfl(to, (int)(column - (uint32_t)first) & (kWave - 1), kWave);
+              if (p < stop) {
+                const int64_t row = before_rows + p - length;
+                if (a.positions) a.positions[row] = p;
+                if (a.slots) a.slots[row] = (uint32_t)held_by < a.from.n_pages ? (int64_t)held_by * page + (p - (int64_t)column * page) : -1;
+              }
             }
           }
         }
       }
     }
-    const int64_t done = (int64_t)(chunk + kThreads) * a.segments;
-    if (unit < done) unit = done < unit1 ? done : unit1;
     rows += all_rows;
     wanted += all_want;
     pages += all_need;
     taken += all_taken;
     given += all_give;
   }
-  if (last && tid == 0) {
-    a.seq_ptr[a.from.n_seqs] = rows;
+  if (s1 == S && segment == 0 && lane == 0) {
+    a.seq_ptr[S] = rows;
     const int64_t first = pool.first + taken;
     a.state_out[0] = first < n ? first : first - n;
     a.state_out[1] = (pool.count + given < n ? pool.count + given : n) - taken;
@@ -235,22 +286,19 @@ __global__ __launch_bounds__(kThreads) void pages_write_kernel(PagesArgs a, int3
 
 __global__ void pages_nothing_kernel(PagesArgs a) {
   a.seq_ptr[0] = 0;
-  const int64_t n = a.from.n_pages;
-  int64_t first = a.state[0] % n, count = a.state[1];
-  a.state_out[0] = first < 0 ? first + n : first;
-  a.state_out[1] = count < 0 ? 0 : count < n ? count : n;
+  const PoolNote pool = read_pool(a);
+  a.state_out[0] = pool.first;
+  a.state_out[1] = pool.count;
 }
 }  // namespace
 
 void plan_pages(PagesArgs& a) {
-  // as many wavefronts as keep the chip's memory busy, as far as a sequence has columns
-  const int64_t S = a.from.n_seqs > 0 ? a.from.n_seqs : 1, C = a.from.pages_per_seq;
-  int64_t segments = 1024 / S;
-  segments = segments < 1 ? 1 : segments > 16 ? 16 : segments;
-  int64_t per = (C + segments - 1) / segments;
-  per = (per + kWave - 1) / kWave * kWave;
-  a.per_segment = (int32_t)per;
-  a.segments = (int32_t)((C + per - 1) / per);
+  // segments of about as many columns as a wavefront asks for at once
+  const int64_t C = a.from.pages_per_seq;
+  int64_t segments = 1;
+  while (segments < kMostSegments && segments * kAsked * kWave < C) segments *= 2;
+  a.segments = (int32_t)segments;
+  a.per_segment = (int32_t)(((C + segments - 1) / segments + kWave - 1) / kWave * kWave);
 }
 
 size_t pages_workspace(const PagesArgs& a) {
@@ -262,12 +310,11 @@ sga_status launch_pages(const PagesArgs& a) {
     pages_nothing_kernel<<<1, 1, 0, a.stream>>>(a);
     return hip_status(hipGetLastError());
   }
-  const int64_t units = (int64_t)a.from.n_seqs * a.segments;
-  const int64_t groups = (units + kWaves - 1) / kWaves;
-  pages_count_kernel<<<(unsigned)(groups < 65536 ? groups : 65536), kThreads, 0, a.stream>>>(a);
-  // (a workgroup sums up all sequences before its own: no more than 1,024 of them do)
-  int64_t per = (groups + 1023) / 1024 * kWaves;
-  pages_write_kernel<<<(unsigned)((units + per - 1) / per), kThreads, 0, a.stream>>>(a, (int32_t)per);
+  const int waves = a.segments > kWaves ? a.segments : kWaves, here = waves / a.segments;
+  pages_count_kernel<<<(unsigned)((a.from.n_seqs + here - 1) / here), waves * kWave, 0, a.stream>>>(a);
+  // (a wavefront sums up all sequences before its own: no more than 4,096 times a segment are they read)
+  const int32_t each = (a.from.n_seqs + 4095) / 4096;
+  pages_write_kernel<<<(unsigned)(((a.from.n_seqs + each - 1) / each + here - 1) / here), waves * kWave, 0, a.stream>>>(a, each);
   return hip_status(hipGetLastError());
 }
 
@@ -335,66 +382,97 @@ __global__ __launch_bounds__(kThreads) void tree_wave_kernel(TreeArgs a) {
   }
 }
 
-// Larger trees: a workgroup each, bits in LDS.
-constexpr int kMostWords = 16;
-__global__ __launch_bounds__(kThreads) void tree_group_kernel(TreeArgs a) {
-  __shared__ int32_t jump[2][32 * kMostWords], depth[2][32 * kMostWords];
-  __shared__ uint32_t bits[32 * kMostWords * kMostWords];
+// Larger trees: a workgroup each, bits in LDS.  What the window leaves of a token's ancestors, itself and those up to `window` steps away, is
+// put together from the same sets on the way: window + 1 as a sum of powers of two, for each of them the set of that size at the place that the ones before
+// have led to.  Only where some token's position is below n_global (or below 0), so that the window does not decide alone, are the bits looked at
+// one by one.  A thread holds up to kItems words of the rows, always the same word of a row, so that nothing is divided.
+constexpr int kMostWords = 16, kMostTokens = 32 * kMostWords, kTreeThreads = 1024, kItems = kMostTokens * kMostWords / kTreeThreads;
+__global__ __launch_bounds__(kTreeThreads) void tree_group_kernel(TreeArgs a) {
+  __shared__ int32_t jump[2][kMostTokens], depth[2][kMostTokens], reach[kMostTokens];
+  __shared__ uint32_t bits[kMostTokens * kMostWords];
   const int tid = threadIdx.x, words = a.words;
   for (int32_t s = blockIdx.x; s < a.batch.n_seqs; s += gridDim.x) {
     const int32_t begin = row_of_sequence(a.batch, s), rows = row_of_sequence(a.batch, s + 1) - begin;
     if (rows <= 0) continue;
     const int32_t most = 32 * words, n = rows < most ? rows : most, used = (n + 31) / 32;
     const int64_t base = (int64_t)a.batch.seq_len[s] - rows;
+    const int shift = used <= 1 ? 0 : 32 - __builtin_clz(used - 1);            // words of a row in LDS: a power of two
+    const int w = tid & ((1 << shift) - 1), t0 = tid >> shift, apart = kTreeThreads >> shift;
+    const bool whole_window = a.window >= n - 1, one_by_one = base < 0 || base < a.n_global;
     __syncthreads();                                  // the sequence before is done with LDS
-    for (int32_t t = tid; t < n; t += kThreads) {
-      const int32_t p = parent_of(a, begin + t, t);
-      jump[0][t] = p;
-      depth[0][t] = p >= 0 ? 1 : 0;
+    if (tid < n) {
+      const int32_t p = parent_of(a, begin + tid, tid);
+      jump[0][tid] = p;
+      depth[0][tid] = p >= 0 ? 1 : 0;
+      reach[tid] = tid;
     }
-    for (int32_t i = tid; i < n * used; i += kThreads) {
-      const int32_t t = i / used, w = i - t * used;
-      bits[i] = t / 32 == w ? 1u << (t % 32) : 0u;
+    uint32_t all[kItems], near[kItems];
+#pragma unroll
+    for (int m = 0; m < kItems; ++m) {
+      const int32_t t = t0 + m * apart;
+      all[m] = t < n && t / 32 == w ? 1u << (t % 32) : 0u;
+      near[m] = 0;
+      if (t < n) bits[(t << shift) + w] = all[m];
     }
+    __syncthreads();
     int now = 0;
-    bool more = true;
-    while (more) {
-      __syncthreads();
-      bool any = false;
-      for (int32_t t = tid; t < n; t += kThreads) {
-        const int32_t j = jump[now][t];
-        jump[1 - now][t] = j >= 0 ? jump[now][j] : -1;
-        depth[1 - now][t] = depth[now][t] + (j >= 0 ? depth[now][j] : 0);
-        any |= j >= 0;
+    // round k: `bits` holds the sets of 2^k tokens, jump[now] the 2^k-th ancestors
+    for (uint32_t steps = whole_window || one_by_one ? 0u : (uint32_t)a.window + 1;; steps >>= 1) {
+      const bool any = __syncthreads_or(tid < n && jump[now][tid] >= 0);
+      if (steps & 1 || (!any && steps)) {             // (no jump left: the sets are whole, larger ones are the same)
+#pragma unroll
+        for (int m = 0; m < kItems; ++m) {
+          const int32_t t = t0 + m * apart;
+          if (t < n && reach[t] >= 0) near[m] |= bits[(reach[t] << shift) + w];
+        }
+        __syncthreads();
+        if (tid < n && reach[tid] >= 0) reach[tid] = jump[now][reach[tid]];
       }
-      // (a row that another thread has already extended holds more of the same ancestors)
-      for (int32_t i = tid; i < n * used; i += kThreads) {
-        const int32_t t = i / used, w = i - t * used, j = jump[now][t];
-        if (j >= 0 && 32 * w <= j) bits[i] |= bits[j * used + w];
+      if (!any) break;
+      uint32_t more[kItems];
+#pragma unroll
+      for (int m = 0; m < kItems; ++m) {
+        const int32_t t = t0 + m * apart, j = t < n ? jump[now][t] : -1;
+        more[m] = j >= 0 ? bits[(j << shift) + w] : 0u;
+      }
+      if (tid < n) {
+        const int32_t j = jump[now][tid];
+        jump[1 - now][tid] = j >= 0 ? jump[now][j] : -1;
+        depth[1 - now][tid] = depth[now][tid] + (j >= 0 ? depth[now][j] : 0);
+      }
+      __syncthreads();
+#pragma unroll
+      for (int m = 0; m < kItems; ++m) {
+        const int32_t t = t0 + m * apart;
+        all[m] |= more[m];
+        if (t < n && more[m]) bits[(t << shift) + w] = all[m];
       }
       now = 1 - now;
-      more = __syncthreads_or(any);
     }
-    for (int32_t t = tid; t < n; t += kThreads) a.depth[begin + t] = depth[now][t];
-    for (int32_t i = tid; i < rows * words; i += kThreads) {
-      const int32_t t = i / words, w = i - t * words;
-      uint32_t x = 0;
-      if (t < n && w < used) {
-        x = bits[t * used + w];
-        const int32_t own = depth[now][t];
-        const int64_t p = base + own;
-        if (p < 0 || p >= a.L) {
-          x = 0;
-        } else if (own > a.window || base < 0) {
-          for (uint32_t left = x; left; left &= left - 1) {
-            const int bit = __ffs(left) - 1;
-            if (!mask_lets(a, base, own, depth[now][32 * w + bit])) x &= ~(1u << bit);
-          }
+    if (tid < n) a.depth[begin + tid] = depth[now][tid];
+    for (int32_t t = n + tid; t < rows; t += kTreeThreads) a.depth[begin + t] = -1;
+#pragma unroll
+    for (int m = 0; m < kItems; ++m) {
+      const int32_t t = t0 + m * apart;
+      if (t >= n || w >= used) continue;
+      const int32_t own = depth[now][t];
+      const int64_t p = base + own;
+      uint32_t x = whole_window || one_by_one ? all[m] : near[m];
+      if (p < 0 || p >= a.L) {
+        x = 0;
+      } else if (one_by_one && (own > a.window || base < 0)) {
+        for (uint32_t left = x; left; left &= left - 1) {
+          const int bit = __ffs(left) - 1;
+          if (!mask_lets(a, base, own, depth[now][32 * w + bit])) x &= ~(1u << bit);
         }
       }
-      a.seen[(int64_t)begin * words + i] = x;
+      a.seen[(int64_t)(begin + t) * words + w] = x;
     }
-    for (int32_t t = n + tid; t < rows; t += kThreads) a.depth[begin + t] = -1;
+    // words that no token of the sequence has, and rows without room in the tree
+    if (used < words)
+      for (int32_t i = tid; i < n * (words - used); i += kTreeThreads)
+        a.seen[(int64_t)(begin + i / (words - used)) * words + used + i % (words - used)] = 0;
+    for (int64_t i = (int64_t)n * words + tid; i < (int64_t)rows * words; i += kTreeThreads) a.seen[(int64_t)begin * words + i] = 0;
   }
 }
 
@@ -405,7 +483,7 @@ sga_status launch_tree(const TreeArgs& a) {
     const int64_t groups = ((int64_t)a.batch.n_seqs + kWaves - 1) / kWaves;
     tree_wave_kernel<<<(unsigned)(groups < 65536 ? groups : 65536), kThreads, 0, a.stream>>>(a);
   } else {
-    tree_group_kernel<<<(unsigned)(a.batch.n_seqs < 65536 ? a.batch.n_seqs : 65536), kThreads, 0, a.stream>>>(a);
+    tree_group_kernel<<<(unsigned)(a.batch.n_seqs < 65536 ? a.batch.n_seqs : 65536), kTreeThreads, 0, a.stream>>>(a);
   }
   return hip_status(hipGetLastError());
 }
@@ -422,6 +500,7 @@ constexpr int kRound = 64, kAtOnce = 8;
 template <typename Piece>
 __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, FastDiv pieces, uint32_t total) {
   __shared__ int64_t from[kRound], to[kRound];
+  __shared__ int32_t moves;
   const int tid = threadIdx.x;
   const PagedArgs& b = a.batch;
   for (int32_t s = blockIdx.x; s < b.n_seqs; s += gridDim.x) {
@@ -434,7 +513,7 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, FastDiv piec
     };
     for (int32_t k0 = 0; k0 < count; k0 += kRound) {
       __syncthreads();
-      if (tid < kRound) {
+      if (tid < kRound) {                                  // (one wavefront) the moves there are, one behind the other
         const int32_t k = k0 + tid;
         int64_t x = -1, y = -1;
         if (k < count) {
@@ -444,24 +523,28 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, FastDiv piec
             y = place(base + k);
           }
         }
-        from[tid] = y < 0 ? -1 : x;
-        to[tid] = y;
+        const uint64_t moving = __ballot(x >= 0 && y >= 0);
+        if (x >= 0 && y >= 0) {
+          const int at = __popcll(moving & ((uint64_t(1) << tid) - 1));
+          from[at] = x;
+          to[at] = y;
+        }
+        if (tid == 0) moves = __popcll(moving);
       }
       __syncthreads();
-      const int32_t here = min(count - k0, kRound);
+      const int32_t here = moves;
       // rows of all layers, keys and values, key heads
-      for (uint32_t i = blockIdx.y * kThreads + tid; i < total; i += gridDim.y * kThreads) {
+      for (uint32_t i = blockIdx.y * kThreads + tid; here > 0 && i < total; i += gridDim.y * kThreads) {
         const uint32_t row = quotient(i, pieces), at = i - row * pieces.value;
         const uint32_t half = row / (uint32_t)a.Hkv, head = row - half * (uint32_t)a.Hkv;
         char* const cache = ((half & 1) ? a.cache_v : a.cache_k) + (int64_t)(half >> 1) * a.layer_bytes + head * a.head_bytes + at * (int64_t)sizeof(Piece);
         for (int32_t k = 0; k < here; k += kAtOnce) {
           Piece x[kAtOnce];
 #pragma unroll
-          for (int e = 0; e < kAtOnce; ++e)
-            if (k + e < here && from[k + e] >= 0) x[e] = *reinterpret_cast<const Piece*>(cache + from[k + e]);
+          for (int e = 0; e < kAtOnce; ++e) x[e] = *reinterpret_cast<const Piece*>(cache + from[min(k + e, here - 1)]);
 #pragma unroll
           for (int e = 0; e < kAtOnce; ++e)
-            if (k + e < here && from[k + e] >= 0) *reinterpret_cast<Piece*>(cache + to[k + e]) = x[e];
+            if (k + e < here) *reinterpret_cast<Piece*>(cache + to[k + e]) = x[e];
         }
       }
     }

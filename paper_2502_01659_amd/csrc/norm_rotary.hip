@@ -47,9 +47,7 @@ __device__ __forceinline__ float weight_at(const NormArg& n, int c) {
   return w + n.offset;
 }
 
-__device__ __forceinline__ float inverse_size(float squares, int d, float epsilon) {
-  return rsqrtf(squares / (float)d + epsilon);
-}
+__device__ __forceinline__ float inverse_size(float squares, float per, float epsilon) { return rsqrtf(fmaf(squares, per, epsilon)); }
 
 // The channels of item k of a row: V from `at` and V from `at2`; where it turns, its cosines and sines are kTurns V k ..
 template <int V>
@@ -148,6 +146,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
   extern __shared__ __align__(16) float shared[];
   __shared__ int64_t position[kMaxTokens], cache_row[kMaxTokens];
   const int tid = threadIdx.x, tokens = shape.tokens.value, d = a.r.d;
+  const float per = 1.f / (float)d;
   float* const weights = shared;                                                     // [tensors][d]
   float2* const turns = reinterpret_cast<float2*>(shared + ((a.r.n_tensors * d + 3) & ~3));     // [tokens][channels / 2]
   const int pairs = a.r.rotary.channels >> 1;
@@ -165,10 +164,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
     const int count = min(a.r.n_rows - row0, tokens);
     __syncthreads();                                          // the rows before these are done with the turns
     find_tokens<kPaged>(a, row0, count, position, cache_row);
-    __syncthreads();
-    find_turns(a.r.rotary, count, position, turns);
-    __syncthreads();
-
+    if constexpr (kPaged) __syncthreads();
     struct Row {
       const T* src;
       T* dst;
@@ -198,6 +194,11 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
       row.there = !kPaged || (position[t] != kNone && !(x.paged && cache_row[t] < 0));
       return row;
     };
+    auto make_turns = [&]() {
+      if constexpr (!kPaged) __syncthreads();
+      find_turns(a.r.rotary, count, position, turns);
+      __syncthreads();
+    };
     const uint32_t total = (uint32_t)tokens * shape.heads.value, step = kThreads / kRowLanes;
     if constexpr (kLanes > 0) {
       using Vec = vec_t<T, V>;
@@ -210,7 +211,8 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
       uint32_t i = tid / kLanes;
       Row row = locate(i);
       Vec u = {}, v = {};
-      if (i < total) load(row, u, v);
+      if (i < total) load(row, u, v);                          // (on its way while the sines are computed)
+      make_turns();
       for (; i < total; i += step) {
         const Row here = row;
         float x[V], y[V];
@@ -232,7 +234,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
 #pragma unroll
             for (int e = 0; e < V; ++e) squares = fmaf(x[e], x[e], fmaf(y[e], y[e], squares));
           }
-          const float r = inverse_size(group_sum<kLanes>(squares), d, norm.epsilon);
+          const float r = inverse_size(group_sum<kLanes>(squares), per, norm.epsilon);
           const float* const w = weights + here.which * d;
           if (k < shape.items) {
 #pragma unroll
@@ -254,6 +256,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
         *reinterpret_cast<Vec*>(here.dst + item.at2) = q;
       }
     } else {
+      make_turns();
       for (uint32_t i = tid / kWave; i < total; i += step) {
         const Row row = locate(i);
         if (!row.there) continue;
@@ -262,7 +265,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
         if (norm.on) {
           float squares = 0.f;
           for (int c = k; c < d; c += kWave) squares = fmaf((float)row.src[c], (float)row.src[c], squares);
-          r = inverse_size(group_sum<kWave>(squares), d, norm.epsilon);
+          r = inverse_size(group_sum<kWave>(squares), per, norm.epsilon);
         }
         const float* const w = weights + row.which * d;
         for (int j = k; j < (d + 1) / 2; j += kWave) {
@@ -348,6 +351,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormGradArgs a, Gra
   extern __shared__ __align__(16) float shared[];
   __shared__ int64_t position[kGradTokens];
   const int tid = threadIdx.x, d = a.d, pairs = a.rotary.channels >> 1;
+  const float per = 1.f / (float)d;
   const int which = (int)blockIdx.x >= shape.groups[0] ? 1 : 0;
   const int32_t group = blockIdx.x - (which ? shape.groups[0] : 0), groups = shape.groups[which];
   const int tokens = shape.tokens[which];
@@ -435,8 +439,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormGradArgs a, Gra
               mixed = fmaf(wu[e], u[e], fmaf(wv[e], v[e], mixed));
             }
           }
-          const float r = inverse_size(group_sum<kLanes>(squares), d, x.norm.epsilon);
-          const float share = group_sum<kLanes>(mixed) * r / (float)d;           // mean of w g n
+          const float r = inverse_size(group_sum<kLanes>(squares), per, x.norm.epsilon);
+          const float share = group_sum<kLanes>(mixed) * r * per;           // mean of w g n
           if (mine) {
 #pragma unroll
             for (int e = 0; e < V; ++e) {
@@ -479,8 +483,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormGradArgs a, Gra
             if (two) mixed = fmaf(weights[item.at2] * q[0], v, mixed);
           }
         }
-        const float r = x.norm.on ? inverse_size(group_sum<kWave>(squares), d, x.norm.epsilon) : 1.f;
-        const float share = group_sum<kWave>(mixed) * r / (float)d;
+        const float r = x.norm.on ? inverse_size(group_sum<kWave>(squares), per, x.norm.epsilon) : 1.f;
+        const float share = group_sum<kWave>(mixed) * r * per;
 #pragma unroll
         for (int n = 0; n < kPieces; ++n) {
           const int j = k + n * kWave;
