@@ -8,10 +8,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 
-__device__ __forceinline__ uint64_t from_lane64(uint64_t v, int lane) {
-  return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(v >> 32), lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)v, lane);
-}
-
 // ---- the next step's pages ---------------------------------------------------------------------------
 // Sequence s had rows(s) = seq_ptr[s + 1] - seq_ptr[s] new tokens, of which kept[s] stay: l = seq_len - rows + kept.  It asks for
 // want tokens more, so it needs columns ceil(l / page) .. ceil((l + want) / page) - 1 of the table; held pages from there on, wholly
@@ -28,7 +24,7 @@ struct alignas(16) SequenceNote {
   int32_t need, give;        // pages
 };
 struct alignas(8) SegmentNote {
-  int32_t need, give;
+  int32_t need, give;        // of the sequence's segments before it
 };
 struct alignas(16) PoolNote {
   int64_t first, count;
@@ -119,33 +115,42 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_count_kernel(Pages
         give += __popcll(__ballot(columns.gives(a, c, held)));
       }
     }
-    if (lane == 0) notes[wave] = segment_notes(a)[(int64_t)s * a.segments + segment] = SegmentNote{need, give};
+    if (lane == 0) notes[wave] = SegmentNote{need, give};
   }
   __syncthreads();
-  if (there && segment == 0 && lane == 0) {
-    for (int i = 1; i < a.segments; ++i) {
-      need += notes[wave + i].need;
-      give += notes[wave + i].give;
+  if (there && lane == 0) {
+    SegmentNote before{0, 0};
+    for (int i = wave - segment; i < wave; ++i) {
+      before.need += notes[i].need;
+      before.give += notes[i].give;
     }
-    sequence_notes(a)[s] = SequenceNote{(int32_t)length, want, need, give};
+    segment_notes(a)[(int64_t)s * a.segments + segment] = before;
+    if (segment == a.segments - 1) sequence_notes(a)[s] = SequenceNote{(int32_t)length, want, before.need + need, before.give + give};
   }
 }
 
-// The wavefront's lanes' sums up to each lane; all: the last one's.
-__device__ __forceinline__ int64_t sum_up(int64_t x, int64_t& all) {
-  const int lane = threadIdx.x & (kWave - 1);
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int64_t below = (int64_t)__shfl_up((unsigned long long)x, off, kWave);
-    if (lane >= off) x += below;
-  }
-  all = (int64_t)from_lane64((uint64_t)x, kWave - 1);
-  return x;
+// Sums that stop at 2^31 - 1: more tokens or pages than there are, whatever comes.
+constexpr uint32_t kFull = 0x7fffffff;
+__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return min(a + b, kFull); }
+template <int kCtrl, int kRows>
+__device__ __forceinline__ uint32_t with_lane(uint32_t x) {
+  return plus(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, kRows, 0xF, false));
 }
+// The sums up to each lane: within 16 lanes by shifts, then the last of 16 and of 32 to those behind them.
+__device__ __forceinline__ uint32_t sum_up(uint32_t x) {
+  x = with_lane<0x111, 0xF>(x);
+  x = with_lane<0x112, 0xF>(x);
+  x = with_lane<0x114, 0xF>(x);
+  x = with_lane<0x118, 0xF>(x);
+  x = with_lane<0x142, 0xA>(x);
+  return with_lane<0x143, 0xC>(x);
+}
+__device__ __forceinline__ uint32_t of_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
 constexpr int kEach = 4;               // sequences of a lane at a time
 
 __global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(PagesArgs a, int32_t seqs_per_wave) {
+  extern __shared__ int32_t asked_for[];                   // [wavefronts][kAsked][kWave]: what a lane has asked for (it is met in a loop)
   const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
   const int32_t groups = blockDim.x / kWave / a.segments, S = a.from.n_seqs, segment = wave % a.segments;
   // this wavefront's sequences, all in the same segment of their columns
@@ -153,9 +158,8 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(Pages
   if (s0 >= s1) return;
   const int64_t n = a.from.n_pages, page = a.from.page.value;
   const int32_t begin = segment * a.per_segment, end = min(begin + a.per_segment, a.from.pages_per_seq);
-  // (a lane keeps what it has asked for in LDS: it is met in a loop)
-  __shared__ int32_t asked_for[kMostSegments][kAsked][kWave];
-  int32_t (*const entries)[kWave] = asked_for[wave];
+  int32_t* const entries = asked_for + wave * (kAsked * kWave) + lane;
+  SegmentNote before;
   auto ask = [&](int32_t s, int32_t from) {
     const int32_t* const row = row_of(a, s);
     int32_t entry[kAsked];
@@ -165,40 +169,53 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(Pages
       entry[i] = c < end ? row[c] : -1;
     }
 #pragma unroll
-    for (int i = 0; i < kAsked; ++i) entries[i][lane] = entry[i];
+    for (int i = 0; i < kAsked; ++i) entries[i * kWave] = entry[i];
   };
-  ask(s0, begin);
   const PoolNote pool = *pool_note(a);
-  int64_t rows = 0, wanted = 0, pages = 0, taken = 0, given = 0;       // over the chunks before
+  uint32_t rows = 0, wanted = 0, pages = 0, taken = 0, given = 0;      // over the chunks before
   for (int32_t chunk = 0; chunk < s1; chunk += kEach * kWave) {
     SequenceNote note[kEach];
-    int64_t want = 0, need = 0, give = 0;
+    uint32_t want = 0, need = 0, give = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       const int32_t s = chunk + lane * kEach + i;
       note[i] = s < S ? sequence_notes(a)[s] : SequenceNote{0, 0, 0, 0};
-      want += max(note[i].want, 0);
-      need += note[i].need;
-      give += note[i].give;
     }
-    int64_t all_want, all_need, all_give, all_rows, all_taken;
-    int64_t want_up = wanted + sum_up(want, all_want) - want, need_up = pages + sum_up(need, all_need) - need;
-    const int64_t give_up = given + sum_up(give, all_give) - give;
-    bool granted[kEach];
-    int64_t own_rows = 0, own_taken = 0;
+    if (chunk == 0) {                                      // (on their way while the sums are made)
+      before = segment_notes(a)[(int64_t)s0 * a.segments + segment];
+      ask(s0, begin);
+    }
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      want_up += max(note[i].want, 0);
-      need_up += note[i].need;
-      granted[i] = note[i].want > 0 && want_up <= a.from.n_tokens && (note[i].need == 0 || need_up <= pool.count);
+      want = plus(want, max(note[i].want, 0));
+      need = plus(need, note[i].need);
+      give = plus(give, note[i].give);
+    }
+    const uint32_t want_sum = sum_up(want), need_sum = sum_up(need), give_sum = sum_up(give);
+    // (what a lane's sequences follow: the sum up to the lane before)
+    auto ahead = [&](uint32_t sum, uint32_t first) {
+      const uint32_t up = __shfl_up(sum, 1, kWave);
+      return plus(first, lane > 0 ? up : 0u);
+    };
+    uint32_t want_up = ahead(want_sum, wanted), need_up = ahead(need_sum, pages);
+    const uint32_t give_up = ahead(give_sum, given);
+    bool granted[kEach];
+    uint32_t own_rows = 0, own_taken = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      want_up = plus(want_up, max(note[i].want, 0));
+      need_up = plus(need_up, note[i].need);
+      granted[i] = note[i].want > 0 && want_up <= (uint32_t)a.from.n_tokens && (note[i].need == 0 || (int64_t)need_up <= pool.count);
       own_rows += granted[i] ? note[i].want : 0;
       own_taken += granted[i] ? note[i].need : 0;
     }
-    const int64_t rows_up = rows + sum_up(own_rows, all_rows) - own_rows, taken_up = taken + sum_up(own_taken, all_taken) - own_taken;
+    // (what is granted fits n_tokens and the ring: 31 bits)
+    const uint32_t rows_sum = sum_up(own_rows), taken_sum = sum_up(own_taken);
+    const uint32_t rows_up = rows + rows_sum - own_rows, taken_up = taken + taken_sum - own_taken;
     for (int32_t s = max(s0, chunk); s < s1 && s < chunk + kEach * kWave; ++s) {
       const int owner = (s - chunk) / kEach, which = (s - chunk) % kEach;
       SequenceNote mine{};
-      int64_t before_rows = rows_up, take = taken_up, back = give_up;
+      uint32_t mine_rows = rows_up, mine_taken = taken_up, mine_given = give_up;
       bool has = false;
 #pragma unroll
       for (int i = 0; i < kEach; ++i) {
@@ -206,21 +223,16 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(Pages
           mine = note[i];
           has = granted[i];
         } else if (i < which) {
-          before_rows += granted[i] ? note[i].want : 0;
-          take += granted[i] ? note[i].need : 0;
-          back += note[i].give;
+          mine_rows += granted[i] ? note[i].want : 0;
+          mine_taken += granted[i] ? note[i].need : 0;
+          mine_given = plus(mine_given, note[i].give);
         }
       }
-      before_rows = (int64_t)from_lane64((uint64_t)before_rows, owner);
-      take = (int64_t)from_lane64((uint64_t)take, owner);
-      back = (int64_t)from_lane64((uint64_t)back, owner);
+      if (s > s0) before = segment_notes(a)[(int64_t)s * a.segments + segment];
+      const int64_t before_rows = of_lane(mine_rows, owner);
+      int64_t take = (int64_t)of_lane(mine_taken, owner) + before.need, back = (int64_t)of_lane(mine_given, owner) + before.give;
       const int32_t length = __builtin_amdgcn_readlane(mine.length, owner), asked = __builtin_amdgcn_readlane(mine.want, owner);
       has = __builtin_amdgcn_readlane(has ? 1 : 0, owner);
-      for (int i = 0; i < segment; ++i) {
-        const SegmentNote x = segment_notes(a)[(int64_t)s * a.segments + i];
-        take += x.need;
-        back += x.give;
-      }
       const Columns columns(a, length, asked);
       const int32_t new_rows = has ? asked : 0;
       if (segment == 0 && lane == 0) {
@@ -234,7 +246,7 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(Pages
         for (int i = 0; i < kAsked; ++i) {
           const int32_t first = c0 + i * kWave, c = first + lane;
           if (first >= end) break;
-          int32_t to = entries[i][lane];
+          int32_t to = entries[i * kWave];
           const bool held = (uint32_t)to < a.from.n_pages;
           const bool gives = columns.gives(a, c, held), needs = c < end && columns.needs(c, held);
           const uint64_t giving = __ballot(gives), needing = __ballot(needs), below = (uint64_t(1) << lane) - 1;
@@ -270,11 +282,11 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(Pages
         }
       }
     }
-    rows += all_rows;
-    wanted += all_want;
-    pages += all_need;
-    taken += all_taken;
-    given += all_give;
+    rows += of_lane(rows_sum, kWave - 1);
+    taken += of_lane(taken_sum, kWave - 1);
+    wanted = plus(wanted, of_lane(want_sum, kWave - 1));
+    pages = plus(pages, of_lane(need_sum, kWave - 1));
+    given = plus(given, of_lane(give_sum, kWave - 1));
   }
   if (s1 == S && segment == 0 && lane == 0) {
     a.seq_ptr[S] = rows;
@@ -314,7 +326,8 @@ sga_status launch_pages(const PagesArgs& a) {
   pages_count_kernel<<<(unsigned)((a.from.n_seqs + here - 1) / here), waves * kWave, 0, a.stream>>>(a);
   // (a wavefront sums up all sequences before its own: no more than 4,096 times a segment are they read)
   const int32_t each = (a.from.n_seqs + 4095) / 4096;
-  pages_write_kernel<<<(unsigned)(((a.from.n_seqs + each - 1) / each + here - 1) / here), waves * kWave, 0, a.stream>>>(a, each);
+  pages_write_kernel<<<(unsigned)(((a.from.n_seqs + each - 1) / each + here - 1) / here), waves * kWave, waves * kAsked * kWave * sizeof(int32_t),
+                       a.stream>>>(a, each);
   return hip_status(hipGetLastError());
 }
 
@@ -503,7 +516,7 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, FastDiv piec
   __shared__ int32_t moves;
   const int tid = threadIdx.x;
   const PagedArgs& b = a.batch;
-  for (int32_t s = blockIdx.x; s < b.n_seqs; s += gridDim.x) {
+  for (int32_t s = blockIdx.y; s < b.n_seqs; s += gridDim.y) {
     const int64_t rows = b.seq_ptr[s + 1] - b.seq_ptr[s], base = (int64_t)b.seq_len[s] - rows;
     const int32_t count = min(a.count[s], a.path_columns);
     auto place = [&](int64_t slot) -> int64_t {
@@ -534,7 +547,7 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, FastDiv piec
       __syncthreads();
       const int32_t here = moves;
       // rows of all layers, keys and values, key heads
-      for (uint32_t i = blockIdx.y * kThreads + tid; here > 0 && i < total; i += gridDim.y * kThreads) {
+      for (uint32_t i = blockIdx.x * kThreads + tid; here > 0 && i < total; i += gridDim.x * kThreads) {
         const uint32_t row = quotient(i, pieces), at = i - row * pieces.value;
         const uint32_t half = row / (uint32_t)a.Hkv, head = row - half * (uint32_t)a.Hkv;
         char* const cache = ((half & 1) ? a.cache_v : a.cache_k) + (int64_t)(half >> 1) * a.layer_bytes + head * a.head_bytes + at * (int64_t)sizeof(Piece);
@@ -559,7 +572,7 @@ sga_status launch_keep_as(const KeepArgs& a) {
   int64_t across = (total + kThreads - 1) / kThreads;
   across = across < 1 ? 1 : across > 256 ? 256 : across;
   const int32_t groups = a.batch.n_seqs < 16384 ? a.batch.n_seqs : 16384;       // (a grid holds fewer than 2^32 threads)
-  keep_kernel<Piece><<<dim3((unsigned)groups, (unsigned)across), kThreads, 0, a.stream>>>(a, fast_div(pieces), (uint32_t)total);
+  keep_kernel<Piece><<<dim3((unsigned)across, (unsigned)groups), kThreads, 0, a.stream>>>(a, fast_div(pieces), (uint32_t)total);
   return hip_status(hipGetLastError());
 }
 
