@@ -15,10 +15,10 @@ constexpr int kWaves = kThreads / kWave;
 // s, it is granted where R fits the packed rows and P what is free (or where it needs no page).  Free pages are a ring: granted
 // sequences take from its front, in their order, and what goes back is put behind its end, in the order (sequence, column), so no
 // place that is read is written and neither order nor result depends on how the work runs.
-// A call is small: what it costs is launches and chains of dependent loads.  Two kernels: the first counts, a wavefront for each segment
-// of a sequence's columns; in the second each wavefront sums up what the first has left of the sequences up to its own (16 bytes for each, from L2, four a lane
-// at a time), and then goes over the same columns again, which it has asked for before that, and writes.  It reads nothing but its own columns, the
-// ring's front and what the first one left, so the arrays may be updated in place.
+// A call is small: what it costs is launches, chains of dependent loads and, at hundreds of sequences, instructions.  Two kernels: the first
+// counts, a wavefront for each segment of a sequence's columns; in the second a sequence's first wavefront sums up what the first kernel has left of the sequences
+// up to its own (16 bytes for each, from L2, two a lane at a time), while the others ask for their columns, and then each goes over the same columns again
+// and writes.  It reads nothing but its own columns, the ring's front and what the first kernel left, so the arrays may be updated in place.
 struct alignas(16) SequenceNote {
   int32_t length, want;      // tokens kept; tokens asked for and possible (0 otherwise), -1 where the sequence ends
   int32_t need, give;        // pages
@@ -43,22 +43,21 @@ __device__ __forceinline__ PoolNote read_pool(const PagesArgs& a) {
 
 // What becomes of a sequence's columns.
 struct Columns {
-  int64_t behind;            // tokens that lie behind the window
-  int32_t first_new, end;    // columns that new tokens begin, and the first that none is in
-  bool ended;
+  int32_t first_new, end;    // columns that new tokens begin, and the first that none is in (all go back where the sequence ends)
+  int32_t global, behind;    // columns from `global` on and below `behind` lie behind the window
   __device__ __forceinline__ Columns(const PagesArgs& a, int32_t length, int32_t want) {
-    const int64_t page = a.from.page.value;
-    ended = want < 0;
-    const int64_t top = a.from.pages_per_seq, f = (length + page - 1) / page, e = ((int64_t)length + (ended ? 0 : want) + page - 1) / page;
-    first_new = (int32_t)(f < top ? f : top);
-    end = (int32_t)(e < top ? e : top);
-    behind = a.give_back ? (int64_t)length - a.window : INT64_MIN;
+    auto below = [&](uint32_t tokens) { return (int32_t)quotient(tokens, a.from.page); };
+    auto up_to = [&](uint32_t tokens) {
+      const uint32_t q = quotient(tokens, a.from.page);
+      return (int32_t)(q + (q * a.from.page.value != tokens));
+    };
+    first_new = min(up_to(length), a.from.pages_per_seq);
+    end = want < 0 ? 0 : min(up_to(length + want), a.from.pages_per_seq);       // (what is asked for fits the columns)
+    global = up_to(a.n_global);
+    behind = a.give_back && length > a.window ? below(length - a.window) : 0;
   }
   // an entry's fate: it goes back, or (want > 0 is what makes end > first_new) its column needs a page
-  __device__ __forceinline__ bool gives(const PagesArgs& a, int32_t column, bool held) const {
-    const int64_t from = (int64_t)column * a.from.page.value;
-    return held && (ended || column >= end || (from + a.from.page.value <= behind && from >= a.n_global));
-  }
+  __device__ __forceinline__ bool gives(int32_t column, bool held) const { return held && (column >= end || (column < behind && column >= global)); }
   __device__ __forceinline__ bool needs(int32_t column, bool held) const { return !held && column >= first_new && column < end; }
 };
 
@@ -112,7 +111,7 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_count_kernel(Pages
         const int32_t c = c0 + i * kWave + lane;
         const bool held = (uint32_t)now[i] < a.from.n_pages;
         need += __popcll(__ballot(c < end && columns.needs(c, held)));
-        give += __popcll(__ballot(columns.gives(a, c, held)));
+        give += __popcll(__ballot(columns.gives(c, held)));
       }
     }
     if (lane == 0) notes[wave] = SegmentNote{need, give};
@@ -147,59 +146,43 @@ __device__ __forceinline__ uint32_t sum_up(uint32_t x) {
 }
 __device__ __forceinline__ uint32_t of_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
-constexpr int kEach = 4;               // sequences of a lane at a time
+constexpr int kEach = 2;               // sequences of a lane at a time
 
-__global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(PagesArgs a, int32_t seqs_per_wave) {
-  extern __shared__ int32_t asked_for[];                   // [wavefronts][kAsked][kWave]: what a lane has asked for (it is met in a loop)
-  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
-  const int32_t groups = blockDim.x / kWave / a.segments, S = a.from.n_seqs, segment = wave % a.segments;
-  // this wavefront's sequences, all in the same segment of their columns
-  const int32_t s0 = (int32_t)min((int64_t)(blockIdx.x * groups + wave / a.segments) * seqs_per_wave, (int64_t)S), s1 = min(s0 + seqs_per_wave, S);
-  if (s0 >= s1) return;
-  const int64_t n = a.from.n_pages, page = a.from.page.value;
-  const int32_t begin = segment * a.per_segment, end = min(begin + a.per_segment, a.from.pages_per_seq);
-  int32_t* const entries = asked_for + wave * (kAsked * kWave) + lane;
-  SegmentNote before;
-  auto ask = [&](int32_t s, int32_t from) {
-    const int32_t* const row = row_of(a, s);
-    int32_t entry[kAsked];
-#pragma unroll
-    for (int i = 0; i < kAsked; ++i) {
-      const int32_t c = from + i * kWave + lane;
-      entry[i] = c < end ? row[c] : -1;
-    }
-#pragma unroll
-    for (int i = 0; i < kAsked; ++i) entries[i * kWave] = entry[i];
-  };
-  const PoolNote pool = *pool_note(a);
-  uint32_t rows = 0, wanted = 0, pages = 0, taken = 0, given = 0;      // over the chunks before
-  for (int32_t chunk = 0; chunk < s1; chunk += kEach * kWave) {
-    SequenceNote note[kEach];
+// A walk over all sequences' notes, a wavefront's: what the sequences of the current kEach * kWave have to themselves and before them.
+struct Walk {
+  int32_t end = 0;                                         // of the sequences at hand
+  uint32_t rows = 0, wanted = 0, pages = 0, taken = 0, given = 0;      // before them
+  SequenceNote note[kEach];
+  bool granted[kEach];
+  uint32_t rows_sum = 0, want_sum = 0, need_sum = 0, taken_sum = 0, give_sum = 0;      // up to and with each lane's
+  uint32_t rows_up = 0, taken_up = 0, give_up = 0;         // before each lane's
+
+  __device__ __forceinline__ void next(const PagesArgs& a, const PoolNote& pool) {
+    const int lane = threadIdx.x & (kWave - 1);
+    rows += of_lane(rows_sum, kWave - 1);
+    taken += of_lane(taken_sum, kWave - 1);
+    wanted = plus(wanted, of_lane(want_sum, kWave - 1));
+    pages = plus(pages, of_lane(need_sum, kWave - 1));
+    given = plus(given, of_lane(give_sum, kWave - 1));
     uint32_t want = 0, need = 0, give = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int32_t s = chunk + lane * kEach + i;
-      note[i] = s < S ? sequence_notes(a)[s] : SequenceNote{0, 0, 0, 0};
-    }
-    if (chunk == 0) {                                      // (on their way while the sums are made)
-      before = segment_notes(a)[(int64_t)s0 * a.segments + segment];
-      ask(s0, begin);
-    }
-#pragma unroll
-    for (int i = 0; i < kEach; ++i) {
+      const int32_t s = end + lane * kEach + i;
+      note[i] = s < a.from.n_seqs ? sequence_notes(a)[s] : SequenceNote{0, 0, 0, 0};
       want = plus(want, max(note[i].want, 0));
       need = plus(need, note[i].need);
       give = plus(give, note[i].give);
     }
-    const uint32_t want_sum = sum_up(want), need_sum = sum_up(need), give_sum = sum_up(give);
+    want_sum = sum_up(want);
+    need_sum = sum_up(need);
+    give_sum = sum_up(give);
     // (what a lane's sequences follow: the sum up to the lane before)
     auto ahead = [&](uint32_t sum, uint32_t first) {
       const uint32_t up = __shfl_up(sum, 1, kWave);
       return plus(first, lane > 0 ? up : 0u);
     };
     uint32_t want_up = ahead(want_sum, wanted), need_up = ahead(need_sum, pages);
-    const uint32_t give_up = ahead(give_sum, given);
-    bool granted[kEach];
+    give_up = ahead(give_sum, given);
     uint32_t own_rows = 0, own_taken = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
@@ -210,89 +193,136 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(Pages
       own_taken += granted[i] ? note[i].need : 0;
     }
     // (what is granted fits n_tokens and the ring: 31 bits)
-    const uint32_t rows_sum = sum_up(own_rows), taken_sum = sum_up(own_taken);
-    const uint32_t rows_up = rows + rows_sum - own_rows, taken_up = taken + taken_sum - own_taken;
-    for (int32_t s = max(s0, chunk); s < s1 && s < chunk + kEach * kWave; ++s) {
-      const int owner = (s - chunk) / kEach, which = (s - chunk) % kEach;
-      SequenceNote mine{};
-      uint32_t mine_rows = rows_up, mine_taken = taken_up, mine_given = give_up;
-      bool has = false;
+    rows_sum = sum_up(own_rows);
+    taken_sum = sum_up(own_taken);
+    rows_up = rows + rows_sum - own_rows;
+    taken_up = taken + taken_sum - own_taken;
+    end += kEach * kWave;
+  }
+};
+// What a sequence's wavefronts have to know of it.
+struct Granted {
+  int32_t length, want;      // want: -1 where the sequence ends
+  int32_t rows;              // new tokens that it gets
+  uint32_t row, take, back;  // before it: packed rows, pages taken, pages given back
+};
+
+__global__ __launch_bounds__(kWave* kMostSegments) void pages_write_kernel(PagesArgs a, int32_t seqs_per_wave) {
+  extern __shared__ int32_t asked_for[];                   // [wavefronts][kAsked][kWave]: what a lane has asked for (it is met in a loop)
+  __shared__ Granted told[kMostSegments];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave;
+  const int32_t groups = blockDim.x / kWave / a.segments, S = a.from.n_seqs, group = wave / a.segments, segment = wave % a.segments;
+  // this wavefront's sequences, all in the same segment of their columns; the first segment's walks over those before them
+  const int64_t s0 = (int64_t)(blockIdx.x * groups + group) * seqs_per_wave;
+  const int64_t n = a.from.n_pages, page = a.from.page.value;
+  const int32_t begin = segment * a.per_segment, end = min(begin + a.per_segment, a.from.pages_per_seq);
+  int32_t* const entries = asked_for + wave * (kAsked * kWave) + lane;
+  const PoolNote pool = *pool_note(a);
+  const bool moved = a.page_table != a.from.page_table;    // all entries are written, not only those that change
+  Walk walk;
+  for (int32_t turn = 0; turn < seqs_per_wave; ++turn) {
+    const int32_t s = (int32_t)min(s0 + turn, (int64_t)S);
+    auto ask = [&](int32_t from) {
+      const int32_t* const row = row_of(a, s);
+      int32_t entry[kAsked];
 #pragma unroll
-      for (int i = 0; i < kEach; ++i) {
-        if (i == which) {
-          mine = note[i];
-          has = granted[i];
-        } else if (i < which) {
-          mine_rows += granted[i] ? note[i].want : 0;
-          mine_taken += granted[i] ? note[i].need : 0;
-          mine_given = plus(mine_given, note[i].give);
+      for (int i = 0; i < kAsked; ++i) {
+        const int32_t c = from + i * kWave + lane;
+        entry[i] = c < end ? row[c] : -1;
+      }
+#pragma unroll
+      for (int i = 0; i < kAsked; ++i) entries[i * kWave] = entry[i];
+    };
+    SegmentNote before{0, 0};
+    if (s < S) {
+      before = segment_notes(a)[(int64_t)s * a.segments + segment];
+      ask(begin);
+      if (segment == 0) {
+        while (walk.end <= s) walk.next(a, pool);
+        const int32_t place = s - (walk.end - kEach * kWave);
+        const int owner = place / kEach, which = place % kEach;
+        Granted g{0, 0, 0, walk.rows_up, walk.taken_up, walk.give_up};
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+          if (i == which) {
+            g.length = walk.note[i].length;
+            g.want = walk.note[i].want;
+            g.rows = walk.granted[i] ? g.want : 0;
+          } else if (i < which) {
+            g.row += walk.granted[i] ? walk.note[i].want : 0;
+            g.take += walk.granted[i] ? walk.note[i].need : 0;
+            g.back = plus(g.back, walk.note[i].give);
+          }
+        }
+        if (lane == owner) {
+          told[group] = g;
+          a.seq_ptr[s] = g.row;
+          a.seq_len[s] = g.length + g.rows;
+        }
+        if (s == S - 1 && lane == kWave - 1) {
+          a.seq_ptr[S] = walk.rows + walk.rows_sum;
+          const int64_t taken = walk.taken + walk.taken_sum, given = plus(walk.given, walk.give_sum);
+          const int64_t first = pool.first + taken;
+          a.state_out[0] = first < n ? first : first - n;
+          a.state_out[1] = (pool.count + given < n ? pool.count + given : n) - taken;
         }
       }
-      if (s > s0) before = segment_notes(a)[(int64_t)s * a.segments + segment];
-      const int64_t before_rows = of_lane(mine_rows, owner);
-      int64_t take = (int64_t)of_lane(mine_taken, owner) + before.need, back = (int64_t)of_lane(mine_given, owner) + before.give;
-      const int32_t length = __builtin_amdgcn_readlane(mine.length, owner), asked = __builtin_amdgcn_readlane(mine.want, owner);
-      has = __builtin_amdgcn_readlane(has ? 1 : 0, owner);
-      const Columns columns(a, length, asked);
-      const int32_t new_rows = has ? asked : 0;
-      if (segment == 0 && lane == 0) {
-        a.seq_ptr[s] = before_rows;
-        a.seq_len[s] = length + new_rows;
-      }
-      if (s > s0) ask(s, begin);
-      for (int32_t c0 = begin; c0 < end; c0 += kAsked * kWave) {
-        if (c0 > begin) ask(s, c0);
+    }
+    __syncthreads();
+    const Granted g = told[group];
+    __syncthreads();                                       // (the next turn's are told in the same place)
+    if (s >= S) continue;
+    const int32_t length = __builtin_amdgcn_readfirstlane(g.length), asked = __builtin_amdgcn_readfirstlane(g.want);
+    const int32_t new_rows = __builtin_amdgcn_readfirstlane(g.rows);
+    int64_t take = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)g.take) + before.need;
+    int64_t back = (int64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)g.back) + before.give;
+    const int64_t first_row = (uint32_t)__builtin_amdgcn_readfirstlane((int)g.row);
+    const Columns columns(a, length, asked);
+    for (int32_t c0 = begin; c0 < end; c0 += kAsked * kWave) {
+      if (c0 > begin) ask(c0);
 #pragma unroll 1
-        for (int i = 0; i < kAsked; ++i) {
-          const int32_t first = c0 + i * kWave, c = first + lane;
-          if (first >= end) break;
-          int32_t to = entries[i * kWave];
-          const bool held = (uint32_t)to < a.from.n_pages;
-          const bool gives = columns.gives(a, c, held), needs = c < end && columns.needs(c, held);
-          const uint64_t giving = __ballot(gives), needing = __ballot(needs), below = (uint64_t(1) << lane) - 1;
+      for (int i = 0; i < kAsked; ++i) {
+        const int32_t first = c0 + i * kWave, c = first + lane;
+        if (first >= end) break;
+        int32_t to = entries[i * kWave];
+        const bool held = (uint32_t)to < a.from.n_pages;
+        const bool gives = columns.gives(c, held), needs = c < end && columns.needs(c, held);
+        const uint64_t giving = __ballot(gives), needing = __ballot(needs);
+        if (giving) {
           if (gives) {
-            const int64_t r = pool.count + back + __popcll(giving & below);
-            if (r < n) {                               // (a page that stands in two tables comes back twice)
+            const int64_t r = pool.count + back + __popcll(giving & ((uint64_t(1) << lane) - 1));
+            if (r < n) {                                   // (a page that stands in two tables comes back twice)
               const int64_t where = pool.first + r;
               a.ring[where < n ? where : where - n] = to;
             }
             to = -1;
           }
-          if (needs && has) {
-            const int64_t where = pool.first + take + __popcll(needing & below);
+          back += __popcll(giving);
+        }
+        if (needing) {
+          if (needs && new_rows > 0) {
+            const int64_t where = pool.first + take + __popcll(needing & ((uint64_t(1) << lane) - 1));
             to = a.ring[where < n ? where : where - n];
           }
-          if (c < end) a.page_table[(int64_t)s * a.from.pages_per_seq + c] = to;
-          back += __popcll(giving);
           take += __popcll(needing);
-          if (has && (a.positions || a.slots)) {
-            // the new tokens in these columns
-            const int64_t from = max((int64_t)length, first * page), stop = min((int64_t)length + new_rows, min((int64_t)first + kWave, (int64_t)end) * page);
-            for (int64_t p0 = from; p0 < stop; p0 += kWave) {
-              const int64_t p = p0 + lane;
-              const uint32_t column = quotient((uint32_t)p, a.from.page);
-              const int32_t held_by = __shfl(to, (int)(column - (uint32_t)first) & (kWave - 1), kWave);
-              if (p < stop) {
-                const int64_t row = before_rows + p - length;
-                if (a.positions) a.positions[row] = p;
-                if (a.slots) a.slots[row] = (uint32_t)held_by < a.from.n_pages ? (int64_t)held_by * page + (p - (int64_t)column * page) : -1;
-              }
+        }
+        if (c < end && (moved || gives || needs)) a.page_table[(int64_t)s * a.from.pages_per_seq + c] = to;
+        if (new_rows > 0 && (a.positions || a.slots)) {
+          // the new tokens in these columns
+          const int64_t from = max((int64_t)length, first * page), stop = min((int64_t)length + new_rows, min((int64_t)first + kWave, (int64_t)end) * page);
+          for (int64_t p0 = from; p0 < stop; p0 += kWave) {
+            const int64_t p = p0 + lane;
+            const uint32_t column = quotient((uint32_t)p, a.from.page);
+            const int32_t held_by = __shfl(to, (int)(column - (uint32_t)first) & (kWave - 1), kWave);
+            if (p < stop) {
+              const int64_t row = first_row + p - length;
+              if (a.positions) a.positions[row] = p;
+              if (a.slots) a.slots[row] = (uint32_t)held_by < a.from.n_pages ? (int64_t)held_by * page + (p - (int64_t)column * page) : -1;
             }
           }
         }
       }
     }
-    rows += of_lane(rows_sum, kWave - 1);
-    taken += of_lane(taken_sum, kWave - 1);
-    wanted = plus(wanted, of_lane(want_sum, kWave - 1));
-    pages = plus(pages, of_lane(need_sum, kWave - 1));
-    given = plus(given, of_lane(give_sum, kWave - 1));
-  }
-  if (s1 == S && segment == 0 && lane == 0) {
-    a.seq_ptr[S] = rows;
-    const int64_t first = pool.first + taken;
-    a.state_out[0] = first < n ? first : first - n;
-    a.state_out[1] = (pool.count + given < n ? pool.count + given : n) - taken;
   }
 }
 
@@ -508,7 +538,17 @@ sga_status launch_tree(const TreeArgs& a) {
 // kRound rows at once.
 namespace {
 
-constexpr int kRound = 64, kAtOnce = 8;
+constexpr int kRound = 64;
+
+// kRows rows' pieces at once: loaded, then stored.  (No condition within: the loads would wait for each other's.)
+template <int kRows, typename Piece>
+__device__ __forceinline__ void move(char* cache, const int64_t* from, const int64_t* to, Piece) {
+  Piece x[kRows];
+#pragma unroll
+  for (int e = 0; e < kRows; ++e) x[e] = *reinterpret_cast<const Piece*>(cache + from[e]);
+#pragma unroll
+  for (int e = 0; e < kRows; ++e) *reinterpret_cast<Piece*>(cache + to[e]) = x[e];
+}
 
 template <typename Piece>
 __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, FastDiv pieces, uint32_t total) {
@@ -545,20 +585,23 @@ __global__ __launch_bounds__(kThreads) void keep_kernel(KeepArgs a, FastDiv piec
         if (tid == 0) moves = __popcll(moving);
       }
       __syncthreads();
-      const int32_t here = moves;
+      const int32_t here = __builtin_amdgcn_readfirstlane(moves);
       // rows of all layers, keys and values, key heads
       for (uint32_t i = blockIdx.x * kThreads + tid; here > 0 && i < total; i += gridDim.x * kThreads) {
         const uint32_t row = quotient(i, pieces), at = i - row * pieces.value;
         const uint32_t half = row / (uint32_t)a.Hkv, head = row - half * (uint32_t)a.Hkv;
         char* const cache = ((half & 1) ? a.cache_v : a.cache_k) + (int64_t)(half >> 1) * a.layer_bytes + head * a.head_bytes + at * (int64_t)sizeof(Piece);
-        for (int32_t k = 0; k < here; k += kAtOnce) {
-          Piece x[kAtOnce];
-#pragma unroll
-          for (int e = 0; e < kAtOnce; ++e) x[e] = *reinterpret_cast<const Piece*>(cache + from[min(k + e, here - 1)]);
-#pragma unroll
-          for (int e = 0; e < kAtOnce; ++e)
-            if (k + e < here) *reinterpret_cast<Piece*>(cache + to[k + e]) = x[e];
+        int32_t k = 0;
+        for (; k + 8 <= here; k += 8) move<8>(cache, from + k, to + k, Piece{});
+        if (here - k >= 4) {
+          move<4>(cache, from + k, to + k, Piece{});
+          k += 4;
         }
+        if (here - k >= 2) {
+          move<2>(cache, from + k, to + k, Piece{});
+          k += 2;
+        }
+        if (here > k) move<1>(cache, from + k, to + k, Piece{});
       }
     }
   }
@@ -581,7 +624,7 @@ sga_status launch_keep_as(const KeepArgs& a) {
 sga_status launch_keep(const KeepArgs& a) {
   const int64_t all = (int64_t)reinterpret_cast<uintptr_t>(a.cache_k) | (int64_t)reinterpret_cast<uintptr_t>(a.cache_v) | a.layer_bytes |
                       a.head_bytes | a.row_bytes | a.page_bytes;
-  if (all % 16 == 0) return launch_keep_as<uint4>(a);
+  if (all % 16 == 0) return launch_keep_as<vec_t<uint32_t, 4>>(a);
   if (all % 4 == 0) return launch_keep_as<uint32_t>(a);
   return launch_keep_as<uint16_t>(a);
 }
