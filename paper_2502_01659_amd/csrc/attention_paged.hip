@@ -32,7 +32,17 @@ constexpr int kWaves = 4;             // wavefronts of a workgroup, which take i
 // least piece 512 / 1,024 / 2,048 keys, 512 tokens behind 8k 128 / 111 / 98, four chunks of 64 behind 8k 106 / 64 / 64, 64 channels
 // and one head per key head 69 / 70 / 121.)
 constexpr int kLeastPiece = 1024, kLeastPieceF32 = 256;
+// ... of drafted tokens, which come few at a time (us, least piece 1,024 / 512 / 256, bf16, 32 / 8 heads of 128: eight sequences of 12 tokens behind 500 to
+// 3,000 35.7 / 26.0 / 28.8, one of 24 behind 8,000 34.2 / 28.2 / 30.4)
+constexpr int kLeastPieceTree = 512;
+constexpr int least_piece(bool tree, int dtype) { return dtype == SGA_F32 ? kLeastPieceF32 : tree ? kLeastPieceTree : kLeastPiece; }
 constexpr int kChunkPieces = 1536;
+// Drafted tokens under a window, or behind contexts of one length: the tiles of 128 rows are all alike.  Where they are more than the places on the
+// chip, whole rounds of them are not cut, and what is left is cut into as many pieces as fill the places once more: fewer prologues and hardly any
+// partial states.  (Key heads that share the XCDs, so that pieces start in their order.  us, cut by kChunkPieces / so: 16 tokens of 64 and of 100 sequences under a
+// window of 2,048, 32 / 8 heads of 128, bf16 133 / 114, 212 / 188; 30 to 200 tokens of 32 sequences under 4,096, 32 / 4 heads, fp16 232 / 225.)
+constexpr float kAlike = 1.25f;
+constexpr int kMostTreeWords = 16;
 
 // Sequences with more rows than this on average take tiles of 128 rows.  (us, short tiles / tiles of 128 rows, 8 heads, behind 4k to 16k; bf16, 32
 // sequences: 29 rows d = 64 123 / 137, d = 128 232 / 252, d = 256 427 / 504; 33 rows 191 / 142, 391 / 255, 854 / 511.  Full precision, 8 sequences, where
@@ -121,14 +131,17 @@ __device__ __forceinline__ int32_t tree_row(const PagedAttention& a, const Tile&
   const int64_t p = (int64_t)(t.length - t.n_new) + depth;
   return depth < 0 || p < 0 || p >= a.L ? -1 : t.begin + token;
 }
-// Which of the keys j0 .. j0 + 31 a row sees as new tokens.
-__device__ __forceinline__ uint32_t new_tokens_seen(const PagedAttention& a, const Tile& t, int32_t row, int32_t j0) {
+// Which of the keys j0 .. j0 + 31 a row sees as new tokens; seen: the row's words.
+__device__ __forceinline__ uint32_t new_tokens_seen(const PagedAttention& a, const Tile& t, const uint32_t* seen, int32_t j0) {
   const int32_t start = j0 - (t.length - t.n_new), word = start >> 5, shift = start & 31;
-  if (row < 0 || start <= -kBlock || word >= a.words || j0 >= t.kept) return 0;
-  const uint32_t* const seen = a.seen + (int64_t)row * a.words;
+  if (start <= -kBlock || word >= a.words || j0 >= t.kept) return 0;
   const uint32_t low = word >= 0 ? seen[word] : 0, high = shift && word + 1 < a.words ? seen[word + 1] : 0;
   const uint32_t bits = shift ? low >> shift | high << (32 - shift) : low;
   return t.kept - j0 < kBlock ? bits & ((1u << (t.kept - j0)) - 1) : bits;
+}
+
+__device__ __forceinline__ uint32_t new_tokens_seen(const PagedAttention& a, const Tile& t, int32_t row, int32_t j0) {
+  return row < 0 ? 0 : new_tokens_seen(a, t, a.seen + (int64_t)row * a.words, j0);
 }
 
 template <bool kTree>
@@ -186,6 +199,7 @@ __device__ __forceinline__ Tile tile_of(const PagedAttention& a, int32_t seq, in
 // drafts at d = 256 60 / 53 / 71; kLeastShare 256 / 512 / 1,024, drafts 72 / 67 / 81.)
 constexpr uint32_t kTileCost = 256;
 constexpr uint32_t kLeastShare = 512;      // keys of the smallest share
+constexpr uint32_t kLeastShareTree = 256;  // ... of drafted tokens (seven behind 2,000, one head of 64, fp32 512 / 256: 17.0 / 15.6 us)
 constexpr uint32_t kWholeTiles = 32;       // tiles shorter than this part of a share are not cut
 // ... nor are a sequence's tiles that are all shorter than this, as long as a share holds one for each wavefront: a cut costs about as much
 // as the unevenness that it takes away.  (us, cut / not: 512 sequences of windows of 128, d = 64 85 / 75, 700 sequences of up to 600
@@ -346,7 +360,8 @@ struct Share {
         uint64_t each = total;
         if (a.groups > 1) {
           each = quotient64(total + a.groups - 1, a.groups);
-          each = each > kLeastShare ? each : kLeastShare;
+          const uint32_t least = kTree ? kLeastShareTree : kLeastShare;
+          each = each > least ? each : least;
         }
         size = each;
         at = each * i;
@@ -472,6 +487,9 @@ struct alignas(16) Note {
 static_assert(sizeof(Note) == kNoteBytes, "the plan counts on this");
 __device__ __forceinline__ Note* notes_of(const PagedAttention& a) { return reinterpret_cast<Note*>(a.notes); }
 
+// Wavefronts per SIMD that registers and the ring of blocks leave to tiles of 128 rows.
+__host__ __device__ constexpr int chunk_waves(int row_bytes) { return row_bytes > 256 ? 1 : row_bytes > 128 ? 2 : 3; }
+
 // Which piece of which tile of 128 rows workgroup `rest` of a key head has.  Not causal, a sequence's first tiles may hold global
 // rows, which see everything, and the others see a window; causal, all count as its longest one.  The tiles of
 // a kind are all cut into as many pieces as make them about the size at which the call has kChunkPieces of them
@@ -492,14 +510,63 @@ __device__ __forceinline__ bool piece_of(const PagedAttention& a, int32_t rest, 
     all_length = (float)w.a0;
     length = (float)(a.causal && w.t1 > 0 ? max(w.a1, w.length_of(w.t1 - 1, step_of<kTileRows>(a))) : w.a1);
   };
-  float total = 0.f;
+  float total = 0.f, longest = 0.f;
+  int32_t tiles = 0;
   for (int32_t c = 0; c < n; c += kWave) {
     look(c + l);
     total += (float)all * all_length + (float)rows * length;
+    if constexpr (kTree) {
+      tiles += rows;
+      longest = fmaxf(longest, rows > 0 ? length : 0.f);
+    }
   }
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) total += __shfl_xor(total, off, kWave);
-  const float size = fmaxf((float)(a.dtype == SGA_F32 ? kLeastPieceF32 : kLeastPiece), total * (float)a.Hkv * (1.f / kChunkPieces));
+  if constexpr (kTree) {
+#pragma unroll
+    for (int off = 1; off < kWave; off <<= 1) {
+      tiles += __shfl_xor(tiles, off, kWave);
+      longest = fmaxf(longest, __shfl_xor(longest, off, kWave));
+    }
+    tiles = __builtin_amdgcn_readfirstlane(tiles);
+    const float most = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, longest)));
+    const bool alike = __builtin_amdgcn_readfirstlane(longest * (float)tiles <= kAlike * total);
+    const int32_t places = 256 * chunk_waves(a.d * (a.dtype == SGA_F32 ? 4 : 2)), whole = tiles * a.Hkv / places * places / a.Hkv;
+    if (a.splits > 1 && 8 % a.Hkv == 0 && whole > 0 && alike) {
+      const int32_t left = tiles - whole;
+      int32_t ordinal = rest;                               // of the tile, over the sequences
+      piece = 0;
+      pieces = 1;
+      apart = max(left, 1);
+      if (rest >= whole) {
+        if (left == 0) return false;
+        pieces = max(1, min(places / (left * a.Hkv), (int32_t)__builtin_amdgcn_readfirstlane((int)(most / (float)least_piece(true, a.dtype)))));
+        piece = (rest - whole) / left;
+        if (piece >= pieces) return false;
+        ordinal = whole + (rest - whole) - piece * left;
+      }
+      int32_t behind = 0;
+      for (int32_t c = 0; c < n; c += kWave) {
+        if (n > kWave) look(c + l);
+        int32_t sum = rows;
+        for (int off = 1; off < kWave && off < n; off <<= 1) {
+          const int32_t below = __shfl_up(sum, off, kWave);
+          if (l >= off) sum += below;
+        }
+        const uint64_t begun = __ballot(rows > 0 && behind + sum - rows <= ordinal && ordinal < behind + sum);
+        if (begun) {
+          const int lane = __builtin_ctzll(begun);
+          index = ordinal - behind - __builtin_amdgcn_readlane(sum - rows, lane);
+          tile = tile_of<kTileRows, kTree>(a, c + lane, __builtin_amdgcn_readlane(w.begin, lane), __builtin_amdgcn_readlane(w.n_new, lane),
+                                           __builtin_amdgcn_readlane(w.length, lane), index);
+          return true;
+        }
+        behind += __builtin_amdgcn_readlane(sum, min(n - c, kWave) - 1);
+      }
+      return false;
+    }
+  }
+  const float size = fmaxf((float)least_piece(kTree, a.dtype), total * (float)a.Hkv * (1.f / kChunkPieces));
   auto cuts = [&](float x) { return a.splits > 1 ? max(1, (int32_t)(x / size + 0.5f)) : 1; };
   int32_t behind = 0;
   for (int32_t c = 0; c < n; c += kWave) {
@@ -1082,9 +1149,8 @@ struct ChunkBlock {
   static __device__ __forceinline__ int k_turn(int row) { return row >> 2 & 3; }
 };
 
-// Row sizes that the ring fits, and the wavefronts per SIMD that registers and LDS then leave.
+// Row sizes that the ring fits.
 __host__ __device__ constexpr bool chunk_fits(int64_t row_bytes) { return row_bytes >= 128 && row_bytes <= 512; }
-constexpr int chunk_waves(int row_bytes) { return row_bytes > 256 ? 1 : row_bytes > 128 ? 2 : 3; }
 
 template <typename T, int D, bool kWholeTiles, bool kTree>
 __global__ __attribute__((amdgpu_waves_per_eu(chunk_waves(sizeof(T) * D), chunk_waves(sizeof(T) * D)))) __launch_bounds__(kWaves* kWave) void
@@ -1099,8 +1165,10 @@ paged_chunk_kernel(PagedAttention a) {
   __shared__ __align__(16) char ring[kChunkSlots * kSlotBytes];
   // Pages that do not hold multiples of 16 tokens: the page of every key of the next kAskBlocks blocks, asked for at once.  (A
   // load into registers between the copies would make its reader wait for all of them.)
-  constexpr int kAskBlocks = 64;
+  constexpr int kAskBlocks = kTree ? 32 : 64;
   __shared__ int32_t page_of_key[kWholeTiles ? 1 : kAskBlocks * kBlock];
+  // (a draft tree) The rows' words of `seen`, for the same reason ahead of the copies.
+  __shared__ uint32_t seen_words[kTree ? kChunkRows * kMostTreeWords : 1];
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = lane & 31, h = lane >> 5;
   // Workgroup i runs on XCD i % 8: a key head stays on one XCD, or on 8 / Hkv of them, whose L2 then holds the keys that
@@ -1143,8 +1211,13 @@ paged_chunk_kernel(PagedAttention a) {
   const int32_t flat = tile.first + (exists ? row : tile.count - 1);
   const int32_t token = (int32_t)quotient((uint32_t)flat, a.group), head = head_kv * group + (flat - token * group);
   Sight sight = row_sight<kTree>(a, tile, token);
-  int32_t seen_row = -1;                                               // (of a draft tree)
-  if constexpr (kTree) seen_row = tree_row(a, tile, token);
+  if constexpr (kTree) {
+    for (int i = tid; i < kChunkRows * a.words; i += kWaves * kWave) {
+      const int r = i / a.words;
+      const int32_t from = r < tile.count ? tree_row(a, tile, (int32_t)quotient((uint32_t)(tile.first + r), a.group)) : -1;
+      seen_words[i] = from >= 0 ? a.seen[(int64_t)from * a.words + (i - r * a.words)] : 0;
+    }
+  }
   if (own_first >= tile.count) sight = Sight{0, -1, 0};                // a wavefront without rows only copies
   Piece qf[kSteps];
   {
@@ -1363,7 +1436,7 @@ paged_chunk_kernel(PagedAttention a) {
     products(k, s);
     const uint32_t held = held_of(j0);
     uint32_t drafted = 0;
-    if constexpr (kTree) drafted = new_tokens_seen(a, tile, seen_row, j0);
+    if constexpr (kTree) drafted = new_tokens_seen(a, tile, seen_words + row * a.words, j0);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       const int in_block = 8 * (r / 4) + 4 * h + r % 4, j = j0 + in_block;
@@ -1667,7 +1740,7 @@ PagedPlan plan_paged(const PagedAttention& a) {
   if (p.tile_rows == kChunkRows) {
     // cut where the chip would have less than four rounds of tiles, and where a tile can be long enough for two pieces (see piece_of; full
     // precision would cut from 128 keys on, for which a join does not pay)
-    const int64_t least = single ? kLeastPieceF32 : kLeastPiece;
+    const int64_t least = least_piece(a.words > 0, a.dtype);
     p.splits = tiles * a.Hkv < 2048 && keys > kLeastShare && 2 * (keys + kTileCost) >= 3 * least ? 2 : 1;
     const int64_t slots = tiles + (p.splits > 1 ? (kChunkPieces + a.Hkv - 1) / a.Hkv + 1 : 0);
     if (slots * a.Hkv + 8 >= int64_t(1) << 24) return p;                    // (a grid holds fewer than 2^32 threads)
@@ -1679,7 +1752,7 @@ PagedPlan plan_paged(const PagedAttention& a) {
   // workgroups that the chip holds at once, and that have the least share to do if every tile met all the keys that it can
   const int64_t row_bytes = (int64_t)a.d * (a.dtype == SGA_F32 ? 4 : 2) * (p.tile_rows / kRows);
   const int64_t groups = a.d == 256 ? 256 : row_bytes > 128 ? 512 : 768;
-  const int64_t work = (tiles * a.Hkv * (keys + kTileCost) + kLeastShare - 1) / kLeastShare;
+  const int64_t share = a.words > 0 ? kLeastShareTree : kLeastShare, work = (tiles * a.Hkv * (keys + kTileCost) + share - 1) / share;
   p.groups = (int32_t)(work < groups ? (work > 1 ? work : 1) : groups);
   if (p.groups > 1) p.bytes = (size_t)p.groups * (kNoteBytes + 2 * p.tile_rows * (a.d + 2) * sizeof(float));
   return p;

@@ -571,6 +571,65 @@ def test_a_chain_is_the_causal_call(dtype, d, new):
     assert (np.abs(host(a) - host(b)) <= 2 * bar).all() and (np.abs(host(la) - host(lb)) <= 2 * lse_bar).all()
 
 
+def tree_on_device(Q, ck, cv, table, ptr, new, length, has, depth, spec, scale, dtype, once):
+    """drafts_oracle.attend, a sequence at a time in 64 bits on the device: (O, lse, bar of O, bar of lse).  has: [T][most] bits as booleans."""
+    page, Hkv, d = ck.shape[2], ck.shape[1], ck.shape[3]
+    G, parts = Q.shape[0] // Hkv, {"f32": 0.0, "f16": 2.0 ** -21, "bf16": 2.0 ** -15}[dtype] if not once else S.HALF_STEP[dtype]
+    out = [[], [], [], []]
+    for s, (n, L) in enumerate(zip(new, length)):
+        base, rows = L - n, slice(int(ptr[s]), int(ptr[s]) + n)
+        low = max(0, base - spec.window) if base >= spec.n_global else 0
+        at = torch.cat((torch.arange(min(spec.n_global, low)), torch.arange(low, L))).cuda()
+        where = torch.from_numpy(table[s].astype(np.int64)).cuda()[at // page]
+        k, v = (c[where, :, at % page].double().transpose(0, 1).unsqueeze(1) for c in (ck, cv))              # [Hkv, 1, keys, d]
+        q = Q[:, rows].double().reshape(Hkv, G, n, d)
+        p = base + depth[rows].long()[:, None]
+        see = ((p - at <= spec.window) | (at < spec.n_global) | (p < spec.n_global)) & (at < base)
+        see[:, at >= base] = has[rows, :n]
+        z = scale * torch.matmul(q, k.transpose(-1, -2).contiguous())
+        size = torch.matmul(q.abs(), k.abs().transpose(-1, -2).contiguous()).masked_fill_(~see, 0.0).amax(-1)
+        off = d * 2.0 ** -24 * abs(scale) * size + 2.0 ** -22 * (1 + z.abs().masked_fill_(~see, 0.0).amax(-1))
+        z.masked_fill_(~see, -math.inf)
+        lse = torch.logsumexp(z, -1)
+        w = (z - lse.unsqueeze(-1)).exp()
+        O, share = torch.matmul(w, v), torch.matmul(w, v.abs())
+        bar = share * (2 * off + parts + (4 + math.sqrt(L)) * 2.0 ** -23).unsqueeze(-1) + O.abs() * S.HALF_STEP[dtype]
+        if dtype == "f16":
+            bar += 2.0 ** -35 * v.abs().sum(-2, keepdim=True) + 2.0 ** -25
+        for x, y in zip(out, (O, lse, bar, 2 * off + 2.0 ** -22 * (1 + lse.abs()))):
+            x.append(y.reshape(Hkv * G, n, *y.shape[3:]))
+    return [host(torch.cat(x, 1)) for x in out]
+
+
+@pytest.mark.parametrize("dtype,Hq,Hkv,d,page,n_seqs,new,alike", [
+    ("f16", 16, 4, 128, 16, 130, 13, True), ("bf16", 16, 8, 64, 24, 100, 20, True), ("f16", 16, 8, 128, 16, 70, 30, False),
+    ("bf16", 8, 1, 256, 16, 270, 9, True), ("f32", 4, 2, 128, 32, 140, 40, True), ("f16", 5, 5, 128, 16, 110, 40, True),
+    ("f16", 16, 4, 128, 16, 65, 70, True), ("f16", 8, 8, 64, 1, 96, 33, True), ("bf16", 2, 2, 128, 16, 256, 40, True),
+])
+def test_tree_attention_of_many_tiles(dtype, Hq, Hkv, d, page, n_seqs, new, alike):
+    """Tiles that are more than the places on the chip: alike, whole rounds of them uncut and the rest in pieces; all in one round; of all lengths."""
+    rng = np.random.default_rng(n_seqs)
+    n = [max(1, new - int(x)) for x in rng.integers(0, 3, n_seqs)]
+    length = [a + int(b) for a, b in zip(n, rng.integers(1500, 2000, n_seqs) if alike else rng.integers(1, 2000, n_seqs))]
+    spec = MaskSpec(KIND_GLOBAL_LOCAL, 2100, window=1000, n_global=7) if alike else MaskSpec(KIND_GLOBAL_LOCAL, 2100, window=2100, n_global=0)
+    batch, table, ptr, lens, n_pages, T = batch_of(n, length, page, padding=2)
+    ck, cv = caches(n_pages, Hkv, page, d, dtype, 1)
+    Q = tokens(Hq, T, d, dtype, 2)
+    parent = random_parents(n, 2, 0.4, 3)
+    tree = tree_of(parent, batch, spec, most=max(n))
+    _, seen = D.tree(parent, ptr, lens, spec, tree.seen.shape[1])
+    has = torch.zeros(T, 32 * tree.seen.shape[1], dtype=torch.bool)
+    for row, x in enumerate(seen[:int(ptr[-1])]):
+        has[row, list(x)] = True
+    once = long_chunks(dtype, T, n_seqs, Hq // Hkv, d, page)
+    want = tree_on_device(Q, ck, cv, table, ptr, n, length, has.cuda(), tree.depth, spec, 0.1, dtype, once)
+    end = int(ptr[-1])
+    for ws in (sga.alloc_paged_workspace(batch, spec, Hq, Hkv, d, dtype, tree=tree), None):
+        print("many tiles", dtype, Hq, Hkv, d, page, n_seqs, new, alike, ws is None, flush=True)
+        got = sga.attention_paged(Q, ck, cv, batch, spec, 0.1, workspace=ws, want_lse=True, tree=tree)
+        assert within(got[0][:, :end], want[0], want[2]) and within(got[1][:, :end], want[1], want[3])
+
+
 def test_tree_attention_far_pages():
     """Offsets of more than 2^31 elements, in both kernels, and in the moves."""
     Hkv, d, page, length = 8, 128, 64, 150
