@@ -957,7 +957,8 @@ def attention_paged(Q, cache_k, cache_v, batch, spec: MaskSpec, scale, causal=Tr
 
 # ---- generation with drafted tokens ----------------------------------------------------------------
 def _check_ints(t, name, dtype, shape, index):
-    if str(t.dtype) != dtype or t.shape != shape or not t.is_contiguous() or not t.is_cuda or t.get_device() != index:
+    # (get_device is -1 of a host tensor)
+    if str(t.dtype) != dtype or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
         raise ValueError(f"{name} must be contiguous {dtype[6:]} {list(shape)} on the batch's device")
 
 
@@ -1118,6 +1119,13 @@ def alloc_norm_workspace(L, Hq, Hkv, d, device="cuda"):
     return torch.empty(norm_workspace_bytes(L, Hq, Hkv, d), dtype=torch.uint8, device=device)
 
 
+def _strides3(x, g, dx, *names):
+    """Records of an input, its result's gradient and its own, which are mostly laid out alike."""
+    first = _strides(dx, names[2], written=True)
+    s = dx.stride()
+    return [_Rows(t.data_ptr(), first.head_stride, first.row_stride) if t.stride() == s else _strides(t, n) for t, n in ((x, names[0]), (g, names[1]))] + [first]
+
+
 def norm_rotary_backward(Q, dQ_out, K=None, dK_out=None, rotary=None, q_norm=None, k_norm=None, positions=None, first=0, dQ=None, dK=None,
                          dq_weight=None, dk_weight=None, workspace=None):
     """The gradient of norm_rotary(Q, K, ...) from those of its results: (dQ, dq_weight), or (dQ, dq_weight, dK, dk_weight).  Weights' gradients
@@ -1148,8 +1156,9 @@ def norm_rotary_backward(Q, dQ_out, K=None, dK_out=None, rotary=None, q_norm=Non
     if workspace is None and (dw[0] is not None or dw[1] is not None):
         workspace = alloc_norm_workspace(Q.shape[1], Q.shape[0], K.shape[0] if K is not None else 0, d, Q.device)
     ws_ptr, ws_n = _workspace_of(workspace, index)
-    k = (_strides(K, "K"), _strides(dK_out, "dK_out"), _strides(dK, "dK", written=True)) if K is not None else (None, None, None)
-    st = _enqueue(index, sga_norm_rotary_backward, _strides(Q, "Q"), _strides(dQ_out, "dQ_out"), _strides(dQ, "dQ", written=True),
+    q = _strides3(Q, dQ_out, dQ, "Q", "dQ_out", "dQ")
+    k = _strides3(K, dK_out, dK, "K", "dK_out", "dK") if K is not None else (None, None, None)
+    st = _enqueue(index, sga_norm_rotary_backward, *q,
                   q_norm._desc if q_norm is not None else None, dw[0].data_ptr() if dw[0] is not None else None, Q.shape[0], *k,
                   k_norm._desc if k_norm is not None else None, dw[1].data_ptr() if dw[1] is not None else None,
                   K.shape[0] if K is not None else 0, at, int(first), Q.shape[1], d, rotary._desc if rotary is not None else None,
@@ -1203,27 +1212,40 @@ def cache_keep(cache_k, cache_v, batch, path, count):
     """Move the batch's accepted tokens into place: keys and values of new token path[s, k] of sequence s to the place of new token k, k <
     count[s].  path: int32 [S, columns], rising; count: int32 [S].  The caches are [n_pages, Hkv, page_size, d], or [layers, n_pages,
     Hkv, page_size, d] for all layers at once.  Lengths stay: pages_advance takes the counts as `kept`."""
+    shape, stride = cache_k.shape, cache_k.stride()
     layers, apart = 1, 0
-    if cache_k.dim() == 5:
-        if cache_v.shape != cache_k.shape or cache_v.stride(0) != cache_k.stride(0):
+    if cache_v.shape != shape:
+        raise ValueError("the caches must be alike")
+    index, dtype = batch.device_index, cache_k.dtype
+    if len(shape) == 5:
+        layers, apart = shape[0], stride[0]
+        shape, stride, stride_v = shape[1:], stride[1:], cache_v.stride()
+        if layers < 1 or (layers > 1 and stride_v[0] != apart):
             raise ValueError("the caches of all layers must be alike")
-        layers, apart = cache_k.shape[0], cache_k.stride(0)
-        if layers < 1:
-            raise ValueError("no layer")
-        if layers > 1 and apart < cache_k.stride(1) * (cache_k.shape[1] - 1) + cache_k[0, 0].numel():
-            # layers may take turns page by page, as pages of keys and values may
-            if apart < cache_k[0, 0].numel() or cache_k.stride(1) < apart * (layers - 1) + cache_k[0, 0].numel():
-                raise ValueError("the caches of different layers overlap")
-        cache_k, cache_v = cache_k[0], cache_v[0]
-    if cache_k.dim() != 4 or not cache_k.is_cuda:
-        raise ValueError("the caches must both be [n_pages, Hkv, page_size, d], or of several layers")
-    struct, Hkv = batch._caches(cache_k[0], cache_k, cache_v)
-    index, S = batch.device_index, batch.seq_len.shape[0]
+        stride_v = stride_v[1:]
+    else:
+        stride_v = cache_v.stride()
+    if len(shape) != 4 or shape[0] != batch.n_pages or shape[2] != batch.page_size:
+        raise ValueError("the caches must both be [n_pages, Hkv, page_size, d], or [layers, n_pages, Hkv, page_size, d]")
+    n_pages, Hkv, page, d = shape
+    whole = Hkv * page * d
+    for sp, sh, st, sc in (stride, stride_v):
+        if sc != 1 or (st != d and page > 1) or (sh != page * d and Hkv > 1):
+            raise ValueError("every page of a cache must be contiguous")
+    between = stride[0] if n_pages > 1 else whole
+    if between < whole or (n_pages > 1 and stride_v[0] != between):
+        raise ValueError("the pages of a cache must not overlap, and both caches must have them at one distance")
+    # a layer behind the other, or layers that take turns page by page
+    if layers > 1 and apart < between * (n_pages - 1) + whole and (apart < whole or between < apart * (layers - 1) + whole):
+        raise ValueError("the caches of different layers overlap")
+    if cache_v.dtype != dtype or cache_k.get_device() != index or cache_v.get_device() != index:
+        raise ValueError("the caches must share dtype, and device with the batch")
+    struct, S = batch._struct(between), batch.seq_len.shape[0]
     if path.dim() != 2:
         raise ValueError("path must be int32 [S, columns]")
     _check_ints(path, "path", "torch.int32", (S, path.shape[1]), index)
     _check_ints(count, "count", "torch.int32", (S,), index)
-    st = _enqueue(index, sga_cache_keep, cache_k.data_ptr(), cache_v.data_ptr(), struct, Hkv, cache_k.shape[3], layers, apart, path.data_ptr(),
-                  path.shape[1], count.data_ptr(), _serving_code(cache_k.dtype))
+    st = _enqueue(index, sga_cache_keep, cache_k.data_ptr(), cache_v.data_ptr(), struct, Hkv, d, layers, apart, path.data_ptr(),
+                  path.shape[1], count.data_ptr(), _serving_code(dtype))
     if st != 0:
         raise SgaError(st, "sga_cache_keep")

@@ -19,7 +19,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxTokens = 4;        // tokens of a workgroup (as in paged_cache.hip)
 constexpr int kMaxGroups = 1 << 20;  // workgroups along the tokens; they stride
-constexpr int kGradGroups = 1024;    // workgroups of the gradient at most: each leaves a partial sum
+constexpr int kGradGroups = 2048;    // workgroups of the gradient at most: each leaves a partial sum
 constexpr int kGradTokens = 16;      // tokens of one round of it at most
 constexpr int64_t kNone = INT64_MIN;
 
@@ -45,6 +45,19 @@ __device__ __forceinline__ float weight_at(const NormArg& n, int c) {
                   : n.dtype == SGA_F16 ? (float)static_cast<const f16_t*>(n.weight)[c]
                                        : (float)static_cast<const bf16_t*>(n.weight)[c];
   return w + n.offset;
+}
+
+constexpr int kMostChannels = 1024;
+// A weight as it lies in memory, and what it stands for.  (0 where there are none.)
+__device__ __forceinline__ uint32_t raw_weight(const NormArg& n, int c) {
+  if (!n.on || !n.weight) return 0;
+  return n.dtype == SGA_F32 ? static_cast<const uint32_t*>(n.weight)[c] : static_cast<const uint16_t*>(n.weight)[c];
+}
+__device__ __forceinline__ float weight_from(const NormArg& n, uint32_t raw) {
+  if (!n.weight) return 1.f;
+  return (n.dtype == SGA_F32   ? __builtin_bit_cast(float, raw)
+          : n.dtype == SGA_F16 ? (float)__builtin_bit_cast(f16_t, (uint16_t)raw)
+                               : __builtin_bit_cast(float, raw << 16)) + n.offset;
 }
 
 __device__ __forceinline__ float inverse_size(float squares, float per, float epsilon) { return rsqrtf(fmaf(squares, per, epsilon)); }
@@ -90,65 +103,262 @@ __device__ __forceinline__ void turn(const Item<V>& item, const float2* cs, floa
 }
 
 struct NormShape {
-  FastDiv heads, tokens;         // rows (heads) of a token here, tokens here
+  FastDiv heads, tokens;         // one pair a lane: rows (heads) of a token here, tokens here
+  FastDiv pairs;                 // that turn
   int32_t all_heads;
   int32_t head_first;            // neighbouring rows in memory are a token's heads, not a head's tokens
-  int32_t items;                 // of a row, a lane each (the kernel's lanes are at least as many)
+  int32_t tokens_log2;           // rows in lanes: tokens of a wavefront at a time
+  int32_t slices;                // rows in lanes: wavefronts that share a token's heads
 };
 
-// Where tokens row0 .. are: their places in the cache and their positions.
-template <bool kPaged>
-__device__ __forceinline__ void find_tokens(const NormRotateArgs& a, int32_t row0, int count, int64_t* position, int64_t* cache_row) {
-  const int tid = threadIdx.x;
-  if constexpr (kPaged) {
-    for (int t = tid / kWave; t < count; t += kThreads / kWave) {
-      const int32_t row = row0 + t;
-      const PagedArgs& b = a.r.batch;
-      const int32_t s = last_not_above(b.n_seqs, row, [&](int32_t i) { return b.seq_ptr[i]; });
-      const int64_t begin = b.seq_ptr[s], end = b.seq_ptr[s + 1];
-      int64_t pos = kNone, place = -1;
-      if (begin <= row && row < end) {
-        const int64_t slot = (int64_t)b.seq_len[s] - (end - row);
-        const int32_t depth = a.depth ? a.depth[row] : 0;
-        if (depth >= 0) {
-          pos = a.depth ? (int64_t)b.seq_len[s] - (end - begin) + depth : slot;
-          if (slot >= 0 && slot < (int64_t)b.pages_per_seq * b.page.value) {
-            const uint32_t column = quotient((uint32_t)slot, b.page), in_page = (uint32_t)slot - column * b.page.value;
-            const uint32_t page = (uint32_t)b.page_table[(int64_t)s * b.pages_per_seq + column];
-            if (page < b.n_pages) place = (int64_t)page * b.page_stride + (int64_t)in_page * a.r.d;
-          }
-        }
-      }
-      if ((tid & (kWave - 1)) == 0) {
-        position[t] = pos;
-        cache_row[t] = place;
+// Position and place in the cache of a token's row; all lanes of the wavefront call it.
+struct Placed {
+  int64_t position, cache_row;   // kNone: none; -1: without a page
+};
+__device__ __forceinline__ Placed find_in_batch(const NormRotateArgs& a, int32_t row) {
+  const PagedArgs& b = a.r.batch;
+  const int32_t s = last_not_above(b.n_seqs, row, [&](int32_t i) { return b.seq_ptr[i]; });
+  const int64_t begin = b.seq_ptr[s], end = b.seq_ptr[s + 1];
+  Placed p{kNone, -1};
+  if (begin <= row && row < end) {
+    const int64_t slot = (int64_t)b.seq_len[s] - (end - row);
+    const int32_t depth = a.depth ? a.depth[row] : 0;
+    if (depth >= 0) {
+      p.position = a.depth ? (int64_t)b.seq_len[s] - (end - begin) + depth : slot;
+      if (slot >= 0 && slot < (int64_t)b.pages_per_seq * b.page.value) {
+        const uint32_t column = quotient((uint32_t)slot, b.page), in_page = (uint32_t)slot - column * b.page.value;
+        const uint32_t page = (uint32_t)b.page_table[(int64_t)s * b.pages_per_seq + column];
+        if (page < b.n_pages) p.cache_row = (int64_t)page * b.page_stride + (int64_t)in_page * a.r.d;
       }
     }
-  } else if (tid < count) {
-    position[tid] = a.r.positions ? a.r.positions[row0 + tid] : a.r.first + row0 + tid;
   }
+  return p;
 }
 
-__device__ __forceinline__ void find_turns(const RotaryArgs& r, int count, const int64_t* position, float2* turns) {
-  const int pairs = r.channels >> 1;
-  for (int i = threadIdx.x; i < count * pairs; i += kThreads) {
-    const int t = i / pairs, k = i - t * pairs;
-    if (position[t] == kNone) continue;
-    const float2 cs = turn_of(position[t], r.frequencies[k]);
-    turns[i] = make_float2(r.magnitude * cs.x, r.inverse ? -r.magnitude * cs.y : r.magnitude * cs.y);
-  }
+__device__ __forceinline__ float2 turned_by(const RotaryArgs& r, int64_t position, double frequency) {
+  const float2 cs = turn_of(position, frequency);
+  return make_float2(r.magnitude * cs.x, r.inverse ? -r.magnitude * cs.y : r.magnitude * cs.y);
 }
 
-// kLanes lanes hold a row, 2 V elements each; kLanes 0: a wavefront goes over the row, one pair at a time, twice (any size and
-// alignment).
+// 2 V channels of a lane in registers: the weights or the turns of its item, which are the same in every row that it meets.
+template <int V>
+struct Own {
+  float u[V], v[V];
+};
+template <int V>
+__device__ __forceinline__ Own<V> weights_of(const float* w, const Item<V>& item) {
+  Own<V> own;
+#pragma unroll
+  for (int e = 0; e < V; ++e) {
+    own.u[e] = w[item.at + e];
+    own.v[e] = w[item.at2 + e];
+  }
+  return own;
+}
+
+// Rows in lanes, kLanes of them a row with 2 V elements each.  A wavefront works by itself: it takes one token (or, where a token has fewer heads than the
+// wavefront holds rows, several) with all its heads, computes the sines into its own part of LDS while the first rows are on their way, and keeps
+// those of its lanes' channels, and their weights, in registers: a lane's channels are the same in every row.  Rows are loaded kBatch at a time.
+constexpr int kBatch = 2;
 template <typename T, int V, int kLanes, bool kPaged>
 __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a, NormShape shape) {
+  using Vec = vec_t<T, V>;
+  constexpr int kRows = kWave / kLanes;
+  extern __shared__ __align__(16) float shared[];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, d = a.r.d;
+  const float per = 1.f / (float)d;
+  float* const weights = shared;                                                     // [tensors][d]
+  const int pairs = shape.pairs.value, tokens = 1 << shape.tokens_log2;
+  float2* const turns = reinterpret_cast<float2*>(shared + ((a.r.n_tensors * d + 3) & ~3)) + wave * tokens * pairs;     // [tokens][pairs]
+  // (weights are on their way while the first tokens are looked for)
+  constexpr int kHeld = (3 * kMostChannels + kThreads - 1) / kThreads;
+  uint32_t held[kHeld];
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = threadIdx.x + j * kThreads;
+    if (j * kThreads >= a.r.n_tensors * d) break;
+    held[j] = i < d ? raw_weight(a.norm[0], i) : i < 2 * d ? raw_weight(a.norm[1], i - d) : i < 3 * d ? raw_weight(a.norm[2], i - 2 * d) : 0;
+  }
+  const int k = lane % kLanes, group = lane / kLanes;
+  const bool mine = k < d / (2 * V);
+  const int token = group & (tokens - 1), apart = kRows >> shape.tokens_log2, head0 = group >> shape.tokens_log2;
+  // the heads of all tensors in rounds of `apart`, a slice of these rounds for each of the wavefronts that share a token
+  int rounds[3], all_rounds = 0;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    rounds[i] = i < a.r.n_tensors ? (a.r.tensor[i].heads + apart - 1) / apart : 0;
+    all_rounds += rounds[i];
+  }
+  const int64_t waves = (int64_t)gridDim.x * (kThreads / kWave), id = (int64_t)blockIdx.x * (kThreads / kWave) + wave;
+  const int slices = shape.slices;
+  const int64_t units = ((a.r.n_rows + (int64_t)tokens - 1) >> shape.tokens_log2) * slices;
+  auto first_row = [&](int64_t unit) { return (int32_t)((unit / slices) << shape.tokens_log2); };
+  auto find = [&](int64_t unit) {                           // of this lane's token
+    const int32_t row0 = first_row(unit);
+    Placed mine{0, -1};
+    if constexpr (kPaged) {
+      for (int t = 0; t < tokens; ++t) {
+        const Placed p = find_in_batch(a, min(row0 + t, a.r.n_rows - 1));
+        if (t == token) mine = p;
+      }
+    } else if (pairs > 0) {
+      mine.position = a.r.positions ? a.r.positions[min(row0 + token, a.r.n_rows - 1)] : a.r.first + row0 + token;
+    }
+    return mine;
+  };
+  // (the frequency of this lane's first turn: of every token's, mostly)
+  const double own_frequency = pairs > 0 ? a.r.rotary.frequencies[lane - (int)quotient((uint32_t)lane, shape.pairs) * pairs] : 0.0;
+  Placed next{0, -1};
+  if (id < units) next = find(id);
+#pragma unroll
+  for (int j = 0; j < kHeld; ++j) {
+    const int i = threadIdx.x + j * kThreads;
+    if (j * kThreads >= a.r.n_tensors * d) break;
+    if (i < a.r.n_tensors * d) weights[i] = i < d ? weight_from(a.norm[0], held[j]) : i < 2 * d ? weight_from(a.norm[1], held[j]) : weight_from(a.norm[2], held[j]);
+  }
+  __syncthreads();
+  for (int64_t unit = id; unit < units; unit += waves) {
+    const int64_t first = unit / slices;
+    const int slice = (int)(unit - first * slices);
+    const int32_t row0 = first_row(unit), row = row0 + token;
+    const int begin = all_rounds * slice / slices, end = all_rounds * (slice + 1) / slices;
+    const int64_t position = next.position, cache_row = next.cache_row;
+    const bool there = row < a.r.n_rows && (!kPaged || position != kNone);
+    if (!kPaged && unit + waves < units) next = find(unit + waves);
+    // (tensor by tensor, so that what describes one is the same in all lanes and known ahead)
+    Vec u[kBatch], v[kBatch];
+    auto heads_of = [&](const RowsArg& x, int i, bool& is) {
+      const int32_t head = head0 + i * apart;
+      is = there && mine && head < x.heads && !(kPaged && x.paged && cache_row < 0);
+      return head;
+    };
+    auto load = [&](const RowsArg& x, int i, int stop) {
+      const Item<V> item(a.r.rotary, x.rotate, k);
+      const T* const src = static_cast<const T*>(x.src) + (int64_t)row * x.src_row;
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        bool is;
+        const int64_t head = heads_of(x, min(i + b, stop - 1), is);
+        const T* const at = src + (is ? head * x.src_head : 0);
+        if (is) {
+          u[b] = *reinterpret_cast<const Vec*>(at + item.at);
+          v[b] = *reinterpret_cast<const Vec*>(at + item.at2);
+        }
+      }
+    };
+    Own<V> cosines{}, sines{};
+    auto finish = [&](const RowsArg& t, const NormArg& norm, const float* w_of, int i, int stop) {
+      const Item<V> item(a.r.rotary, t.rotate, k);
+      T* const dst = static_cast<T*>(t.dst) + (kPaged && t.paged ? cache_row : (int64_t)row * t.dst_row);
+#pragma unroll
+      for (int b = 0; b < kBatch; ++b) {
+        if (i + b >= stop) break;
+        bool is;
+        const int64_t head = heads_of(t, i + b, is);
+        float x[V], y[V];
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          x[e] = (float)u[b][e];
+          y[e] = (float)v[b][e];
+        }
+        if (norm.on) {
+          float squares = 0.f;
+          if (is) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) squares = fmaf(x[e], x[e], fmaf(y[e], y[e], squares));
+          }
+          const float size = inverse_size(group_sum<kLanes>(squares), per, norm.epsilon);
+          if (mine) {
+            const Own<V> w = weights_of<V>(w_of, item);
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              x[e] = x[e] * size * w.u[e];
+              y[e] = y[e] * size * w.v[e];
+            }
+          }
+        }
+        if (t.rotate && !a.r.rotary.interleaved) {
+          if (item.turns) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+              const float p = x[e], q = y[e];
+              x[e] = p * cosines.u[e] - q * sines.u[e];
+              y[e] = p * sines.u[e] + q * cosines.u[e];
+            }
+          }
+        } else if (t.rotate) {
+          if (item.turns) {
+#pragma unroll
+            for (int e = 0; e < V; e += 2) {
+              const float p = x[e], q = x[e + 1], p2 = y[e], q2 = y[e + 1];
+              x[e] = p * cosines.u[e / 2] - q * sines.u[e / 2];
+              x[e + 1] = p * sines.u[e / 2] + q * cosines.u[e / 2];
+              y[e] = p2 * cosines.u[(V + e) / 2] - q2 * sines.u[(V + e) / 2];
+              y[e + 1] = p2 * sines.u[(V + e) / 2] + q2 * cosines.u[(V + e) / 2];
+            }
+          }
+        }
+        if (is) {
+          Vec p, q;
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            p[e] = (T)x[e];
+            q[e] = (T)y[e];
+          }
+          T* const to = dst + head * t.dst_head;
+          *reinterpret_cast<Vec*>(to + item.at) = p;
+          *reinterpret_cast<Vec*>(to + item.at2) = q;
+        }
+      }
+    };
+    const int first_stop = min(end, rounds[0]);
+    if (begin < first_stop) load(a.r.tensor[0], begin, first_stop);
+    // sines of the wavefront's tokens
+    if (pairs > 0) {
+      for (int i0 = 0; i0 < tokens * pairs; i0 += kWave) {
+        const int i = i0 + lane, t = (int)quotient((uint32_t)i, shape.pairs), p = i - t * pairs;
+        // (the position of token t: of the lanes that hold its rows)
+        const int from = (t & (tokens - 1)) * kLanes;
+        const int64_t at = (int64_t)((uint64_t)(uint32_t)__shfl((int)(position >> 32), from, kWave) << 32 | (uint32_t)__shfl((int)position, from, kWave));
+        if (i < tokens * pairs) turns[i] = at == kNone ? make_float2(0.f, 0.f) : turned_by(a.r.rotary, at, i0 == 0 ? own_frequency : a.r.rotary.frequencies[p]);
+      }
+      __builtin_amdgcn_wave_barrier();
+      // interleaved, pair e of an item's 2 V channels is (2 e, 2 e + 1); split, (e, V + e)
+      const Item<V> item(a.r.rotary, true, k);
+      if (item.turns && mine) {
+        const float2* const cs = turns + token * pairs + k * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          cosines.u[e] = cs[e].x;
+          sines.u[e] = cs[e].y;
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    int before = 0;
+#pragma unroll
+    for (int which = 0; which < 3; ++which) {
+      if (which >= a.r.n_tensors) break;
+      const int from = max(begin - before, 0), stop = min(end - before, rounds[which]);
+      for (int i = from; i < stop; i += kBatch) {
+        if (which > 0 || i > from) load(a.r.tensor[which], i, stop);
+        finish(a.r.tensor[which], a.norm[which], weights + which * d, i, stop);
+      }
+      before += rounds[which];
+    }
+    if (kPaged && unit + waves < units) next = find(unit + waves);
+  }
+}
+
+// Any size and alignment: a workgroup takes a few tokens, a wavefront goes over a row, a pair a lane, twice.
+template <typename T, bool kPaged>
+__global__ __launch_bounds__(kThreads) void norm_rotate_any_kernel(NormRotateArgs a, NormShape shape) {
   extern __shared__ __align__(16) float shared[];
   __shared__ int64_t position[kMaxTokens], cache_row[kMaxTokens];
   const int tid = threadIdx.x, tokens = shape.tokens.value, d = a.r.d;
   const float per = 1.f / (float)d;
   float* const weights = shared;                                                     // [tensors][d]
-  float2* const turns = reinterpret_cast<float2*>(shared + ((a.r.n_tensors * d + 3) & ~3));     // [tokens][channels / 2]
+  float2* const turns = reinterpret_cast<float2*>(shared + ((a.r.n_tensors * d + 3) & ~3));     // [tokens][pairs]
   const int pairs = a.r.rotary.channels >> 1;
   for (int i = tid; i < a.r.n_tensors * d; i += kThreads) {
     const int which = i / d;
@@ -156,23 +366,30 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
   }
   const int32_t head0 = blockIdx.y * shape.heads.value;
   const int heads = min(shape.all_heads - head0, (int)shape.heads.value);
-  constexpr int kRowLanes = kLanes ? kLanes : kWave;
-  const int k = tid % kRowLanes;
-
+  const int k = tid % kWave;
   for (int64_t row0_ = (int64_t)blockIdx.x * tokens; row0_ < a.r.n_rows; row0_ += (int64_t)gridDim.x * tokens) {
     const int32_t row0 = (int32_t)row0_;
     const int count = min(a.r.n_rows - row0, tokens);
     __syncthreads();                                          // the rows before these are done with the turns
-    find_tokens<kPaged>(a, row0, count, position, cache_row);
-    if constexpr (kPaged) __syncthreads();
-    struct Row {
-      const T* src;
-      T* dst;
-      int which, t;
-      bool there;
-    };
-    auto locate = [&](uint32_t i) {
-      Row row{};
+    if constexpr (kPaged) {
+      for (int t = tid / kWave; t < count; t += kThreads / kWave) {
+        const Placed p = find_in_batch(a, row0 + t);
+        if (k == 0) {
+          position[t] = p.position;
+          cache_row[t] = p.cache_row;
+        }
+      }
+    } else if (tid < count) {
+      position[tid] = a.r.positions ? a.r.positions[row0 + tid] : a.r.first + row0 + tid;
+    }
+    __syncthreads();
+    for (int i = tid; i < count * pairs; i += kThreads) {
+      const int t = i / pairs;
+      if (position[t] != kNone) turns[i] = turned_by(a.r.rotary, position[t], a.r.rotary.frequencies[i - t * pairs]);
+    }
+    __syncthreads();
+    const uint32_t total = (uint32_t)tokens * shape.heads.value;
+    for (uint32_t i = tid / kWave; i < total; i += kThreads / kWave) {
       uint32_t t, h;
       if (shape.head_first) {
         t = quotient(i, shape.heads);
@@ -181,131 +398,81 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
         h = quotient(i, shape.tokens);
         t = i - h * shape.tokens.value;
       }
-      if ((int)t >= count || (int)h >= heads) return row;
+      if ((int)t >= count || (int)h >= heads) continue;
       h += head0;
       int which = 0;
       while (which < a.r.n_tensors - 1 && (int)h >= a.r.tensor[which].heads) h -= a.r.tensor[which++].heads;
       const RowsArg& x = a.r.tensor[which];
+      if (kPaged && (position[t] == kNone || (x.paged && cache_row[t] < 0))) continue;
       const int64_t at = row0 + (int)t;
-      row.src = static_cast<const T*>(x.src) + (int64_t)h * x.src_head + at * x.src_row;
-      row.dst = static_cast<T*>(x.dst) + (int64_t)h * x.dst_head + (kPaged && x.paged ? cache_row[t] : at * x.dst_row);
-      row.which = which;
-      row.t = (int)t;
-      row.there = !kPaged || (position[t] != kNone && !(x.paged && cache_row[t] < 0));
-      return row;
-    };
-    auto make_turns = [&]() {
-      if constexpr (!kPaged) __syncthreads();
-      find_turns(a.r.rotary, count, position, turns);
-      __syncthreads();
-    };
-    const uint32_t total = (uint32_t)tokens * shape.heads.value, step = kThreads / kRowLanes;
-    if constexpr (kLanes > 0) {
-      using Vec = vec_t<T, V>;
-      auto load = [&](const Row& row, Vec& u, Vec& v) {
-        if (!row.there || k >= shape.items) return;
-        const Item<V> item(a.r.rotary, a.r.tensor[row.which].rotate, k);
-        u = *reinterpret_cast<const Vec*>(row.src + item.at);
-        v = *reinterpret_cast<const Vec*>(row.src + item.at2);
-      };
-      uint32_t i = tid / kLanes;
-      Row row = locate(i);
-      Vec u = {}, v = {};
-      if (i < total) load(row, u, v);                          // (on its way while the sines are computed)
-      make_turns();
-      for (; i < total; i += step) {
-        const Row here = row;
-        float x[V], y[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          x[e] = (float)u[e];
-          y[e] = (float)v[e];
-        }
-        if (i + step < total) {                                // the next row is on its way while this one is worked on
-          row = locate(i + step);
-          load(row, u, v);
-        }
-        if (!here.there) continue;
-        const NormArg& norm = a.norm[here.which];
-        const Item<V> item(a.r.rotary, a.r.tensor[here.which].rotate, k);
-        if (norm.on) {
-          float squares = 0.f;
-          if (k < shape.items) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) squares = fmaf(x[e], x[e], fmaf(y[e], y[e], squares));
-          }
-          const float r = inverse_size(group_sum<kLanes>(squares), per, norm.epsilon);
-          const float* const w = weights + here.which * d;
-          if (k < shape.items) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              x[e] = x[e] * r * w[item.at + e];
-              y[e] = y[e] * r * w[item.at2 + e];
-            }
-          }
-        }
-        if (k >= shape.items) continue;
-        if (item.turns) turn<V>(item, turns + here.t * pairs + k * V, x, y);
-        Vec p, q;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          p[e] = (T)x[e];
-          q[e] = (T)y[e];
-        }
-        *reinterpret_cast<Vec*>(here.dst + item.at) = p;
-        *reinterpret_cast<Vec*>(here.dst + item.at2) = q;
+      const T* const src = static_cast<const T*>(x.src) + (int64_t)h * x.src_head + at * x.src_row;
+      T* const dst = static_cast<T*>(x.dst) + (int64_t)h * x.dst_head + (kPaged && x.paged ? cache_row[t] : at * x.dst_row);
+      const NormArg& norm = a.norm[which];
+      float r = 1.f;
+      if (norm.on) {
+        float squares = 0.f;
+        for (int c = k; c < d; c += kWave) squares = fmaf((float)src[c], (float)src[c], squares);
+        r = inverse_size(group_sum<kWave>(squares), per, norm.epsilon);
       }
-    } else {
-      make_turns();
-      for (uint32_t i = tid / kWave; i < total; i += step) {
-        const Row row = locate(i);
-        if (!row.there) continue;
-        const NormArg& norm = a.norm[row.which];
-        float r = 1.f;
+      const float* const w = weights + which * d;
+      for (int j = k; j < (d + 1) / 2; j += kWave) {
+        const Item<1> item(a.r.rotary, x.rotate, j);
+        const bool two = item.at2 < d;                       // (not the last channel of an odd number)
+        float p[1] = {(float)src[item.at]}, q[1] = {two ? (float)src[item.at2] : 0.f};
         if (norm.on) {
-          float squares = 0.f;
-          for (int c = k; c < d; c += kWave) squares = fmaf((float)row.src[c], (float)row.src[c], squares);
-          r = inverse_size(group_sum<kWave>(squares), per, norm.epsilon);
+          p[0] = p[0] * r * w[item.at];
+          if (two) q[0] = q[0] * r * w[item.at2];
         }
-        const float* const w = weights + row.which * d;
-        for (int j = k; j < (d + 1) / 2; j += kWave) {
-          const Item<1> item(a.r.rotary, a.r.tensor[row.which].rotate, j);
-          const bool two = item.at2 < d;                       // (not the last channel of an odd number)
-          float x[1] = {(float)row.src[item.at]}, y[1] = {two ? (float)row.src[item.at2] : 0.f};
-          if (norm.on) {
-            x[0] = x[0] * r * w[item.at];
-            if (two) y[0] = y[0] * r * w[item.at2];
-          }
-          if (item.turns) turn<1>(item, turns + row.t * pairs + j, x, y);
-          row.dst[item.at] = (T)x[0];
-          if (two) row.dst[item.at2] = (T)y[0];
-        }
+        if (item.turns) turn<1>(item, turns + (int)t * pairs + j, p, q);
+        dst[item.at] = (T)p[0];
+        if (two) dst[item.at2] = (T)q[0];
       }
     }
   }
 }
 
+constexpr int kMostBlocks = 256 * 8;      // workgroups of wavefronts that each take tokens until there are none: what the chip holds and as much again
+
 template <typename T, int V, int kLanes>
 sga_status launch_norm_as(const NormRotateArgs& a) {
   const bool paged = a.r.batch.page_table != nullptr;
   NormShape s{};
-  for (int i = 0; i < a.r.n_tensors; ++i) s.all_heads += a.r.tensor[i].heads;
-  constexpr int kRowLanes = kLanes ? kLanes : kWave;
-  // tokens and heads of a workgroup: as for the rotation alone
-  int tokens = kMaxTokens;
-  while (tokens > 1 && a.r.n_rows / tokens < 1024) tokens >>= 1;
-  int heads = s.all_heads;
-  const int64_t groups = ((int64_t)a.r.n_rows + tokens - 1) / tokens;
-  while (heads > 1 && groups * ((s.all_heads + heads - 1) / heads) < 256 && heads * kRowLanes * tokens > kThreads)
-    heads = (heads + 1) / 2;
-  s.heads = fast_div(heads);
-  s.tokens = fast_div(tokens);
-  s.head_first = a.r.tensor[0].src_head <= a.r.tensor[0].src_row;
-  s.items = a.r.d / (2 * V);
-  const dim3 grid((unsigned)(groups < kMaxGroups ? groups : kMaxGroups), (unsigned)((s.all_heads + heads - 1) / heads));
-  const size_t lds = (size_t)((a.r.n_tensors * a.r.d + 3) & ~3) * sizeof(float) + (size_t)tokens * (a.r.rotary.channels / 2) * sizeof(float2);
-  if (paged) norm_rotate_kernel<T, V, kLanes, true><<<grid, kThreads, lds, a.r.stream>>>(a, s);
-  else norm_rotate_kernel<T, V, kLanes, false><<<grid, kThreads, lds, a.r.stream>>>(a, s);
+  const int pairs = a.r.rotary.channels / 2;
+  s.pairs = fast_div(pairs > 0 ? pairs : 1);
+  s.pairs.value = pairs;
+  const size_t weights = (size_t)((a.r.n_tensors * a.r.d + 3) & ~3) * sizeof(float);
+  if constexpr (kLanes > 0) {
+    constexpr int kRows = kWave / kLanes;
+    int most = 0;
+    for (int i = 0; i < a.r.n_tensors; ++i) most = a.r.tensor[i].heads > most ? a.r.tensor[i].heads : most;
+    while ((2 << s.tokens_log2) * most <= kRows) ++s.tokens_log2;
+    const int apart = kRows >> s.tokens_log2;
+    int rounds = 0;
+    for (int i = 0; i < a.r.n_tensors; ++i) rounds += (a.r.tensor[i].heads + apart - 1) / apart;
+    const int64_t units = ((int64_t)a.r.n_rows + (1 << s.tokens_log2) - 1) >> s.tokens_log2;
+    s.slices = 1;
+    while (s.slices < rounds && units * s.slices < 1024) ++s.slices;
+    const int64_t blocks = (units * s.slices + kThreads / kWave - 1) / (kThreads / kWave);
+    const unsigned grid = (unsigned)(blocks < kMostBlocks ? blocks : kMostBlocks);
+    const size_t lds = weights + (size_t)(kThreads / kWave) * ((size_t)pairs << s.tokens_log2) * sizeof(float2);
+    if (paged) norm_rotate_kernel<T, V, kLanes, true><<<grid, kThreads, lds, a.r.stream>>>(a, s);
+    else norm_rotate_kernel<T, V, kLanes, false><<<grid, kThreads, lds, a.r.stream>>>(a, s);
+  } else {
+    for (int i = 0; i < a.r.n_tensors; ++i) s.all_heads += a.r.tensor[i].heads;
+    // tokens and heads of a workgroup: as for the rotation alone
+    int tokens = kMaxTokens;
+    while (tokens > 1 && a.r.n_rows / tokens < 1024) tokens >>= 1;
+    int heads = s.all_heads;
+    const int64_t groups = ((int64_t)a.r.n_rows + tokens - 1) / tokens;
+    while (heads > 1 && groups * ((s.all_heads + heads - 1) / heads) < 256 && heads * kWave * tokens > kThreads) heads = (heads + 1) / 2;
+    s.heads = fast_div(heads);
+    s.tokens = fast_div(tokens);
+    s.head_first = a.r.tensor[0].src_head <= a.r.tensor[0].src_row;
+    const dim3 grid((unsigned)(groups < kMaxGroups ? groups : kMaxGroups), (unsigned)((s.all_heads + heads - 1) / heads));
+    const size_t lds = weights + (size_t)tokens * pairs * sizeof(float2);
+    if (paged) norm_rotate_any_kernel<T, true><<<grid, kThreads, lds, a.r.stream>>>(a, s);
+    else norm_rotate_any_kernel<T, false><<<grid, kThreads, lds, a.r.stream>>>(a, s);
+  }
   return hip_status(hipGetLastError());
 }
 
@@ -339,15 +506,179 @@ sga_status launch_norm_type(const NormRotateArgs& a) {
 
 // ---- gradient ---------------------------------------------------------------------------------------
 struct GradShape {
-  FastDiv heads[2];
+  FastDiv heads[2], pairs;
   int32_t groups[2];         // workgroups of each tensor
-  int32_t tokens[2];         // tokens of a round
-  int32_t items;
+  int32_t tokens[2];         // one pair a lane: tokens of a round; rows in lanes: log2 of a wavefront's tokens
   int32_t head_first[2];
 };
 
+// The workgroup's sums of its wavefronts' (in `sums`, [wavefronts][d]), in their order, into the workspace.
+__device__ __forceinline__ void leave_sums(const NormGradArgs& a, const float* sums) {
+  const int d = a.d;
+  __syncthreads();
+  float* const out = a.partials + (int64_t)blockIdx.x * d;
+  for (int c = threadIdx.x; c < d; c += kThreads) out[c] = (sums[c] + sums[d + c]) + (sums[2 * d + c] + sums[3 * d + c]);
+}
+
+// Rows in lanes: a wavefront takes tokens by itself, as in the forward pass.
 template <typename T, int V, int kLanes>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormGradArgs a, GradShape shape) {
+  using Vec = vec_t<T, V>;
+  constexpr int kRows = kWave / kLanes;
+  extern __shared__ __align__(16) float shared[];
+  const int lane = threadIdx.x & (kWave - 1), wave = threadIdx.x / kWave, d = a.d;
+  const float per = 1.f / (float)d;
+  const int which = (int)blockIdx.x >= shape.groups[0] ? 1 : 0;
+  const NormGradRows& x = which ? a.tensor[1] : a.tensor[0];
+  const int groups = which ? shape.groups[1] : shape.groups[0], tokens_log2 = which ? shape.tokens[1] : shape.tokens[0], tokens = 1 << tokens_log2;
+  const int pairs = shape.pairs.value;
+  float* const weights = shared;                                                   // [d]
+  float2* const turns = reinterpret_cast<float2*>(shared + ((d + 3) & ~3)) + wave * tokens * pairs;     // [tokens][pairs]
+  if (x.norm.on)
+    for (int c = threadIdx.x; c < d; c += kThreads) weights[c] = weight_at(x.norm, c);
+  __syncthreads();
+  const int k = lane % kLanes, group = lane / kLanes;
+  const bool mine = k < d / (2 * V);
+  const int token = group & (tokens - 1), apart = kRows >> tokens_log2, head0 = group >> tokens_log2;
+  const Item<V> item(a.rotary, true, k);
+  Own<V> w{}, sums{}, cosines{}, sines{};
+  if (x.norm.on && mine) w = weights_of<V>(weights, item);
+  const int rounds = (x.heads + apart - 1) / apart;
+  const int64_t waves = (int64_t)groups * (kThreads / kWave);
+  const int64_t units = ((int64_t)a.n_rows + tokens - 1) >> tokens_log2;
+  const double own_frequency = pairs > 0 ? a.rotary.frequencies[lane - (int)quotient((uint32_t)lane, shape.pairs) * pairs] : 0.0;
+  auto position_of = [&](int64_t unit) -> int64_t {
+    const int32_t row = (int32_t)((unit << tokens_log2) + token);
+    return pairs == 0 ? 0 : a.positions ? a.positions[min(row, a.n_rows - 1)] : a.first + row;
+  };
+  int64_t unit = (int64_t)(blockIdx.x - (which ? shape.groups[0] : 0)) * (kThreads / kWave) + wave;
+  int64_t next = unit < units ? position_of(unit) : 0;
+  Vec xu, xv, gu, gv;
+  for (; unit < units; unit += waves) {
+    const int32_t row = (int32_t)((unit << tokens_log2) + token);
+    const bool there = row < a.n_rows && mine;
+    const int64_t position = next;
+    if (unit + waves < units) next = position_of(unit + waves);
+    const T* const g = static_cast<const T*>(x.g) + (int64_t)row * x.g_row;
+    const T* const xs = static_cast<const T*>(x.x) + (int64_t)row * x.x_row;
+    T* const dx = static_cast<T*>(x.dx) + (int64_t)row * x.dx_row;
+    auto load = [&](int i) {
+      const int64_t head = head0 + i * apart;
+      if (there && head < x.heads) {
+        gu = *reinterpret_cast<const Vec*>(g + head * x.g_head + item.at);
+        gv = *reinterpret_cast<const Vec*>(g + head * x.g_head + item.at2);
+        if (x.norm.on) {
+          xu = *reinterpret_cast<const Vec*>(xs + head * x.x_head + item.at);
+          xv = *reinterpret_cast<const Vec*>(xs + head * x.x_head + item.at2);
+        }
+      }
+    };
+    load(0);
+    if (pairs > 0) {
+      for (int i0 = 0; i0 < tokens * pairs; i0 += kWave) {
+        const int i = i0 + lane, t = (int)quotient((uint32_t)i, shape.pairs), p = i - t * pairs, from = (t & (tokens - 1)) * kLanes;
+        const int64_t at = (int64_t)((uint64_t)(uint32_t)__shfl((int)(position >> 32), from, kWave) << 32 | (uint32_t)__shfl((int)position, from, kWave));
+        if (i < tokens * pairs) turns[i] = turned_by(a.rotary, at, i0 == 0 ? own_frequency : a.rotary.frequencies[p]);
+      }
+      __builtin_amdgcn_wave_barrier();
+      if (item.turns && mine) {
+        const float2* const cs = turns + token * pairs + k * V;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          cosines.u[e] = cs[e].x;
+          sines.u[e] = cs[e].y;
+        }
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    for (int i = 0; i < rounds; ++i) {
+      const int64_t head = head0 + i * apart;
+      const bool is = there && head < x.heads;
+      float u[V], v[V], p[V], q[V];
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        u[e] = (float)xu[e];
+        v[e] = (float)xv[e];
+        p[e] = (float)gu[e];
+        q[e] = (float)gv[e];
+      }
+      if (i + 1 < rounds) load(i + 1);                        // (on its way while this round is worked on)
+      if (item.split) {
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float b = p[e], c = q[e];
+          p[e] = b * cosines.u[e] - c * sines.u[e];
+          q[e] = b * sines.u[e] + c * cosines.u[e];
+        }
+      } else if (item.turns) {
+#pragma unroll
+        for (int e = 0; e < V; e += 2) {
+          const float b = p[e], c = p[e + 1], b2 = q[e], c2 = q[e + 1];
+          p[e] = b * cosines.u[e / 2] - c * sines.u[e / 2];
+          p[e + 1] = b * sines.u[e / 2] + c * cosines.u[e / 2];
+          q[e] = b2 * cosines.u[(V + e) / 2] - c2 * sines.u[(V + e) / 2];
+          q[e + 1] = b2 * sines.u[(V + e) / 2] + c2 * cosines.u[(V + e) / 2];
+        }
+      }
+      if (x.norm.on) {
+        float squares = 0.f, mixed = 0.f, wu[V], wv[V];
+        if (is) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            wu[e] = w.u[e] * p[e];
+            wv[e] = w.v[e] * q[e];
+            squares = fmaf(u[e], u[e], fmaf(v[e], v[e], squares));
+            mixed = fmaf(wu[e], u[e], fmaf(wv[e], v[e], mixed));
+          }
+        }
+        const float r = inverse_size(group_sum<kLanes>(squares), per, x.norm.epsilon);
+        const float share = group_sum<kLanes>(mixed) * r * per;                // mean of w g n
+        if (is) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) {
+            const float nu = u[e] * r, nv = v[e] * r;
+            sums.u[e] = fmaf(p[e], nu, sums.u[e]);
+            sums.v[e] = fmaf(q[e], nv, sums.v[e]);
+            p[e] = r * fmaf(-nu, share, wu[e]);
+            q[e] = r * fmaf(-nv, share, wv[e]);
+          }
+        }
+      }
+      if (is) {
+        Vec yu, yv;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          yu[e] = (T)p[e];
+          yv[e] = (T)q[e];
+        }
+        *reinterpret_cast<Vec*>(dx + head * x.dx_head + item.at) = yu;
+        *reinterpret_cast<Vec*>(dx + head * x.dx_head + item.at2) = yv;
+      }
+    }
+  }
+  if (!a.partials) return;
+  // over the rows of a wavefront, then over the wavefronts
+#pragma unroll
+  for (int off = kLanes; off < kWave; off <<= 1)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      sums.u[e] += __shfl_xor(sums.u[e], off, kWave);
+      sums.v[e] += __shfl_xor(sums.v[e], off, kWave);
+    }
+  __syncthreads();                                            // (weights and turns are in the same place)
+  if (group == 0 && mine) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      shared[wave * d + item.at + e] = sums.u[e];
+      shared[wave * d + item.at2 + e] = sums.v[e];
+    }
+  }
+  leave_sums(a, shared);
+}
+
+// Any size and alignment: a wavefront goes over a row, a pair a lane, twice.
+template <typename T>
+__global__ __launch_bounds__(kThreads) void norm_grad_any_kernel(NormGradArgs a, GradShape shape) {
   extern __shared__ __align__(16) float shared[];
   __shared__ int64_t position[kGradTokens];
   const int tid = threadIdx.x, d = a.d, pairs = a.rotary.channels >> 1;
@@ -358,34 +689,22 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormGradArgs a, Gra
   const FastDiv heads = which ? shape.heads[1] : shape.heads[0];
   const NormGradRows& x = a.tensor[which];
   float* const weights = shared;                                                   // [d]
-  float2* const turns = reinterpret_cast<float2*>(shared + ((d + 3) & ~3));        // [tokens][channels / 2]
-  // (behind them, at the end, the wavefronts' sums [4][d], in the same place)
+  float2* const turns = reinterpret_cast<float2*>(shared + ((d + 3) & ~3));        // [tokens][pairs]
   if (x.norm.on)
     for (int c = tid; c < d; c += kThreads) weights[c] = weight_at(x.norm, c);
-  constexpr int kRowLanes = kLanes ? kLanes : kWave;
-  constexpr int kPieces = kLanes ? 1 : 8;                       // (d up to 1,024: 512 pairs)
-  const int k = tid % kRowLanes;
-  float sum_u[kPieces][V], sum_v[kPieces][V];
-#pragma unroll
-  for (int p = 0; p < kPieces; ++p)
-#pragma unroll
-    for (int e = 0; e < V; ++e) sum_u[p][e] = sum_v[p][e] = 0.f;
-
+  constexpr int kPieces = kMostChannels / 2 / kWave;
+  const int k = tid % kWave;
+  float sum_u[kPieces] = {}, sum_v[kPieces] = {};
   for (int64_t row0_ = (int64_t)group * tokens; row0_ < a.n_rows; row0_ += (int64_t)groups * tokens) {
     const int32_t row0 = (int32_t)row0_;
     const int count = min(a.n_rows - row0, tokens);
     __syncthreads();
     if (tid < count) position[tid] = a.positions ? a.positions[row0 + tid] : a.first + row0 + tid;
     __syncthreads();
-    find_turns(a.rotary, count, position, turns);
+    for (int i = tid; i < count * pairs; i += kThreads) turns[i] = turned_by(a.rotary, position[i / pairs], a.rotary.frequencies[i % pairs]);
     __syncthreads();
-    const uint32_t total = (uint32_t)count * heads.value, step = kThreads / kRowLanes;
-    struct Row {
-      const T *x, *g;
-      T* dx;
-      int t;
-    };
-    auto locate = [&](uint32_t i) {
+    const uint32_t total = (uint32_t)count * heads.value;
+    for (uint32_t i = tid / kWave; i < total; i += kThreads / kWave) {
       uint32_t t, h;
       if (shape.head_first[which]) {
         t = quotient(i, heads);
@@ -395,199 +714,129 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(NormGradArgs a, Gra
         t = i - h * (uint32_t)count;
       }
       const int64_t at = row0 + (int)t;
-      return Row{static_cast<const T*>(x.x) + (int64_t)h * x.x_head + at * x.x_row, static_cast<const T*>(x.g) + (int64_t)h * x.g_head + at * x.g_row,
-                 static_cast<T*>(x.dx) + (int64_t)h * x.dx_head + at * x.dx_row, (int)t};
-    };
-    if constexpr (kLanes > 0) {
-      using Vec = vec_t<T, V>;
-      const Item<V> item(a.rotary, true, k);
-      const bool mine = k < shape.items;
-      uint32_t i = tid / kLanes;
-      Row row{};
-      Vec xu = {}, xv = {}, gu = {}, gv = {};
-      auto load = [&](uint32_t at) {
-        row = locate(at);
-        if (!mine) return;
-        gu = *reinterpret_cast<const Vec*>(row.g + item.at);
-        gv = *reinterpret_cast<const Vec*>(row.g + item.at2);
-        if (x.norm.on) {
-          xu = *reinterpret_cast<const Vec*>(row.x + item.at);
-          xv = *reinterpret_cast<const Vec*>(row.x + item.at2);
-        }
+      const T* const xs = static_cast<const T*>(x.x) + (int64_t)h * x.x_head + at * x.x_row;
+      const T* const g = static_cast<const T*>(x.g) + (int64_t)h * x.g_head + at * x.g_row;
+      T* const dx = static_cast<T*>(x.dx) + (int64_t)h * x.dx_head + at * x.dx_row;
+      float squares = 0.f, mixed = 0.f;
+      auto pair = [&](int j, const Item<1>& item, bool two, float (&p)[1], float (&q)[1]) {
+        p[0] = (float)g[item.at];
+        q[0] = two ? (float)g[item.at2] : 0.f;
+        if (item.turns) turn<1>(item, turns + (int)t * pairs + j, p, q);
       };
-      if (i < total) load(i);
-      for (; i < total; i += step) {
-        const Row here = row;
-        float u[V], v[V], p[V], q[V];
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          u[e] = (float)xu[e];
-          v[e] = (float)xv[e];
-          p[e] = (float)gu[e];
-          q[e] = (float)gv[e];
-        }
-        if (i + step < total) load(i + step);
-        if (mine && item.turns) turn<V>(item, turns + here.t * pairs + k * V, p, q);
-        if (x.norm.on) {
-          float squares = 0.f, mixed = 0.f, wu[V], wv[V];
-          if (mine) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              wu[e] = weights[item.at + e] * p[e];
-              wv[e] = weights[item.at2 + e] * q[e];
-              squares = fmaf(u[e], u[e], fmaf(v[e], v[e], squares));
-              mixed = fmaf(wu[e], u[e], fmaf(wv[e], v[e], mixed));
-            }
-          }
-          const float r = inverse_size(group_sum<kLanes>(squares), per, x.norm.epsilon);
-          const float share = group_sum<kLanes>(mixed) * r * per;           // mean of w g n
-          if (mine) {
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-              const float nu = u[e] * r, nv = v[e] * r;
-              sum_u[0][e] = fmaf(p[e], nu, sum_u[0][e]);
-              sum_v[0][e] = fmaf(q[e], nv, sum_v[0][e]);
-              p[e] = r * fmaf(-nu, share, wu[e]);
-              q[e] = r * fmaf(-nv, share, wv[e]);
-            }
-          }
-        }
-        if (!mine) continue;
-        Vec yu, yv;
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          yu[e] = (T)p[e];
-          yv[e] = (T)q[e];
-        }
-        *reinterpret_cast<Vec*>(here.dx + item.at) = yu;
-        *reinterpret_cast<Vec*>(here.dx + item.at2) = yv;
-      }
-    } else {
-      for (uint32_t i = tid / kWave; i < total; i += step) {
-        const Row row = locate(i);
-        float squares = 0.f, mixed = 0.f;
-        auto pair = [&](int j, const Item<1>& item, bool two, float (&p)[1], float (&q)[1]) {
-          p[0] = (float)row.g[item.at];
-          q[0] = two ? (float)row.g[item.at2] : 0.f;
-          if (item.turns) turn<1>(item, turns + row.t * pairs + j, p, q);
-        };
-        if (x.norm.on) {
-          for (int j = k; j < (d + 1) / 2; j += kWave) {
-            const Item<1> item(a.rotary, true, j);
-            const bool two = item.at2 < d;
-            float p[1], q[1];
-            pair(j, item, two, p, q);
-            const float u = (float)row.x[item.at], v = two ? (float)row.x[item.at2] : 0.f;
-            squares = fmaf(u, u, fmaf(v, v, squares));
-            mixed = fmaf(weights[item.at] * p[0], u, mixed);
-            if (two) mixed = fmaf(weights[item.at2] * q[0], v, mixed);
-          }
-        }
-        const float r = x.norm.on ? inverse_size(group_sum<kWave>(squares), per, x.norm.epsilon) : 1.f;
-        const float share = group_sum<kWave>(mixed) * r * per;
-#pragma unroll
-        for (int n = 0; n < kPieces; ++n) {
-          const int j = k + n * kWave;
-          if (j >= (d + 1) / 2) break;
+      if (x.norm.on) {
+        for (int j = k; j < (d + 1) / 2; j += kWave) {
           const Item<1> item(a.rotary, true, j);
           const bool two = item.at2 < d;
           float p[1], q[1];
           pair(j, item, two, p, q);
-          if (x.norm.on) {
-            const float nu = (float)row.x[item.at] * r, nv = two ? (float)row.x[item.at2] * r : 0.f;
-            sum_u[n][0] = fmaf(p[0], nu, sum_u[n][0]);
-            sum_v[n][0] = fmaf(q[0], nv, sum_v[n][0]);
-            p[0] = r * fmaf(-nu, share, weights[item.at] * p[0]);
-            if (two) q[0] = r * fmaf(-nv, share, weights[item.at2] * q[0]);
-          }
-          row.dx[item.at] = (T)p[0];
-          if (two) row.dx[item.at2] = (T)q[0];
+          const float u = (float)xs[item.at], v = two ? (float)xs[item.at2] : 0.f;
+          squares = fmaf(u, u, fmaf(v, v, squares));
+          mixed = fmaf(weights[item.at] * p[0], u, mixed);
+          if (two) mixed = fmaf(weights[item.at2] * q[0], v, mixed);
         }
+      }
+      const float r = x.norm.on ? inverse_size(group_sum<kWave>(squares), per, x.norm.epsilon) : 1.f;
+      const float share = group_sum<kWave>(mixed) * r * per;
+#pragma unroll
+      for (int n = 0; n < kPieces; ++n) {
+        const int j = k + n * kWave;
+        if (j >= (d + 1) / 2) break;
+        const Item<1> item(a.rotary, true, j);
+        const bool two = item.at2 < d;
+        float p[1], q[1];
+        pair(j, item, two, p, q);
+        if (x.norm.on) {
+          const float nu = (float)xs[item.at] * r, nv = two ? (float)xs[item.at2] * r : 0.f;
+          sum_u[n] = fmaf(p[0], nu, sum_u[n]);
+          sum_v[n] = fmaf(q[0], nv, sum_v[n]);
+          p[0] = r * fmaf(-nu, share, weights[item.at] * p[0]);
+          if (two) q[0] = r * fmaf(-nv, share, weights[item.at2] * q[0]);
+        }
+        dx[item.at] = (T)p[0];
+        if (two) dx[item.at2] = (T)q[0];
       }
     }
   }
   if (!a.partials) return;
-  // the workgroup's sums: over the rows of a wavefront, then over the wavefronts, in their order
-  if constexpr (kLanes > 0) {
-#pragma unroll
-    for (int off = kLanes; off < kWave; off <<= 1)
-#pragma unroll
-      for (int e = 0; e < V; ++e) {
-        sum_u[0][e] += __shfl_xor(sum_u[0][e], off, kWave);
-        sum_v[0][e] += __shfl_xor(sum_v[0][e], off, kWave);
-      }
-  }
   __syncthreads();
   float* const sums = shared + (tid / kWave) * d;
 #pragma unroll
-  for (int p = 0; p < kPieces; ++p) {
-    const int j = k + p * kRowLanes;
-    if (tid % kWave >= kRowLanes || j >= (kLanes ? shape.items : (d + 1) / 2)) continue;
-    const Item<V> item(a.rotary, true, j);
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      sums[item.at + e] = sum_u[p][e];
-      if (item.at2 + e < d) sums[item.at2 + e] = sum_v[p][e];
-    }
+  for (int n = 0; n < kPieces; ++n) {
+    const int j = k + n * kWave;
+    if (j >= (d + 1) / 2) break;
+    const Item<1> item(a.rotary, true, j);
+    sums[item.at] = sum_u[n];
+    if (item.at2 < d) sums[item.at2] = sum_v[n];
   }
-  __syncthreads();
-  float* const out = a.partials + (int64_t)blockIdx.x * d;
-  for (int c = tid; c < d; c += kThreads) out[c] = (shared[c] + shared[d + c]) + (shared[2 * d + c] + shared[3 * d + c]);
+  leave_sums(a, shared);
 }
 
-// dw of both tensors: 32 channels a workgroup, 32 threads for each, which add every 32nd partial sum.
-__global__ __launch_bounds__(1024) void norm_join_kernel(NormGradArgs a, int32_t groups0, int32_t groups1) {
-  __shared__ double sums[32][33];
+// dw of both tensors: 16 channels a workgroup, 64 threads for each, which add every 64th partial sum.
+constexpr int kJoinChannels = 16, kJoinParts = 64;
+__global__ __launch_bounds__(kJoinChannels* kJoinParts) void norm_join_kernel(NormGradArgs a, int32_t groups0, int32_t groups1) {
+  __shared__ double sums[kJoinParts][kJoinChannels + 1];
   const NormGradRows& x = a.tensor[blockIdx.y];
   if (!x.dw) return;
   const int32_t first = blockIdx.y ? groups0 : 0, count = blockIdx.y ? groups1 : groups0;
-  const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+  const int lane = threadIdx.x % kJoinChannels, part = threadIdx.x / kJoinChannels, c = blockIdx.x * kJoinChannels + lane;
   double sum = 0.0;
   if (c < a.d) {
     const float* p = a.partials + (int64_t)first * a.d + c;
 #pragma unroll 8
-    for (int32_t i = part; i < count; i += 32) sum += (double)p[(int64_t)i * a.d];
+    for (int32_t i = part; i < count; i += kJoinParts) sum += (double)p[(int64_t)i * a.d];
   }
   sums[part][lane] = sum;
   __syncthreads();
-  if (part == 0 && c < a.d) {
-    sum = 0.0;
-    for (int i = 0; i < 32; ++i) sum += sums[i][lane];
-    x.dw[c] = (float)sum;
+  if (part < 4) {
+    for (int i = part + 4; i < kJoinParts; i += 4) sum += sums[i][lane];
+    sums[part][lane] = sum;
   }
+  __syncthreads();
+  if (part == 0 && c < a.d) x.dw[c] = (float)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
 }
 
-// Workgroups of each tensor: in proportion to their heads, as many as have a round of rows each, kGradGroups in all at most.
-void grad_groups(int64_t n_rows, int32_t Hq, int32_t Hkv, int32_t (&groups)[2], int32_t (&tokens)[2]) {
+// Workgroups of each tensor: in proportion to their heads, no more than a fourth of its rows, kGradGroups in all at most.
+void grad_groups(int64_t n_rows, int32_t Hq, int32_t Hkv, int32_t (&groups)[2]) {
   const int32_t heads[2] = {Hq, Hkv};
   for (int i = 0; i < 2; ++i) {
-    groups[i] = tokens[i] = 0;
-    if (heads[i] < 1) continue;
-    int32_t t = (128 + heads[i] - 1) / heads[i];
-    t = t < 1 ? 1 : t > kGradTokens ? kGradTokens : t;
-    while (t > 1 && n_rows / t < 256) t >>= 1;
-    const int64_t most = ((int64_t)kGradGroups * heads[i] + Hq + Hkv - 1) / (Hq + Hkv), rounds = (n_rows + t - 1) / t;
-    tokens[i] = t;
-    groups[i] = (int32_t)(rounds < most ? (rounds < 1 ? 1 : rounds) : most);
+    const int64_t most = heads[i] < 1 ? 0 : ((int64_t)kGradGroups * heads[i] + Hq + Hkv - 1) / (Hq + Hkv), enough = (n_rows + 3) / 4;
+    groups[i] = (int32_t)(heads[i] < 1 ? 0 : enough < 1 ? 1 : enough < most ? enough : most);
   }
 }
 
 template <typename T, int V, int kLanes>
 sga_status launch_grad_as(const NormGradArgs& a) {
   GradShape s{};
-  grad_groups(a.n_rows, a.tensor[0].heads, a.n_tensors > 1 ? a.tensor[1].heads : 0, s.groups, s.tokens);
-  for (int i = 0; i < a.n_tensors; ++i) s.head_first[i] = a.tensor[i].x_head <= a.tensor[i].x_row;
-  s.items = a.d / (2 * V);
-  s.heads[0] = fast_div(a.tensor[0].heads);
-  s.heads[1] = fast_div(a.n_tensors > 1 ? a.tensor[1].heads : 1);
-  const int most = s.tokens[0] > s.tokens[1] ? s.tokens[0] : s.tokens[1];
-  size_t lds = (size_t)((a.d + 3) & ~3) * sizeof(float) + (size_t)most * (a.rotary.channels / 2) * sizeof(float2);
+  grad_groups(a.n_rows, a.tensor[0].heads, a.n_tensors > 1 ? a.tensor[1].heads : 0, s.groups);
+  const int pairs = a.rotary.channels / 2;
+  s.pairs = fast_div(pairs > 0 ? pairs : 1);
+  s.pairs.value = pairs;
+  int most = 1;                                       // tokens whose turns a workgroup holds
+  for (int i = 0; i < a.n_tensors; ++i) {
+    const int heads = a.tensor[i].heads;
+    s.heads[i] = fast_div(heads);
+    s.head_first[i] = a.tensor[i].x_head <= a.tensor[i].x_row;
+    if constexpr (kLanes > 0) {
+      while ((2 << s.tokens[i]) * heads <= kWave / kLanes) ++s.tokens[i];
+      most = (kThreads / kWave) << s.tokens[i] > most ? (kThreads / kWave) << s.tokens[i] : most;
+    } else {
+      int t = (128 + heads - 1) / heads;
+      t = t > kGradTokens ? kGradTokens : t;
+      while (t > 1 && a.n_rows / t < 256) t >>= 1;
+      s.tokens[i] = t;
+      most = t > most ? t : most;
+    }
+  }
+  size_t lds = (size_t)((a.d + 3) & ~3) * sizeof(float) + (size_t)most * pairs * sizeof(float2);
   const size_t sums = (size_t)(kThreads / kWave) * a.d * sizeof(float);
   lds = lds > sums ? lds : sums;
-  if (a.n_rows > 0) norm_grad_kernel<T, V, kLanes><<<s.groups[0] + s.groups[1], kThreads, lds, a.stream>>>(a, s);
+  if (a.n_rows > 0) {
+    if constexpr (kLanes > 0) norm_grad_kernel<T, V, kLanes><<<s.groups[0] + s.groups[1], kThreads, lds, a.stream>>>(a, s);
+    else norm_grad_any_kernel<T><<<s.groups[0] + s.groups[1], kThreads, lds, a.stream>>>(a, s);
+  }
   if (a.partials) {
     const bool any = a.n_rows > 0;                     // (no rows: dw is 0)
-    norm_join_kernel<<<dim3((a.d + 31) / 32, a.n_tensors), 1024, 0, a.stream>>>(a, any ? s.groups[0] : 0, any ? s.groups[1] : 0);
+    norm_join_kernel<<<dim3((a.d + kJoinChannels - 1) / kJoinChannels, a.n_tensors), kJoinChannels * kJoinParts, 0, a.stream>>>(a, any ? s.groups[0] : 0, any ? s.groups[1] : 0);
   }
   return hip_status(hipGetLastError());
 }
@@ -613,8 +862,8 @@ sga_status launch_grad_type(const NormGradArgs& a) {
 }  // namespace
 
 size_t norm_partial_bytes(int64_t n_rows, int32_t Hq, int32_t Hkv, int32_t d) {
-  int32_t groups[2], tokens[2];
-  grad_groups(n_rows, Hq, Hkv, groups, tokens);
+  int32_t groups[2];
+  grad_groups(n_rows, Hq, Hkv, groups);
   return (size_t)(groups[0] + groups[1]) * d * sizeof(float);
 }
 
