@@ -517,7 +517,7 @@ typedef struct {
  *   batch      read: the last step's.  next: written, alike in sizes; its arrays may be batch's.  (page_stride is not looked at.)
  *   pool       read; its ring is written.  state_out: device, int64 [2], written; may be pool's state.
  *   ask        device, int32 [n_seqs].  kept: device, int32 [n_seqs] (brought into 0 .. rows), or NULL
- *   mask       host, SGA_MASK_SLIDING or SGA_MASK_GLOBAL_LOCAL (L is not looked at), or NULL: nothing goes back behind a window
+ *   mask       host, SGA_MASK_SLIDING or SGA_MASK_GLOBAL_LOCAL (of L only that it is valid), or NULL: nothing goes back behind a window
  *   positions  device, int64 [n_tokens], or NULL: written, the place in its sequence of every new token's row
  *   slots      device, int64 [n_tokens], or NULL: written, page * page_size + row in the page of every new token, -1 without a page
  *   workspace  device, 256-byte aligned, sga_pages_workspace_bytes; calls that overlap in time need one each
@@ -615,7 +615,7 @@ sga_status sga_attention_tree(const sga_rows* Q, const void* cache_k, const void
  *   path    device, int32 [n_seqs][path_columns]; an entry outside k .. new - 1 moves nothing.  (Rising paths are never
  *           below k.)  All moves are of what the cache held before the call.
  *   count   device, int32 [n_seqs]; no more than path_columns are looked at
- * Nothing moves from or to a place without a page.  d 2..1024, any dtype of serving.
+ * Nothing moves from or to a place without a page; no two sequences may have new tokens in one page.  d 2..1024, any dtype of serving.
  * Errors: SGA_ERR_INVALID_ARG, SGA_ERR_OVERFLOW (layers * Hkv * d of 2^29 and more).
  */
 sga_status sga_cache_keep(void* cache_k, void* cache_v, const sga_paged_batch* batch, int32_t Hkv, int32_t d, int32_t n_layers,

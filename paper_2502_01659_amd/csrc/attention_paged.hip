@@ -1,4 +1,4 @@
-// Attention of new tokens over a paged cache (sga_attention_paged).
+// Attention of new tokens over a paged cache (sga_attention_paged), of drafted ones that form a tree too (sga_attention_tree).
 //
 // Two kernels: paged_kernel for short chunks, which memory bounds, and paged_chunk_kernel (below) for long ones, which the
 // matrix cores bound.  In the first a tile is 16 or 32 consecutive rows of one sequence and key head, a row being a new
@@ -116,7 +116,9 @@ __device__ __forceinline__ int32_t kept_of(const PagedAttention& a, int32_t leng
 // Drafted tokens.  New token t of a sequence lies at place base + t of the cache, base = length - n_new, but at position base + depth(t), and
 // sees of the context, the tokens before base, what the mask shows that position, and of the new tokens those whose bits are set in
 // its row of `seen`.  Both kernels meet the context's keys as they do others', and the blocks that reach base as blocks at an edge, in which every key is
-// tested: the bits of a block's 32 keys are two words of the row, put together.  All rows of a sequence meet the same keys.
+// tested: the bits of a block's 32 keys are two words of the row, put together.  All rows of a sequence meet the same keys.  Measured (us, in turn with
+// the same call without a tree): 5 to 16 drafts of 64 sequences behind 512 to 32,768, 32 / 8 heads of 128, bf16 407 / 414 (5.0 TB/s, a large copy 4.8); 30 to 200 of 32
+// under a window of 4,096, 32 / 4 heads, fp16 232 / 230 (700 TFLOP/s of the products that the mask asks for; the library's 1,151).
 __device__ __forceinline__ Sight context_sight(const PagedAttention& a, const Tile& t, int32_t token) {
   const int32_t base = t.length - t.n_new, depth = a.depth[t.begin + token];
   const int64_t p = (int64_t)base + depth;

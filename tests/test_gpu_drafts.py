@@ -61,7 +61,7 @@ def run_pages(table, ptr, length, ring, state, ask, kept, T, page, n_pages, spec
     (1, 1, 1, False, None, 3), (1, 700, 16, True, None, 2000), (7, 20, 16, True, MaskSpec(KIND_SLIDING, 64, window=40), 30),
     (64, 130, 16, True, MaskSpec(KIND_GLOBAL_LOCAL, 4000, window=300, n_global=33), 200), (300, 9, 5, False, None, 12),
     (1500, 64, 3, True, MaskSpec(KIND_SLIDING, 64, window=0), 5), (5000, 3, 8, True, None, 4), (3, 5000, 1, False, MaskSpec(KIND_SLIDING, 9, window=99), 900),
-    (260, 100, 7, True, MaskSpec(KIND_GLOBAL_LOCAL, 9, window=7, n_global=9), 60),
+    (260, 100, 7, True, MaskSpec(KIND_GLOBAL_LOCAL, 9, window=7, n_global=9), 60), (65536, 2, 16, True, None, 9),
 ])
 def test_pages(n_seqs, columns, page, kept, spec, most, in_place):
     rng = np.random.default_rng(n_seqs + columns)
@@ -219,6 +219,26 @@ def test_norm_gradient(dtype, layout, Hq, Hkv, T, d, channels, memory):
     got = sga.norm_rotary_backward(Q, G, K, GK, rotary=rot, k_norm=sga.Norm(wk, 1e-6, 0.0), first=900)
     want, _, size, _ = D.norm_gradient(host(Q), host(G), at, f, layout, 0.8, None, 1e-6, 0.0, normed=False)
     assert got[1] is None and within(got[0], want, D.gradient_bar(want, size, dtype))
+
+
+def test_norms_of_far_rows():
+    """Offsets of more than 2^32 elements, forward and back, in place."""
+    L, d = (1 << 27) + 5, 32
+    x = torch.zeros(1, L, d, dtype=torch.float16, device="cuda")
+    g = torch.zeros_like(x)
+    at = torch.tensor([0, 1, (1 << 26) + 3, (1 << 27) - 1, L - 1], device="cuda")
+    x[0, at], g[0, at] = (torch.randn(5, d, generator=torch.Generator().manual_seed(s)).half().cuda() for s in (1, 2))
+    w = weights_of("f32", d, "f16", 0.0, 3)
+    freqs, _ = sga.rotary_frequencies(d)
+    rot, n, f = sga.Rotary(freqs), sga.Norm(w), freqs.cpu().numpy()
+    few_x, few_g, where = host(x[:, at]), host(g[:, at]), at.cpu().numpy() + 7
+    dx, dw = sga.norm_rotary_backward(x, g, rotary=rot, q_norm=n, first=7, dQ=g)
+    want, want_w, size, w_size = D.norm_gradient(few_x, few_g, where, f, "half", 1.0, host(w), 1e-6, 0.0)
+    assert dx is g and within(g[:, at], want, D.gradient_bar(want, size, "f16")) and within(dw, want_w, D.weight_bar(w_size))
+    assert int(torch.count_nonzero(g[0, :, 0])) <= 5
+    assert sga.norm_rotary(x, rotary=rot, q_norm=n, first=7, Q_out=x) is x
+    y, size = D.norm_rotate(few_x, where, f, "half", 1.0, host(w), 1e-6, 0.0)
+    assert within(x[:, at], y, D.norm_bar(y, size, "f16")) and int(torch.count_nonzero(x[0, :, 0])) <= 5
 
 
 @pytest.mark.parametrize("layout", ["half", "interleaved"])
