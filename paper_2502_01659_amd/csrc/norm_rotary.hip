@@ -798,12 +798,18 @@ __global__ __launch_bounds__(kJoinChannels* kJoinParts) void norm_join_kernel(No
   if (part == 0 && c < a.d) x.dw[c] = (float)((sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
 }
 
-// Workgroups of each tensor: in proportion to their heads, no more than a fourth of its rows, kGradGroups in all at most.
+// Workgroups of each tensor: in proportion to their heads, kGradGroups in all at most; no more than a fourth of its tokens, and beyond one a compute unit than a sixteenth
+// (us, kernel and join, a fourth / a sixteenth: 10,007 tokens, 8 + 2 heads of 64, fp32 18.0 + 4.6 / 16.4 + 4.1).
 void grad_groups(int64_t n_rows, int32_t Hq, int32_t Hkv, int32_t (&groups)[2]) {
   const int32_t heads[2] = {Hq, Hkv};
   for (int i = 0; i < 2; ++i) {
-    const int64_t most = heads[i] < 1 ? 0 : ((int64_t)kGradGroups * heads[i] + Hq + Hkv - 1) / (Hq + Hkv), enough = (n_rows + 3) / 4;
-    groups[i] = (int32_t)(heads[i] < 1 ? 0 : enough < 1 ? 1 : enough < most ? enough : most);
+    if (heads[i] < 1) {
+      groups[i] = 0;
+      continue;
+    }
+    const int64_t most = ((int64_t)kGradGroups * heads[i] + Hq + Hkv - 1) / (Hq + Hkv), few = (n_rows + 3) / 4, many = (n_rows + 15) / 16;
+    const int64_t enough = many > 256 ? many : few < 256 ? few : 256;
+    groups[i] = (int32_t)(enough < 1 ? 1 : enough < most ? enough : most);
   }
 }
 
