@@ -41,14 +41,6 @@ __device__ __forceinline__ float group_sum(float x) {
   return x;
 }
 
-__device__ __forceinline__ float weight_at(const NormArg& n, int c) {
-  if (!n.weight) return 1.f;
-  const float w = n.dtype == SGA_F32   ? static_cast<const float*>(n.weight)[c]
-                  : n.dtype == SGA_F16 ? (float)static_cast<const f16_t*>(n.weight)[c]
-                                       : (float)static_cast<const bf16_t*>(n.weight)[c];
-  return w + n.offset;
-}
-
 constexpr int kMostChannels = 1024;
 // A weight as it lies in memory, and what it stands for.  (0 where there are none.)
 __device__ __forceinline__ uint32_t raw_weight(const NormArg& n, int c) {
@@ -62,9 +54,12 @@ __device__ __forceinline__ float weight_from(const NormArg& n, uint32_t raw) {
                                : __builtin_bit_cast(float, raw << 16)) + n.offset;
 }
 
+__device__ __forceinline__ float weight_at(const NormArg& n, int c) { return weight_from(n, raw_weight(n, c)); }
+
 __device__ __forceinline__ float inverse_size(float squares, float per, float epsilon) { return rsqrtf(fmaf(squares, per, epsilon)); }
 
-// The channels of item k of a row: V from `at` and V from `at2`; where it turns, its cosines and sines are kTurns V k ..
+// The channels of item k of a row: V from `at` and V from `at2`; where it turns, its pairs are V k ..  Split, pair e is (at + e, at2 + e), else the
+// pairs are (at, at + 1) and so on through all 2 V.
 template <int V>
 struct Item {
   int at, at2;
@@ -77,31 +72,11 @@ struct Item {
   }
 };
 
-// The pair (a[e], b[e]) if split, else (a[2i], a[2i + 1]) and (b[2i], b[2i + 1]).
-template <int V>
-__device__ __forceinline__ void turn(const Item<V>& item, const float2* cs, float (&u)[V], float (&v)[V]) {
-  if (item.split) {
-#pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float p = u[e], q = v[e];
-      u[e] = p * cs[e].x - q * cs[e].y;
-      v[e] = p * cs[e].y + q * cs[e].x;
-    }
-  } else if constexpr (V > 1) {
-#pragma unroll
-    for (int e = 0; e < V; e += 2) {
-      const float2 c = cs[e / 2], c2 = cs[(V + e) / 2];
-      const float p = u[e], q = u[e + 1], p2 = v[e], q2 = v[e + 1];
-      u[e] = p * c.x - q * c.y;
-      u[e + 1] = p * c.y + q * c.x;
-      v[e] = p2 * c2.x - q2 * c2.y;
-      v[e + 1] = p2 * c2.y + q2 * c2.x;
-    }
-  } else {
-    const float p = u[0], q = v[0];
-    u[0] = p * cs[0].x - q * cs[0].y;
-    v[0] = p * cs[0].y + q * cs[0].x;
-  }
+// One pair.
+__device__ __forceinline__ void turn(float2 cs, float& a, float& b) {
+  const float p = a, q = b;
+  a = p * cs.x - q * cs.y;
+  b = p * cs.y + q * cs.x;
 }
 
 struct NormShape {
@@ -160,7 +135,7 @@ __device__ __forceinline__ Own<V> weights_of(const float* w, const Item<V>& item
 
 // Rows in lanes, kLanes of them a row with 2 V elements each.  A wavefront works by itself: it takes one token (or, where a token has fewer heads than the
 // wavefront holds rows, several) with all its heads, computes the sines into its own part of LDS while the first rows are on their way, and keeps
-// those of its lanes' channels, and their weights, in registers: a lane's channels are the same in every row.  Rows are loaded kBatch at a time
+// those of its lanes' channels in registers: a lane's channels are the same in every row.  Rows are loaded kBatch at a time
 // (us, 1 / 2 / 3 / 4 / 8: 32,768 tokens, 32 + 8 heads of 128, bf16 128 / 129 / 136 / 149 / 196: registers).
 constexpr int kBatch = 2;
 template <typename T, int V, int kLanes, bool kPaged>
@@ -421,14 +396,14 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_any_kernel(NormRotateArg
       for (int j = k; j < (d + 1) / 2; j += kWave) {
         const Item<1> item(a.r.rotary, x.rotate, j);
         const bool two = item.at2 < d;                       // (not the last channel of an odd number)
-        float p[1] = {(float)src[item.at]}, q[1] = {two ? (float)src[item.at2] : 0.f};
+        float p = (float)src[item.at], q = two ? (float)src[item.at2] : 0.f;
         if (norm.on) {
-          p[0] = p[0] * r * w[item.at];
-          if (two) q[0] = q[0] * r * w[item.at2];
+          p = p * r * w[item.at];
+          if (two) q = q * r * w[item.at2];
         }
-        if (item.turns) turn<1>(item, turns + (int)t * pairs + j, p, q);
-        dst[item.at] = (T)p[0];
-        if (two) dst[item.at2] = (T)q[0];
+        if (item.turns) turn(turns[(int)t * pairs + j], p, q);
+        dst[item.at] = (T)p;
+        if (two) dst[item.at2] = (T)q;
       }
     }
   }
@@ -721,21 +696,21 @@ __global__ __launch_bounds__(kThreads) void norm_grad_any_kernel(NormGradArgs a,
       const T* const g = static_cast<const T*>(x.g) + (int64_t)h * x.g_head + at * x.g_row;
       T* const dx = static_cast<T*>(x.dx) + (int64_t)h * x.dx_head + at * x.dx_row;
       float squares = 0.f, mixed = 0.f;
-      auto pair = [&](int j, const Item<1>& item, bool two, float (&p)[1], float (&q)[1]) {
-        p[0] = (float)g[item.at];
-        q[0] = two ? (float)g[item.at2] : 0.f;
-        if (item.turns) turn<1>(item, turns + (int)t * pairs + j, p, q);
+      auto pair = [&](int j, const Item<1>& item, bool two, float& p, float& q) {
+        p = (float)g[item.at];
+        q = two ? (float)g[item.at2] : 0.f;
+        if (item.turns) turn(turns[(int)t * pairs + j], p, q);
       };
       if (x.norm.on) {
         for (int j = k; j < (d + 1) / 2; j += kWave) {
           const Item<1> item(a.rotary, true, j);
           const bool two = item.at2 < d;
-          float p[1], q[1];
+          float p, q;
           pair(j, item, two, p, q);
           const float u = (float)xs[item.at], v = two ? (float)xs[item.at2] : 0.f;
           squares = fmaf(u, u, fmaf(v, v, squares));
-          mixed = fmaf(weights[item.at] * p[0], u, mixed);
-          if (two) mixed = fmaf(weights[item.at2] * q[0], v, mixed);
+          mixed = fmaf(weights[item.at] * p, u, mixed);
+          if (two) mixed = fmaf(weights[item.at2] * q, v, mixed);
         }
       }
       const float r = x.norm.on ? inverse_size(group_sum<kWave>(squares), per, x.norm.epsilon) : 1.f;
@@ -746,17 +721,17 @@ __global__ __launch_bounds__(kThreads) void norm_grad_any_kernel(NormGradArgs a,
         if (j >= (d + 1) / 2) break;
         const Item<1> item(a.rotary, true, j);
         const bool two = item.at2 < d;
-        float p[1], q[1];
+        float p, q;
         pair(j, item, two, p, q);
         if (x.norm.on) {
           const float nu = (float)xs[item.at] * r, nv = two ? (float)xs[item.at2] * r : 0.f;
-          sum_u[n] = fmaf(p[0], nu, sum_u[n]);
-          sum_v[n] = fmaf(q[0], nv, sum_v[n]);
-          p[0] = r * fmaf(-nu, share, weights[item.at] * p[0]);
-          if (two) q[0] = r * fmaf(-nv, share, weights[item.at2] * q[0]);
+          sum_u[n] = fmaf(p, nu, sum_u[n]);
+          sum_v[n] = fmaf(q, nv, sum_v[n]);
+          p = r * fmaf(-nu, share, weights[item.at] * p);
+          if (two) q = r * fmaf(-nv, share, weights[item.at2] * q);
         }
-        dx[item.at] = (T)p[0];
-        if (two) dx[item.at2] = (T)q[0];
+        dx[item.at] = (T)p;
+        if (two) dx[item.at2] = (T)q;
       }
     }
   }
