@@ -131,9 +131,8 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_count_kernel(Pages
   }
 }
 
-// Sums that stop at 2^31 - 1: more tokens or pages than there are, whatever comes.
-constexpr uint32_t kFull = 0x7fffffff;
-__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return min(a + b, kFull); }
+// Sums that stop at 2^32 - 1: more tokens or pages than there can be (fewer than 2^31 of each), so that a sum that has stopped passes no limit.
+__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
 template <int kCtrl, int kRows>
 __device__ __forceinline__ uint32_t with_lane(uint32_t x) {
   return plus(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, kRows, 0xF, false));

@@ -96,6 +96,32 @@ def test_pages_of_nothing_and_of_bad_records():
         assert np.array_equal(pool.pages.cpu().numpy(), want[3]) and pool.state.tolist() == want[4].tolist()
 
 
+@pytest.mark.parametrize("asks,granted", [
+    ([2 * 10 ** 9, 2 * 10 ** 9], 1), ([1 << 30, (1 << 30) - 1], 2), ([1 << 30, 1 << 30, 1], 1), ([1 << 30] * 4 + [5, 1 << 30], 1),
+    ([(1 << 31) - 65536, 65535, 1], 2), ([7] + [2 * 10 ** 9] * 299, 2), ([1 << 30] * 130 + [1], 1),
+])
+def test_pages_of_requests_beyond_every_number(asks, granted):
+    """As many rows as a batch may have, 2^31 - 1, and requests whose sum passes that, 2^32 and 2^33: those that fit are granted, the one that fills
+    the rows to the last among them, and none behind the first that does not."""
+    print("pages beyond", len(asks), asks[:4], flush=True)
+    page, T = 65536, (1 << 31) - 1
+    needs = [-(-a // page) for a in asks]
+    columns, n_pages = min(max(needs), 32767), max(sum(needs), 5)
+    table = torch.full((len(asks), columns), -1, dtype=torch.int32, device="cuda")
+    batch = sga.PagedBatch(table, torch.zeros(len(asks) + 1, dtype=torch.int64, device="cuda"), torch.zeros(len(asks), dtype=torch.int32, device="cuda"),
+                           T, page, n_pages)
+    pool = sga.PagePool.full(n_pages)
+    sga.pages_advance(batch, pool, torch.tensor(asks, dtype=torch.int32, device="cuda"))
+    rows = [a if i < granted else 0 for i, a in enumerate(asks)]
+    assert batch.seq_len.tolist() == rows and batch.seq_ptr.tolist() == [0] + np.cumsum(rows).tolist()
+    taken = 0
+    for i, n in enumerate(needs):
+        n = n if i < granted else 0
+        assert table[i, :n].tolist() == list(range(taken, taken + n)) and (table[i, n:] == -1).all()
+        taken += n
+    assert pool.state.tolist() == [taken % n_pages, n_pages - taken]
+
+
 def test_pages_over_many_steps_captured():
     """A captured call, in place: pages are neither lost nor given twice, and every replay is the oracle's step."""
     rng = np.random.default_rng(5)
