@@ -23,7 +23,7 @@ constexpr int kMaxGroups = 1 << 20;  // workgroups along the tokens; they stride
 // 4,096 198 + 15.)
 constexpr int kGradGroups = 2048;
 constexpr int kGradTokens = 16;      // (any alignment) tokens of one round of it at most
-constexpr int64_t kNone = INT64_MIN;
+constexpr int64_t kNone = INT64_MIN;  // (rows of a batch) no position; a program's own positions may be any number
 
 // Sum over groups of kLanes neighbouring lanes, in every one of them.  (The lanes of a group are active together.)
 template <int kCtrl>
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
         // (the position of token t: of the lanes that hold its rows)
         const int from = (t & (tokens - 1)) * kLanes;
         const int64_t at = (int64_t)((uint64_t)(uint32_t)__shfl((int)(position >> 32), from, kWave) << 32 | (uint32_t)__shfl((int)position, from, kWave));
-        if (i < tokens * pairs) turns[i] = at == kNone ? make_float2(0.f, 0.f) : turned_by(a.r.rotary, at, i0 == 0 ? own_frequency : a.r.rotary.frequencies[p]);
+        if (i < tokens * pairs) turns[i] = kPaged && at == kNone ? make_float2(0.f, 0.f) : turned_by(a.r.rotary, at, i0 == 0 ? own_frequency : a.r.rotary.frequencies[p]);
       }
       __builtin_amdgcn_wave_barrier();
       // interleaved, pair e of an item's 2 V channels is (2 e, 2 e + 1); split, (e, V + e)
@@ -363,7 +363,7 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_any_kernel(NormRotateArg
     __syncthreads();
     for (int i = tid; i < count * pairs; i += kThreads) {
       const int t = i / pairs;
-      if (position[t] != kNone) turns[i] = turned_by(a.r.rotary, position[t], a.r.rotary.frequencies[i - t * pairs]);
+      if (!kPaged || position[t] != kNone) turns[i] = turned_by(a.r.rotary, position[t], a.r.rotary.frequencies[i - t * pairs]);
     }
     __syncthreads();
     const uint32_t total = (uint32_t)tokens * shape.heads.value;

@@ -203,6 +203,26 @@ def test_norm_rotary(dtype, layout, Hq, Hkv, T, d, channels, memory):
         assert within(sga.norm_rotary(Q, q_norm=norms[0]), y, D.norm_bar(y, size, dtype))
 
 
+@pytest.mark.parametrize("layout", ["half", "interleaved"])
+@pytest.mark.parametrize("d", [64, 6])
+def test_norm_rotary_of_the_farthest_positions(d, layout):
+    """Positions are any 64-bit numbers, the lowest among them: in rows in lanes and one pair a lane, forward and back."""
+    print("farthest", d, layout, flush=True)
+    f = 1e-9 * 0.7 ** np.arange(d // 2)                       # (angles below 10^10: extended precision holds them to 2^-30)
+    rot, n = sga.Rotary(torch.from_numpy(f).cuda(), layout=layout), sga.Norm()
+    at = np.array([-2 ** 63, 5, -2 ** 63 + 1, 2 ** 63 - 1, -2 ** 63])
+    Q, G = tokens(3, 5, d, "f32", 1), tokens(3, 5, d, "f32", 2)
+    where = torch.from_numpy(at).cuda()
+    y, size = D.norm_rotate(host(Q), at, f, layout, 1.0, None, 1e-6, 0.0)
+    got = sga.norm_rotary(Q, rotary=rot, q_norm=n, positions=where)
+    assert within(got, y, D.norm_bar(y, size, "f32"))
+    dx, _ = sga.norm_rotary_backward(Q, G, rotary=rot, q_norm=n, positions=where)
+    want, _, size, _ = D.norm_gradient(host(Q), host(G), at, f, layout, 1.0, None, 1e-6, 0.0)
+    assert within(dx, want, D.gradient_bar(want, size, "f32"))
+    first = sga.norm_rotary(Q[:, :1].contiguous(), rotary=rot, q_norm=n, first=-2 ** 63)
+    assert torch.equal(first, got[:, :1])
+
+
 def test_norm_of_rows_of_zeros_and_of_no_rows():
     x = torch.zeros(2, 3, 64, device="cuda")
     x[1, 1] = 1e-30
