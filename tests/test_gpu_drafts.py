@@ -267,6 +267,35 @@ def test_norm_gradient(dtype, layout, Hq, Hkv, T, d, channels, memory):
     assert got[1] is None and within(got[0], want, D.gradient_bar(want, size, dtype))
 
 
+# Calls whose workgroups and wavefronts take many tokens, one behind the other, with a remainder.  A lane adds at most 36 rows' terms of a weight's gradient in
+# these (rows of one pair a lane: up to 16 tokens' heads over four wavefronts, up to four times; rows in lanes: up to eight tokens, four rounds of heads
+# each), a wavefront and a workgroup up to 20 of its lanes' and wavefronts' sums in six steps: below the 72 half steps of weight_bar.
+@pytest.mark.parametrize("dtype,Hq,Hkv,T,d,channels,memory,layout", [
+    # one pair a lane: wide rows whose turns fill most of the memory that a workgroup shares, odd sizes, several rounds
+    ("f32", 2, 1, 4097, 1024, 1024, "token", "half"), ("bf16", 4, 1, 4100, 1000, 1000, "head", "interleaved"), ("f16", 3, 2, 4099, 7, 6, "token", "half"),
+    ("f32", 3, 2, 40003, 7, 6, "head", "interleaved"), ("bf16", 3, 2, 4099, 80, 20, "token", "interleaved"), ("f16", 16, 1, 4101, 80, 20, "slice", "half"),
+    # rows in lanes: one token and several a wavefront
+    ("f16", 16, 2, 4099, 80, 80, "token", "half"), ("bf16", 8, 2, 16411, 64, 64, "token", "half"), ("f16", 32, 8, 9001, 128, 128, "token", "interleaved"),
+    ("f32", 5, 5, 20011, 64, 32, "head", "half"),
+])
+def test_norms_of_many_tokens(dtype, Hq, Hkv, T, d, channels, memory, layout):
+    print("many tokens", dtype, Hq, Hkv, T, d, channels, memory, layout, flush=True)
+    freqs, _ = sga.rotary_frequencies(channels)
+    rot, f = sga.Rotary(freqs, layout=layout, magnitude=0.9), freqs.cpu().numpy()
+    Q, K, G, GK = (tokens(H, T, d, dtype, T + i, m) for i, (H, m) in enumerate(((Hq, memory), (Hkv, memory), (Hq, "token"), (Hkv, "head"))))
+    wq, wk = weights_of("same", d, dtype, 0.0, 1), weights_of("f32", d, dtype, 1.0, 2)
+    qn, kn = sga.Norm(wq), sga.Norm(wk, 0.25, 1.0)
+    at = np.random.default_rng(d).integers(0, 1 << 20, T)
+    where = torch.from_numpy(at).cuda()
+    out = sga.norm_rotary(Q, K, rotary=rot, q_norm=qn, k_norm=kn, positions=where)
+    grads = sga.norm_rotary_backward(Q, G, K, GK, rotary=rot, q_norm=qn, k_norm=kn, positions=where)
+    for x, g, w, (epsilon, offset), y, dx, dw in ((Q, G, wq, (1e-6, 0.0), out[0], *grads[:2]), (K, GK, wk, (0.25, 1.0), out[1], *grads[2:])):
+        want, size = D.norm_rotate(host(x), at, f, layout, 0.9, host(w), epsilon, offset)
+        assert within(y, want, D.norm_bar(want, size, dtype))
+        want, want_w, size, w_size = D.norm_gradient(host(x), host(g), at, f, layout, 0.9, host(w), epsilon, offset)
+        assert within(dx, want, D.gradient_bar(want, size, dtype)) and within(dw, want_w, D.weight_bar(w_size))
+
+
 def test_norms_of_far_rows():
     """Offsets of more than 2^32 elements, forward and back, in place."""
     L, d = (1 << 27) + 5, 32
@@ -426,6 +455,44 @@ def test_append_of_normed_drafts(dtype, new, length, page, Hq, Hkv, d, channels,
     sga.cache_append(K, V, ck4, cv4, batch, Q=Q, Q_out=q4, q_norm=qn, k_norm=kn)
     y, size = D.norm_rotate(host(Q), None, None, None, 1.0, host(wq), 1e-6, 0.0)
     assert within(host(q4)[:, real], y[:, real], D.norm_bar(y, size, dtype)[:, real])
+
+
+@pytest.mark.parametrize("dtype,new,length,page,Hq,Hkv,d,channels,tree", [
+    # prompts: more tokens than the chip's wavefronts take at once, one and four of them a wavefront
+    ("f16", [20000, 1, 0, 3011, 9990], [20000, 700, 5, 4000, 30000], 16, 8, 4, 128, 128, False),
+    ("bf16", [20000, 1, 0, 3011, 19990], [20017, 1, 9, 3011, 20000], 24, 4, 1, 64, 64, False),
+    # one pair a lane, four tokens a workgroup
+    ("f16", [40] * 100 + [107], [90] * 50 + [40] * 50 + [107], 16, 3, 2, 80, 20, True), ("f32", [4096, 3], [5000, 3], 7, 3, 1, 7, 6, False),
+    # ... and more of them than a grid's
+    ("f16", [(1 << 22) + 9, 2], [(1 << 22) + 9, 4], 64, 1, 1, 3, 2, False),
+])
+def test_append_of_many_normed_tokens(dtype, new, length, page, Hq, Hkv, d, channels, tree):
+    print("append many", dtype, new[:5], page, d, tree, flush=True)
+    batch, table, ptr, lens, n_pages, T = batch_of(new, length, page, padding=5)
+    ck, cv = caches(n_pages, Hkv, page, d, dtype, 9)
+    K, V, Q = tokens(Hkv, T, d, dtype, 1), tokens(Hkv, T, d, dtype, 2), tokens(Hq, T, d, dtype, 3)
+    freqs, _ = sga.rotary_frequencies(channels)
+    f, rot = freqs.cpu().numpy(), sga.Rotary(freqs)
+    wq, wk = weights_of("same", d, dtype, 0.0, 1), weights_of("f32", d, dtype, 1.0, 2)
+    end = int(ptr[-1])
+    seq = np.repeat(np.arange(len(new)), new)
+    slot = (lens - np.diff(ptr))[seq] + np.arange(end) - ptr[seq]
+    at, made = slot, None
+    if tree:
+        parent = random_parents(new, 5, 0.3, 4)
+        made = tree_of(parent, batch, most=max(new))
+        depth, _ = D.tree(parent, ptr, lens, full(1 << 20), 16)
+        at = (lens - np.diff(ptr))[seq] + np.array(depth[:end])
+    k, k_size = D.norm_rotate(host(K[:, :end]), at, f, "half", 1.0, host(wk), 0.25, 1.0)
+    q, q_size = D.norm_rotate(host(Q[:, :end]), at, f, "half", 1.0, host(wq), 1e-6, 0.0)
+    want_k, want_v, bar = host(ck), host(cv), np.zeros(ck.shape)
+    p, i = table[seq, slot // page], slot % page
+    want_k[p, :, i], want_v[p, :, i] = k.transpose(1, 0, 2), host(V[:, :end]).transpose(1, 0, 2)
+    bar[p, :, i] = D.norm_bar(k, k_size, dtype).transpose(1, 0, 2)
+    out = torch.full((Hq, T, d), 7.0, dtype=DTYPE[dtype], device="cuda")
+    sga.cache_append(K, V, ck, cv, batch, rotary=rot, Q=Q, Q_out=out, q_norm=sga.Norm(wq), k_norm=sga.Norm(wk, 0.25, 1.0), tree=made)
+    assert within(ck, want_k, bar) and np.array_equal(host(cv), want_v)
+    assert (out[:, end:] == 7).all() and within(out[:, :end], q, D.norm_bar(q, q_size, dtype))
 
 
 def test_append_leaves_out_what_the_tree_does_not_have():
