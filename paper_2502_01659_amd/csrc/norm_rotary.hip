@@ -22,7 +22,10 @@ constexpr int kMaxGroups = 1 << 20;  // workgroups along the tokens; they stride
 // Workgroups of the gradient at most: each leaves a partial sum.  (us, kernel and join, 32,768 tokens, 32 + 8 heads of 128, bf16: 1,024 226 + 5, 1,536 210 + 9, 2,048 200 + 8,
 // 4,096 198 + 15.)
 constexpr int kGradGroups = 2048;
-constexpr int kGradTokens = 16;      // (any alignment) tokens of one round of it at most
+constexpr int kGradTokens = 16;      // (any alignment) tokens of one round of it at most ...
+// ... and no more than leave four workgroups a compute unit their weights and turns, a fourth of its LDS each.  (us, as many as 16 / so / 16 KB less: fp32, 32,768 tokens, 8 + 2 heads
+// of 1,024 2,861 / 1,980 / 2,159, 4 heads of 768 705 / 539 / 536.  16 tokens of 1,024 channels would take 68 KB.)
+constexpr size_t kGradShared = 40 * 1024;
 constexpr int64_t kNone = INT64_MIN;  // (rows of a batch) no position; a program's own positions may be any number
 
 // Sum over groups of kLanes neighbouring lanes, in every one of them.  (The lanes of a group are active together.)
@@ -806,7 +809,7 @@ sga_status launch_grad_as(const NormGradArgs& a) {
     } else {
       int t = (128 + heads - 1) / heads;
       t = t > kGradTokens ? kGradTokens : t;
-      while (t > 1 && a.n_rows / t < 256) t >>= 1;
+      while (t > 1 && (a.n_rows / t < 256 || (size_t)((a.d + 3) & ~3) * sizeof(float) + (size_t)t * pairs * sizeof(float2) > kGradShared)) t >>= 1;
       s.tokens[i] = t;
       most = t > most ? t : most;
     }

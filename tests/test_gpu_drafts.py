@@ -271,7 +271,7 @@ def test_norm_gradient(dtype, layout, Hq, Hkv, T, d, channels, memory):
 # these (rows of one pair a lane: up to 16 tokens' heads over four wavefronts, up to four times; rows in lanes: up to eight tokens, four rounds of heads
 # each), a wavefront and a workgroup up to 20 of its lanes' and wavefronts' sums in six steps: below the 72 half steps of weight_bar.
 @pytest.mark.parametrize("dtype,Hq,Hkv,T,d,channels,memory,layout", [
-    # one pair a lane: wide rows whose turns fill most of the memory that a workgroup shares, odd sizes, several rounds
+    # one pair a lane: wide rows, of whose turns a workgroup holds fewer, odd sizes, several rounds
     ("f32", 2, 1, 4097, 1024, 1024, "token", "half"), ("bf16", 4, 1, 4100, 1000, 1000, "head", "interleaved"), ("f16", 3, 2, 4099, 7, 6, "token", "half"),
     ("f32", 3, 2, 40003, 7, 6, "head", "interleaved"), ("bf16", 3, 2, 4099, 80, 20, "token", "interleaved"), ("f16", 16, 1, 4101, 80, 20, "slice", "half"),
     # rows in lanes: one token and several a wavefront
