@@ -131,20 +131,30 @@ __global__ __launch_bounds__(kWave* kMostSegments) void pages_count_kernel(Pages
   }
 }
 
-// Sums that stop at 2^32 - 1: more tokens or pages than there can be (fewer than 2^31 of each), so that a sum that has stopped passes no limit.
-__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
-template <int kCtrl, int kRows>
+// Sums of what is asked for and of what goes back stop at 2^31: more tokens or pages than there can be, so that a sum that has stopped passes no
+// limit.  The middle one of a + b, a and 2^31 is that, also where both have stopped and a + b is 0.  The others need not stop: a page that is needed
+// holds a token that is asked for, so where the tokens fit their packed rows there are fewer than 2^31 pages, and where they do not, nothing
+// is granted whatever the pages' sum is.
+constexpr uint32_t kFull = 0x80000000;
+template <bool kStops>
+__device__ __forceinline__ uint32_t sum_of(uint32_t a, uint32_t b) {
+  const uint32_t sum = a + b;
+  return kStops ? max(min(sum, a), min(max(sum, a), kFull)) : sum;
+}
+__device__ __forceinline__ uint32_t plus(uint32_t a, uint32_t b) { return sum_of<true>(a, b); }
+template <int kCtrl, int kRows, bool kStops>
 __device__ __forceinline__ uint32_t with_lane(uint32_t x) {
-  return plus(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, kRows, 0xF, false));
+  return sum_of<kStops>(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, kCtrl, kRows, 0xF, false));
 }
 // The sums up to each lane: within 16 lanes by shifts, then the last of 16 and of 32 to those behind them.
+template <bool kStops>
 __device__ __forceinline__ uint32_t sum_up(uint32_t x) {
-  x = with_lane<0x111, 0xF>(x);
-  x = with_lane<0x112, 0xF>(x);
-  x = with_lane<0x114, 0xF>(x);
-  x = with_lane<0x118, 0xF>(x);
-  x = with_lane<0x142, 0xA>(x);
-  return with_lane<0x143, 0xC>(x);
+  x = with_lane<0x111, 0xF, kStops>(x);
+  x = with_lane<0x112, 0xF, kStops>(x);
+  x = with_lane<0x114, 0xF, kStops>(x);
+  x = with_lane<0x118, 0xF, kStops>(x);
+  x = with_lane<0x142, 0xA, kStops>(x);
+  return with_lane<0x143, 0xC, kStops>(x);
 }
 __device__ __forceinline__ uint32_t of_lane(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)x, lane); }
 
@@ -164,7 +174,7 @@ struct Walk {
     rows += of_lane(rows_sum, kWave - 1);
     taken += of_lane(taken_sum, kWave - 1);
     wanted = plus(wanted, of_lane(want_sum, kWave - 1));
-    pages = plus(pages, of_lane(need_sum, kWave - 1));
+    pages += of_lane(need_sum, kWave - 1);
     given = plus(given, of_lane(give_sum, kWave - 1));
     uint32_t want = 0, need = 0, give = 0;
 #pragma unroll
@@ -172,31 +182,31 @@ struct Walk {
       const int32_t s = end + lane * kEach + i;
       note[i] = s < a.from.n_seqs ? sequence_notes(a)[s] : SequenceNote{0, 0, 0, 0};
       want = plus(want, max(note[i].want, 0));
-      need = plus(need, note[i].need);
+      need += note[i].need;
       give = plus(give, note[i].give);
     }
-    want_sum = sum_up(want);
-    need_sum = sum_up(need);
-    give_sum = sum_up(give);
+    want_sum = sum_up<true>(want);
+    need_sum = sum_up<false>(need);
+    give_sum = sum_up<true>(give);
     // (what a lane's sequences follow: the sum up to the lane before)
-    auto ahead = [&](uint32_t sum, uint32_t first) {
+    auto ahead = [&](uint32_t sum) {
       const uint32_t up = __shfl_up(sum, 1, kWave);
-      return plus(first, lane > 0 ? up : 0u);
+      return lane > 0 ? up : 0u;
     };
-    uint32_t want_up = ahead(want_sum, wanted), need_up = ahead(need_sum, pages);
-    give_up = ahead(give_sum, given);
+    uint32_t want_up = plus(wanted, ahead(want_sum)), need_up = pages + ahead(need_sum);
+    give_up = plus(given, ahead(give_sum));
     uint32_t own_rows = 0, own_taken = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
       want_up = plus(want_up, max(note[i].want, 0));
-      need_up = plus(need_up, note[i].need);
+      need_up += note[i].need;
       granted[i] = note[i].want > 0 && want_up <= (uint32_t)a.from.n_tokens && (note[i].need == 0 || (int64_t)need_up <= pool.count);
       own_rows += granted[i] ? note[i].want : 0;
       own_taken += granted[i] ? note[i].need : 0;
     }
     // (what is granted fits n_tokens and the ring: 31 bits)
-    rows_sum = sum_up(own_rows);
-    taken_sum = sum_up(own_taken);
+    rows_sum = sum_up<false>(own_rows);
+    taken_sum = sum_up<false>(own_taken);
     rows_up = rows + rows_sum - own_rows;
     taken_up = taken + taken_sum - own_taken;
     end += kEach * kWave;
