@@ -541,11 +541,12 @@ typedef struct {
 /*
  * Norms every head's row and turns it by its position (sga_rotary), of queries and keys in one pass; results are rounded once.
  *   Q      read, Q_out written, [Hq][L][d]; K, K_out both NULL, or read and written, [Hkv][L][d].  Each out may be its input
- *          (same address and strides), else no two may overlap.
+ *          (same address and strides), else no two may overlap; an out that is the other input is refused.
  *   q_norm, k_norm   NULL: not normed.  rotary NULL: not turned.  (A call has to do something: not all are NULL.)
  *   positions, first, L, d, H, dtype   as for sga_rotary
  * The gradient: dQ_out is that of the result, dQ that of Q, and dq_weight float32 [d] that of the weights, summed over all rows
- * (NULL: not asked for; without weights or norm there is none).  dQ may be dQ_out or Q (same address and strides).
+ * (NULL: not asked for; without weights or norm there is none).  dQ may be dQ_out or Q (same address and strides), not K or
+ * dK_out; dK likewise.
  *   workspace  device, 256-byte aligned, sga_norm_workspace_bytes: needed where a gradient of weights is asked for
  * The sums run in a fixed order: the same call gives the same bits.
  * Errors: SGA_ERR_INVALID_ARG as for sga_rotary, SGA_ERR_WORKSPACE.

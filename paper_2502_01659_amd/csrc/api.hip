@@ -740,6 +740,8 @@ sga_status sga_norm_rotary(const sga_rows* Q, const sga_rows* Q_out, const sga_n
   if (L == 0) return SGA_OK;
   if (!valid_rows(Q, dtype) || !valid_rows(Q_out, dtype) || !apart_or_same(*Q, *Q_out)) return SGA_ERR_INVALID_ARG;
   if (K && (!valid_rows(K, dtype) || !valid_rows(K_out, dtype) || !apart_or_same(*K, *K_out) || K_out->data == Q_out->data)) return SGA_ERR_INVALID_ARG;
+  // (rows are read and written in any order: what one tensor's are written to must not be what the other's are read from)
+  if (K && (Q_out->data == K->data || K_out->data == Q->data)) return SGA_ERR_INVALID_ARG;
   if (!aligned_to(positions, 8)) return SGA_ERR_INVALID_ARG;
   (void)hipGetLastError();
   NormRotateArgs a{};
@@ -804,6 +806,8 @@ sga_status sga_norm_rotary_backward(const sga_rows* Q, const sga_rows* dQ_out, c
   };
   if (!add(Q, dQ_out, dQ, q_norm, dq_weight, Hq)) return SGA_ERR_INVALID_ARG;
   if (two && (!add(K, dK_out, dK, k_norm, dk_weight, Hkv) || (L > 0 && dK->data == dQ->data))) return SGA_ERR_INVALID_ARG;
+  if (two && L > 0 && (dQ->data == dK_out->data || dK->data == dQ_out->data || (k_norm && dQ->data == K->data) || (q_norm && dK->data == Q->data)))
+    return SGA_ERR_INVALID_ARG;                               // (as in the forward pass)
   a.n_rows = (int32_t)L; a.d = d;
   a.positions = positions; a.first = first;
   a.rotary = rotary_args(rotary, 1);
@@ -849,6 +853,7 @@ sga_status sga_cache_append_normed(const sga_rows* K, const sga_rows* V, void* c
   if (!valid_rows(K, dtype) || !valid_rows(V, dtype) || !cache_k || !cache_v || cache_k == cache_v) return SGA_ERR_INVALID_ARG;
   if (!aligned_to(cache_k, element_bytes(dtype)) || !aligned_to(cache_v, element_bytes(dtype))) return SGA_ERR_INVALID_ARG;
   if (Q && (!valid_rows(Q, dtype) || !valid_rows(Q_out, dtype) || !apart_or_same(*Q, *Q_out))) return SGA_ERR_INVALID_ARG;
+  if (Q && (Q_out->data == K->data || Q_out->data == V->data)) return SGA_ERR_INVALID_ARG;
   (void)hipGetLastError();
   NormRotateArgs a{};
   const int64_t head = (int64_t)batch->page_size * d;      // from head to head within a page

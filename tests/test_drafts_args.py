@@ -96,6 +96,27 @@ def test_norm_gradient_argument_errors():
     assert sga.sga_norm_workspace_bytes((1 << 31) - 1, 32, 8, 128)[1] < 1 << 21                # a few sums, however many rows
 
 
+def test_outs_that_are_the_other_input():
+    """What one tensor's rows are written to must not be what the other's are read from: rows run in any order."""
+    a, b, c, d = (rows(x) for x in (0x10000, 0x20000, 0x30000, 0x40000))
+
+    def forward(Q=a, Q_out=b, K=c, K_out=d):
+        return sga.sga_norm_rotary(Q, Q_out, norm(), 2, K, K_out, norm(), 2, None, 0, 4, 64, desc(), 1, None)
+    for bad in (dict(Q_out=c), dict(K_out=a), dict(Q_out=c, K_out=a), dict(K=a, Q_out=a), dict(K=a, K_out=a), dict(K=a, Q_out=a, K_out=a)):
+        assert forward(**bad) == -1, bad
+    e, f = rows(0x50000), rows(0x60000)
+
+    def back(Q=a, g=b, dQ=c, K=d, gk=e, dK=f, qn=norm(), kn=norm()):
+        return sga.sga_norm_rotary_backward(Q, g, dQ, qn, None, 2, K, gk, dK, kn, None, 2, None, 0, 4, 64, desc(), 1, None, 0, None)
+    for bad in (dict(dQ=d), dict(dQ=e), dict(dK=a), dict(dK=b), dict(gk=b, dQ=b), dict(gk=b, dK=b), dict(K=a, dQ=a), dict(dQ=e, kn=None), dict(dK=b, qn=None)):
+        assert back(**bad) == -1, bad
+
+    def append(K=a, V=b, Q=c, Q_out=d):
+        return sga.sga_cache_append_normed(K, V, OK, 0x4000, batch(), 2, 64, desc(), norm(), Q, Q_out, 4, norm(), None, 1, None)
+    for bad in (dict(Q_out=a), dict(Q_out=b), dict(Q=a, Q_out=a)):
+        assert append(**bad) == -1, bad
+
+
 def test_tree_argument_errors():
     def call(parent=OK, b=batch(), spec=SPEC, t=tree()):
         return sga.sga_draft_tree_build(parent, b, spec, t, None)
