@@ -223,6 +223,43 @@ def test_norm_rotary_of_the_farthest_positions(d, layout):
     assert torch.equal(first, got[:, :1])
 
 
+@pytest.mark.parametrize("dtype,d,channels", [("bf16", 128, 64), ("f32", 10, 4)])
+def test_norms_of_packed_and_of_broadcast_rows(dtype, d, channels):
+    """Queries and keys that are slices of one projection, in place, values beside them untouched; one row that stands for all heads, and one for all
+    tokens, forward and back."""
+    rot, n = sga.Rotary(sga.rotary_frequencies(channels)[0]), sga.Norm(weights_of("f32", d, dtype, 0.0, 1))
+    packed = tokens(1, 50, 8 * d, dtype, 1, "head").view(50, 8, d)
+    Q, K, before = packed[:, :4].transpose(0, 1), packed[:, 4:6].transpose(0, 1), packed.clone()
+    want = sga.norm_rotary(Q.clone(), K.clone(), rotary=rot, q_norm=n, k_norm=n, first=3)
+    got = sga.norm_rotary(Q, K, rotary=rot, q_norm=n, k_norm=n, first=3, Q_out=Q, K_out=K)
+    assert got[0] is Q and torch.equal(Q, want[0]) and torch.equal(K, want[1]) and torch.equal(packed[:, 6:], before[:, 6:])
+    grads = tokens(1, 50, 8 * d, dtype, 2, "head").view(50, 8, d)
+    G, GK, before = grads[:, :4].transpose(0, 1), grads[:, 4:6].transpose(0, 1), grads.clone()
+    a = sga.norm_rotary_backward(Q, G.clone(), K, GK.clone(), rotary=rot, q_norm=n, k_norm=n, first=3)
+    b = sga.norm_rotary_backward(Q, G, K, GK, rotary=rot, q_norm=n, k_norm=n, first=3, dQ=G, dK=GK)
+    assert all(torch.equal(x, y) for x, y in zip(a, b)) and torch.equal(grads[:, 6:], before[:, 6:])
+    for one in (tokens(1, 50, d, dtype, 3).expand(4, 50, d), tokens(4, 1, d, dtype, 3).expand(4, 50, d)):
+        whole, g = one.contiguous(), tokens(4, 50, d, dtype, 4)
+        assert torch.equal(sga.norm_rotary(one, rotary=rot, q_norm=n), sga.norm_rotary(whole, rotary=rot, q_norm=n))
+        for x, y in ((one, g), (whole, one)):                 # (a gradient may be broadcast too)
+            a, b = (sga.norm_rotary_backward(*z, rotary=rot, q_norm=n) for z in ((x, y), (x.contiguous(), y.contiguous())))
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("d,channels", [(128, 128), (7, 6)])
+def test_norms_of_rows_with_infinities(d, channels):
+    """A row that holds an infinity or a NaN says nothing about the others, in rows in lanes and one pair a lane."""
+    rot, n = sga.Rotary(sga.rotary_frequencies(channels)[0]), sga.Norm(weights_of("f32", d, "f32", 0.0, 1))
+    Q, G = tokens(3, 20, d, "f32", 1), tokens(3, 20, d, "f32", 2)
+    y, dx = sga.norm_rotary(Q, rotary=rot, q_norm=n), sga.norm_rotary_backward(Q, G, rotary=rot, q_norm=n)[0]
+    Q[1, 4, 2], Q[0, 19, 0], Q[2, 0, d - 1] = float("inf"), float("nan"), -float("inf")
+    good = torch.ones(3, 20, dtype=torch.bool, device="cuda")
+    good[1, 4] = good[0, 19] = good[2, 0] = False
+    y2, dx2 = sga.norm_rotary(Q, rotary=rot, q_norm=n), sga.norm_rotary_backward(Q, G, rotary=rot, q_norm=n)[0]
+    assert torch.equal(y[good], y2[good]) and torch.equal(dx[good], dx2[good])
+    assert y2[~good].isnan().any(-1).all() and dx2[~good].isnan().any(-1).all()
+
+
 def test_norm_of_rows_of_zeros_and_of_no_rows():
     x = torch.zeros(2, 3, 64, device="cuda")
     x[1, 1] = 1e-30
@@ -558,6 +595,21 @@ def test_tree_captured_of_many_sequences():
             assert tree.depth.tolist() == depth and D.unpack(tree.seen.cpu().numpy()) == seen
 
 
+@pytest.mark.parametrize("n_seqs,words", [(70000, 3), (270000, 1)])
+def test_trees_of_more_sequences_than_a_grid(n_seqs, words):
+    print("trees", n_seqs, words, flush=True)
+    rng = np.random.default_rng(words)
+    new = rng.integers(0, 3, n_seqs)
+    new[[0, 65535, 65536, n_seqs - 1]] = 3
+    lens = new + rng.integers(0, 9, n_seqs)
+    batch, _, ptr, lens, _, T = batch_of(new.tolist(), lens.tolist(), 16)
+    parent = random_parents(new.tolist(), 0, 0.5, 1)
+    spec = MaskSpec(KIND_GLOBAL_LOCAL, 1000, window=1, n_global=4)
+    tree = tree_of(parent, batch, spec, words)
+    depth, seen = D.tree(parent, ptr, lens, spec, words)
+    assert tree.depth.tolist() == depth and D.unpack(tree.seen.cpu().numpy()) == seen
+
+
 # ---- attention ------------------------------------------------------------------------------------------
 def check_tree_attention(dtype, new, length, page, Hq, Hkv, d, spec, padding=0, memory="token", missing=(), scale=None, workspace=True, chain=0.3,
                          seed=0, words=None, columns=None, change=None):
@@ -637,6 +689,13 @@ def test_tree_attention_split_sequences(dtype):
 @pytest.mark.parametrize("memory", ["head", "token", "slice"])
 def test_tree_attention_strides(memory):
     check_tree_attention("f16", [7, 1, 30], [40, 90, 30], 32, 6, 3, 64, full(96), memory=memory)
+
+
+@pytest.mark.parametrize("scale", [-0.3, 0.0, 2.5])
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+def test_tree_attention_scales(dtype, scale):
+    check_tree_attention(dtype, [7, 1, 12], [40, 90, 30], 16, 4, 2, 64, MaskSpec(KIND_GLOBAL_LOCAL, 96, window=20, n_global=3), scale=scale)
+    check_tree_attention(dtype, [60, 80], [140, 90], 16, 4, 2, 64, MaskSpec(KIND_GLOBAL_LOCAL, 160, window=40, n_global=3), scale=scale)
 
 
 def test_tree_attention_of_missing_pages_and_short_tables():
@@ -814,6 +873,20 @@ def test_keep(dtype, layers, Hkv, d, page):
             path[s, :len(chosen)] = chosen
     path[0, :5] = [2, 2, 7, 3, 99]                            # an index twice, falling ones, none of the tokens: what is not below k moves
     count[5] = 10 ** 6                                        # no more than the columns
+    want = [D.keep(host(c), table, ptr, lens, path, count) for c in (ck, cv)]
+    sga.cache_keep(ck, cv, batch, torch.from_numpy(path).cuda(), torch.from_numpy(count).cuda())
+    assert np.array_equal(host(ck), want[0]) and np.array_equal(host(cv), want[1])
+
+
+def test_keep_of_more_sequences_than_a_grid():
+    S_, page = 40000, 4
+    rng = np.random.default_rng(1)
+    new = rng.integers(0, 4, S_)
+    lens = -(-rng.integers(0, 5, S_) // page) * page + new   # (no two sequences have new tokens in one page, and each begins one)
+    batch, table, ptr, lens, n_pages, T = batch_of(new.tolist(), lens.tolist(), page)
+    ck, cv = caches(n_pages, 1, page, 8, "f16", 1)
+    path = np.sort(rng.integers(0, 4, (S_, 3)), 1).astype(np.int32)
+    count = rng.integers(0, 4, S_).astype(np.int32)
     want = [D.keep(host(c), table, ptr, lens, path, count) for c in (ck, cv)]
     sga.cache_keep(ck, cv, batch, torch.from_numpy(path).cuda(), torch.from_numpy(count).cuda())
     assert np.array_equal(host(ck), want[0]) and np.array_equal(host(cv), want[1])
