@@ -512,6 +512,8 @@ typedef struct {
  *   Granted is a request if it fits the page table's columns, if all such requests up to its sequence's (granted or not) fit n_tokens, and
  *          if it needs no page or all pages needed up to its sequence are no more than `count`.  A sequence whose request is not
  *          granted gets no rows and keeps its l tokens (and pages).  Pages that go back are free from the next call on.
+ *          (So a request of more than n_tokens, or the first that does not fit behind others, keeps every later one from rows, in this call and while it is repeated: a program
+ *          bounds what it asks for.  Pages that lack keep back only those that need some.)
  * Results: page_table, seq_ptr, seq_len = l + granted tokens, the pool's state; pages that go back are put behind the ring's last, in
  * the order (sequence, column).  The same arrays give the same results whatever runs when.
  *   batch      read: the last step's.  next: written, alike in sizes; its arrays may be batch's.  (page_stride is not looked at.)
@@ -589,8 +591,8 @@ sga_status sga_draft_tree_build(const int32_t* parent, const sga_paged_batch* ba
 
 /*
  * sga_cache_append with norms and a tree: keys and queries are normed (k_norm, q_norm; NULL: not) before they are turned (rotary NULL:
- * not), and with a tree (NULL: none) turned by the tree's positions.  A call with Q needs rotary or q_norm.  Rows that the tree does not
- * have are left out: nothing is written for them, Q_out neither.
+ * not), and with a tree (NULL: none) turned by the tree's positions.  A call with Q needs rotary or q_norm; Q_out must not be K or V.  Rows that the
+ * tree does not have are left out: nothing is written for them, Q_out neither.
  */
 sga_status sga_cache_append_normed(const sga_rows* K, const sga_rows* V, void* cache_k, void* cache_v, const sga_paged_batch* batch,
                                    int32_t Hkv, int32_t d, const sga_rotary_desc* rotary, const sga_norm_desc* k_norm, const sga_rows* Q,

@@ -1009,7 +1009,8 @@ def pages_advance(batch, pool, ask, kept=None, spec=None, positions=None, slots=
     spec       a sliding or global + local mask: pages behind its window go back (None: none does)
     positions  int64 [n_tokens], slots int64 [n_tokens]: written, the place in its sequence of every new token, and
                page * page_size + row where it lies in the cache
-    A sequence whose request does not fit gets no rows (seq_ptr tells) and keeps what it has.  Returns the batch written."""
+    A sequence whose request does not fit gets no rows (seq_ptr tells) and keeps what it has; where it does not fit the rows, neither do those behind it,
+    so ask for n_tokens in all at most.  Returns the batch written."""
     index = batch.device_index
     S = batch.seq_len.shape[0]
     to, to_pool = out if out is not None else (batch, pool)

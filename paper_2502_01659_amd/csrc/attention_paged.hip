@@ -39,8 +39,9 @@ constexpr int least_piece(bool tree, int dtype) { return dtype == SGA_F32 ? kLea
 constexpr int kChunkPieces = 1536;
 // Drafted tokens under a window, or behind contexts of one length: the tiles of 128 rows are all alike.  Where they are more than the places on the
 // chip, whole rounds of them are not cut, and what is left is cut into as many pieces as fill the places once more: fewer prologues and hardly any
-// partial states.  (Key heads that share the XCDs, so that pieces start in their order.  us, cut by kChunkPieces / so: 16 tokens of 64 and of 100 sequences under a
-// window of 2,048, 32 / 8 heads of 128, bf16 133 / 114, 212 / 188; 30 to 200 tokens of 32 sequences under 4,096, 32 / 4 heads, fp16 232 / 225.)
+// partial states.  (Key heads that share the XCDs, so that pieces start in their order.  us, whole calls with their joins, in turn on one card, cut by kChunkPieces / so: 16
+// tokens of 64 and of 100 sequences under a window of 2,048, 32 / 8 heads of 128, bf16 144 / 114, 212 / 188; 30 to 200 tokens of 32 sequences under 4,096, 32 / 4 heads,
+// fp16 231 / 224.)
 constexpr float kAlike = 1.25f;
 constexpr int kMostTreeWords = 16;
 
@@ -116,9 +117,10 @@ __device__ __forceinline__ int32_t kept_of(const PagedAttention& a, int32_t leng
 // Drafted tokens.  New token t of a sequence lies at place base + t of the cache, base = length - n_new, but at position base + depth(t), and
 // sees of the context, the tokens before base, what the mask shows that position, and of the new tokens those whose bits are set in
 // its row of `seen`.  Both kernels meet the context's keys as they do others', and the blocks that reach base as blocks at an edge, in which every key is
-// tested: the bits of a block's 32 keys are two words of the row, put together.  All rows of a sequence meet the same keys.  Measured (us, in turn with
-// the same call without a tree): 5 to 16 drafts of 64 sequences behind 512 to 32,768, 32 / 8 heads of 128, bf16 407 / 414 (5.0 TB/s, a large copy 4.8); 30 to 200 of 32
-// under a window of 4,096, 32 / 4 heads, fp16 232 / 230 (700 TFLOP/s of the products that the mask asks for; the library's 1,151).
+// tested: the bits of a block's 32 keys are two words of the row, put together.  All rows of a sequence meet the same keys.  Measured (us, whole calls with their joins, in turn with
+// the same call without a tree): 5 to 16 drafts of 64 sequences behind 512 to 32,768, 32 / 8 heads of 128, bf16 417 / 415 (4.8 TB/s, as a large copy); 30 to 200 of 32
+// under a window of 4,096, 32 / 4 heads, fp16 224 / 223 on one card, 219 / 218 on another (212 to 232 over six: 690 TFLOP/s of the products that the mask asks for at
+// 218; the library's 1,171).
 __device__ __forceinline__ Sight context_sight(const PagedAttention& a, const Tile& t, int32_t token) {
   const int32_t base = t.length - t.n_new, depth = a.depth[t.begin + token];
   const int64_t p = (int64_t)base + depth;
@@ -1059,7 +1061,10 @@ __global__ __launch_bounds__(kWaves* kWave) __attribute__((amdgpu_waves_per_eu(D
 // P is rounded to the storage type once: fp16 2^-11 of a numerator, and at least 2^-25 where the largest of the row is 2^10 or more; bf16
 // 2^-8.  Scores that differ are rounded independently of each other, equal ones alike, so O is off by at most that part
 // of the weighted mean of |V|.  The matrix cores bound this kernel, and a second number for P costs a third of its time (us: prompt under a window 1,223 / 1,622, chunks
-// behind long contexts 261 / 342).  l sums the unrounded numerators.
+// behind long contexts 261 / 342).  l sums the unrounded numerators.  Drafted tokens keep this, so that a chain of them is rounded as the same tokens without a tree are: O is 1.4
+// times as far from the exact result as its own rounding makes it (bf16 2.3e-3 of its size against 1.7e-3).  A second number would cost them little where memory bounds the
+// call and as much as others where it does not (us: 5 to 16 drafts of 64 sequences behind up to 32,768 417 / 430, of 8 behind up to 3,000 26 / 30, 16 under a window of 2,048
+// 114 / 119, 30 to 200 under 4,096 225 / 292, 100 behind 4,000 265 / 363).
 // Measured (us and TFLOP/s of the products that the mask asks for): a causal prompt of 32,768 tokens, 8 heads of 128, bf16
 // 2,310 (950 of a library product's 1,266); the same with 32 heads under a window of 2,048, fp16 1,250 (850: a tile meets
 // 68 blocks, eight of them edges that test every key); 16,384 tokens, causal, 8 heads of 64, fp32 2,570 (107 of 154).

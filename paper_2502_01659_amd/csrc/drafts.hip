@@ -15,12 +15,13 @@ constexpr int kWaves = kThreads / kWave;
 // s, it is granted where R fits the packed rows and P what is free (or where it needs no page).  Free pages are a ring: granted
 // sequences take from its front, in their order, and what goes back is put behind its end, in the order (sequence, column), so no
 // place that is read is written and neither order nor result depends on how the work runs.
-// A call is small: what it costs is launches, chains of dependent loads and, at hundreds of sequences, instructions.  Two kernels: the first
+// A call is small: what it costs is launches, chains of dependent loads and, at hundreds of sequences, one wavefront's walk over them.  Two kernels: the first
 // counts, a wavefront for each segment of a sequence's columns; in the second a sequence's first wavefront sums up what the first kernel has left of the sequences
 // up to its own (16 bytes for each, from L2, two a lane at a time), while the others ask for their columns, and then each goes over the same columns again
 // and writes.  It reads nothing but its own columns, the ring's front and what the first kernel left, so the arrays may be updated in place.
-// Measured (us, both kernels): 64 sequences of up to 32,768 tokens, pages of 16 4.4 + 6.1; 700 of up to 40,000, 1 to 2,000 new tokens each 6.0 + 15.8 (every segment's wavefront
-// summing up by itself 25 + 6, one column at a time without asking ahead 29 + 13).
+// Measured (us, both kernels): 64 sequences of up to 32,768 tokens, pages of 16 4.3 + 6.1; 700 of up to 40,000, 1 to 2,000 new tokens each 6.0 + 15.4 (every segment's wavefront
+// summing up by itself 25 + 6, one column at a time without asking ahead 29 + 13).  Of the latter's 15.4 vector instructions take about 4; 62 % of the wavefronts' time
+// is waiting, for the walk of their workgroup's first one and for its loads.
 struct alignas(16) SequenceNote {
   int32_t length, want;      // tokens kept; tokens asked for and possible (0 otherwise), -1 where the sequence ends
   int32_t need, give;        // pages
@@ -377,7 +378,8 @@ sga_status launch_pages(const PagesArgs& a) {
 // A token's ancestors by doubling: with J_k the 2^k-th ancestor, A_k the ancestors nearer than that and itself as bits, and D_k their number,
 //   A_{k+1}(t) = A_k(t) | A_k(J_k(t)),   J_{k+1}(t) = J_k(J_k(t)),   D_{k+1}(t) = D_k(t) + D_k(J_k(t)),
 // which takes log2 of the depth steps whatever the tree looks like.  Then what the mask hides of them, by the depths, is taken out.  Latency bounds it.  Measured (us):
-// 16 trees of 5 to 16 tokens 3.0; 256 trees of 16 to 500, window 24 15.8 (256 threads a tree, the window's bits one by one 47.5).
+// 16 trees of 5 to 16 tokens 3.0; 256 trees of 16 to 500, window 24 15.7 (256 threads a tree, the window's bits one by one 47.5): half of their tokens follow the one before,
+// the middle tree is 14 deep and the deepest 30 to 39, so four to six rounds of three barriers of 16 wavefronts, and 57 % of their time is waiting.
 namespace {
 
 // Parent of token t: an entry that is no earlier token stands for the last token of the context.

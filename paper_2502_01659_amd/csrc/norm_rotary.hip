@@ -4,7 +4,9 @@
 // with R the rotation of paged_cache.hip, pair by pair.  A row is read and written once and costs about ten operations a channel, so memory bounds
 // it, as it does the rotation alone.  A row lies in d / 2V neighbouring lanes (V elements of 16 bytes, two such pieces a lane, those that turn together), which
 // add their squares by register exchanges.  Which channels a lane has is the same in every row: a wavefront takes a token with all its heads and keeps the
-// token's turns in registers.  Measured: 32,768 tokens, 32 + 8 heads of 128, bf16 128 us (5.2 TB/s read and written; a large copy 4.8).  (A workgroup for a few tokens, turns
+// token's turns in registers (weights are read from LDS for every row).  Measured: 32,768 tokens, 32 + 8 heads of 128, bf16 128 us
+// (5.2 TB/s read and written; a large copy 4.8); into pages, with as many values as keys, fp16 165 (4.9).  16 sequences of 5 to 16 drafts into pages take 7.5, 66 % of the wavefronts' time
+// waiting: the search for a row's sequence, its length and depth, its page, then the rows.  (A workgroup for a few tokens, turns
 // and weights in LDS, a row's tensor picked by its lane: 166, three quarters of the time waiting for what describes the tensor.)
 // The gradient of G = dL/dy: with g = R^T G (the rotation by the negative angle),
 //   dx_c = r (w_c g_c - x_c r^2 mean_k(w_k g_k x_k)),   dw_c = sum over rows of g_c x_c r.
@@ -331,7 +333,8 @@ __global__ __launch_bounds__(kThreads) void norm_rotate_kernel(NormRotateArgs a,
   }
 }
 
-// Any size and alignment: a workgroup takes a few tokens, a wavefront goes over a row, a pair a lane, twice.
+// Any size and alignment: a workgroup takes a few tokens, a wavefront goes over a row, a pair a lane, twice.  (us, 32,768 tokens, 32 + 8 heads of 96, bf16: 32 channels turn, rows
+// in lanes, 108 and the gradient 160; 24, which are no multiple of the 16 of a lane's two pieces, so 597 and 1,007.)
 template <typename T, bool kPaged>
 __global__ __launch_bounds__(kThreads) void norm_rotate_any_kernel(NormRotateArgs a, NormShape shape) {
   extern __shared__ __align__(16) float shared[];
